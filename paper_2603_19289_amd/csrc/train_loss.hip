@@ -1,0 +1,332 @@
+// Losses over rows of router logits, each with its gradient in the same pass over the logits.
+//
+// Distillation (paper: Appendix A), p and q the softmax of the teacher's and of the student's row, n the valid rows:
+//   loss = 1/n sum_t sum_e p (log p - log q),  d loss / d student = (q - p) / (n tau)
+//   sum_e p (log p - log q) = sum_e p (a_e - b_e) - log A + log B  with a, b the logits less their maxima, A = sum exp a, ...
+// Balance, c_e the choices of expert e and f_e = c_e / (n k):
+//   loss = coef E sum_e f_e 1/n sum_t p_te = coef E / n sum_t inner_t  with inner_t = sum_e f_e p_te, the very sum that the
+//   gradient needs:  d loss / d z_te = coef E / n p_te (f_e - inner_t).  So no per-expert sum of probabilities is formed.
+//
+// Bound by memory: logits are read once, gradients written once; the gradient's factors (n, f) come first, from the mask and
+// the ids, which are a few per cent of the bytes.  A row lies in the registers of a group of 1 to 32 lanes, eight
+// values each.  Exponentials go through the hardware's 2^x: its argument x log2 e is rounded to float, which moves exp(x) by
+// |x| 2^-24 relative, so by at most 0.37 * 2^-24 of the row's largest term.  Row results are added up in double.
+#include "train_common.h"
+
+#include <type_traits>
+
+namespace moe_spec {
+namespace {
+
+constexpr int kLossBlock = 256, kLossBlocks = 2048, kCountBlocks = 64, kVals = 8;
+
+struct LossArgs {
+  const void *z, *teacher;              // z: the student's logits, or the router's
+  void *grad;
+  const uint8_t *valid;
+  const int32_t *ids;
+  int32_t *counts;
+  float *loss;
+  int *counted;                         // [kCountBlocks][bins + 1]: choices of each expert, then valid rows; or null: all are
+  double *partial;                      // [blocks]
+  int64_t z_stride, teacher_stride, grad_stride, ids_stride, rows;
+  int experts, bins, top_k, blocks;     // bins: experts, or 0 where no choices are counted
+  float inv_tau, coef;
+};
+
+template <typename WT> __device__ __forceinline__ WT lowest();            // minus infinity
+template <> __device__ __forceinline__ float lowest<float>() { return -INFINITY; }
+template <> __device__ __forceinline__ uint16_t lowest<uint16_t>() { return 0xff80; }
+
+struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+
+// Valid rows and their choices, a share of the rows for each workgroup.
+__global__ __launch_bounds__(kLossBlock) void loss_count_kernel(const LossArgs a) {
+  __shared__ int hist[MOE_SPEC_MAX_EXPERTS + 1];
+  for (int i = threadIdx.x; i <= a.bins; i += kLossBlock) hist[i] = 0;
+  __syncthreads();
+  int live = 0;
+  for (int64_t row = int64_t(blockIdx.x) * kLossBlock + threadIdx.x; row < a.rows; row += int64_t(gridDim.x) * kLossBlock) {
+    if (a.valid && !a.valid[row]) continue;
+    ++live;
+    if (a.bins) {
+      const int32_t *ids = a.ids + row * a.ids_stride;
+      for (int j = 0; j < a.top_k; ++j) {
+        const int e = ids[j];
+        if (e >= 0 && e < a.bins) atomicAdd(&hist[e], 1);
+      }
+    }
+  }
+  atomicAdd(&hist[a.bins], live);
+  __syncthreads();
+  for (int i = threadIdx.x; i <= a.bins; i += kLossBlock) a.counted[blockIdx.x * (a.bins + 1) + i] = hist[i];
+}
+
+// Sum over the workgroup of one double per thread, in every thread.
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double part[kLossBlock / kWave];
+  v = wave_sum(v);
+  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+  __syncthreads();
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < kLossBlock / kWave; ++i) s += part[i];
+  return s;
+}
+
+// ST: the logits' type; TT: the teacher's (void: balance loss); G lanes per row.
+template <typename ST, typename TT, int G>
+__global__ __launch_bounds__(kLossBlock) void loss_kernel(const LossArgs a) {
+  constexpr bool kDistill = !__is_same(TT, void);
+  using Teacher = std::conditional_t<kDistill, TT, float>;
+  constexpr int kRows = kLossBlock / G;
+  const int lane = threadIdx.x % G, slot = threadIdx.x / G, col = lane * kVals;
+  __shared__ int total[MOE_SPEC_MAX_EXPERTS + 1];
+  // the valid rows and the choices, added up over what loss_count_kernel's workgroups left
+  if (a.counted) {
+    for (int i = threadIdx.x; i <= a.bins; i += kLossBlock) {
+      int s = 0;
+#pragma unroll 8
+      for (int b = 0; b < kCountBlocks; ++b) s += a.counted[b * (a.bins + 1) + i];
+      total[i] = s;
+      if (!kDistill && blockIdx.x == 0 && i < a.bins) a.counts[i] = s;
+    }
+    __syncthreads();
+  }
+  const float n = a.counted ? float(total[a.bins]) : float(a.rows);
+  const float share = n > 0.0f ? 1.0f / n : 0.0f;
+  float f[kVals];
+  float scale;
+  if constexpr (kDistill) {
+    scale = share * a.inv_tau;
+  } else {
+    scale = a.coef * float(a.experts) * share;
+#pragma unroll
+    for (int i = 0; i < kVals; ++i) f[i] = col + i < a.experts ? float(total[col + i]) * (share / float(a.top_k)) : 0.0f;
+  }
+
+  Run<ST, kVals> next_z;
+  Run<Teacher, kVals> next_t;
+  const int64_t step = int64_t(gridDim.x) * kRows;
+  auto alive = [&](int64_t row) { return row < a.rows && (!a.valid || a.valid[row]); };
+  auto fetch = [&](int64_t row, bool live) {
+    const int here = live ? a.experts - col : 0;        // rows that do not count are not read
+    next_z.load(static_cast<const ST *>(a.z) + row * a.z_stride + col, here, lowest<ST>());
+    if constexpr (kDistill) next_t.load(static_cast<const Teacher *>(a.teacher) + row * a.teacher_stride + col, here, lowest<Teacher>());
+  };
+  double sum = 0.0;
+  int64_t row = int64_t(blockIdx.x) * kRows + slot;
+  bool live = alive(row), next_live = alive(row + step);
+  fetch(row, live);
+  for (int64_t first = int64_t(blockIdx.x) * kRows; first < a.rows; first += step, row += step) {
+    float z[kVals], t[kVals], grad[kVals];
+    next_z.get(z);
+    if constexpr (kDistill) next_t.get(t);
+    const bool counts = live;
+    live = next_live;
+    fetch(row + step, live);
+    next_live = alive(row + 2 * step);
+    float result;
+    if constexpr (kDistill) {
+      float top_z = -INFINITY, top_t = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kVals; ++i) {
+        z[i] *= a.inv_tau;
+        t[i] *= a.inv_tau;
+        top_z = fmaxf(top_z, z[i]);
+        top_t = fmaxf(top_t, t[i]);
+      }
+      top_z = group_reduce<G>(top_z, Max());
+      top_t = group_reduce<G>(top_t, Max());
+      if (top_z == -INFINITY) top_z = 0.0f;
+      if (top_t == -INFINITY) top_t = 0.0f;
+      float sum_z = 0.0f, sum_t = 0.0f, cross = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kVals; ++i) {
+        z[i] -= top_z;
+        t[i] -= top_t;
+        sum_z += grad[i] = __expf(z[i]);
+        sum_t += __expf(t[i]);
+      }
+      sum_z = group_sum<G>(sum_z);
+      sum_t = group_sum<G>(sum_t);
+      const bool nothing = sum_t == 0.0f;                                  // the teacher's row is masked out whole
+      const float inv_z = sum_z == 0.0f || nothing ? 0.0f : 1.0f / sum_z, inv_t = nothing ? 0.0f : 1.0f / sum_t;
+#pragma unroll
+      for (int i = 0; i < kVals; ++i) {
+        const float p = __expf(t[i]) * inv_t;
+        cross += p == 0.0f ? 0.0f : p * (t[i] - z[i]);                     // 0 log 0 = 0
+        grad[i] = nothing ? 0.0f : (grad[i] * inv_z - p) * scale;
+      }
+      cross = group_sum<G>(cross);
+      result = nothing ? 0.0f : cross - logf(sum_t) + (sum_z == 0.0f ? 0.0f : logf(sum_z));
+    } else {
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kVals; ++i) top = fmaxf(top, z[i]);
+      top = group_reduce<G>(top, Max());
+      if (top == -INFINITY) top = 0.0f;
+      float total_e = 0.0f, inner = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kVals; ++i) {
+        z[i] = __expf(z[i] - top);
+        total_e += z[i];
+        inner += z[i] * f[i];
+      }
+      total_e = group_sum<G>(total_e);
+      inner = group_sum<G>(inner);
+      const float inv = total_e == 0.0f ? 0.0f : 1.0f / total_e;
+      result = inner * inv;
+#pragma unroll
+      for (int i = 0; i < kVals; ++i) grad[i] = z[i] * inv * (f[i] - result) * scale;
+    }
+    if (counts && lane == 0) sum += double(result);
+    if (a.grad && row < a.rows && col < a.experts) {
+      if (!counts) {
+#pragma unroll
+        for (int i = 0; i < kVals; ++i) grad[i] = 0.0f;
+      }
+      store_run<ST, kVals>(static_cast<ST *>(a.grad) + row * a.grad_stride + col, grad, a.experts - col);
+    }
+  }
+  sum = block_sum(sum) * double(kDistill ? share : scale);
+  if (threadIdx.x == 0) {
+    if (gridDim.x == 1) *a.loss = float(sum);
+    else a.partial[blockIdx.x] = sum;
+  }
+}
+
+__global__ __launch_bounds__(kLossBlock) void loss_finish_kernel(const LossArgs a) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < a.blocks; i += kLossBlock) s += a.partial[i];
+  s = block_sum(s);
+  if (threadIdx.x == 0) *a.loss = float(s);
+}
+
+// No rows: a loss of zero, no choices.
+__global__ void loss_none_kernel(const LossArgs a) {
+  if (threadIdx.x == 0) *a.loss = 0.0f;
+  if (a.counts && int(threadIdx.x) < a.experts) a.counts[threadIdx.x] = 0;
+}
+
+template <typename ST, typename TT, int G>
+hipError_t run_loss(hipStream_t stream, LossArgs &a) {
+  const int64_t need = (a.rows + kLossBlock / G - 1) / (kLossBlock / G);
+  a.blocks = int(need < kLossBlocks ? need : kLossBlocks);
+  hipError_t e = hipSuccess;
+  if (a.counted) e = launch(loss_count_kernel, kCountBlocks, kLossBlock, stream, a);
+  if (e == hipSuccess) e = launch(loss_kernel<ST, TT, G>, a.blocks, kLossBlock, stream, a);
+  if (e == hipSuccess && a.blocks > 1) e = launch(loss_finish_kernel, 1, kLossBlock, stream, a);
+  return e;
+}
+
+template <typename ST, typename TT>
+hipError_t run_loss(hipStream_t stream, LossArgs &a) {
+  if (a.rows == 0) return launch(loss_none_kernel, 1, MOE_SPEC_MAX_EXPERTS, stream, a);
+  const int lanes = (a.experts + kVals - 1) / kVals;
+  if (lanes <= 1) return run_loss<ST, TT, 1>(stream, a);
+  if (lanes <= 2) return run_loss<ST, TT, 2>(stream, a);
+  if (lanes <= 4) return run_loss<ST, TT, 4>(stream, a);
+  if (lanes <= 8) return run_loss<ST, TT, 8>(stream, a);
+  if (lanes <= 16) return run_loss<ST, TT, 16>(stream, a);
+  return run_loss<ST, TT, 32>(stream, a);
+}
+
+size_t partial_bytes() { return kLossBlocks * sizeof(double); }
+size_t counted_bytes(int experts) { return (size_t(kCountBlocks) * (experts + 1) * sizeof(int) + 15) / 16 * 16; }
+
+bool sizes_fit(int64_t rows, int experts) {
+  return rows >= 0 && rows <= MOE_SPEC_TRAIN_MAX_ROWS && experts >= 1 && experts <= MOE_SPEC_MAX_EXPERTS;
+}
+
+const char *grad_fault(const void *grad, int64_t grad_stride, const void *z, int64_t z_stride, int64_t rows, int cols, int elem) {
+  if (!grad) return nullptr;
+  if (const char *why = matrix_fault(grad, grad_stride, rows, cols, elem, true)) return why;
+  if (grad == z && grad_stride != z_stride && rows > 1) return "has another stride than the logits it overwrites";
+  return nullptr;
+}
+
+const char *workspace_fault(const void *workspace, size_t bytes, size_t need) {
+  if (!workspace || misaligned(workspace, 16)) return "must be given and aligned to 16 bytes";
+  return bytes < need ? "is too small" : nullptr;
+}
+
+}  // namespace
+}  // namespace moe_spec
+
+using namespace moe_spec;
+
+extern "C" size_t moe_spec_distill_loss_workspace_bytes(int64_t rows, int n_experts) {
+  return sizes_fit(rows, n_experts) ? partial_bytes() + counted_bytes(0) : 0;
+}
+
+extern "C" size_t moe_spec_balance_loss_workspace_bytes(int64_t rows, int n_experts, int top_k) {
+  if (!sizes_fit(rows, n_experts) || top_k < 1 || top_k > MOE_SPEC_MAX_TOP_K) return 0;
+  return partial_bytes() + counted_bytes(n_experts);
+}
+
+extern "C" int moe_spec_distill_loss(void *stream, int student_dtype, const void *student, int64_t student_stride,
+                                     int teacher_dtype, const void *teacher, int64_t teacher_stride, int64_t rows,
+                                     int n_experts, float temperature, const uint8_t *valid, float *loss, void *grad,
+                                     int64_t grad_stride, void *workspace, size_t workspace_bytes) {
+  if (!known_type(student_dtype) || !known_type(teacher_dtype)) return train_fail(MOE_SPEC_EINVAL, "distill_loss: unknown dtype");
+  if (!sizes_fit(rows, n_experts)) return train_fail(MOE_SPEC_EINVAL, "distill_loss: rows or n_experts out of range");
+  if (!(temperature > 0.0f) || !(1.0f / temperature > 0.0f) || !(1.0f / temperature < INFINITY))
+    return train_fail(MOE_SPEC_EINVAL, "distill_loss: temperature must be positive and finite, and so its reciprocal");
+  if (const char *why = matrix_fault(student, student_stride, rows, n_experts, size_of(student_dtype), false))
+    return train_fail(MOE_SPEC_EINVAL, "distill_loss: student %s", why);
+  if (const char *why = matrix_fault(teacher, teacher_stride, rows, n_experts, size_of(teacher_dtype), false))
+    return train_fail(MOE_SPEC_EINVAL, "distill_loss: teacher %s", why);
+  if (const char *why = grad_fault(grad, grad_stride, student, student_stride, rows, n_experts, size_of(student_dtype)))
+    return train_fail(MOE_SPEC_EINVAL, "distill_loss: grad %s", why);
+  if (grad && grad == teacher) return train_fail(MOE_SPEC_EINVAL, "distill_loss: grad must not be the teacher");
+  if (!loss || misaligned(loss, 4)) return train_fail(MOE_SPEC_EINVAL, "distill_loss: loss is null or not aligned to 4 bytes");
+  if (const char *why = workspace_fault(workspace, workspace_bytes, moe_spec_distill_loss_workspace_bytes(rows, n_experts)))
+    return train_fail(MOE_SPEC_EINVAL, "distill_loss: the workspace %s", why);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const OnDeviceOf on(s);
+  if (on.error() != hipSuccess) return train_fail(MOE_SPEC_EHIP, "distill_loss: %s", hipGetErrorString(on.error()));
+  LossArgs a = {};
+  a.z = student; a.teacher = teacher; a.grad = grad; a.valid = valid; a.loss = loss;
+  a.z_stride = student_stride; a.teacher_stride = teacher_stride; a.grad_stride = grad_stride; a.rows = rows;
+  a.experts = n_experts; a.inv_tau = 1.0f / temperature;
+  a.partial = static_cast<double *>(workspace);
+  if (valid) a.counted = reinterpret_cast<int *>(static_cast<char *>(workspace) + partial_bytes());
+  hipError_t e;
+  if (student_dtype == MOE_SPEC_BF16)
+    e = teacher_dtype == MOE_SPEC_BF16 ? run_loss<uint16_t, uint16_t>(s, a) : run_loss<uint16_t, float>(s, a);
+  else
+    e = teacher_dtype == MOE_SPEC_BF16 ? run_loss<float, uint16_t>(s, a) : run_loss<float, float>(s, a);
+  return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "distill_loss: %s", hipGetErrorString(e));
+}
+
+extern "C" int moe_spec_balance_loss(void *stream, int dtype, const void *logits, int64_t logits_stride, int64_t rows,
+                                     int n_experts, const int32_t *ids, int64_t ids_stride, int top_k, float coef,
+                                     const uint8_t *valid, float *loss, int32_t *counts, void *grad, int64_t grad_stride,
+                                     void *workspace, size_t workspace_bytes) {
+  if (!known_type(dtype)) return train_fail(MOE_SPEC_EINVAL, "balance_loss: unknown dtype %d", dtype);
+  if (!sizes_fit(rows, n_experts)) return train_fail(MOE_SPEC_EINVAL, "balance_loss: rows or n_experts out of range");
+  if (top_k < 1 || top_k > MOE_SPEC_MAX_TOP_K || rows * top_k > INT32_MAX)
+    return train_fail(MOE_SPEC_EINVAL, "balance_loss: top_k must be 1 to %d and rows * top_k below 2^31", MOE_SPEC_MAX_TOP_K);
+  if (!(coef == coef)) return train_fail(MOE_SPEC_EINVAL, "balance_loss: coef is no number");
+  if (const char *why = matrix_fault(logits, logits_stride, rows, n_experts, size_of(dtype), false))
+    return train_fail(MOE_SPEC_EINVAL, "balance_loss: logits %s", why);
+  if (const char *why = matrix_fault(ids, ids_stride, rows, top_k, 4, false)) return train_fail(MOE_SPEC_EINVAL, "balance_loss: ids %s", why);
+  if (const char *why = grad_fault(grad, grad_stride, logits, logits_stride, rows, n_experts, size_of(dtype)))
+    return train_fail(MOE_SPEC_EINVAL, "balance_loss: grad %s", why);
+  if (!loss || misaligned(loss, 4) || !counts || misaligned(counts, 4))
+    return train_fail(MOE_SPEC_EINVAL, "balance_loss: loss or counts is null or not aligned to 4 bytes");
+  if (const char *why = workspace_fault(workspace, workspace_bytes, moe_spec_balance_loss_workspace_bytes(rows, n_experts, top_k)))
+    return train_fail(MOE_SPEC_EINVAL, "balance_loss: the workspace %s", why);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const OnDeviceOf on(s);
+  if (on.error() != hipSuccess) return train_fail(MOE_SPEC_EHIP, "balance_loss: %s", hipGetErrorString(on.error()));
+  LossArgs a = {};
+  a.z = logits; a.grad = grad; a.valid = valid; a.ids = ids; a.loss = loss; a.counts = counts;
+  a.z_stride = logits_stride; a.grad_stride = grad_stride; a.ids_stride = ids_stride; a.rows = rows;
+  a.experts = a.bins = n_experts; a.top_k = top_k; a.coef = coef; a.inv_tau = 1.0f;
+  a.partial = static_cast<double *>(workspace);
+  a.counted = reinterpret_cast<int *>(static_cast<char *>(workspace) + partial_bytes());
+  const hipError_t e = dtype == MOE_SPEC_BF16 ? run_loss<uint16_t, void>(s, a) : run_loss<float, void>(s, a);
+  return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "balance_loss: %s", hipGetErrorString(e));
+}

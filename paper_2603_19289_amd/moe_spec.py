@@ -15,6 +15,7 @@ MODE_ON_DEMAND, MODE_SPECULATIVE, MODE_PREFETCH_HINT = 0, 1, 2
 F32, BF16 = 0, 1
 COPY_DMA, COPY_KERNEL, COPY_DMA2 = 0, 1, 2
 STATIC_SCRATCH_BYTES = 8 << 20
+MOMENTS_32BIT, MOMENTS_8BIT, MOMENT_BLOCK = 0, 1, 128
 
 
 class Config(C.Structure):
@@ -51,6 +52,17 @@ class LayerDiag(C.Structure):
 class StepOutputs(C.Structure):
     _fields_ = [("true_ids", C.c_void_p), ("true_gates", C.c_void_p), ("exec_ids", C.c_void_p),
                 ("exec_gates", C.c_void_p), ("next_ids", C.c_void_p), ("next_gates", C.c_void_p)]
+
+
+class AdamWTensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_exp", C.c_void_p),
+                ("v_exp", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64)]
+
+
+class AdamWConfig(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("grad_scale", C.c_double), ("step", C.c_int64), ("step_dev", C.c_void_p),
+                ("grad_scale_dev", C.c_void_p), ("seed", C.c_uint32), ("grad_dtype", C.c_int32), ("moments", C.c_int32)]
 
 
 class MoeSpecError(RuntimeError):
@@ -94,6 +106,20 @@ def lib():
         L.moe_spec_last_error.restype = C.c_char_p
         L.moe_spec_time_kernel.argtypes = [vp, i32, i32, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
         L.moe_spec_synth_advance.argtypes = [vp, vp, vp, vp, C.c_double, C.c_double, i32, i32, vp]
+        i64, f32 = C.c_int64, C.c_float
+        L.moe_spec_layernorm_forward.argtypes = [vp, i32, vp, i64, i64, i32, vp, vp, f32, vp, i64, vp, vp]
+        L.moe_spec_layernorm_backward_workspace_bytes.argtypes = [i64, i32]
+        L.moe_spec_layernorm_backward_workspace_bytes.restype = sz
+        L.moe_spec_layernorm_backward.argtypes = [vp, i32, vp, i64, vp, i64, i64, i32, vp, vp, vp, vp, i64, vp, vp, vp, sz]
+        L.moe_spec_distill_loss_workspace_bytes.argtypes = [i64, i32]
+        L.moe_spec_distill_loss_workspace_bytes.restype = sz
+        L.moe_spec_distill_loss.argtypes = [vp, i32, vp, i64, i32, vp, i64, i64, i32, f32, vp, vp, vp, i64, vp, sz]
+        L.moe_spec_balance_loss_workspace_bytes.argtypes = [i64, i32, i32]
+        L.moe_spec_balance_loss_workspace_bytes.restype = sz
+        L.moe_spec_balance_loss.argtypes = [vp, i32, vp, i64, i64, i32, vp, i64, i32, f32, vp, vp, vp, vp, i64, vp, sz]
+        L.moe_spec_adamw_step.argtypes = [vp, C.POINTER(AdamWTensor), i32, C.POINTER(AdamWConfig)]
+        L.moe_spec_adamw_read_moments.argtypes = [vp, C.POINTER(AdamWTensor), i32, i32, C.POINTER(vp), C.POINTER(vp)]
+        L.moe_spec_train_last_error.restype = C.c_char_p
         _lib = L
     return _lib
 
@@ -189,3 +215,52 @@ def moe_spec_synth_advance(stream_ptr, r_ptr, out_ptr, eps_ptr, a, b, batch, hid
     rc = lib().moe_spec_synth_advance(stream_ptr, r_ptr, out_ptr, eps_ptr, a, b, batch, hidden, r_next_ptr)
     if rc != 0:
         raise MoeSpecError(rc, "moe_spec_synth_advance failed")
+
+
+# ---- include/moe_spec_train.h: operators for training the estimator (torch tensors: training.py)
+def _check_train(rc):
+    if rc != OK:
+        raise MoeSpecError(rc, (lib().moe_spec_train_last_error() or b"").decode())
+
+
+def moe_spec_layernorm_forward(stream, dtype, x, x_stride, rows, cols, gain, bias, eps, y, y_stride, mean, rstd):
+    _check_train(lib().moe_spec_layernorm_forward(stream, dtype, x, x_stride, rows, cols, gain, bias, eps, y, y_stride, mean, rstd))
+
+
+def moe_spec_layernorm_backward_workspace_bytes(rows, cols) -> int:
+    return lib().moe_spec_layernorm_backward_workspace_bytes(rows, cols)
+
+
+def moe_spec_layernorm_backward(stream, dtype, dy, dy_stride, x, x_stride, rows, cols, mean, rstd, gain, dx, dx_stride, dgain,
+                                dbias, workspace, workspace_bytes):
+    _check_train(lib().moe_spec_layernorm_backward(stream, dtype, dy, dy_stride, x, x_stride, rows, cols, mean, rstd, gain, dx,
+                                                   dx_stride, dgain, dbias, workspace, workspace_bytes))
+
+
+def moe_spec_distill_loss_workspace_bytes(rows, n_experts) -> int:
+    return lib().moe_spec_distill_loss_workspace_bytes(rows, n_experts)
+
+
+def moe_spec_distill_loss(stream, student_dtype, student, student_stride, teacher_dtype, teacher, teacher_stride, rows, n_experts,
+                          temperature, valid, loss, grad, grad_stride, workspace, workspace_bytes):
+    _check_train(lib().moe_spec_distill_loss(stream, student_dtype, student, student_stride, teacher_dtype, teacher, teacher_stride,
+                                             rows, n_experts, temperature, valid, loss, grad, grad_stride, workspace,
+                                             workspace_bytes))
+
+
+def moe_spec_balance_loss_workspace_bytes(rows, n_experts, top_k) -> int:
+    return lib().moe_spec_balance_loss_workspace_bytes(rows, n_experts, top_k)
+
+
+def moe_spec_balance_loss(stream, dtype, logits, logits_stride, rows, n_experts, ids, ids_stride, top_k, coef, valid, loss, counts,
+                          grad, grad_stride, workspace, workspace_bytes):
+    _check_train(lib().moe_spec_balance_loss(stream, dtype, logits, logits_stride, rows, n_experts, ids, ids_stride, top_k, coef,
+                                             valid, loss, counts, grad, grad_stride, workspace, workspace_bytes))
+
+
+def moe_spec_adamw_step(stream, tensors, n_tensors, cfg: AdamWConfig):
+    _check_train(lib().moe_spec_adamw_step(stream, tensors, n_tensors, C.byref(cfg)))
+
+
+def moe_spec_adamw_read_moments(stream, tensors, n_tensors, out_dtype, m_out, v_out):
+    _check_train(lib().moe_spec_adamw_read_moments(stream, tensors, n_tensors, out_dtype, m_out, v_out))

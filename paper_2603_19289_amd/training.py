@@ -1,0 +1,253 @@
+"""Training of the expert estimator (paper: Sec. 6, Appendix A) and of routers: torch tensors into the operators of
+include/moe_spec_train.h.  Torch supplies memory and streams; the operators are the library's kernels.
+
+Every function queues its kernels on the current stream of its tensors' device and returns tensors that are valid in that
+stream's order.  Gradients are results of explicit calls (a loss returns its own, `layernorm_backward` takes one): nothing here
+records or reads an autograd graph.  All calls can be captured into a graph."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import List, Optional, Sequence
+
+import torch
+
+from . import moe_spec as M
+
+_TYPES = {torch.float32: M.F32, torch.bfloat16: M.BF16}
+
+
+def _stream(dev: torch.device):
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+def _queue(dev: torch.device, call, *args):
+    """call(stream, *args) with the tensors' device as the current one."""
+    if torch.cuda.current_device() == dev.index:
+        call(_stream(dev), *args)
+    else:
+        with torch.cuda.device(dev):
+            call(_stream(dev), *args)
+
+
+def _rows(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> int:
+    """Type number of a matrix whose rows are contiguous."""
+    if t.dtype not in _TYPES or t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name} must be a two-dimensional float32 or bfloat16 tensor on a GPU")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the values of a row must be contiguous")
+    if like is not None and (t.shape != like.shape or t.device != like.device):
+        raise ValueError(f"{name} must have the shape and the device of the other matrix")
+    return _TYPES[t.dtype]
+
+
+def _vector(t: Optional[torch.Tensor], name: str, n: int, dev: torch.device, dtype=torch.float32):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous() or t.device != dev:
+        raise ValueError(f"{name} must be a contiguous {dtype} vector of {n} values on {dev}")
+    return t.data_ptr()
+
+
+def _mask(valid: Optional[torch.Tensor], rows: int, dev: torch.device):
+    if valid is None:
+        return None
+    if valid.dtype not in (torch.bool, torch.uint8):
+        raise ValueError("valid must be a bool or uint8 vector")
+    return _vector(valid, "valid", rows, dev, valid.dtype)
+
+
+def _bytes(n: int, dev: torch.device) -> torch.Tensor:
+    return torch.empty(n, dtype=torch.uint8, device=dev)
+
+
+def layernorm_forward(x: torch.Tensor, gain: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                      eps: float = 1e-5, *, out: Optional[torch.Tensor] = None):
+    """LayerNorm over the last dimension of x [rows, cols] (rows may be strided) -> (y, mean [rows], rstd [rows]).  gain and
+    bias: float32 [cols] or None.  out: where y goes, x itself included."""
+    dtype = _rows(x, "x")
+    rows, cols = x.shape
+    dev = x.device
+    y = torch.empty((rows, cols), dtype=x.dtype, device=dev) if out is None else out
+    if out is not None and _rows(y, "out", x) != dtype:
+        raise ValueError("out must have the type of x")
+    stats = torch.empty((2, rows), dtype=torch.float32, device=dev)
+    mean, rstd = stats[0], stats[1]
+    _queue(dev, M.moe_spec_layernorm_forward, dtype, x.data_ptr(), x.stride(0), rows, cols, _vector(gain, "gain", cols, dev),
+           _vector(bias, "bias", cols, dev), eps, y.data_ptr(), y.stride(0), mean.data_ptr(), rstd.data_ptr())
+    return y, mean, rstd
+
+
+def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                       gain: Optional[torch.Tensor] = None, *, input_grad: bool = True, weight_grads: bool = True):
+    """Gradients of LayerNorm for dy [rows, cols], with x, mean and rstd of the forward pass -> (dx, dgain, dbias): dx in x's
+    type, the weights' float32 [cols], summed over the rows in an order of their own (the same bits every time).  None in the
+    place of what is not asked for."""
+    dtype = _rows(x, "x")
+    if _rows(dy, "dy", x) != dtype:
+        raise ValueError("dy must have the type of x")
+    rows, cols = x.shape
+    dev = x.device
+    dx = torch.empty((rows, cols), dtype=x.dtype, device=dev) if input_grad else None
+    dgain = dbias = None
+    need, space = 0, None
+    if weight_grads:
+        dgain, dbias = torch.empty((2, cols), dtype=torch.float32, device=dev).unbind(0)
+        need = M.moe_spec_layernorm_backward_workspace_bytes(rows, cols)
+        space = _bytes(need, dev)
+    _queue(dev, M.moe_spec_layernorm_backward, dtype, dy.data_ptr(), dy.stride(0), x.data_ptr(), x.stride(0), rows, cols,
+           _vector(mean, "mean", rows, dev), _vector(rstd, "rstd", rows, dev), _vector(gain, "gain", cols, dev),
+           dx.data_ptr() if input_grad else None, cols, dgain.data_ptr() if weight_grads else None,
+           dbias.data_ptr() if weight_grads else None, space.data_ptr() if weight_grads else None, need)
+    return dx, dgain, dbias
+
+
+def distill_loss(student: torch.Tensor, teacher: torch.Tensor, *, temperature: float = 1.0,
+                 valid: Optional[torch.Tensor] = None, grad: bool = True):
+    """Mean over the valid rows of KL(softmax(teacher / temperature) || softmax(student / temperature)) for logits
+    [rows, experts] -> (loss, its gradient with respect to the student's logits, in their type, or None)."""
+    ts, tt = _rows(student, "student"), _rows(teacher, "teacher", student)
+    rows, experts = student.shape
+    dev = student.device
+    loss = torch.empty((), dtype=torch.float32, device=dev)
+    dz = torch.empty((rows, experts), dtype=student.dtype, device=dev) if grad else None
+    need = M.moe_spec_distill_loss_workspace_bytes(rows, experts)
+    space = _bytes(need, dev)
+    _queue(dev, M.moe_spec_distill_loss, ts, student.data_ptr(), student.stride(0), tt, teacher.data_ptr(), teacher.stride(0),
+           rows, experts, temperature, _mask(valid, rows, dev), loss.data_ptr(), dz.data_ptr() if grad else None, experts,
+           space.data_ptr(), need)
+    return loss, dz
+
+
+def balance_loss(logits: torch.Tensor, ids: torch.Tensor, *, coef: float = 1.0, valid: Optional[torch.Tensor] = None,
+                 grad: bool = True):
+    """coef * experts * sum_e f_e P_e for logits [rows, experts] and the experts that each row chose, ids int32 [rows, k]
+    -> (loss, counts int32 [experts], gradient with respect to the logits or None)."""
+    dtype = _rows(logits, "logits")
+    rows, experts = logits.shape
+    dev = logits.device
+    if ids.dtype != torch.int32 or ids.dim() != 2 or ids.shape[0] != rows or ids.device != dev:
+        raise ValueError("ids must be an int32 tensor [rows, k] on the logits' device")
+    if ids.shape[1] > 1 and ids.stride(1) != 1:
+        raise ValueError("ids: the values of a row must be contiguous")
+    k = ids.shape[1]
+    loss = torch.empty((), dtype=torch.float32, device=dev)
+    counts = torch.empty(experts, dtype=torch.int32, device=dev)
+    dz = torch.empty((rows, experts), dtype=logits.dtype, device=dev) if grad else None
+    need = M.moe_spec_balance_loss_workspace_bytes(rows, experts, k)
+    space = _bytes(need, dev)
+    _queue(dev, M.moe_spec_balance_loss, dtype, logits.data_ptr(), logits.stride(0), rows, experts, ids.data_ptr(), ids.stride(0),
+           k, coef, _mask(valid, rows, dev), loss.data_ptr(), counts.data_ptr(), dz.data_ptr() if grad else None, experts,
+           space.data_ptr(), need)
+    return loss, counts, dz
+
+
+class AdamW:
+    """AdamW over many float32 tensors in one call, moments in 32 ("f32") or 8 bits ("f8").  Holds the tensors and their
+    moments; `lr`, `betas`, `eps` and `weight_decay` may be set between steps.
+
+    copies: bfloat16 tensors (or None in places) that get the updated parameters, rounded: what an Engine reads its weights
+    from.  states: moments to go on with, as `states()` of another AdamW gave them; used in place."""
+
+    def __init__(self, params: Sequence[torch.Tensor], *, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
+                 weight_decay: float = 0.01, state: str = "f32", copies: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                 seed: int = 0, states: Optional[dict] = None, steps: int = 0):
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("no parameters")
+        if state not in ("f32", "f8"):
+            raise ValueError('state must be "f32" or "f8"')
+        self.lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
+        self.state, self.seed, self.steps = state, int(seed) & 0xffffffff, int(steps)
+        dev = self.device = self.params[0].device
+        for p in self.params:
+            self._tensor(p, "a parameter", torch.float32, p.numel())
+        if len({p.data_ptr() for p in self.params if p.numel()}) < sum(p.numel() > 0 for p in self.params):
+            raise ValueError("a parameter is named twice")
+        self.copies = list(copies) if copies is not None else [None] * len(self.params)
+        eight = state == "f8"
+        held = torch.uint8 if eight else torch.float32
+        blocks = lambda p: -(-p.numel() // M.MOMENT_BLOCK)  # noqa: E731
+        if states is None:
+            new = lambda n, t: torch.zeros(n, dtype=t, device=dev)  # noqa: E731
+            states = {k: [new(p.numel(), held) for p in self.params] for k in ("m", "v")}
+            if eight:
+                states.update({k: [new(blocks(p), torch.uint8) for p in self.params] for k in ("m_exp", "v_exp")})
+        self._states = {k: list(states[k]) for k in (("m", "v", "m_exp", "v_exp") if eight else ("m", "v"))}
+        if any(len(t) != len(self.params) for t in (*self._states.values(), self.copies)):
+            raise ValueError("as many moments and copies as parameters are needed")
+        self._desc = (M.AdamWTensor * len(self.params))()
+        for i, p in enumerate(self.params):
+            for k, t in self._states.items():
+                self._tensor(t[i], k, held, blocks(p) if k.endswith("exp") else p.numel())
+            if self.copies[i] is not None:
+                self._tensor(self.copies[i], "a copy", torch.bfloat16, p.numel())
+        self._config = M.AdamWConfig(seed=self.seed, moments=M.MOMENTS_8BIT if eight else M.MOMENTS_32BIT)
+
+    def _tensor(self, t, name, dtype, n):
+        if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.device or not t.is_cuda:
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} values on the parameters' GPU")
+
+    def states(self) -> dict:
+        """The moments: m and v, with 8 bits their codes and m_exp and v_exp."""
+        return {k: list(t) for k, t in self._states.items()}
+
+    def _describe(self):
+        s = self._states
+        for i, (d, p) in enumerate(zip(self._desc, self.params)):
+            d.p, d.n, d.m, d.v = p.data_ptr(), p.numel(), s["m"][i].data_ptr(), s["v"][i].data_ptr()
+            if self.state == "f8":
+                d.m_exp, d.v_exp = s["m_exp"][i].data_ptr(), s["v_exp"][i].data_ptr()
+            d.copy = self.copies[i].data_ptr() if self.copies[i] is not None else None
+
+    def step(self, grads: Sequence[Optional[torch.Tensor]], *, step=None, grad_scale=1.0):
+        """One step with a gradient for each parameter, all float32 or all bfloat16; a parameter whose gradient is None stays as
+        it is.  step: the step's number, counted from 1 (by itself if left out), or an int64 tensor on the GPU that the kernels
+        read it from, which a captured graph needs.  grad_scale: a factor of the gradients, a number or a float32 tensor on the GPU."""
+        if len(grads) != len(self.params):
+            raise ValueError("as many gradients as parameters are needed")
+        dtype = next((g.dtype for g in grads if g is not None), torch.float32)
+        if dtype not in _TYPES:
+            raise ValueError("gradients must be float32 or bfloat16")
+        self._describe()
+        for d, p, g in zip(self._desc, self.params, grads):
+            if g is None:
+                d.n = 0
+                continue
+            self._tensor(g, "a gradient", dtype, p.numel())
+            d.grad = g.data_ptr()
+        c = self._config
+        c.lr, (c.beta1, c.beta2), c.eps, c.weight_decay, c.grad_dtype = self.lr, self.betas, self.eps, self.weight_decay, _TYPES[dtype]
+        c.step_dev = c.grad_scale_dev = None
+        c.grad_scale = 1.0
+        if isinstance(grad_scale, torch.Tensor):
+            self._tensor(grad_scale, "grad_scale", torch.float32, 1)
+            c.grad_scale_dev = grad_scale.data_ptr()
+        else:
+            c.grad_scale = grad_scale
+        if isinstance(step, torch.Tensor):
+            self._tensor(step, "step", torch.int64, 1)
+            c.step_dev = step.data_ptr()
+        else:
+            c.step = self.steps + 1 if step is None else step
+        _queue(self.device, M.moe_spec_adamw_step, self._desc, len(self._desc), c)
+        if not isinstance(step, torch.Tensor):
+            self.steps = c.step
+
+    def read_moments(self, m_out: Optional[List[torch.Tensor]] = None, v_out: Optional[List[torch.Tensor]] = None):
+        """The values of 8-bit moments, into float32 or bfloat16 tensors (bfloat16 holds them exactly) or new float32 ones
+        -> (m, v)."""
+        if self.state != "f8":
+            raise ValueError("32-bit moments are tensors of their own: states()")
+        if m_out is None and v_out is None:
+            m_out, v_out = ([torch.empty_like(p) for p in self.params] for _ in range(2))
+        given = [t for out in (m_out, v_out) if out is not None for t in out]
+        dtype = given[0].dtype
+        if dtype not in _TYPES or any(out is not None and len(out) != len(self.params) for out in (m_out, v_out)):
+            raise ValueError("a float32 or bfloat16 tensor for each parameter is needed")
+        for out in (m_out, v_out):
+            for t, p in zip(out or (), self.params):
+                self._tensor(t, "an output", dtype, p.numel())
+        self._describe()
+        pointers = lambda out: None if out is None else (C.c_void_p * len(out))(*[t.data_ptr() for t in out])  # noqa: E731
+        _queue(self.device, M.moe_spec_adamw_read_moments, self._desc, len(self._desc), _TYPES[dtype], pointers(m_out), pointers(v_out))
+        return m_out, v_out

@@ -1,0 +1,735 @@
+"""The training operators against their formulas in 64 bits.
+
+Tolerances.  u = 2^-24 is half a step of float, `half(t)` that of an output's type.  A sum of n terms in a tree or chain of
+depth d is off by at most d u times the sum of the magnitudes; each further operation adds one u of its result.  Every bound
+below is such a count, written beside it; what goes out as bfloat16 is off by half a step of that on top."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def half(t):
+    return torch.finfo(t).eps / 2
+
+
+def rng(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def on_gpu(t, dtype=None):
+    return t.to(device="cuda", dtype=dtype or t.dtype)
+
+
+def close(got, want, bound, what):
+    """Everywhere |got - want| <= bound, in 64 bits on the CPU."""
+    got = got.detach().cpu().double()
+    assert got.shape == want.shape, what
+    off = (got - want).abs() - bound
+    worst = off.max().item() if off.numel() else -1.0
+    assert not math.isnan(worst) and worst <= 0.0, f"{what}: over its bound by {worst:.3e}, largest error {(got - want).abs().max().item():.3e}"
+
+
+# ------------------------------------------------------------------------------------------------ LayerNorm
+def ln_inputs(rows, cols, dtype, seed, offset=0.0):
+    g = rng(seed)
+    x = (torch.randn(rows, cols, generator=g) * (0.5 + torch.rand(rows, 1, generator=g)) + offset).to(TYPES[dtype])
+    dy = torch.randn(rows, cols, generator=g).to(TYPES[dtype])
+    return x, dy, 1.0 + 0.2 * torch.randn(cols, generator=g), 0.3 * torch.randn(cols, generator=g)
+
+
+def ln_forward_checks(x, gain, bias, eps, got, dtype, what):
+    """Depth of a row's sums: 16 values of a lane, 6 steps over a wavefront, 8 wavefronts: 30, and a division."""
+    y, mean, rstd = got
+    x = x.double()
+    g = torch.ones(x.shape[1], dtype=torch.float64) if gain is None else gain.double()
+    b = torch.zeros(x.shape[1], dtype=torch.float64) if bias is None else bias.double()
+    mu = x.mean(1, keepdim=True)
+    var = (x - mu).square().mean(1, keepdim=True)
+    r = 1.0 / torch.sqrt(var + eps)
+    size = x.abs().mean(1, keepdim=True)
+    off_mean = 32 * U * size
+    close(mean, mu[:, 0], off_mean[:, 0], what + " mean")
+    # variance: 36 u of itself and the square of the mean's error; rstd half of its relative error, and two operations
+    off_r = r * (0.5 * (36 * U * var + off_mean ** 2) / (var + eps) + 4 * U)
+    close(rstd, r[:, 0], off_r[:, 0], what + " rstd")
+    h = (x - mu) * r
+    want = h * g + b
+    bound = g.abs() * (r * off_mean + h.abs() * (off_r / r + 4 * U)) + 2 * U * (b.abs() + want.abs()) + half(TYPES[dtype]) * want.abs() * 1.01
+    close(y, want, bound, what + " y")
+
+
+SHAPES = [(1, 1), (1, 8), (3, 7), (5, 64), (33, 65), (2, 128), (70, 129), (9, 256), (17, 511), (130, 512), (7, 720), (5, 1023), (6, 1024),
+          (3, 1025), (11, 2048), (4, 2049), (9, 2880), (5, 4096), (3, 4097), (2, 8191), (3, 8192), (4100, 40), (2300, 1024)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_layernorm_forward(rows, cols, dtype):
+    from paper_2603_19289_amd import training as T
+    x, _, gain, bias = ln_inputs(rows, cols, dtype, rows * 10007 + cols, offset=0.5)
+    got = T.layernorm_forward(on_gpu(x), on_gpu(gain), on_gpu(bias), 1e-5)
+    ln_forward_checks(x, gain, bias, 1e-5, got, dtype, f"{rows}x{cols}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_layernorm_backward(rows, cols, dtype):
+    from paper_2603_19289_amd import training as T
+    x, dy, gain, _ = ln_inputs(rows, cols, dtype, rows * 10007 + cols + 1)
+    xd, d = x.double(), dy.double()
+    mean = xd.mean(1).float()
+    rstd = (1.0 / torch.sqrt((xd - mean.double()[:, None]).square().mean(1) + 1e-5)).float()
+    dx, dgain, dbias = T.layernorm_backward(on_gpu(dy), on_gpu(x), on_gpu(mean), on_gpu(rstd), on_gpu(gain))
+    mu, r, g = mean.double()[:, None], rstd.double()[:, None], gain.double()
+    h = (xd - mu) * r                                     # two roundings in float
+    w = d * g                                             # one
+    c1, c2 = w.mean(1, keepdim=True), (w * h).mean(1, keepdim=True)
+    want = r * (w - c1 - h * c2)
+    # sums of depth 30 over terms of up to four roundings, a product; then three operations on what they give
+    terms = 36 * U * (w.abs().mean(1, keepdim=True) + h.abs() * (w * h).abs().mean(1, keepdim=True)) + 8 * U * (w.abs() + c1.abs() + (h * c2).abs())
+    close(dx, want, r * terms + half(TYPES[dtype]) * want.abs() * 1.01 + 2 * U * want.abs(), "dx")
+    # a lane adds up at most rows / 256 + 1 rows, 6 steps join the rows of a wavefront, 4 wavefronts; the rest is in double
+    depth = rows / 256 + 16
+    close(dgain, (d * h).sum(0), depth * U * (d * h).abs().sum(0), "dgain")
+    close(dbias, d.sum(0), depth * U * d.abs().sum(0), "dbias")
+
+
+def test_layernorm_backward_against_differences():
+    """The gradient as the slope of sum(w * y): central differences of the forward formula in 64 bits."""
+    from paper_2603_19289_amd import training as T
+    x, dy, gain, bias = ln_inputs(3, 12, "f32", 5)
+    f = lambda x, g, b: (dy.double() * (((x - x.mean(1, keepdim=True)) / torch.sqrt(x.var(1, correction=0, keepdim=True) + 1e-5)) * g + b)).sum()  # noqa: E731
+    _, mean, rstd = T.layernorm_forward(on_gpu(x), on_gpu(gain), on_gpu(bias), 1e-5)
+    got = T.layernorm_backward(on_gpu(dy), on_gpu(x), mean, rstd, on_gpu(gain))
+    args = [x.double(), gain.double(), bias.double()]
+    for k, t in enumerate(args):
+        slope = torch.zeros_like(t)
+        for i in range(t.numel()):
+            up, down = [a.clone() for a in args], [a.clone() for a in args]
+            up[k].view(-1)[i] += 1e-5
+            down[k].view(-1)[i] -= 1e-5
+            slope.view(-1)[i] = (f(*up) - f(*down)) / 2e-5
+        # differences: 1e-10 of a third derivative that is at most some hundreds here, and 1e-16 / 1e-5; float: 64 u of sums below 40
+        close(got[k], slope, torch.full_like(slope, 64 * U * 40 + 1e-6), ("dx", "dgain", "dbias")[k])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [40, 720, 2880])
+def test_layernorm_strided_odd_and_in_place(cols, dtype):
+    """Rows of a wider matrix that begin at odd elements, no gain or bias, one row for all, y over x; what lies between the rows
+    and behind the last one stays."""
+    from paper_2603_19289_amd import moe_spec as M
+    from paper_2603_19289_amd import training as T
+    rows = 37
+    x, dy, gain, bias = ln_inputs(rows, cols, dtype, 77)
+    wide = torch.full((rows + 2, cols + 13), 9.0, dtype=TYPES[dtype], device="cuda")
+    inner = wide[1:rows + 1, 3:3 + cols]
+    inner.copy_(on_gpu(x))
+    ln_forward_checks(x, None, None, 0.0, T.layernorm_forward(inner, eps=0.0), dtype, "strided")
+    dx, dgain, dbias = T.layernorm_backward(on_gpu(dy), inner, *T.layernorm_forward(inner)[1:])
+    same = T.layernorm_backward(on_gpu(dy), on_gpu(x), *T.layernorm_forward(on_gpu(x))[1:])
+    for a, b in zip((dx, dgain, dbias), same):
+        assert torch.equal(a, b)
+    got = T.layernorm_forward(inner, on_gpu(gain), on_gpu(bias), out=inner)
+    ln_forward_checks(x, gain, bias, 1e-5, got, dtype, "in place")
+    outside = wide.clone()
+    outside[1:rows + 1, 3:3 + cols] = 9.0
+    assert torch.equal(outside, torch.full_like(outside, 9.0))
+    one = on_gpu(x)[:1].expand(rows, cols)                 # every row the same memory
+    y, _, _ = T.layernorm_forward(one)
+    assert torch.equal(y, y[:1].expand(rows, cols))
+    bound = M.moe_spec_layernorm_backward_workspace_bytes(rows, cols)
+    assert bound >= 2 * cols * 4
+
+
+def test_layernorm_rows_that_are_constant_or_not_finite():
+    from paper_2603_19289_amd import training as T
+    x, dy, gain, bias = ln_inputs(6, 300, "f32", 3)
+    x[0] = 7.25
+    x[1] = 0.0
+    x[2, 17], x[3, 299], x[4, 0] = float("nan"), float("inf"), float("-inf")
+    y, mean, rstd = T.layernorm_forward(on_gpu(x), on_gpu(gain), on_gpu(bias), 1e-5)
+    fine = [0, 1, 5]
+    ln_forward_checks(x[fine], gain, bias, 1e-5, (y[fine], mean[fine], rstd[fine]), "f32", "finite rows")
+    assert not torch.isfinite(y[2:5]).any()
+    dx, dgain, _ = T.layernorm_backward(on_gpu(dy), on_gpu(x), mean, rstd, on_gpu(gain))
+    assert torch.isfinite(dx[fine]).all() and not torch.isfinite(dx[2:5]).any() and torch.isnan(dgain).all()
+
+
+def test_layernorm_without_rows_and_partial_outputs():
+    from paper_2603_19289_amd import training as T
+    x = torch.empty(0, 48, device="cuda")
+    y, mean, rstd = T.layernorm_forward(x)
+    assert y.shape == (0, 48) and mean.shape == rstd.shape == (0,)
+    dx, dgain, dbias = T.layernorm_backward(x, x, mean, rstd)
+    assert dx.shape == (0, 48) and not dgain.any() and not dbias.any()
+    x, dy, gain, _ = ln_inputs(50, 720, "bf16", 4)
+    x, dy, gain = on_gpu(x), on_gpu(dy), on_gpu(gain)
+    _, mean, rstd = T.layernorm_forward(x)
+    full = T.layernorm_backward(dy, x, mean, rstd, gain)
+    only = T.layernorm_backward(dy, x, mean, rstd, gain, weight_grads=False)
+    assert only[1] is None and torch.equal(only[0], full[0])
+    rest = T.layernorm_backward(dy, x, mean, rstd, gain, input_grad=False)
+    assert rest[0] is None and torch.equal(rest[1], full[1]) and torch.equal(rest[2], full[2])
+
+
+# ------------------------------------------------------------------------------------------------ losses
+def kl_oracle(student, teacher, tau, valid):
+    """Loss, gradient, and their bounds.  A softmax value: its exponent is off by 4 u max|z / tau| (two roundings in z / tau on
+    either side of the difference) and |a| u, a sum of 8 + 5 terms, a root operation or two: relative u (24 + 6 max|z / tau|).  The
+    row's loss: terms p (a - b) of that relative error and the two logarithms."""
+    zt, zs = teacher.double() / tau, student.double() / tau
+    nothing = (zt == -math.inf).all(1)
+    finite = lambda z: torch.where(torch.isfinite(z), z.abs(), torch.zeros_like(z)).amax(1, keepdim=True)  # noqa: E731
+    big = finite(zt) + finite(zs)
+    zt = torch.where(nothing[:, None], torch.zeros_like(zt), zt)
+    p = torch.softmax(zt, 1)
+    none = (zs == -math.inf).all(1, keepdim=True)
+    q = torch.where(none, torch.zeros_like(zs), torch.softmax(torch.where(none, torch.zeros_like(zs), zs), 1))
+    log_q = torch.where(none, torch.full_like(zs, -math.inf), torch.log_softmax(torch.where(none, torch.zeros_like(zs), zs), 1))
+    log_p = torch.log_softmax(zt, 1)
+    terms = torch.where(p > 0, p * (log_p - log_q), torch.zeros_like(p))
+    live = torch.ones(len(p), dtype=torch.bool) if valid is None else valid
+    n = live.sum().clamp(min=1).double()
+    use = live & ~nothing
+    loss = terms.sum(1)[use].sum() / n
+    grad = torch.where(use[:, None], (q - p) / n / tau, torch.zeros_like(p))
+    rel = U * (24 + 6 * big)
+    off_loss = ((rel[:, 0] + 20 * U) * (terms.abs().sum(1) + (p * (torch.where(p > 0, log_p, torch.zeros_like(p))).abs()).sum(1) + 12 + big[:, 0]))[use].sum() / n
+    return loss, grad, off_loss + 4 * U * loss.abs(), torch.where(use[:, None], rel * (p + q) / n / tau, torch.zeros_like(p)) + 4 * U * grad.abs()
+
+
+def logits(rows, experts, seed, scale=2.0):
+    g = rng(seed)
+    t = torch.randn(rows, experts, generator=g) * scale
+    return t, 0.7 * t + torch.randn(rows, experts, generator=g), torch.rand(rows, generator=g) < 0.7, g
+
+
+LOSS_SHAPES = [(1, 2), (1, 1), (5, 8), (301, 32), (64, 7), (33, 9), (1000, 128), (17, 129), (70, 250), (257, 256), (2050, 64), (9000, 3), (40000, 16)]
+
+
+@pytest.mark.parametrize("student_type,teacher_type,tau,masked", [("f32", "f32", 1.0, False), ("bf16", "f32", 1.0, True), ("f32", "bf16", 2.5, True),
+                                                                 ("bf16", "bf16", 0.5, False)])
+@pytest.mark.parametrize("rows,experts", LOSS_SHAPES)
+def test_distill_loss(rows, experts, student_type, teacher_type, tau, masked):
+    from paper_2603_19289_amd import training as T
+    t, s, valid, _ = logits(rows, experts, rows * 1009 + experts)
+    t, s = t.to(TYPES[teacher_type]), s.to(TYPES[student_type])
+    valid = valid if masked else None
+    loss, grad = T.distill_loss(on_gpu(s), on_gpu(t), temperature=tau, valid=on_gpu(valid) if masked else None)
+    want, dz, off, off_dz = kl_oracle(s, t, tau, valid)
+    close(loss, want, off, "loss")
+    assert grad.dtype == s.dtype
+    close(grad, dz, off_dz + half(s.dtype) * dz.abs() * 1.01 + 1e-40, "gradient")
+    alone, none = T.distill_loss(on_gpu(s), on_gpu(t), temperature=tau, valid=on_gpu(valid) if masked else None, grad=False)
+    assert none is None and torch.equal(alone, loss)
+
+
+def test_distill_loss_against_differences():
+    from paper_2603_19289_amd import training as T
+    t, s, valid, _ = logits(5, 6, 9)
+    valid[:] = torch.tensor([True, False, True, True, True])
+    _, grad = T.distill_loss(on_gpu(s), on_gpu(t), temperature=1.5, valid=on_gpu(valid))
+    slope = torch.zeros(5, 6, dtype=torch.float64)
+    for i in range(30):
+        both = []
+        for sign in (1, -1):
+            z = s.double().clone()
+            z.view(-1)[i] += sign * 1e-5
+            both.append(kl_oracle(z, t.double(), 1.5, valid)[0])
+        slope.view(-1)[i] = (both[0] - both[1]) / 2e-5
+    close(grad, slope, torch.full_like(slope, 1e-6), "gradient")   # below 1: 50 u, and 1e-10 and 1e-16 / 1e-5 of the differences
+
+
+def balance_oracle(z, ids, coef, valid):
+    """A probability is off by u (24 + 2 max|z|) of itself as above, f by 3 u, their sum over a row by 13 u more."""
+    z = z.double()
+    rows, experts = z.shape
+    live = torch.ones(rows, dtype=torch.bool) if valid is None else valid
+    dead = (z == -math.inf).all(1)
+    p = torch.where(dead[:, None], torch.zeros_like(z), torch.softmax(torch.where(dead[:, None], torch.zeros_like(z), z), 1))
+    chosen = ids[live].reshape(-1).long()
+    counts = torch.bincount(chosen[(chosen >= 0) & (chosen < experts)], minlength=experts)
+    n = live.sum().clamp(min=1).double()
+    f = counts.double() / n / ids.shape[1]
+    inner = p @ f
+    scale = coef * experts / n
+    loss = scale * inner[live].sum()
+    grad = torch.where(live[:, None], scale * p * (f - inner[:, None]), torch.zeros_like(p))
+    big = torch.where(torch.isfinite(z), z.abs(), torch.zeros_like(z)).amax(1, keepdim=True)
+    rel = U * (48 + 4 * big)
+    off = abs(scale) * (rel[:, 0] * inner)[live].sum() + 4 * U * loss.abs()
+    off_grad = torch.where(live[:, None], abs(scale) * rel * p * (f + inner[:, None]), torch.zeros_like(p))
+    return loss, counts, grad, off, off_grad
+
+
+@pytest.mark.parametrize("dtype,masked", [("f32", False), ("bf16", True)])
+@pytest.mark.parametrize("rows,experts", LOSS_SHAPES)
+def test_balance_loss(rows, experts, dtype, masked):
+    from paper_2603_19289_amd import training as T
+    z, _, valid, g = logits(rows, experts, rows * 1013 + experts)
+    z = z.to(TYPES[dtype])
+    k = min(experts, 1 + rows % 8)
+    ids = torch.rand(rows, experts, generator=g).topk(k, 1).indices.to(torch.int32)
+    valid = valid if masked else None
+    loss, counts, grad = T.balance_loss(on_gpu(z), on_gpu(ids), coef=0.03, valid=on_gpu(valid) if masked else None)
+    want, want_counts, dz, off, off_dz = balance_oracle(z, ids, 0.03, valid)
+    assert torch.equal(counts.cpu().long(), want_counts)
+    close(loss, want, off, "loss")
+    close(grad, dz, off_dz + half(z.dtype) * dz.abs() * 1.01 + 1e-40, "gradient")
+    alone = T.balance_loss(on_gpu(z), on_gpu(ids), coef=0.03, valid=on_gpu(valid) if masked else None, grad=False)
+    assert alone[2] is None and torch.equal(alone[0], loss) and torch.equal(alone[1], counts)
+
+
+def test_balance_loss_ids_that_repeat_or_are_no_choice():
+    """An id twice in a row counts twice, one outside the experts not at all; a uniform router with even choices gives coef."""
+    from paper_2603_19289_amd import training as T
+    ids = torch.tensor([[0, 0, 3], [-1, 2, 2], [4, 7, 1], [-2147483648, 2147483647, 3]], dtype=torch.int32)
+    z = torch.randn(4, 4, generator=rng(1))
+    loss, counts, grad = T.balance_loss(on_gpu(z), on_gpu(ids), coef=0.5)
+    want, want_counts, dz, off, off_dz = balance_oracle(z, ids, 0.5, None)
+    assert counts.tolist() == want_counts.tolist() == [2, 1, 2, 2]
+    close(loss, want, off, "loss")
+    close(grad, dz, off_dz + U * dz.abs(), "gradient")
+    even = torch.arange(64, dtype=torch.int32).view(32, 2) % 8
+    loss, counts, grad = T.balance_loss(torch.zeros(32, 8, device="cuda"), on_gpu(even), coef=0.25)
+    assert counts.tolist() == [8] * 8 and loss.item() == 0.25 and not grad.any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_losses_with_masked_and_non_finite_logits(dtype):
+    """Minus infinity is probability zero on either side; rows that nothing is left of; NaN and infinities spoil their own row
+    only, and none where the row does not count; the type's lowest value is an ordinary logit."""
+    from paper_2603_19289_amd import training as T
+    t, s, _, _ = logits(12, 20, 42)
+    t, s = t.to(TYPES[dtype]), s.to(TYPES[dtype])
+    inf, low = math.inf, torch.finfo(TYPES[dtype]).min
+    t[0, 3:9] = s[0, 3:9] = -inf                      # both masked
+    t[1, :19] = -inf                                  # one expert left
+    t[2] = -inf                                       # nothing to teach
+    t[3, 5] = low
+    s[4, :7] = low
+    valid = torch.ones(12, dtype=torch.bool)
+    valid[9:] = False
+    s[9, 1], t[10, 2], s[11] = math.nan, inf, -inf    # rows that do not count
+    loss, grad = T.distill_loss(on_gpu(s), on_gpu(t), valid=on_gpu(valid))
+    tt, ss = t.clone(), s.clone()
+    tt[9:], ss[9:] = 0, 0
+    want, dz, _, _ = kl_oracle(ss, tt, 1.0, valid)
+    # the row with the type's lowest values: a term of about 1e38 of them all, of which 30 u count
+    close(loss, want, want.abs() * 64 * U, "loss")
+    close(grad, dz, (80 * U + half(TYPES[dtype]) * 1.01) * dz.abs() + 80 * U / 9, "gradient")
+    assert not grad[2].any() and not grad[9:].any()
+    s[5, 2] = -inf                                    # the teacher wants it: an infinite loss, a finite gradient
+    loss, grad = T.distill_loss(on_gpu(s), on_gpu(t), valid=on_gpu(valid))
+    assert loss.item() == inf and torch.isfinite(grad).all()
+    s[6] = -inf
+    loss, grad = T.distill_loss(on_gpu(s), on_gpu(t), valid=on_gpu(valid))
+    assert loss.item() == inf and torch.isfinite(grad).all()
+    close(grad[6], -torch.softmax(t[6].double(), 0) / 9, half(TYPES[dtype]) / 4 + 1e-6, "gradient against a student with nothing")
+    s[7, 0], t[8, 4] = math.nan, inf
+    loss, grad = T.distill_loss(on_gpu(s), on_gpu(t), valid=on_gpu(valid))
+    assert math.isnan(loss.item()) and torch.isnan(grad[7:9]).all() and torch.isfinite(grad[[0, 1, 2, 3, 4, 5, 6, 9, 10, 11]]).all()
+
+    z = t.clone()
+    z[8, 4] = 0.0
+    ids = (torch.arange(24, dtype=torch.int32).view(12, 2) * 7) % 20
+    loss, counts, grad = T.balance_loss(on_gpu(z), on_gpu(ids), valid=on_gpu(valid))
+    zz = z.clone()
+    zz[9:] = 0
+    want, want_counts, dz, off, off_dz = balance_oracle(torch.where(zz < -1e30, torch.full_like(zz, -inf), zz), ids, 1.0, valid)
+    assert torch.equal(counts.cpu().long(), want_counts) and not grad[2].any() and not grad[9:].any()
+    close(loss, want, off, "balance")
+    close(grad, dz, off_dz + half(TYPES[dtype]) * dz.abs() * 1.01, "balance gradient")
+    z[3, 0] = math.nan
+    loss, counts, grad = T.balance_loss(on_gpu(z), on_gpu(ids), valid=on_gpu(valid))
+    assert math.isnan(loss.item()) and torch.isnan(grad[3]).all() and torch.isfinite(grad[[0, 1, 2, 4, 5, 6, 7, 8]]).all()
+
+
+def test_losses_without_rows_or_valid_rows():
+    from paper_2603_19289_amd import training as T
+    z = torch.empty(0, 8, device="cuda")
+    loss, grad = T.distill_loss(z, z)
+    assert loss.item() == 0.0 and grad.shape == (0, 8)
+    loss, counts, _ = T.balance_loss(z, torch.empty(0, 2, dtype=torch.int32, device="cuda"))
+    assert loss.item() == 0.0 and not counts.any()
+    for rows in (3, 5000):
+        z = torch.randn(rows, 8, device="cuda")
+        z[1] = math.nan
+        none = torch.zeros(rows, dtype=torch.uint8, device="cuda")
+        loss, grad = T.distill_loss(z, z, valid=none)
+        assert loss.item() == 0.0 and not grad.any()
+        loss, counts, grad = T.balance_loss(z, torch.ones(rows, 2, dtype=torch.int32, device="cuda"), valid=none)
+        assert loss.item() == 0.0 and not counts.any() and not grad.any()
+
+
+@pytest.mark.parametrize("experts", [30, 128])
+def test_losses_strided_odd_and_in_place(experts):
+    """Views of wider matrices at odd elements and odd mask addresses; the gradient over the student's logits (C entry)."""
+    from paper_2603_19289_amd import moe_spec as M
+    from paper_2603_19289_amd import training as T
+    rows = 333
+    t, s, valid, g = logits(rows, experts, 8)
+    s = s.to(torch.bfloat16)
+    ids = torch.rand(rows, experts, generator=g).topk(3, 1).indices.to(torch.int32)
+    wide_s = torch.zeros(rows, experts + 5, dtype=torch.bfloat16, device="cuda")
+    wide_t = torch.zeros(rows, experts + 3, device="cuda")
+    wide_i = torch.full((rows, 9), -5, dtype=torch.int32, device="cuda")
+    wide_v = torch.zeros(rows + 1, dtype=torch.bool, device="cuda")
+    vs, vt, vi, vv = wide_s[:, 3:3 + experts], wide_t[:, 1:1 + experts], wide_i[:, 4:7], wide_v[1:]
+    vs.copy_(on_gpu(s)), vt.copy_(on_gpu(t)), vi.copy_(on_gpu(ids)), vv.copy_(on_gpu(valid))
+    plain = T.distill_loss(on_gpu(s), on_gpu(t), valid=on_gpu(valid))
+    for a, b in zip(T.distill_loss(vs, vt, valid=vv), plain):
+        assert torch.equal(a, b)
+    for a, b in zip(T.balance_loss(vs, vi, valid=vv), T.balance_loss(on_gpu(s), on_gpu(ids), valid=on_gpu(valid))):
+        assert torch.equal(a, b)
+    need = M.moe_spec_distill_loss_workspace_bytes(rows, experts)
+    space, loss = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty((), device="cuda")
+    M.moe_spec_distill_loss(torch.cuda.current_stream().cuda_stream, M.BF16, vs.data_ptr(), vs.stride(0), M.F32, vt.data_ptr(), vt.stride(0),
+                            rows, experts, 1.0, vv.data_ptr(), loss.data_ptr(), vs.data_ptr(), vs.stride(0), space.data_ptr(), need)
+    assert torch.equal(loss, plain[0]) and torch.equal(vs, plain[1])
+    assert not wide_s[:, :3].any() and not wide_s[:, 3 + experts:].any()
+
+
+# ------------------------------------------------------------------------------------------------ AdamW
+F = np.float32
+ODD1, ODD2 = 0x9E3779B1, 0x85EBCA77
+
+
+def mix(x):
+    x &= 0xffffffff
+    x = ((x ^ (x >> 16)) * ODD1) & 0xffffffff
+    x = ((x ^ (x >> 15)) * ODD2) & 0xffffffff
+    return x ^ (x >> 16)
+
+
+def noise(seed, step, place, n):
+    """32 random bits for each element of the tensor at a place of the call."""
+    key1 = mix(mix(seed + ODD1 * step) + ODD2 * (place + 1))
+    key2 = mix(key1 ^ ODD1)
+    x = (np.arange(n, dtype=np.uint64) + np.uint64(key1)) & np.uint64(0xffffffff)
+    x = ((x ^ (x >> np.uint64(16))) * np.uint64(ODD1)) & np.uint64(0xffffffff)
+    x = (((x ^ (x >> np.uint64(15))) + np.uint64(key2)) * np.uint64(ODD2)) & np.uint64(0xffffffff)
+    return (x ^ (x >> np.uint64(16))).astype(np.uint32)
+
+
+def blocks_of(x):
+    return np.concatenate([x, np.zeros(-len(x) % 128, x.dtype)]).reshape(-1, 128)
+
+
+def encode(x, drop, bits):
+    """Codes and exponents by the written rule, from the values and 16 random bits each."""
+    n, low = len(x), 23 - drop
+    y, r = blocks_of(x.astype(np.float64)), blocks_of(bits).astype(np.float64)
+    size = np.abs(y)
+    top = np.where(np.isfinite(size), size, 0.0).max(1, keepdims=True)
+    X = np.maximum(np.frexp(top)[1] - 1 + 127, 0) * (top > 0)
+    ratio = np.where(np.isfinite(size), size, 0.0) * 2.0 ** (14.0 - X + 126)     # in units where field 1 begins at 1
+    field = np.maximum(np.frexp(np.maximum(ratio, 1e-300))[1] - 1, 0)
+    code = np.floor(ratio / 2.0 ** (field - low) + (r + 0.5) / 65536)            # mantissa units above the field's start (or 0)
+    code = np.where(ratio >= 1.0, field * 2 ** low + code, code)
+    if drop == 19:
+        code = np.where((size > 0) & (code == 0), 1, code)
+    code = np.where(np.isfinite(size), code, 127 if drop == 20 else 255)
+    if drop == 20:
+        code = code + 128 * np.signbit(y)
+    return code.astype(np.uint8).reshape(-1)[:n], X.astype(np.uint8).reshape(-1)
+
+
+def decode(code, X, drop):
+    low = 23 - drop
+    c = blocks_of(code.astype(np.int64))
+    size = c & 0x7f if drop == 20 else c
+    field, part = size >> low, (size & (2 ** low - 1)) / 2.0 ** low
+    value = np.where(field > 0, 1.0 + part, part) * 2.0 ** (np.maximum(field, 1) - 127.0 + X[:, None].astype(np.float64) - 14)
+    value = np.where(size == (127 if drop == 20 else 255), np.nan, value)
+    return (np.where((c > 127) & (drop == 20), -value, value)).reshape(-1)[:len(code)].astype(F)
+
+
+def adam_float(p, g, m, v, lr, b1, b2, eps, wd, t, scale=1.0):
+    """The step in float, one rounding an operation."""
+    with np.errstate(all="ignore"):
+        g = g * F(scale)
+        m = m * F(b1) + g * F(1.0 - b1)
+        v = v * F(b2) + (g * g) * F(1.0 - b2)
+        root = np.sqrt(v) * F(1.0 / math.sqrt(1.0 - b2 ** t)) + F(eps)
+        return p * F(1.0 - lr * wd) - (m / root) * F(lr / (1.0 - b1 ** t)), m, v
+
+
+SIZES = [1, 7, 8, 127, 128, 129, 2047, 2048, 2049, 5000, 3, 0, 12345]
+
+
+def adam_case(sizes, seed, grad_type):
+    g = rng(seed)
+    params = [torch.randn(n, generator=g) * 0.05 for n in sizes]
+    grads = [[(torch.randn(n, generator=g) * 10.0 ** (-4 * torch.rand(n, generator=g))).to(TYPES[grad_type]) for n in sizes] for _ in range(4)]
+    return params, grads
+
+
+@pytest.mark.parametrize("state", ["f32", "f8"])
+@pytest.mark.parametrize("grad_type", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes", [[12345], SIZES, [300] * 45 + SIZES + [17] * 50])
+def test_adamw_equals_its_formula_bit_for_bit(sizes, grad_type, state):
+    """Four steps: parameters, moments (codes and exponents with 8 bits) and copies equal the float formula's."""
+    from paper_2603_19289_amd import training as T
+    params, grads = adam_case(sizes, 31, grad_type)
+    hyper = dict(lr=2e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.1)
+    dev = [on_gpu(p) for p in params]
+    copies = [torch.zeros(p.shape, dtype=torch.bfloat16, device="cuda") if i % 3 else None for i, p in enumerate(params)]
+    opt = T.AdamW(dev, state=state, copies=copies, seed=99, **hyper)
+    for step in range(4):
+        opt.step([on_gpu(g) for g in grads[step]], grad_scale=0.75)
+    held = opt.states()
+    if state == "f8":
+        read_m, read_v = opt.read_moments()
+    assert opt.steps == 4
+    for i, p in enumerate(params):
+        n = len(p)
+        q, m, v = p.numpy(), np.zeros(n, F), np.zeros(n, F)
+        if state == "f8":
+            cm, em, cv, ev = (np.zeros(k, np.uint8) for k in (n, -(-n // 128), n, -(-n // 128)))
+        for t in range(1, 5):
+            q, m, v = adam_float(q, grads[t - 1][i].float().numpy(), m, v, 2e-3, 0.9, 0.999, 1e-8, 0.1, t, 0.75)
+            if state == "f8":
+                r = noise(99, t, i, n)
+                (cm, em), (cv, ev) = encode(m, 20, r >> 16), encode(v, 19, r & 0xffff)
+                m, v = decode(cm, em, 20), decode(cv, ev, 19)
+        assert np.array_equal(dev[i].cpu().numpy(), q), i
+        if state == "f8":
+            for key, want in (("m", cm), ("m_exp", em), ("v", cv), ("v_exp", ev)):
+                assert np.array_equal(held[key][i].cpu().numpy(), want), (i, key)
+            assert np.array_equal(read_m[i].cpu().numpy(), m) and np.array_equal(read_v[i].cpu().numpy(), v)
+        else:
+            assert np.array_equal(held["m"][i].cpu().numpy(), m) and np.array_equal(held["v"][i].cpu().numpy(), v)
+        if copies[i] is not None:
+            assert torch.equal(copies[i].cpu(), torch.from_numpy(q).to(torch.bfloat16))
+
+
+def test_adamw_against_64_bits():
+    """One operation after the other, each half a step of float off: m and v three of them, the update ten."""
+    from paper_2603_19289_amd import training as T
+    params, grads = adam_case([4001], 7, "f32")
+    p = on_gpu(params[0])
+    opt = T.AdamW([p], lr=1e-2, betas=(0.8, 0.95), eps=1e-6, weight_decay=0.2)
+    q, m, v = params[0].double(), torch.zeros(4001, dtype=torch.float64), torch.zeros(4001, dtype=torch.float64)
+    moved = torch.zeros_like(q)
+    for t in range(1, 5):
+        opt.step([on_gpu(grads[t - 1][0])])
+        g = grads[t - 1][0].double()
+        m, v = 0.8 * m + 0.2 * g, 0.95 * v + 0.05 * g * g
+        update = 1e-2 * (m / (1 - 0.8 ** t)) / (torch.sqrt(v / (1 - 0.95 ** t)) + 1e-6)
+        size = 1e-2 * (sum(0.8 ** (t - j) * 0.2 * grads[j - 1][0].double().abs() for j in range(1, t + 1)) / (1 - 0.8 ** t)) / (torch.sqrt(v / (1 - 0.95 ** t)) + 1e-6)
+        moved += 3 * q.abs() + 24 * size
+        q = q * (1 - 1e-2 * 0.2) - update
+    close(p, q, U * moved * 1.01, "p")
+
+
+def test_adamw_8bit_values_at_the_edges():
+    """Blocks of zeros, of denormals, of one large value among small ones, infinities and NaN: codes by the written rule; what is
+    finite keeps its exponent, a second moment that is not zero stays so."""
+    from paper_2603_19289_amd import training as T
+    n = 128 * 9 + 5
+    g = torch.randn(n, generator=rng(2))
+    g[:128] = 0.0
+    g[128:256] *= 1e-38                                    # squares vanish, first moments are denormal
+    g[256:384] *= 1e-21                                    # squares are denormal
+    g[384:512] *= 1e-6
+    g[400] = 1000.0
+    g[512], g[640], g[641] = math.inf, math.nan, -math.inf
+    g[768:896] = math.inf
+    g[896:1024] *= 1e18
+    p = torch.zeros(n)
+    dev = on_gpu(p)
+    opt = T.AdamW([dev], lr=1e-3, betas=(0.5, 0.75), state="f8", seed=5, weight_decay=0.0)
+    m = v = np.zeros(n, F)
+    q = p.numpy()
+    for t in (1, 2):
+        opt.step([on_gpu(g)])
+        q, m, v = adam_float(q, g.numpy(), m, v, 1e-3, 0.5, 0.75, 1e-8, 0.0, t)
+        r = noise(5, t, 0, n)
+        (cm, em), (cv, ev) = encode(m, 20, r >> 16), encode(v, 19, r & 0xffff)
+        m, v = decode(cm, em, 20), decode(cv, ev, 19)
+        held = opt.states()
+        assert np.array_equal(held["m_exp"][0].cpu().numpy(), em) and np.array_equal(held["v_exp"][0].cpu().numpy(), ev), t
+        assert np.array_equal(held["m"][0].cpu().numpy(), cm) and np.array_equal(held["v"][0].cpu().numpy(), cv), t
+        assert np.array_equal(dev.cpu().numpy(), q, equal_nan=True), t
+    read_m, read_v = opt.read_moments([torch.empty(n, dtype=torch.bfloat16, device="cuda")], [torch.empty(n, dtype=torch.bfloat16, device="cuda")])
+    small = np.abs(m) < 2.0 ** -120                        # bfloat16 has no room for the last bits of denormals
+    for got, want in ((read_m[0], m), (read_v[0], v)):
+        got = got.float().cpu().numpy()
+        assert np.array_equal(np.where(small | (np.abs(want) < 2.0 ** -120), 0, got), np.where(small | (np.abs(want) < 2.0 ** -120), 0, want), equal_nan=True)
+    assert (v[(g.numpy() != 0) & (np.abs(g.numpy()) > 1e-20)] != 0).all()
+
+
+def test_adamw_8bit_moments_are_unbiased_and_move():
+    """A gradient of constant size: v goes to 1 - beta2^t as in 32 bits, on the average, although one step moves it by less than
+    the code's step.  Its noise: what is stored lies on the code's grid, so a step that moves it by d < h jumps by h with
+    probability d / h: variance d h, less what decays, 0.002 of the variance so far.  With s = t / 1000, d = 0.001 e^-s, v = 1 - e^-s
+    and h = 0.0451 v on the average over an octave (1/16 to 1/32):
+      variance = 0.0451 e^-2s (e^s - 1 - s), which at s = 1.5 is 0.00445: a standard deviation of 0.0858 of v.
+    A tenth of that for h, which is only the average.  The mean's own is 0.0858 / 256 over 65536 elements; five of them, and 0.002 for
+    beta2^t against e^-s.  m arrives at 1, which is on its grid, with probability 0.1 or more a step, and a rounding of 1e-7 seldom
+    moves it away."""
+    from paper_2603_19289_amd import training as T
+    n, steps = 65536, 1500
+    g = (torch.randint(0, 2, (n,), generator=rng(1)) * 2 - 1).float()
+    p, dg = torch.zeros(n, device="cuda"), on_gpu(g)
+    opt = T.AdamW([p], lr=0.0, betas=(0.9, 0.999), state="f8", seed=3)
+    for _ in range(steps):
+        opt.step([dg])
+    m, v = (x[0].double().cpu() for x in opt.read_moments())
+    want = 1 - 0.999 ** steps
+    assert abs((v / want).mean().item() - 1) < 5 * 0.0858 / 256 + 0.002
+    assert abs((v / want).std().item() - 0.0858) < 0.0086
+    ratio = m / g.double()
+    assert abs(ratio.mean().item() - 1) < 0.002 and ratio.std().item() < 0.01
+
+
+def test_adamw_8bit_moments_under_noisy_gradients():
+    """Normally distributed gradients, the noise as above with d = 0.001 |g^2 - v|, 0.968 v on the average: variance 500 * 0.001 *
+    0.968 v h = 0.484 v h, h between 1/32 and 1/16 around v = 1, and 0.001 of the running mean itself: a standard deviation between 0.127
+    and 0.177 (at t = 4000 all but e^-8 of it).  No bias: the mean over 65536 elements has 0.18 / 256; five of them."""
+    from paper_2603_19289_amd import training as T
+    n, steps = 65536, 4000
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    p = torch.zeros(n, device="cuda")
+    opt = T.AdamW([p], lr=0.0, betas=(0.9, 0.999), state="f8", seed=13)
+    for _ in range(steps):
+        opt.step([torch.randn(n, generator=gen, device="cuda")])
+    m, v = (x[0].double().cpu() for x in opt.read_moments())
+    want = 1 - 0.999 ** steps
+    assert abs((v / want).mean().item() - 1) < 5 * 0.18 / 256
+    assert 0.127 < (v / want).std().item() < 0.177
+    # m: a mean of variance 0.1 / 1.9, its mean over the elements 0.229 / 256
+    assert abs(m.mean().item()) < 5 * 0.235 / 256 and abs(m.std().item() - 0.2294) < 0.01
+
+
+def test_adamw_odd_addresses_and_missing_gradients():
+    """Views that begin at odd elements and bytes; a parameter without a gradient stays as it is and keeps its place in the random
+    numbers; 32 and 8 bits."""
+    from paper_2603_19289_amd import training as T
+    n = 3000
+    for state in ("f32", "f8"):
+        params, grads = adam_case([n, n], 11, "bf16")
+        results = []
+        for odd in (0, 1):
+            dev = [torch.zeros(n + 8, device="cuda")[odd:odd + n] for _ in range(2)]
+            for d, p in zip(dev, params):
+                d.copy_(on_gpu(p))
+            gr = torch.zeros(n + 8, dtype=torch.bfloat16, device="cuda")[odd:odd + n]
+            gr.copy_(on_gpu(grads[0][1]))
+            held = torch.uint8 if state == "f8" else torch.float32
+            states = {k: [torch.zeros(n + 8, dtype=held, device="cuda")[odd:odd + n] for _ in range(2)] for k in ("m", "v")}
+            states.update({k: [torch.zeros(64, dtype=torch.uint8, device="cuda")[odd:odd + 24] for _ in range(2)] for k in ("m_exp", "v_exp")})
+            copies = [torch.zeros(n + 8, dtype=torch.bfloat16, device="cuda")[odd:odd + n] for _ in range(2)]
+            opt = T.AdamW(dev, lr=1e-3, state=state, seed=4, states=states, copies=copies)
+            opt.step([None, gr])
+            assert torch.equal(dev[0].cpu(), params[0]) and not states["m"][0].any() and not copies[0].any()
+            results.append([t.clone() for t in (dev[1], states["m"][1], states["v"][1], copies[1])])
+        for a, b in zip(*results):
+            assert torch.equal(a, b)
+        assert not torch.equal(results[0][0].cpu(), params[1])
+    with pytest.raises(ValueError):
+        opt.step([None])
+    with pytest.raises(ValueError):
+        opt.step([None, gr[:5]])
+    with pytest.raises(ValueError):
+        T.AdamW([dev[0], dev[0]], lr=1e-3)
+    with pytest.raises(ValueError):
+        T.AdamW([dev[0]], lr=1e-3, states=dict(m=[dev[0]], v=[dev[1], dev[1]]))
+
+
+# ------------------------------------------------------------------------------------------------ together
+class Step:
+    """LayerNorm, a head, both losses and AdamW, as one training step of the estimator's end."""
+
+    def __init__(self, state, step=None):
+        g = rng(50)
+        self.rows, self.cols, self.experts = 300, 96, 24
+        cuda = lambda *s: torch.randn(*s, generator=g).cuda()  # noqa: E731
+        self.x, self.teacher = cuda(self.rows, self.cols), cuda(self.rows, self.experts)
+        self.valid = (torch.rand(self.rows, generator=g) < 0.8).cuda()
+        self.ids = self.teacher.topk(3, 1).indices.to(torch.int32)
+        self.gain, self.bias, self.head = 1 + 0.1 * cuda(self.cols), 0.1 * cuda(self.cols), 0.1 * cuda(self.experts, self.cols)
+        from paper_2603_19289_amd import training as T
+        self.T, self.counter = T, step
+        self.opt = T.AdamW([self.gain, self.bias, self.head], lr=1e-2, state=state, seed=8)
+
+    def __call__(self):
+        T = self.T
+        if self.counter is not None:
+            self.counter.add_(1)
+        y, mean, rstd = T.layernorm_forward(self.x, self.gain, self.bias)
+        z = y @ self.head.T
+        loss, dz = T.distill_loss(z, self.teacher, valid=self.valid)
+        extra, counts, dz2 = T.balance_loss(z, self.ids, coef=0.01, valid=self.valid)
+        dz = dz + dz2
+        dx, dgain, dbias = T.layernorm_backward(dz @ self.head, self.x, mean, rstd, self.gain)
+        self.opt.step([dgain, dbias, dz.T.contiguous() @ y], step=self.counter)
+        return loss, extra, counts, dx
+
+    def held(self):
+        return [self.gain, self.bias, self.head, *(t for s in self.opt.states().values() for t in s)]
+
+
+@pytest.mark.parametrize("state", ["f32", "f8"])
+def test_a_captured_training_step_equals_an_eager_one(state):
+    """Replays of one capture, with eager work and synchronisations between them, against the same steps run one by one: the
+    number of the step and the random numbers go on from replay to replay."""
+    eager = Step(state, torch.zeros(1, dtype=torch.int64, device="cuda"))
+    plain = Step(state)
+    captured = Step(state, torch.zeros(1, dtype=torch.int64, device="cuda"))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        captured()                                         # the libraries' own set-up; a first step
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = captured()
+    eager(), plain()
+    for replay in range(4):
+        shift = 0.1 * (replay + 1)
+        for s in (eager, plain, captured):
+            s.x.add_(shift)
+        graph.replay()
+        want, host = eager(), plain()
+        torch.cuda.synchronize()
+        for a, b, c in zip(out, want, host):
+            assert torch.equal(a, b) and torch.equal(a, c), replay
+        for a, b, c in zip(captured.held(), eager.held(), plain.held()):
+            assert torch.equal(a, b) and torch.equal(a, c), replay
+    assert captured.counter.item() == 5
+
+
+def test_operators_on_another_stream_and_two_at_once():
+    """The current stream is the one that counts; two streams with workspaces of their own do not disturb each other."""
+    from paper_2603_19289_amd import training as T
+    x, dy, gain, bias = (on_gpu(t) for t in ln_inputs(3000, 720, "bf16", 6))
+    t, s, valid, _ = logits(20000, 128, 6)
+    t, s, valid = on_gpu(t), on_gpu(s), on_gpu(valid)
+
+    def both():
+        y, mean, rstd = T.layernorm_forward(x, gain, bias)
+        return (y, *T.layernorm_backward(dy, x, mean, rstd, gain), *T.distill_loss(s, t, valid=valid))
+
+    want = both()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(3):
+        for stream in streams:
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                got.append(both())
+    torch.cuda.synchronize()
+    for g in got:
+        for a, b in zip(g, want):
+            assert torch.equal(a, b)
