@@ -18,7 +18,8 @@
  * give the same bits: no atomics on floating-point values.  Values are bfloat16 or float (MOE_SPEC_BF16, MOE_SPEC_F32);
  * statistics, sums and moments are held in float or wider, and what goes out as bfloat16 is rounded once, to nearest even.
  *
- * Calls that need scratch take a workspace (dev, 16-byte aligned) of at least the bytes that the matching function names;
+ * Calls that need scratch take a workspace (dev, 16-byte aligned) of at least the bytes that the matching function names (0 for
+ * small sizes: NULL will do; also 0 for sizes that the call refuses);
  * nothing in it has to be set and nothing is kept in it, but two calls that may run at the same time need two.
  *
  * Returns 0 (MOE_SPEC_OK), MOE_SPEC_EINVAL for arguments it refuses (nothing has been queued then) or MOE_SPEC_EHIP;

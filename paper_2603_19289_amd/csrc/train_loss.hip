@@ -18,7 +18,9 @@
 namespace moe_spec {
 namespace {
 
-constexpr int kLossBlock = 256, kLossBlocks = 2048, kCountBlocks = 64, kVals = 8;
+constexpr int kLossBlock = 256, kLossBlocks = 1024, kVals = 8;
+constexpr int kCountBlock = 1024, kCountBlocks = 32;
+constexpr int kOneBlock = 1024, kOneBlockRounds = 4;     // rows that one workgroup deals with in so many rounds: one launch
 
 struct LossArgs {
   const void *z, *teacher;              // z: the student's logits, or the router's
@@ -27,7 +29,7 @@ struct LossArgs {
   const int32_t *ids;
   int32_t *counts;
   float *loss;
-  int *counted;                         // [kCountBlocks][bins + 1]: choices of each expert, then valid rows; or null: all are
+  int *counted;                         // [kCountBlocks][bins + 1]: choices of each expert, then valid rows
   double *partial;                      // [blocks]
   int64_t z_stride, teacher_stride, grad_stride, ids_stride, rows;
   int experts, bins, top_k, blocks;     // bins: experts, or 0 where no choices are counted
@@ -40,60 +42,83 @@ template <> __device__ __forceinline__ uint16_t lowest<uint16_t>() { return 0xff
 
 struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 
-// Valid rows and their choices, a share of the rows for each workgroup.
-__global__ __launch_bounds__(kLossBlock) void loss_count_kernel(const LossArgs a) {
-  __shared__ int hist[MOE_SPEC_MAX_EXPERTS + 1];
-  for (int i = threadIdx.x; i <= a.bins; i += kLossBlock) hist[i] = 0;
-  __syncthreads();
+template <int CHUNK>
+__device__ __forceinline__ void count_choices(const int32_t *ids, int bins, int *hist) {
+  int e[CHUNK];
+  __builtin_memcpy(e, ids, sizeof(e));
+#pragma unroll
+  for (int i = 0; i < CHUNK; ++i) if (e[i] >= 0 && e[i] < bins) atomicAdd(&hist[e[i]], 1);
+}
+// Adds the choices of the valid rows from `row` on, `step` apart, to hist, and their number to hist[bins].
+__device__ __forceinline__ void count_rows(const LossArgs &a, int64_t row, int64_t step, int *hist) {
   int live = 0;
-  for (int64_t row = int64_t(blockIdx.x) * kLossBlock + threadIdx.x; row < a.rows; row += int64_t(gridDim.x) * kLossBlock) {
+  for (; row < a.rows; row += step) {
     if (a.valid && !a.valid[row]) continue;
     ++live;
     if (a.bins) {
       const int32_t *ids = a.ids + row * a.ids_stride;
-      for (int j = 0; j < a.top_k; ++j) {
-        const int e = ids[j];
-        if (e >= 0 && e < a.bins) atomicAdd(&hist[e], 1);
-      }
+      int j = 0;
+      for (; j + 8 <= a.top_k; j += 8) count_choices<8>(ids + j, a.bins, hist);
+      for (; j + 4 <= a.top_k; j += 4) count_choices<4>(ids + j, a.bins, hist);
+      for (; j < a.top_k; ++j) count_choices<1>(ids + j, a.bins, hist);
     }
   }
-  atomicAdd(&hist[a.bins], live);
+  for (int m = 1; m < kWave; m <<= 1) live += __shfl_xor(live, m);
+  if (threadIdx.x % kWave == 0) atomicAdd(&hist[a.bins], live);
+}
+
+// Valid rows and their choices, a share of the rows for each workgroup.
+__global__ __launch_bounds__(kCountBlock) void loss_count_kernel(const LossArgs a) {
+  __shared__ int hist[MOE_SPEC_MAX_EXPERTS + 1];
+  for (int i = threadIdx.x; i <= a.bins; i += kCountBlock) hist[i] = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i <= a.bins; i += kLossBlock) a.counted[blockIdx.x * (a.bins + 1) + i] = hist[i];
+  count_rows(a, int64_t(blockIdx.x) * kCountBlock + threadIdx.x, int64_t(gridDim.x) * kCountBlock, hist);
+  __syncthreads();
+  for (int i = threadIdx.x; i <= a.bins; i += kCountBlock) a.counted[blockIdx.x * (a.bins + 1) + i] = hist[i];
 }
 
 // Sum over the workgroup of one double per thread, in every thread.
+template <int BLOCK>
 __device__ __forceinline__ double block_sum(double v) {
-  __shared__ double part[kLossBlock / kWave];
+  __shared__ double part[BLOCK / kWave];
   v = wave_sum(v);
   if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
   __syncthreads();
   double s = 0.0;
 #pragma unroll
-  for (int i = 0; i < kLossBlock / kWave; ++i) s += part[i];
+  for (int i = 0; i < BLOCK / kWave; ++i) s += part[i];
   return s;
 }
 
-// ST: the logits' type; TT: the teacher's (void: balance loss); G lanes per row.
-template <typename ST, typename TT, int G>
-__global__ __launch_bounds__(kLossBlock) void loss_kernel(const LossArgs a) {
+// ST: the logits' type; TT: the teacher's (void: balance loss); G lanes per row.  One workgroup of kOneBlock threads does it all:
+// it counts for itself and writes the loss.
+template <typename ST, typename TT, int G, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void loss_kernel(const LossArgs a) {
   constexpr bool kDistill = !__is_same(TT, void);
   using Teacher = std::conditional_t<kDistill, TT, float>;
-  constexpr int kRows = kLossBlock / G;
+  constexpr int kRows = BLOCK / G;
   const int lane = threadIdx.x % G, slot = threadIdx.x / G, col = lane * kVals;
   __shared__ int total[MOE_SPEC_MAX_EXPERTS + 1];
-  // the valid rows and the choices, added up over what loss_count_kernel's workgroups left
-  if (a.counted) {
-    for (int i = threadIdx.x; i <= a.bins; i += kLossBlock) {
+  const bool counting = a.bins || a.valid;
+  if (counting) {                       // the valid rows and the choices, counted here or added up over what was counted
+    for (int i = threadIdx.x; i <= a.bins; i += BLOCK) {
       int s = 0;
-#pragma unroll 8
-      for (int b = 0; b < kCountBlocks; ++b) s += a.counted[b * (a.bins + 1) + i];
+      if (BLOCK != kOneBlock) {
+#pragma unroll
+        for (int b = 0; b < kCountBlocks; ++b) s += a.counted[b * (a.bins + 1) + i];
+      }
       total[i] = s;
-      if (!kDistill && blockIdx.x == 0 && i < a.bins) a.counts[i] = s;
     }
     __syncthreads();
+    if (BLOCK == kOneBlock) {
+      count_rows(a, threadIdx.x, BLOCK, total);
+      __syncthreads();
+    }
+    if (!kDistill && blockIdx.x == 0) {
+      for (int i = threadIdx.x; i < a.bins; i += BLOCK) a.counts[i] = total[i];
+    }
   }
-  const float n = a.counted ? float(total[a.bins]) : float(a.rows);
+  const float n = counting ? float(total[a.bins]) : float(a.rows);
   const float share = n > 0.0f ? 1.0f / n : 0.0f;
   float f[kVals];
   float scale;
@@ -189,17 +214,15 @@ __global__ __launch_bounds__(kLossBlock) void loss_kernel(const LossArgs a) {
       store_run<ST, kVals>(static_cast<ST *>(a.grad) + row * a.grad_stride + col, grad, a.experts - col);
     }
   }
-  sum = block_sum(sum) * double(kDistill ? share : scale);
+  sum = block_sum<BLOCK>(sum) * double(kDistill ? share : scale);
   if (threadIdx.x == 0) {
-    if (gridDim.x == 1) *a.loss = float(sum);
+    if (BLOCK == kOneBlock) *a.loss = float(sum);
     else a.partial[blockIdx.x] = sum;
   }
 }
 
-__global__ __launch_bounds__(kLossBlock) void loss_finish_kernel(const LossArgs a) {
-  double s = 0.0;
-  for (int i = threadIdx.x; i < a.blocks; i += kLossBlock) s += a.partial[i];
-  s = block_sum(s);
+__global__ __launch_bounds__(kLossBlocks) void loss_finish_kernel(const LossArgs a) {
+  const double s = block_sum<kLossBlocks>(int(threadIdx.x) < a.blocks ? a.partial[threadIdx.x] : 0.0);
   if (threadIdx.x == 0) *a.loss = float(s);
 }
 
@@ -209,27 +232,36 @@ __global__ void loss_none_kernel(const LossArgs a) {
   if (a.counts && int(threadIdx.x) < a.experts) a.counts[threadIdx.x] = 0;
 }
 
+int lanes_for(int experts) {
+  int g = 1;
+  while (g * kVals < experts) g *= 2;
+  return g;
+}
+bool in_one_block(int64_t rows, int experts) { return rows * lanes_for(experts) <= int64_t(kOneBlock) * kOneBlockRounds; }
+
 template <typename ST, typename TT, int G>
 hipError_t run_loss(hipStream_t stream, LossArgs &a) {
+  if (in_one_block(a.rows, a.experts)) return launch(loss_kernel<ST, TT, G, kOneBlock>, 1, kOneBlock, stream, a);
   const int64_t need = (a.rows + kLossBlock / G - 1) / (kLossBlock / G);
   a.blocks = int(need < kLossBlocks ? need : kLossBlocks);
   hipError_t e = hipSuccess;
-  if (a.counted) e = launch(loss_count_kernel, kCountBlocks, kLossBlock, stream, a);
-  if (e == hipSuccess) e = launch(loss_kernel<ST, TT, G>, a.blocks, kLossBlock, stream, a);
-  if (e == hipSuccess && a.blocks > 1) e = launch(loss_finish_kernel, 1, kLossBlock, stream, a);
+  if (a.bins || a.valid) e = launch(loss_count_kernel, kCountBlocks, kCountBlock, stream, a);
+  if (e == hipSuccess) e = launch(loss_kernel<ST, TT, G, kLossBlock>, a.blocks, kLossBlock, stream, a);
+  if (e == hipSuccess) e = launch(loss_finish_kernel, 1, kLossBlocks, stream, a);
   return e;
 }
 
 template <typename ST, typename TT>
 hipError_t run_loss(hipStream_t stream, LossArgs &a) {
   if (a.rows == 0) return launch(loss_none_kernel, 1, MOE_SPEC_MAX_EXPERTS, stream, a);
-  const int lanes = (a.experts + kVals - 1) / kVals;
-  if (lanes <= 1) return run_loss<ST, TT, 1>(stream, a);
-  if (lanes <= 2) return run_loss<ST, TT, 2>(stream, a);
-  if (lanes <= 4) return run_loss<ST, TT, 4>(stream, a);
-  if (lanes <= 8) return run_loss<ST, TT, 8>(stream, a);
-  if (lanes <= 16) return run_loss<ST, TT, 16>(stream, a);
-  return run_loss<ST, TT, 32>(stream, a);
+  switch (lanes_for(a.experts)) {
+    case 1: return run_loss<ST, TT, 1>(stream, a);
+    case 2: return run_loss<ST, TT, 2>(stream, a);
+    case 4: return run_loss<ST, TT, 4>(stream, a);
+    case 8: return run_loss<ST, TT, 8>(stream, a);
+    case 16: return run_loss<ST, TT, 16>(stream, a);
+    default: return run_loss<ST, TT, 32>(stream, a);
+  }
 }
 
 size_t partial_bytes() { return kLossBlocks * sizeof(double); }
@@ -247,6 +279,7 @@ const char *grad_fault(const void *grad, int64_t grad_stride, const void *z, int
 }
 
 const char *workspace_fault(const void *workspace, size_t bytes, size_t need) {
+  if (need == 0) return nullptr;
   if (!workspace || misaligned(workspace, 16)) return "must be given and aligned to 16 bytes";
   return bytes < need ? "is too small" : nullptr;
 }
@@ -257,12 +290,12 @@ const char *workspace_fault(const void *workspace, size_t bytes, size_t need) {
 using namespace moe_spec;
 
 extern "C" size_t moe_spec_distill_loss_workspace_bytes(int64_t rows, int n_experts) {
-  return sizes_fit(rows, n_experts) ? partial_bytes() + counted_bytes(0) : 0;
+  return sizes_fit(rows, n_experts) && !in_one_block(rows, n_experts) ? partial_bytes() + counted_bytes(0) : 0;
 }
 
 extern "C" size_t moe_spec_balance_loss_workspace_bytes(int64_t rows, int n_experts, int top_k) {
   if (!sizes_fit(rows, n_experts) || top_k < 1 || top_k > MOE_SPEC_MAX_TOP_K) return 0;
-  return partial_bytes() + counted_bytes(n_experts);
+  return in_one_block(rows, n_experts) ? 0 : partial_bytes() + counted_bytes(n_experts);
 }
 
 extern "C" int moe_spec_distill_loss(void *stream, int student_dtype, const void *student, int64_t student_stride,
@@ -291,7 +324,7 @@ extern "C" int moe_spec_distill_loss(void *stream, int student_dtype, const void
   a.z_stride = student_stride; a.teacher_stride = teacher_stride; a.grad_stride = grad_stride; a.rows = rows;
   a.experts = n_experts; a.inv_tau = 1.0f / temperature;
   a.partial = static_cast<double *>(workspace);
-  if (valid) a.counted = reinterpret_cast<int *>(static_cast<char *>(workspace) + partial_bytes());
+  if (workspace) a.counted = reinterpret_cast<int *>(static_cast<char *>(workspace) + partial_bytes());
   hipError_t e;
   if (student_dtype == MOE_SPEC_BF16)
     e = teacher_dtype == MOE_SPEC_BF16 ? run_loss<uint16_t, uint16_t>(s, a) : run_loss<uint16_t, float>(s, a);
@@ -326,7 +359,7 @@ extern "C" int moe_spec_balance_loss(void *stream, int dtype, const void *logits
   a.z_stride = logits_stride; a.grad_stride = grad_stride; a.ids_stride = ids_stride; a.rows = rows;
   a.experts = a.bins = n_experts; a.top_k = top_k; a.coef = coef; a.inv_tau = 1.0f;
   a.partial = static_cast<double *>(workspace);
-  a.counted = reinterpret_cast<int *>(static_cast<char *>(workspace) + partial_bytes());
+  if (workspace) a.counted = reinterpret_cast<int *>(static_cast<char *>(workspace) + partial_bytes());
   const hipError_t e = dtype == MOE_SPEC_BF16 ? run_loss<uint16_t, void>(s, a) : run_loss<float, void>(s, a);
   return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "balance_loss: %s", hipGetErrorString(e));
 }

@@ -16,34 +16,32 @@ from . import moe_spec as M
 _TYPES = {torch.float32: M.F32, torch.bfloat16: M.BF16}
 
 
-def _stream(dev: torch.device):
-    return torch.cuda.current_stream(dev).cuda_stream
-
-
 def _queue(dev: torch.device, call, *args):
-    """call(stream, *args) with the tensors' device as the current one."""
-    if torch.cuda.current_device() == dev.index:
-        call(_stream(dev), *args)
+    """call(stream, *args) on the current stream of the tensors' device, with that device as the current one."""
+    i = dev.index
+    if torch._C._cuda_getDevice() == i:
+        M._check_train(call(torch._C._cuda_getCurrentRawStream(i), *args))
     else:
-        with torch.cuda.device(dev):
-            call(_stream(dev), *args)
+        with torch.cuda.device(i):
+            M._check_train(call(torch._C._cuda_getCurrentRawStream(i), *args))
 
 
 def _rows(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> int:
     """Type number of a matrix whose rows are contiguous."""
-    if t.dtype not in _TYPES or t.dim() != 2 or not t.is_cuda:
+    dtype = _TYPES.get(t.dtype)
+    if dtype is None or t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{name} must be a two-dimensional float32 or bfloat16 tensor on a GPU")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    if t.stride(1) != 1 and t.shape[1] > 1:
         raise ValueError(f"{name}: the values of a row must be contiguous")
     if like is not None and (t.shape != like.shape or t.device != like.device):
         raise ValueError(f"{name} must have the shape and the device of the other matrix")
-    return _TYPES[t.dtype]
+    return dtype
 
 
 def _vector(t: Optional[torch.Tensor], name: str, n: int, dev: torch.device, dtype=torch.float32):
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous() or t.device != dev:
+    if t.dtype != dtype or t.dim() != 1 or t.numel() != n or not t.is_contiguous() or t.device != dev:
         raise ValueError(f"{name} must be a contiguous {dtype} vector of {n} values on {dev}")
     return t.data_ptr()
 
@@ -56,10 +54,6 @@ def _mask(valid: Optional[torch.Tensor], rows: int, dev: torch.device):
     return _vector(valid, "valid", rows, dev, valid.dtype)
 
 
-def _bytes(n: int, dev: torch.device) -> torch.Tensor:
-    return torch.empty(n, dtype=torch.uint8, device=dev)
-
-
 def layernorm_forward(x: torch.Tensor, gain: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
                       eps: float = 1e-5, *, out: Optional[torch.Tensor] = None):
     """LayerNorm over the last dimension of x [rows, cols] (rows may be strided) -> (y, mean [rows], rstd [rows]).  gain and
@@ -67,14 +61,15 @@ def layernorm_forward(x: torch.Tensor, gain: Optional[torch.Tensor] = None, bias
     dtype = _rows(x, "x")
     rows, cols = x.shape
     dev = x.device
-    y = torch.empty((rows, cols), dtype=x.dtype, device=dev) if out is None else out
-    if out is not None and _rows(y, "out", x) != dtype:
+    if out is None:
+        out = x.new_empty((rows, cols))
+    elif _rows(out, "out", x) != dtype:
         raise ValueError("out must have the type of x")
-    stats = torch.empty((2, rows), dtype=torch.float32, device=dev)
-    mean, rstd = stats[0], stats[1]
-    _queue(dev, M.moe_spec_layernorm_forward, dtype, x.data_ptr(), x.stride(0), rows, cols, _vector(gain, "gain", cols, dev),
-           _vector(bias, "bias", cols, dev), eps, y.data_ptr(), y.stride(0), mean.data_ptr(), rstd.data_ptr())
-    return y, mean, rstd
+    mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind(0)
+    at = mean.data_ptr()
+    _queue(dev, M.lib().moe_spec_layernorm_forward, dtype, x.data_ptr(), x.stride(0), rows, cols, _vector(gain, "gain", cols, dev),
+           _vector(bias, "bias", cols, dev), eps, out.data_ptr(), out.stride(0), at, at + 4 * rows)
+    return out, mean, rstd
 
 
 def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
@@ -87,17 +82,19 @@ def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rs
         raise ValueError("dy must have the type of x")
     rows, cols = x.shape
     dev = x.device
-    dx = torch.empty((rows, cols), dtype=x.dtype, device=dev) if input_grad else None
-    dgain = dbias = None
-    need, space = 0, None
+    lib = M.lib()
+    dx = x.new_empty((rows, cols)) if input_grad else None
+    dgain = dbias = space = at = None
+    need = 0
     if weight_grads:
-        dgain, dbias = torch.empty((2, cols), dtype=torch.float32, device=dev).unbind(0)
-        need = M.moe_spec_layernorm_backward_workspace_bytes(rows, cols)
-        space = _bytes(need, dev)
-    _queue(dev, M.moe_spec_layernorm_backward, dtype, dy.data_ptr(), dy.stride(0), x.data_ptr(), x.stride(0), rows, cols,
+        dgain, dbias = x.new_empty((2, cols), dtype=torch.float32).unbind(0)
+        at = dgain.data_ptr()
+        need = lib.moe_spec_layernorm_backward_workspace_bytes(rows, cols)
+        space = x.new_empty(need, dtype=torch.uint8) if need else None
+    _queue(dev, lib.moe_spec_layernorm_backward, dtype, dy.data_ptr(), dy.stride(0), x.data_ptr(), x.stride(0), rows, cols,
            _vector(mean, "mean", rows, dev), _vector(rstd, "rstd", rows, dev), _vector(gain, "gain", cols, dev),
-           dx.data_ptr() if input_grad else None, cols, dgain.data_ptr() if weight_grads else None,
-           dbias.data_ptr() if weight_grads else None, space.data_ptr() if weight_grads else None, need)
+           dx.data_ptr() if input_grad else None, cols, at, at + 4 * cols if weight_grads else None,
+           space.data_ptr() if need else None, need)
     return dx, dgain, dbias
 
 
@@ -108,13 +105,15 @@ def distill_loss(student: torch.Tensor, teacher: torch.Tensor, *, temperature: f
     ts, tt = _rows(student, "student"), _rows(teacher, "teacher", student)
     rows, experts = student.shape
     dev = student.device
-    loss = torch.empty((), dtype=torch.float32, device=dev)
-    dz = torch.empty((rows, experts), dtype=student.dtype, device=dev) if grad else None
-    need = M.moe_spec_distill_loss_workspace_bytes(rows, experts)
-    space = _bytes(need, dev)
-    _queue(dev, M.moe_spec_distill_loss, ts, student.data_ptr(), student.stride(0), tt, teacher.data_ptr(), teacher.stride(0),
-           rows, experts, temperature, _mask(valid, rows, dev), loss.data_ptr(), dz.data_ptr() if grad else None, experts,
-           space.data_ptr(), need)
+    lib = M.lib()
+    mask = _mask(valid, rows, dev)
+    loss = student.new_empty((), dtype=torch.float32)
+    dz = student.new_empty((rows, experts)) if grad else None
+    need = lib.moe_spec_distill_loss_workspace_bytes(rows, experts)
+    space = student.new_empty(need, dtype=torch.uint8) if need else None
+    _queue(dev, lib.moe_spec_distill_loss, ts, student.data_ptr(), student.stride(0), tt, teacher.data_ptr(), teacher.stride(0),
+           rows, experts, temperature, mask, loss.data_ptr(), dz.data_ptr() if grad else None, experts,
+           space.data_ptr() if need else None, need)
     return loss, dz
 
 
@@ -127,23 +126,26 @@ def balance_loss(logits: torch.Tensor, ids: torch.Tensor, *, coef: float = 1.0, 
     dev = logits.device
     if ids.dtype != torch.int32 or ids.dim() != 2 or ids.shape[0] != rows or ids.device != dev:
         raise ValueError("ids must be an int32 tensor [rows, k] on the logits' device")
-    if ids.shape[1] > 1 and ids.stride(1) != 1:
-        raise ValueError("ids: the values of a row must be contiguous")
     k = ids.shape[1]
-    loss = torch.empty((), dtype=torch.float32, device=dev)
-    counts = torch.empty(experts, dtype=torch.int32, device=dev)
-    dz = torch.empty((rows, experts), dtype=logits.dtype, device=dev) if grad else None
-    need = M.moe_spec_balance_loss_workspace_bytes(rows, experts, k)
-    space = _bytes(need, dev)
-    _queue(dev, M.moe_spec_balance_loss, dtype, logits.data_ptr(), logits.stride(0), rows, experts, ids.data_ptr(), ids.stride(0),
-           k, coef, _mask(valid, rows, dev), loss.data_ptr(), counts.data_ptr(), dz.data_ptr() if grad else None, experts,
-           space.data_ptr(), need)
+    if ids.stride(1) != 1 and k > 1:
+        raise ValueError("ids: the values of a row must be contiguous")
+    lib = M.lib()
+    mask = _mask(valid, rows, dev)
+    loss = logits.new_empty((), dtype=torch.float32)
+    counts = logits.new_empty(experts, dtype=torch.int32)
+    dz = logits.new_empty((rows, experts)) if grad else None
+    need = lib.moe_spec_balance_loss_workspace_bytes(rows, experts, k)
+    space = logits.new_empty(need, dtype=torch.uint8) if need else None
+    _queue(dev, lib.moe_spec_balance_loss, dtype, logits.data_ptr(), logits.stride(0), rows, experts, ids.data_ptr(), ids.stride(0),
+           k, coef, mask, loss.data_ptr(), counts.data_ptr(), dz.data_ptr() if grad else None, experts,
+           space.data_ptr() if need else None, need)
     return loss, counts, dz
 
 
 class AdamW:
     """AdamW over many float32 tensors in one call, moments in 32 ("f32") or 8 bits ("f8").  Holds the tensors and their
-    moments; `lr`, `betas`, `eps` and `weight_decay` may be set between steps.
+    moments; `lr`, `betas`, `eps` and `weight_decay` may be set between steps.  A captured step keeps those it was captured with;
+    its number and grad_scale it reads anew where they are tensors.
 
     copies: bfloat16 tensors (or None in places) that get the updated parameters, rounded: what an Engine reads its weights
     from.  states: moments to go on with, as `states()` of another AdamW gave them; used in place."""
@@ -159,29 +161,24 @@ class AdamW:
         self.lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
         self.state, self.seed, self.steps = state, int(seed) & 0xffffffff, int(steps)
         dev = self.device = self.params[0].device
-        for p in self.params:
-            self._tensor(p, "a parameter", torch.float32, p.numel())
-        if len({p.data_ptr() for p in self.params if p.numel()}) < sum(p.numel() > 0 for p in self.params):
-            raise ValueError("a parameter is named twice")
+        self._sizes = [p.numel() for p in self.params]
         self.copies = list(copies) if copies is not None else [None] * len(self.params)
         eight = state == "f8"
-        held = torch.uint8 if eight else torch.float32
-        blocks = lambda p: -(-p.numel() // M.MOMENT_BLOCK)  # noqa: E731
         if states is None:
             new = lambda n, t: torch.zeros(n, dtype=t, device=dev)  # noqa: E731
-            states = {k: [new(p.numel(), held) for p in self.params] for k in ("m", "v")}
+            states = {k: [new(n, torch.uint8 if eight else torch.float32) for n in self._sizes] for k in ("m", "v")}
             if eight:
-                states.update({k: [new(blocks(p), torch.uint8) for p in self.params] for k in ("m_exp", "v_exp")})
+                states.update({k: [new(-(-n // M.MOMENT_BLOCK), torch.uint8) for n in self._sizes] for k in ("m_exp", "v_exp")})
         self._states = {k: list(states[k]) for k in (("m", "v", "m_exp", "v_exp") if eight else ("m", "v"))}
         if any(len(t) != len(self.params) for t in (*self._states.values(), self.copies)):
             raise ValueError("as many moments and copies as parameters are needed")
+        written = [t for t in (*self.params, *self.copies, *(t for k in self._states.values() for t in k)) if t is not None and t.numel()]
+        if len({t.data_ptr() for t in written}) < len(written):
+            raise ValueError("a tensor is named twice")
+        self._held, self._at = [t for t in (*self.params, *self.copies) if t is not None], None
         self._desc = (M.AdamWTensor * len(self.params))()
-        for i, p in enumerate(self.params):
-            for k, t in self._states.items():
-                self._tensor(t[i], k, held, blocks(p) if k.endswith("exp") else p.numel())
-            if self.copies[i] is not None:
-                self._tensor(self.copies[i], "a copy", torch.bfloat16, p.numel())
         self._config = M.AdamWConfig(seed=self.seed, moments=M.MOMENTS_8BIT if eight else M.MOMENTS_32BIT)
+        self._describe()
 
     def _tensor(self, t, name, dtype, n):
         if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.device or not t.is_cuda:
@@ -192,12 +189,28 @@ class AdamW:
         return {k: list(t) for k, t in self._states.items()}
 
     def _describe(self):
+        """The tensors' table for the library; made anew where a tensor has got other storage since."""
+        at = [t.data_ptr() for t in self._held]
+        if at == self._at:
+            return
         s = self._states
         for i, (d, p) in enumerate(zip(self._desc, self.params)):
-            d.p, d.n, d.m, d.v = p.data_ptr(), p.numel(), s["m"][i].data_ptr(), s["v"][i].data_ptr()
+            d.p, d.m, d.v = p.data_ptr(), s["m"][i].data_ptr(), s["v"][i].data_ptr()
             if self.state == "f8":
                 d.m_exp, d.v_exp = s["m_exp"][i].data_ptr(), s["v_exp"][i].data_ptr()
             d.copy = self.copies[i].data_ptr() if self.copies[i] is not None else None
+        self._check()
+        self._at = at
+
+    def _check(self):
+        eight = self.state == "f8"
+        held = torch.uint8 if eight else torch.float32
+        for i, p in enumerate(self.params):
+            self._tensor(p, "a parameter", torch.float32, self._sizes[i])
+            for k, t in self._states.items():
+                self._tensor(t[i], k, held, -(-p.numel() // M.MOMENT_BLOCK) if k.endswith("exp") else p.numel())
+            if self.copies[i] is not None:
+                self._tensor(self.copies[i], "a copy", torch.bfloat16, p.numel())
 
     def step(self, grads: Sequence[Optional[torch.Tensor]], *, step=None, grad_scale=1.0):
         """One step with a gradient for each parameter, all float32 or all bfloat16; a parameter whose gradient is None stays as
@@ -209,12 +222,14 @@ class AdamW:
         if dtype not in _TYPES:
             raise ValueError("gradients must be float32 or bfloat16")
         self._describe()
-        for d, p, g in zip(self._desc, self.params, grads):
+        dev = self.device
+        for d, n, g in zip(self._desc, self._sizes, grads):
             if g is None:
                 d.n = 0
                 continue
-            self._tensor(g, "a gradient", dtype, p.numel())
-            d.grad = g.data_ptr()
+            if g.dtype != dtype or g.numel() != n or g.device != dev or not g.is_contiguous():
+                self._tensor(g, "a gradient", dtype, n)
+            d.n, d.grad = n, g.data_ptr()
         c = self._config
         c.lr, (c.beta1, c.beta2), c.eps, c.weight_decay, c.grad_dtype = self.lr, self.betas, self.eps, self.weight_decay, _TYPES[dtype]
         c.step_dev = c.grad_scale_dev = None
@@ -229,7 +244,7 @@ class AdamW:
             c.step_dev = step.data_ptr()
         else:
             c.step = self.steps + 1 if step is None else step
-        _queue(self.device, M.moe_spec_adamw_step, self._desc, len(self._desc), c)
+        _queue(dev, M.lib().moe_spec_adamw_step, self._desc, len(self._desc), C.byref(c))
         if not isinstance(step, torch.Tensor):
             self.steps = c.step
 
@@ -248,6 +263,8 @@ class AdamW:
             for t, p in zip(out or (), self.params):
                 self._tensor(t, "an output", dtype, p.numel())
         self._describe()
+        for d, n in zip(self._desc, self._sizes):
+            d.n = n
         pointers = lambda out: None if out is None else (C.c_void_p * len(out))(*[t.data_ptr() for t in out])  # noqa: E731
-        _queue(self.device, M.moe_spec_adamw_read_moments, self._desc, len(self._desc), _TYPES[dtype], pointers(m_out), pointers(v_out))
+        _queue(self.device, M.lib().moe_spec_adamw_read_moments, self._desc, len(self._desc), _TYPES[dtype], pointers(m_out), pointers(v_out))
         return m_out, v_out

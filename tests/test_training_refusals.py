@@ -66,12 +66,13 @@ def test_workspace_sizes():
     assert size(0, 64) == 0 < size(1, 64) <= size(100, 64) <= size(100, 65)
     assert M.moe_spec_distill_loss_workspace_bytes(4, 257) == M.moe_spec_distill_loss_workspace_bytes(-1, 8) == 0
     assert M.moe_spec_balance_loss_workspace_bytes(4, 8, 17) == M.moe_spec_balance_loss_workspace_bytes(4, 8, 0) == 0
-    assert M.moe_spec_balance_loss_workspace_bytes(4, 256, 16) > M.moe_spec_distill_loss_workspace_bytes(4, 256) > 0
+    assert M.moe_spec_balance_loss_workspace_bytes(100000, 256, 16) > M.moe_spec_distill_loss_workspace_bytes(100000, 256) > 0
+    assert M.moe_spec_balance_loss_workspace_bytes(1, 256, 16) == M.moe_spec_distill_loss_workspace_bytes(1, 256) == 0    # one workgroup
 
 
 def distill(**kw):
     a = dict(stream=None, student_dtype=M.F32, student=ADDR, student_stride=32, teacher_dtype=M.BF16, teacher=ADDR * 2,
-             teacher_stride=32, rows=4, n_experts=32, temperature=1.0, valid=None, loss=ADDR, grad=ADDR * 3, grad_stride=32,
+             teacher_stride=32, rows=100000, n_experts=32, temperature=1.0, valid=None, loss=ADDR, grad=ADDR * 3, grad_stride=32,
              workspace=ADDR, workspace_bytes=1 << 20)
     a.update(kw)
     return M.lib().moe_spec_distill_loss(*a.values())
@@ -90,7 +91,7 @@ def test_distill_loss_refuses(bad, word):
 
 
 def balance(**kw):
-    a = dict(stream=None, dtype=M.F32, logits=ADDR, logits_stride=32, rows=4, n_experts=32, ids=ADDR, ids_stride=4, top_k=4,
+    a = dict(stream=None, dtype=M.F32, logits=ADDR, logits_stride=32, rows=100000, n_experts=32, ids=ADDR, ids_stride=4, top_k=4,
              coef=1.0, valid=None, loss=ADDR, counts=ADDR, grad=ADDR * 3, grad_stride=32, workspace=ADDR, workspace_bytes=1 << 20)
     a.update(kw)
     return M.lib().moe_spec_balance_loss(*a.values())
