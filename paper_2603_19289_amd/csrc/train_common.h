@@ -70,11 +70,10 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
 }
 __device__ __forceinline__ uint16_t to_bf16(float x) { return uint16_t(pack_bf16(x, 0.0f)); }
-__device__ __forceinline__ float from_bf16(uint16_t b) { return __uint_as_float(uint32_t(b) << 16); }
 
-template <typename WT> __device__ __forceinline__ float to_float(WT x);
-template <> __device__ __forceinline__ float to_float<float>(float x) { return x; }
-template <> __device__ __forceinline__ float to_float<uint16_t>(uint16_t x) { return from_bf16(x); }
+template <typename WT> __device__ __forceinline__ WT from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ uint16_t from_float<uint16_t>(float x) { return to_bf16(x); }
 
 // N values at p[0 .. N), of which the first n exist (the rest are `fill`); N a multiple of what 16 bytes hold.
 template <typename WT, int N>

@@ -10,7 +10,8 @@
 // Bound by memory: logits are read once, gradients written once; the gradient's factors (n, f) come first, from the mask and
 // the ids, which are a few per cent of the bytes.  A row lies in the registers of a group of 1 to 32 lanes, eight
 // values each.  Exponentials go through the hardware's 2^x: its argument x log2 e is rounded to float, which moves exp(x) by
-// |x| 2^-24 relative, so by at most 0.37 * 2^-24 of the row's largest term.  Row results are added up in double.
+// |x| 2^-24 relative, so by at most 0.37 * 2^-24 of the row's largest term.  One reciprocal and one logarithm a row are the
+// hardware's too (a unit in the last place).  Row results are added up in double.
 #include "train_common.h"
 
 #include <type_traits>
@@ -18,22 +19,24 @@
 namespace moe_spec {
 namespace {
 
-constexpr int kLossBlock = 256, kLossBlocks = 1024, kVals = 8;
-constexpr int kCountBlock = 1024, kCountBlocks = 32;
-constexpr int kOneBlock = 1024, kOneBlockRounds = 4;     // rows that one workgroup deals with in so many rounds: one launch
+constexpr int kLossBlock = 256, kLossBlocks = 1536, kVals = 8, kFinishBlock = 512;
+constexpr int kCountBlock = 1024, kCountBlocks = 64;
+constexpr int kOneBlock = 1024, kOneBlockRounds = 2;     // rows that one workgroup deals with in so many rounds: one launch
 
 struct LossArgs {
   const void *z, *teacher;              // z: the student's logits, or the router's
   void *grad;
   const uint8_t *valid;
+  const uint8_t *mask;                  // valid, or without one any byte that can be read, with a stride of 0: loads need no condition
   const int32_t *ids;
   int32_t *counts;
   float *loss;
-  int *counted;                         // [kCountBlocks][bins + 1]: choices of each expert, then valid rows
+  int *counted;                         // [kCountBlocks][padded_bins]: choices of each expert, then valid rows
   double *partial;                      // [blocks]
-  int64_t z_stride, teacher_stride, grad_stride, ids_stride, rows;
+  int64_t z_stride, teacher_stride, grad_stride, ids_stride, mask_stride, rows;
   int experts, bins, top_k, blocks;     // bins: experts, or 0 where no choices are counted
-  float inv_tau, coef;
+  int count_blocks;                     // workgroups that count
+  float inv_tau, to_log2, coef;         // to_log2: log2 e / tau
 };
 
 template <typename WT> __device__ __forceinline__ WT lowest();            // minus infinity
@@ -42,39 +45,61 @@ template <> __device__ __forceinline__ uint16_t lowest<uint16_t>() { return 0xff
 
 struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 
-template <int CHUNK>
-__device__ __forceinline__ void count_choices(const int32_t *ids, int bins, int *hist) {
-  int e[CHUNK];
-  __builtin_memcpy(e, ids, sizeof(e));
-#pragma unroll
-  for (int i = 0; i < CHUNK; ++i) if (e[i] >= 0 && e[i] < bins) atomicAdd(&hist[e[i]], 1);
-}
-// Adds the choices of the valid rows from `row` on, `step` apart, to hist, and their number to hist[bins].
-__device__ __forceinline__ void count_rows(const LossArgs &a, int64_t row, int64_t step, int *hist) {
+// Adds the choices of the valid rows from `row` on, `step` apart, to hist, and the number of those rows to hist[bins].  A thread
+// takes two rows at a time, whose loads go out together: without a condition (behind the end: the last row's), so that none is
+// waited for before the others are out.
+template <int UNITS>                    // four choices each
+__device__ __forceinline__ int count_rows(const LossArgs &a, int64_t row, int64_t step, int *hist) {
+  constexpr int kAhead = 2;
   int live = 0;
-  for (; row < a.rows; row += step) {
-    if (a.valid && !a.valid[row]) continue;
-    ++live;
-    if (a.bins) {
-      const int32_t *ids = a.ids + row * a.ids_stride;
-      int j = 0;
-      for (; j + 8 <= a.top_k; j += 8) count_choices<8>(ids + j, a.bins, hist);
-      for (; j + 4 <= a.top_k; j += 4) count_choices<4>(ids + j, a.bins, hist);
-      for (; j < a.top_k; ++j) count_choices<1>(ids + j, a.bins, hist);
+  for (; row < a.rows; row += kAhead * step) {
+    int e[kAhead][4 * UNITS + 1], alive[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int64_t at = row + u * step < a.rows ? row + u * step : a.rows - 1;
+      alive[u] = a.mask[at * a.mask_stride];
+      if constexpr (UNITS > 0) {
+        const int32_t *ids = a.ids + at * a.ids_stride;
+        if (a.top_k == 4 * UNITS) {
+          __builtin_memcpy(e[u], ids, 16 * UNITS);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4 * UNITS; ++j) e[u][j] = ids[j < a.top_k ? j : 0];
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (row + u * step >= a.rows || (a.valid && !alive[u])) continue;
+      ++live;
+#pragma unroll
+      for (int j = 0; j < 4 * UNITS; ++j)
+        if (j < a.top_k && e[u][j] >= 0 && e[u][j] < a.bins) atomicAdd(&hist[e[u][j]], 1);
     }
   }
+  return live;
+}
+__device__ __forceinline__ void count_rows(const LossArgs &a, int64_t first, int64_t step, int *hist) {
+  int live;
+  if (!a.bins) live = count_rows<0>(a, first, step, hist);
+  else if (a.top_k <= 4) live = count_rows<1>(a, first, step, hist);
+  else if (a.top_k <= 8) live = count_rows<2>(a, first, step, hist);
+  else live = count_rows<4>(a, first, step, hist);
   for (int m = 1; m < kWave; m <<= 1) live += __shfl_xor(live, m);
   if (threadIdx.x % kWave == 0) atomicAdd(&hist[a.bins], live);
 }
 
+// The choices of each expert and the number of valid rows, as many as 16-byte loads take.
+constexpr __host__ __device__ int padded_bins(int bins) { return (bins + 1 + 3) / 4 * 4; }
+
 // Valid rows and their choices, a share of the rows for each workgroup.
 __global__ __launch_bounds__(kCountBlock) void loss_count_kernel(const LossArgs a) {
-  __shared__ int hist[MOE_SPEC_MAX_EXPERTS + 1];
-  for (int i = threadIdx.x; i <= a.bins; i += kCountBlock) hist[i] = 0;
+  __shared__ int hist[padded_bins(MOE_SPEC_MAX_EXPERTS)];
+  for (int i = threadIdx.x; i < padded_bins(a.bins); i += kCountBlock) hist[i] = 0;
   __syncthreads();
   count_rows(a, int64_t(blockIdx.x) * kCountBlock + threadIdx.x, int64_t(gridDim.x) * kCountBlock, hist);
   __syncthreads();
-  for (int i = threadIdx.x; i <= a.bins; i += kCountBlock) a.counted[blockIdx.x * (a.bins + 1) + i] = hist[i];
+  for (int i = threadIdx.x; i < padded_bins(a.bins); i += kCountBlock) a.counted[blockIdx.x * padded_bins(a.bins) + i] = hist[i];
 }
 
 // Sum over the workgroup of one double per thread, in every thread.
@@ -97,23 +122,53 @@ __global__ __launch_bounds__(BLOCK) void loss_kernel(const LossArgs a) {
   constexpr bool kDistill = !__is_same(TT, void);
   using Teacher = std::conditional_t<kDistill, TT, float>;
   constexpr int kRows = BLOCK / G;
-  const int lane = threadIdx.x % G, slot = threadIdx.x / G, col = lane * kVals;
-  __shared__ int total[MOE_SPEC_MAX_EXPERTS + 1];
+  const int lane = threadIdx.x % G, slot = threadIdx.x / G;
+  // a lane's columns: [col + skip, col + count); the last lane's eight are moved back to end with the row, so that they are one load
+  int col = lane * kVals, skip = 0, count = col < a.experts ? (a.experts < kVals ? a.experts : kVals) : 0;
+  if (a.experts >= kVals && count && col + kVals > a.experts) {
+    skip = col + kVals - a.experts;
+    col = a.experts - kVals;
+  }
+  Run<ST, kVals> next_z;
+  Run<Teacher, kVals> next_t;
+  const int64_t step = int64_t(gridDim.x) * kRows;
+  auto mask = [&](int64_t row) { return int(a.mask[(row < a.rows ? row : a.rows - 1) * a.mask_stride]); };
+  auto fetch = [&](int64_t row, bool live) {
+    const int here = live ? count : 0;                  // rows that do not count are not read
+    next_z.load(static_cast<const ST *>(a.z) + row * a.z_stride + col, here, lowest<ST>());
+    if constexpr (kDistill) next_t.load(static_cast<const Teacher *>(a.teacher) + row * a.teacher_stride + col, here, lowest<Teacher>());
+  };
+  double sum = 0.0;
+  int64_t row = int64_t(blockIdx.x) * kRows + slot;
+  int ahead = mask(row + step);
+  bool live = row < a.rows && (mask(row) || !a.valid);
+  fetch(row, live);
+
+  __shared__ int total[padded_bins(MOE_SPEC_MAX_EXPERTS)];
   const bool counting = a.bins || a.valid;
   if (counting) {                       // the valid rows and the choices, counted here or added up over what was counted
-    for (int i = threadIdx.x; i <= a.bins; i += BLOCK) {
-      int s = 0;
-      if (BLOCK != kOneBlock) {
-#pragma unroll
-        for (int b = 0; b < kCountBlocks; ++b) s += a.counted[b * (a.bins + 1) + i];
+    for (int i = threadIdx.x; i < padded_bins(a.bins); i += BLOCK) total[i] = 0;
+    __syncthreads();
+    if constexpr (BLOCK == kOneBlock) {
+      count_rows(a, threadIdx.x, BLOCK, total);
+    } else {                            // four bins a load, the counting workgroups' rows over the threads
+      const int quads = padded_bins(a.bins) / 4, wide = quads > 64 ? 128 : quads > 32 ? 64 : quads > 8 ? 32 : 8;
+      const int q = threadIdx.x % wide, rows = BLOCK / wide;
+      const int4 *from = reinterpret_cast<const int4 *>(a.counted) + (q < quads ? q : 0);
+      int4 sum = {0, 0, 0, 0};
+#pragma unroll 8
+      for (int b = threadIdx.x / wide; b < a.count_blocks; b += rows) {
+        const int4 v = from[b * quads];
+        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
       }
-      total[i] = s;
+      if (q < quads) {
+        atomicAdd(&total[4 * q], sum.x);
+        atomicAdd(&total[4 * q + 1], sum.y);
+        atomicAdd(&total[4 * q + 2], sum.z);
+        atomicAdd(&total[4 * q + 3], sum.w);
+      }
     }
     __syncthreads();
-    if (BLOCK == kOneBlock) {
-      count_rows(a, threadIdx.x, BLOCK, total);
-      __syncthreads();
-    }
     if (!kDistill && blockIdx.x == 0) {
       for (int i = threadIdx.x; i < a.bins; i += BLOCK) a.counts[i] = total[i];
     }
@@ -127,91 +182,94 @@ __global__ __launch_bounds__(BLOCK) void loss_kernel(const LossArgs a) {
   } else {
     scale = a.coef * float(a.experts) * share;
 #pragma unroll
-    for (int i = 0; i < kVals; ++i) f[i] = col + i < a.experts ? float(total[col + i]) * (share / float(a.top_k)) : 0.0f;
+    for (int i = 0; i < kVals; ++i) f[i] = i < count ? float(total[col + i]) * (share / float(a.top_k)) : 0.0f;
   }
 
-  Run<ST, kVals> next_z;
-  Run<Teacher, kVals> next_t;
-  const int64_t step = int64_t(gridDim.x) * kRows;
-  auto alive = [&](int64_t row) { return row < a.rows && (!a.valid || a.valid[row]); };
-  auto fetch = [&](int64_t row, bool live) {
-    const int here = live ? a.experts - col : 0;        // rows that do not count are not read
-    next_z.load(static_cast<const ST *>(a.z) + row * a.z_stride + col, here, lowest<ST>());
-    if constexpr (kDistill) next_t.load(static_cast<const Teacher *>(a.teacher) + row * a.teacher_stride + col, here, lowest<Teacher>());
-  };
-  double sum = 0.0;
-  int64_t row = int64_t(blockIdx.x) * kRows + slot;
-  bool live = alive(row), next_live = alive(row + step);
-  fetch(row, live);
   for (int64_t first = int64_t(blockIdx.x) * kRows; first < a.rows; first += step, row += step) {
     float z[kVals], t[kVals], grad[kVals];
     next_z.get(z);
     if constexpr (kDistill) next_t.get(t);
-    const bool counts = live;
-    live = next_live;
-    fetch(row + step, live);
-    next_live = alive(row + 2 * step);
-    float result;
-    if constexpr (kDistill) {
-      float top_z = -INFINITY, top_t = -INFINITY;
+    if (a.experts % kVals) {
 #pragma unroll
-      for (int i = 0; i < kVals; ++i) {
-        z[i] *= a.inv_tau;
-        t[i] *= a.inv_tau;
-        top_z = fmaxf(top_z, z[i]);
-        top_t = fmaxf(top_t, t[i]);
+      for (int i = 0; i < kVals - 1; ++i) {
+        if (i >= skip) continue;
+        z[i] = -INFINITY;
+        if constexpr (kDistill) t[i] = -INFINITY;
       }
-      top_z = group_reduce<G>(top_z, Max());
-      top_t = group_reduce<G>(top_t, Max());
-      if (top_z == -INFINITY) top_z = 0.0f;
-      if (top_t == -INFINITY) top_t = 0.0f;
-      float sum_z = 0.0f, sum_t = 0.0f, cross = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kVals; ++i) {
-        z[i] -= top_z;
-        t[i] -= top_t;
-        sum_z += grad[i] = __expf(z[i]);
-        sum_t += __expf(t[i]);
-      }
-      sum_z = group_sum<G>(sum_z);
-      sum_t = group_sum<G>(sum_t);
-      const bool nothing = sum_t == 0.0f;                                  // the teacher's row is masked out whole
-      const float inv_z = sum_z == 0.0f || nothing ? 0.0f : 1.0f / sum_z, inv_t = nothing ? 0.0f : 1.0f / sum_t;
-#pragma unroll
-      for (int i = 0; i < kVals; ++i) {
-        const float p = __expf(t[i]) * inv_t;
-        cross += p == 0.0f ? 0.0f : p * (t[i] - z[i]);                     // 0 log 0 = 0
-        grad[i] = nothing ? 0.0f : (grad[i] * inv_z - p) * scale;
-      }
-      cross = group_sum<G>(cross);
-      result = nothing ? 0.0f : cross - logf(sum_t) + (sum_z == 0.0f ? 0.0f : logf(sum_z));
-    } else {
-      float top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < kVals; ++i) top = fmaxf(top, z[i]);
-      top = group_reduce<G>(top, Max());
-      if (top == -INFINITY) top = 0.0f;
-      float total_e = 0.0f, inner = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kVals; ++i) {
-        z[i] = __expf(z[i] - top);
-        total_e += z[i];
-        inner += z[i] * f[i];
-      }
-      total_e = group_sum<G>(total_e);
-      inner = group_sum<G>(inner);
-      const float inv = total_e == 0.0f ? 0.0f : 1.0f / total_e;
-      result = inner * inv;
-#pragma unroll
-      for (int i = 0; i < kVals; ++i) grad[i] = z[i] * inv * (f[i] - result) * scale;
     }
-    if (counts && lane == 0) sum += double(result);
-    if (a.grad && row < a.rows && col < a.experts) {
-      if (!counts) {
+    const bool counts = live;
+    live = row + step < a.rows && (ahead || !a.valid);
+    fetch(row + step, live);
+    ahead = mask(row + 2 * step);
 #pragma unroll
-        for (int i = 0; i < kVals; ++i) grad[i] = 0.0f;
+    for (int i = 0; i < kVals; ++i) grad[i] = 0.0f;
+    if (__any(counts)) {                // padding lies together: whole wavefronts pass by
+      float result;
+      if constexpr (kDistill) {
+        float top_z = -INFINITY, top_t = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kVals; ++i) {
+          top_z = fmaxf(top_z, z[i]);
+          top_t = fmaxf(top_t, t[i]);
+        }
+        top_z = group_reduce<G>(top_z, Max());
+        top_t = group_reduce<G>(top_t, Max());
+        if (top_z == -INFINITY) top_z = 0.0f;
+        if (top_t == -INFINITY) top_t = 0.0f;
+        float sum_z = 0.0f, sum_t = 0.0f, cross = 0.0f, p[kVals];
+#pragma unroll
+        for (int i = 0; i < kVals; ++i) {
+          z[i] -= top_z;
+          t[i] -= top_t;
+          sum_z += grad[i] = __builtin_amdgcn_exp2f(z[i] * a.to_log2);
+          sum_t += p[i] = __builtin_amdgcn_exp2f(t[i] * a.to_log2);
+        }
+        sum_z = group_sum<G>(sum_z);
+        sum_t = group_sum<G>(sum_t);
+        const bool nothing = sum_t == 0.0f || !counts;                     // the teacher's row is masked out whole
+        const bool empty = sum_z == 0.0f;                                  // the student's is
+        const float inv_z = nothing || empty ? 0.0f : __builtin_amdgcn_rcpf(sum_z), inv_t = nothing ? 0.0f : __builtin_amdgcn_rcpf(sum_t);
+#pragma unroll
+        for (int i = 0; i < kVals; ++i) {
+          p[i] *= inv_t;
+          cross += p[i] == 0.0f ? 0.0f : p[i] * (t[i] - z[i]);             // 0 log 0 = 0
+          grad[i] = nothing ? 0.0f : (grad[i] * inv_z - p[i]) * scale;
+        }
+        cross = group_sum<G>(cross);
+        constexpr float kLn2 = 0.693147180559945f;
+        result = cross * a.inv_tau + kLn2 * ((empty ? 0.0f : __builtin_amdgcn_logf(sum_z)) - __builtin_amdgcn_logf(sum_t));
+        if (nothing) result = 0.0f;
+      } else {
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kVals; ++i) top = fmaxf(top, z[i]);
+        top = group_reduce<G>(top, Max());
+        if (top == -INFINITY) top = 0.0f;
+        float total_e = 0.0f, inner = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kVals; ++i) {
+          z[i] = __builtin_amdgcn_exp2f((z[i] - top) * a.to_log2);
+          total_e += z[i];
+          inner += z[i] * f[i];
+        }
+        total_e = group_sum<G>(total_e);
+        inner = group_sum<G>(inner);
+        const bool nothing = total_e == 0.0f || !counts;
+        const float inv = nothing ? 0.0f : __builtin_amdgcn_rcpf(total_e);
+        result = nothing ? 0.0f : inner * inv;
+#pragma unroll
+        for (int i = 0; i < kVals; ++i) grad[i] = nothing ? 0.0f : z[i] * inv * (f[i] - result) * scale;
       }
-      store_run<ST, kVals>(static_cast<ST *>(a.grad) + row * a.grad_stride + col, grad, a.experts - col);
+      if (lane == 0) sum += double(result);
+    }
+    if (a.grad && row < a.rows && count) {
+      ST *to = static_cast<ST *>(a.grad) + row * a.grad_stride + col;
+      if (!skip) {
+        store_run<ST, kVals>(to, grad, count);
+      } else {
+#pragma unroll
+        for (int i = 1; i < kVals; ++i) if (i >= skip) to[i] = from_float<ST>(grad[i]);
+      }
     }
   }
   sum = block_sum<BLOCK>(sum) * double(kDistill ? share : scale);
@@ -221,8 +279,11 @@ __global__ __launch_bounds__(BLOCK) void loss_kernel(const LossArgs a) {
   }
 }
 
-__global__ __launch_bounds__(kLossBlocks) void loss_finish_kernel(const LossArgs a) {
-  const double s = block_sum<kLossBlocks>(int(threadIdx.x) < a.blocks ? a.partial[threadIdx.x] : 0.0);
+__global__ __launch_bounds__(kFinishBlock) void loss_finish_kernel(const LossArgs a) {
+  double s = 0.0;
+#pragma unroll
+  for (int i = threadIdx.x; i < kLossBlocks; i += kFinishBlock) s += i < a.blocks ? a.partial[i] : 0.0;
+  s = block_sum<kFinishBlock>(s);
   if (threadIdx.x == 0) *a.loss = float(s);
 }
 
@@ -245,14 +306,20 @@ hipError_t run_loss(hipStream_t stream, LossArgs &a) {
   const int64_t need = (a.rows + kLossBlock / G - 1) / (kLossBlock / G);
   a.blocks = int(need < kLossBlocks ? need : kLossBlocks);
   hipError_t e = hipSuccess;
-  if (a.bins || a.valid) e = launch(loss_count_kernel, kCountBlocks, kCountBlock, stream, a);
+  if (a.bins || a.valid) {
+    const int64_t need = (a.rows + 2 * kCountBlock - 1) / (2 * kCountBlock);
+    a.count_blocks = int(need < kCountBlocks ? need : kCountBlocks);
+    e = launch(loss_count_kernel, a.count_blocks, kCountBlock, stream, a);
+  }
   if (e == hipSuccess) e = launch(loss_kernel<ST, TT, G, kLossBlock>, a.blocks, kLossBlock, stream, a);
-  if (e == hipSuccess) e = launch(loss_finish_kernel, 1, kLossBlocks, stream, a);
+  if (e == hipSuccess) e = launch(loss_finish_kernel, 1, kFinishBlock, stream, a);
   return e;
 }
 
 template <typename ST, typename TT>
 hipError_t run_loss(hipStream_t stream, LossArgs &a) {
+  a.mask = a.valid ? a.valid : static_cast<const uint8_t *>(a.z);
+  a.mask_stride = a.valid ? 1 : 0;
   if (a.rows == 0) return launch(loss_none_kernel, 1, MOE_SPEC_MAX_EXPERTS, stream, a);
   switch (lanes_for(a.experts)) {
     case 1: return run_loss<ST, TT, 1>(stream, a);
@@ -265,7 +332,7 @@ hipError_t run_loss(hipStream_t stream, LossArgs &a) {
 }
 
 size_t partial_bytes() { return kLossBlocks * sizeof(double); }
-size_t counted_bytes(int experts) { return (size_t(kCountBlocks) * (experts + 1) * sizeof(int) + 15) / 16 * 16; }
+size_t counted_bytes(int bins) { return size_t(kCountBlocks) * padded_bins(bins) * sizeof(int); }
 
 bool sizes_fit(int64_t rows, int experts) {
   return rows >= 0 && rows <= MOE_SPEC_TRAIN_MAX_ROWS && experts >= 1 && experts <= MOE_SPEC_MAX_EXPERTS;
@@ -322,7 +389,7 @@ extern "C" int moe_spec_distill_loss(void *stream, int student_dtype, const void
   LossArgs a = {};
   a.z = student; a.teacher = teacher; a.grad = grad; a.valid = valid; a.loss = loss;
   a.z_stride = student_stride; a.teacher_stride = teacher_stride; a.grad_stride = grad_stride; a.rows = rows;
-  a.experts = n_experts; a.inv_tau = 1.0f / temperature;
+  a.experts = n_experts; a.inv_tau = 1.0f / temperature; a.to_log2 = 1.442695040888963f / temperature;
   a.partial = static_cast<double *>(workspace);
   if (workspace) a.counted = reinterpret_cast<int *>(static_cast<char *>(workspace) + partial_bytes());
   hipError_t e;
@@ -357,7 +424,7 @@ extern "C" int moe_spec_balance_loss(void *stream, int dtype, const void *logits
   LossArgs a = {};
   a.z = logits; a.grad = grad; a.valid = valid; a.ids = ids; a.loss = loss; a.counts = counts;
   a.z_stride = logits_stride; a.grad_stride = grad_stride; a.ids_stride = ids_stride; a.rows = rows;
-  a.experts = a.bins = n_experts; a.top_k = top_k; a.coef = coef; a.inv_tau = 1.0f;
+  a.experts = a.bins = n_experts; a.top_k = top_k; a.coef = coef; a.inv_tau = 1.0f; a.to_log2 = 1.442695040888963f;
   a.partial = static_cast<double *>(workspace);
   if (workspace) a.counted = reinterpret_cast<int *>(static_cast<char *>(workspace) + partial_bytes());
   const hipError_t e = dtype == MOE_SPEC_BF16 ? run_loss<uint16_t, void>(s, a) : run_loss<float, void>(s, a);

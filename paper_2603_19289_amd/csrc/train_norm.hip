@@ -13,7 +13,11 @@
 namespace moe_spec {
 namespace {
 
-constexpr int kMaxBlocks = 1024;        // workgroups of a launch: four or more per compute unit
+// Wavefronts of a launch, which walk over the rows: 16 a compute unit forward (32 of the shapes with one chunk a lane), 8
+// backward, where each workgroup's column sums are written and read once more and fewer of them cost less.  Measured, TB/s:
+// forward 32768 x 2048 bf16 with 8 / 16 / 20 / 32 wavefronts a compute unit 4.7 / 6.3 / 6.0 / 5.8, 65536 x 512 with 16 / 32
+// 5.2 / 5.8; backward 16387 x 4096 bf16 with 4 / 6 / 8 / 10 / 12 3.7 / 4.9 / 5.2 / 4.8 / 4.7.
+constexpr int kForwardWaves = 4096, kBackwardWaves = 2048, kMaxBlocks = 512;
 
 struct NormForwardArgs {
   const void *x;
@@ -39,15 +43,16 @@ struct NormBackwardArgs {
 // Row shape: LANES lanes with C chunks of V values each; chunk c of a lane begins at column (c * LANES + lane) * V.
 template <typename WT, int LANES, int C>
 struct Shape {
-  static constexpr int V = Packed<WT>::N, kLanes = LANES, kChunks = C;
-  static constexpr int kBlock = LANES <= kWave ? 256 : LANES, kRows = kBlock / LANES, kGroup = LANES < kWave ? LANES : kWave;
+  static constexpr int V = Packed<WT>::N, kLanes = LANES, kChunks = C, kGroup = LANES < kWave ? LANES : kWave;
   static constexpr int kWavesPerRow = LANES <= kWave ? 1 : LANES / kWave;
+  static constexpr int kBlock = LANES <= kWave ? 256 : LANES, kRows = kBlock / LANES;   // workgroup of the forward pass
+  static constexpr int kBlock2 = LANES <= kWave || LANES > 256 ? 512 : 256, kRows2 = kBlock2 / LANES;   // and of the backward pass
 };
 
 // Sums over a row's lanes of N values at once.  Rows of several wavefronts meet in LDS, in one of two places by turns: a
 // wavefront writes a place again only behind the barrier of the sum in between, which the others reach after they have read.
-template <int N, int GROUP, int WAVES>
-__device__ __forceinline__ void row_sums(float (&v)[N], float (*place)[N * WAVES], int &turn) {
+template <int N, int GROUP, int WAVES, int BLOCK>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*place)[N * BLOCK / kWave], int &turn) {
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = group_sum<GROUP>(v[i]);
   if constexpr (WAVES > 1) {
@@ -56,43 +61,64 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*place)[N * WAVES
     turn ^= 1;
     if (threadIdx.x % kWave == 0) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) at[i * WAVES + wave] = v[i];
+      for (int i = 0; i < N; ++i) at[wave * N + i] = v[i];
     }
     __syncthreads();
+    at += wave / WAVES * WAVES * N;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float s = 0.0f;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) s += at[i * WAVES + w];
+      for (int w = 0; w < WAVES; ++w) s += at[w * N + i];
       v[i] = s;
     }
   }
 }
 
-template <int V>
-__device__ __forceinline__ void load_columns(const float *p, int col, int cols, float none, float (&f)[V]) {
+// Where a lane's chunk lies in its row.
+template <int V, bool RAGGED>
+struct Place {
+  int col, count, skip;                 // first column; values that exist; those of them that are the neighbour's
+  bool used;
+  __device__ __forceinline__ Place(int index, int cols) {
+    col = index * V;
+    used = col < cols;
+    count = V;
+    skip = 0;
+    if constexpr (RAGGED) {
+      if (cols < V) count = cols;
+      else if (used && col + V > cols) {
+        skip = col + V - cols;
+        col = cols - V;
+      }
+    }
+  }
+  __device__ __forceinline__ bool mine(int i) const { return !RAGGED || (i >= skip && i < count); }
+};
+
+template <int V, bool RAGGED>
+__device__ __forceinline__ void load_columns(const float *p, const Place<V, RAGGED> &at, float none, float (&f)[V]) {
 #pragma unroll
   for (int i = 0; i < V; ++i) f[i] = none;
-  if (!p) return;
+  if (!p || !at.used) return;
   Run<float, V> r;
-  r.clear();
-  if (col < cols) r.load(p + col, cols - col, none);
+  r.load(p + at.col, at.count, none);
   r.get(f);
 }
 
-template <typename WT, int LANES, int C>
+template <typename WT, int LANES, int C, bool RAGGED>
 __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock)) void norm_forward_kernel(const NormForwardArgs a) {
   using S = Shape<WT, LANES, C>;
   constexpr int V = S::V;
-  __shared__ float place[2][S::kWavesPerRow];
+  __shared__ float place[2][S::kBlock / kWave];
   const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
   int turn = 0;
   float gain[C][V], bias[C][V];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int col = (c * LANES + lane) * V;
-    load_columns<V>(a.gain, col, a.cols, 1.0f, gain[c]);
-    load_columns<V>(a.bias, col, a.cols, 0.0f, bias[c]);
+    const Place<V, RAGGED> at(c * LANES + lane, a.cols);
+    load_columns(a.gain, at, 1.0f, gain[c]);
+    load_columns(a.bias, at, 0.0f, bias[c]);
   }
   const int64_t step = int64_t(gridDim.x) * S::kRows;
   Run<WT, V> next[C];
@@ -100,9 +126,9 @@ __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock)) void norm_forward_ke
     const WT *x = static_cast<const WT *>(a.x) + row * a.x_stride;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = (c * LANES + lane) * V;
+      const Place<V, RAGGED> at(c * LANES + lane, a.cols);
       next[c].clear();
-      if (row < a.rows && col < a.cols) next[c].load(x + col, a.cols - col);
+      if (row < a.rows && at.used) next[c].load(x + at.col, at.count);
     }
   };
   int64_t row = int64_t(blockIdx.x) * S::kRows + slot;
@@ -114,32 +140,34 @@ __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock)) void norm_forward_ke
     fetch(row + step);                  // the next row is on its way while this one is worked on
     float sum[1] = {0.0f};
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c) {
+      const Place<V, RAGGED> at(c * LANES + lane, a.cols);
 #pragma unroll
-      for (int i = 0; i < V; ++i) sum[0] += f[c][i];
-    row_sums<1, S::kGroup, S::kWavesPerRow>(sum, place, turn);
+      for (int i = 0; i < V; ++i) sum[0] += at.mine(i) ? f[c][i] : 0.0f;
+    }
+    row_sums<1, S::kGroup, S::kWavesPerRow, S::kBlock>(sum, place, turn);
     const float mean = sum[0] * a.inv_cols;
     float sq[1] = {0.0f};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int left = a.cols - (c * LANES + lane) * V;
+      const Place<V, RAGGED> at(c * LANES + lane, a.cols);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         f[c][i] -= mean;
-        if (i < left) sq[0] += f[c][i] * f[c][i];
+        if (at.used && at.mine(i)) sq[0] += f[c][i] * f[c][i];
       }
     }
-    row_sums<1, S::kGroup, S::kWavesPerRow>(sq, place, turn);
+    row_sums<1, S::kGroup, S::kWavesPerRow, S::kBlock>(sq, place, turn);
     const float rstd = 1.0f / sqrtf(sq[0] * a.inv_cols + a.eps);
     if (row < a.rows) {
       WT *y = static_cast<WT *>(a.y) + row * a.y_stride;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const int col = (c * LANES + lane) * V;
-        if (col < a.cols) {
+        const Place<V, RAGGED> at(c * LANES + lane, a.cols);
+        if (at.used) {
 #pragma unroll
           for (int i = 0; i < V; ++i) f[c][i] = f[c][i] * rstd * gain[c][i] + bias[c][i];
-          store_run<WT, V>(y + col, f[c], a.cols - col);
+          store_run<WT, V>(y + at.col, f[c], at.count);
         }
       }
       if (lane == 0) {
@@ -152,21 +180,21 @@ __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock)) void norm_forward_ke
 
 // One row after the other as above; the column sums of a workgroup's rows stay in registers and go out once, to its place in
 // the workspace, where norm_columns_kernel adds up the workgroups'.  No atomics: the order of the sums is fixed.
-template <typename WT, int LANES, int C>
-__global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock)) void norm_backward_kernel(const NormBackwardArgs a) {
+template <typename WT, int LANES, int C, bool RAGGED>
+__global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock2)) void norm_backward_kernel(const NormBackwardArgs a) {
   using S = Shape<WT, LANES, C>;
   constexpr int V = S::V;
-  __shared__ float place[2][2 * S::kWavesPerRow];
+  __shared__ float place[2][2 * S::kBlock2 / kWave];
   const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
   int turn = 0;
   float gain[C][V], dgain[C][V], dbias[C][V];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    load_columns<V>(a.gain, (c * LANES + lane) * V, a.cols, 1.0f, gain[c]);
+    load_columns(a.gain, Place<V, RAGGED>(c * LANES + lane, a.cols), 1.0f, gain[c]);
 #pragma unroll
     for (int i = 0; i < V; ++i) dgain[c][i] = dbias[c][i] = 0.0f;
   }
-  const int64_t step = int64_t(gridDim.x) * S::kRows;
+  const int64_t step = int64_t(gridDim.x) * S::kRows2;
   Run<WT, V> next_x[C], next_dy[C];
   float next_mean, next_rstd;
   auto fetch = [&](int64_t row) {
@@ -174,20 +202,20 @@ __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock)) void norm_backward_k
     const WT *dy = static_cast<const WT *>(a.dy) + row * a.dy_stride;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = (c * LANES + lane) * V;
+      const Place<V, RAGGED> at(c * LANES + lane, a.cols);
       next_x[c].clear();
       next_dy[c].clear();
-      if (row < a.rows && col < a.cols) {
-        next_x[c].load(x + col, a.cols - col);
-        next_dy[c].load(dy + col, a.cols - col);
+      if (row < a.rows && at.used) {
+        next_x[c].load(x + at.col, at.count);
+        next_dy[c].load(dy + at.col, at.count);
       }
     }
     next_mean = row < a.rows ? a.mean[row] : 0.0f;
     next_rstd = row < a.rows ? a.rstd[row] : 0.0f;
   };
-  int64_t row = int64_t(blockIdx.x) * S::kRows + slot;
+  int64_t row = int64_t(blockIdx.x) * S::kRows2 + slot;
   fetch(row);
-  for (int64_t first = int64_t(blockIdx.x) * S::kRows; first < a.rows; first += step, row += step) {
+  for (int64_t first = int64_t(blockIdx.x) * S::kRows2; first < a.rows; first += step, row += step) {
     float h[C][V], w[C][V], sums[2] = {0.0f, 0.0f};
     const float mean = next_mean, rstd = next_rstd;
 #pragma unroll
@@ -198,6 +226,7 @@ __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock)) void norm_backward_k
     fetch(row + step);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+      const Place<V, RAGGED> at(c * LANES + lane, a.cols);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float dy = w[c][i];       // zero behind the last column and the last row
@@ -205,21 +234,21 @@ __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock)) void norm_backward_k
         dgain[c][i] += dy * h[c][i];
         dbias[c][i] += dy;
         w[c][i] = dy * gain[c][i];
-        sums[0] += w[c][i];
-        sums[1] += w[c][i] * h[c][i];
+        sums[0] += at.mine(i) ? w[c][i] : 0.0f;
+        sums[1] += at.mine(i) ? w[c][i] * h[c][i] : 0.0f;
       }
     }
-    row_sums<2, S::kGroup, S::kWavesPerRow>(sums, place, turn);
+    row_sums<2, S::kGroup, S::kWavesPerRow, S::kBlock2>(sums, place, turn);
     const float c1 = sums[0] * a.inv_cols, c2 = sums[1] * a.inv_cols;
     if (a.dx && row < a.rows) {
       WT *dx = static_cast<WT *>(a.dx) + row * a.dx_stride;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const int col = (c * LANES + lane) * V;
-        if (col < a.cols) {
+        const Place<V, RAGGED> at(c * LANES + lane, a.cols);
+        if (at.used) {
 #pragma unroll
           for (int i = 0; i < V; ++i) w[c][i] = rstd * (w[c][i] - c1 - h[c][i] * c2);
-          store_run<WT, V>(dx + col, w[c], a.cols - col);
+          store_run<WT, V>(dx + at.col, w[c], at.count);
         }
       }
     }
@@ -236,37 +265,30 @@ __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock)) void norm_backward_k
       }
     }
   float *out = a.partial + size_t(blockIdx.x) * 2 * a.ld;
-  if constexpr (LANES <= kWave) {
-    constexpr int W = 256 / kWave, N = LANES * C * V;
-    __shared__ float sums[W][2][N];
-    const int wave = threadIdx.x / kWave;
+  // then the rows of the workgroup, one of the two sums after the other
+  constexpr int kParts = S::kBlock2 / (LANES < kWave ? kWave : LANES);
+  __shared__ float sums[kParts][LANES * C * V];
+  const int part = threadIdx.x / (LANES < kWave ? kWave : LANES);
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    if (which) __syncthreads();
     if (threadIdx.x % kWave < LANES) {
 #pragma unroll
-      for (int c = 0; c < C; ++c)
+      for (int c = 0; c < C; ++c) {
+        const Place<V, RAGGED> at(c * LANES + lane, a.cols);
+        if (!at.used) continue;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          sums[wave][0][(c * LANES + lane) * V + i] = dgain[c][i];
-          sums[wave][1][(c * LANES + lane) * V + i] = dbias[c][i];
-        }
+        for (int i = 0; i < V; ++i) sums[part][at.col + i] = which ? dbias[c][i] : dgain[c][i];
+      }
     }
     __syncthreads();
-    for (int at = threadIdx.x; at < 2 * a.ld; at += 256) {
-      const int which = at >= a.ld, col = which ? at - a.ld : at;
+    for (int col = threadIdx.x; col < a.ld; col += S::kBlock2) {
       float s = 0.0f;
       if (col < a.cols) {
 #pragma unroll
-        for (int v = 0; v < W; ++v) s += sums[v][which][col];
+        for (int k = 0; k < kParts; ++k) s += sums[k][col];
       }
-      out[at] = s;
-    }
-  } else {
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int col = (c * LANES + lane) * V;
-      if (col < a.cols) {               // a lane's columns end within ld, which is a multiple of eight
-        store_run<float, V>(out + col, dgain[c], V);
-        store_run<float, V>(out + a.ld + col, dbias[c], V);
-      }
+      out[which * a.ld + col] = s;
     }
   }
 }
@@ -278,7 +300,7 @@ __global__ __launch_bounds__(32 * kSlices) void norm_columns_kernel(const NormBa
   const int at = blockIdx.x * 32 + threadIdx.x % 32, slice = threadIdx.x / 32;
   double s = 0.0;
   if (at < 2 * a.ld) {
-#pragma unroll 4
+#pragma unroll 8
     for (int b = slice; b < a.blocks; b += kSlices) s += double(a.partial[size_t(b) * 2 * a.ld + at]);
   }
   part[slice][threadIdx.x % 32] = s;
@@ -293,9 +315,9 @@ __global__ __launch_bounds__(32 * kSlices) void norm_columns_kernel(const NormBa
   }
 }
 
-int blocks_for(int64_t rows, int rows_per_block) {
+int blocks_for(int64_t rows, int rows_per_block, int most) {
   const int64_t need = (rows + rows_per_block - 1) / rows_per_block;
-  return int(need < kMaxBlocks ? need : kMaxBlocks);
+  return int(need < most ? need : most);
 }
 
 // Calls f with the row shape for a number of columns, by the rule at the top.
@@ -317,7 +339,9 @@ template <typename WT>
 hipError_t forward(hipStream_t stream, NormForwardArgs &a) {
   return with_shape<WT>(a.cols, [&](auto shape) {
     using S = decltype(shape);
-    return launch(norm_forward_kernel<WT, S::kLanes, S::kChunks>, blocks_for(a.rows, S::kRows), S::kBlock, stream, a);
+    const int blocks = blocks_for(a.rows, S::kRows, (S::kChunks == 1 ? 2 : 1) * kForwardWaves * kWave / S::kBlock);
+    if (a.cols % S::V) return launch(norm_forward_kernel<WT, S::kLanes, S::kChunks, true>, blocks, S::kBlock, stream, a);
+    return launch(norm_forward_kernel<WT, S::kLanes, S::kChunks, false>, blocks, S::kBlock, stream, a);
   });
 }
 
@@ -325,9 +349,10 @@ template <typename WT>
 hipError_t backward(hipStream_t stream, NormBackwardArgs &a) {
   return with_shape<WT>(a.cols, [&](auto shape) {
     using S = decltype(shape);
-    a.blocks = blocks_for(a.rows, S::kRows);
+    a.blocks = blocks_for(a.rows, S::kRows2, kBackwardWaves * kWave / S::kBlock2);
     if (a.blocks) {
-      const hipError_t e = launch(norm_backward_kernel<WT, S::kLanes, S::kChunks>, a.blocks, S::kBlock, stream, a);
+      const hipError_t e = a.cols % S::V ? launch(norm_backward_kernel<WT, S::kLanes, S::kChunks, true>, a.blocks, S::kBlock2, stream, a)
+                                         : launch(norm_backward_kernel<WT, S::kLanes, S::kChunks, false>, a.blocks, S::kBlock2, stream, a);
       if (e != hipSuccess) return e;
     }
     if (!a.partial) return hipSuccess;
@@ -335,6 +360,7 @@ hipError_t backward(hipStream_t stream, NormBackwardArgs &a) {
   });
 }
 
+static_assert(kBackwardWaves * kWave / 256 <= kMaxBlocks, "the workspace has room for the shape with the most workgroups");
 int padded(int cols) { return (cols + 7) / 8 * 8; }
 
 }  // namespace
@@ -366,7 +392,7 @@ extern "C" int moe_spec_layernorm_forward(void *stream, int dtype, const void *x
 
 extern "C" size_t moe_spec_layernorm_backward_workspace_bytes(int64_t rows, int cols) {
   if (rows < 0 || rows > MOE_SPEC_TRAIN_MAX_ROWS || cols < 1 || cols > MOE_SPEC_TRAIN_MAX_COLS) return 0;
-  return size_t(blocks_for(rows, 1)) * 2 * padded(cols) * sizeof(float);
+  return size_t(blocks_for(rows, 1, kMaxBlocks)) * 2 * padded(cols) * sizeof(float);
 }
 
 extern "C" int moe_spec_layernorm_backward(void *stream, int dtype, const void *dy, int64_t dy_stride, const void *x,
