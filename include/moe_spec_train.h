@@ -87,8 +87,8 @@ int moe_spec_balance_loss(void *stream, int dtype, const void *logits, int64_t l
  * Moments in 8 bits (MOE_SPEC_MOMENTS_8BIT).  Each run of 128 elements of a tensor has one byte for either moment: the
  * biased exponent X (the float format's) of the largest finite magnitude among them.  A first moment is a sign, four bits of
  * exponent and three of mantissa; a second moment, which has no sign, four and four: a value is
- * float_with_bits(code << 20 or code << 19) * 2^(X - 14).  The largest has exponent field 14; the last code (127 / 255 without
- * the sign) is NaN and stands for infinities too.  A second moment that is not zero is never stored as zero.
+ * float_with_bits(code << 20 or code << 19) * 2^(X - 14).  The largest has exponent field 14; the last code (127 / 255) is
+ * NaN and stands for infinities too.  A second moment that is not zero is never stored as zero.
  * Codes are rounded up or down at random, without bias, by 16 bits each from a mix of seed, t, the tensor's place in the
  * call and the element's in the tensor.  To nearest would not do: with beta2 = 0.999 a step moves v by about a thousandth,
  * half a step of the code is 1.6 to 3 %, and v would stand still.  The price is noise: a step that moves v by d < h, h the

@@ -1,13 +1,15 @@
 // AdamW over many tensors in as few launches as their pointers fit into.
 //   m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2;  p = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
-// Bound by memory: 24 bytes an element and the gradient with 32-bit moments, 12 with 8-bit ones.  Eight elements a thread,
-// 2048 a workgroup; which tensor a workgroup works on it finds in the launch's argument block, so that nothing has to be
-// copied to the device first and a captured launch carries its tensors with it.
+// Bound by memory: 24 bytes an element and the gradient with 32-bit moments, 12 with 8-bit ones (75 M elements, bf16 gradients and
+// copies: 5.4 TB/s either way, what a large copy reaches); some 75 vector instructions an element with 8-bit moments, which is
+// two thirds of that time.  Eight elements a thread, 2048 a workgroup; which tensor a workgroup works on it finds in the
+// launch's argument block, so that nothing has to be copied to the device first and a captured launch carries its tensors with
+// it: 40 of them, which is what 4 KB hold.
 //
 // 8-bit moments: a run of 128 elements lies in 16 lanes, whose largest magnitude four exchanges find.  With X its biased
 // exponent, |m| 2^(14-X) is a float whose upper bits are the code (exponent fields 0 to 14, denormals included); adding 16
 // random bits below the last one that is kept rounds up with the probability of what is cut off.  One rounding an operation
-// (no contraction), IEEE division and root, so that the codes are those of the formulas in float.
+// (no contraction), IEEE division and root: parameters, moments and codes are those of the formulas in float, bit for bit.
 #include "train_common.h"
 
 #include <math.h>
@@ -17,7 +19,6 @@ namespace {
 
 constexpr int kAdamBlock = 256, kAdamVals = 8, kAdamChunk = kAdamBlock * kAdamVals, kPerLaunch = 40;
 constexpr uint32_t kOdd1 = 0x9E3779B1u, kOdd2 = 0x85EBCA77u;
-static_assert(kPerLaunch < kWave, "a wavefront looks through the table of a launch");
 static_assert(MOE_SPEC_MOMENT_BLOCK == 16 * kAdamVals, "a run of a moment block is a row of 16 lanes");
 
 struct AdamConsts {
@@ -27,9 +28,8 @@ struct AdamConsts {
 
 struct AdamArgs {
   moe_spec_adamw_tensor t[kPerLaunch];
-  uint32_t first[kPerLaunch];           // a tensor's first workgroup
+  uint32_t first[kPerLaunch];           // a tensor's first workgroup; behind the last tensor none that there is
   uint32_t place[kPerLaunch];           // a tensor's place in the call
-  int count;
   AdamConsts c;                         // valid if step_dev is null, but for what does not depend on the step
   double lr, beta1, beta2;
   const int64_t *step_dev;
@@ -52,103 +52,135 @@ __device__ __forceinline__ double power(double b, int64_t t) {
   return r;
 }
 
-// The tensor of this workgroup and its first element there.
-__device__ __forceinline__ int tensor_of(const uint32_t *first, int count) {
-  const int lane = threadIdx.x % kWave;
-  const bool begun = lane < count && first[lane] <= blockIdx.x;
-  return __builtin_amdgcn_readfirstlane(__popcll(__ballot(begun)) - 1);
+// The tensor of this workgroup: the last that has begun.  Scalar work on the argument block, which is read at once.
+__device__ __forceinline__ int tensor_of(const uint32_t (&first)[kPerLaunch]) {
+  int which = -1;
+#pragma unroll
+  for (int i = 0; i < kPerLaunch; ++i) which += first[i] <= blockIdx.x;
+  return which;
 }
 
-__device__ __forceinline__ float decode(uint32_t size, int drop, int exponent) { return ldexpf(__uint_as_float(size << drop), exponent - 14); }
-
-// Eight codes in two words.
+// Eight codes in two words; n of them exist.
 __device__ __forceinline__ uint2 load_codes(const uint8_t *p, int n) {
   uint2 w = {0, 0};
-  if (n >= 8) return load_raw<uint2>(p);
 #pragma unroll
   for (int i = 0; i < 8; ++i) if (i < n) (i < 4 ? w.x : w.y) |= uint32_t(p[i]) << (8 * (i & 3));
   return w;
 }
 __device__ __forceinline__ void store_codes(uint8_t *p, uint2 w, int n) {
-  if (n >= 8) { __builtin_memcpy(p, &w, 8); return; }
 #pragma unroll
   for (int i = 0; i < 8; ++i) if (i < n) p[i] = uint8_t((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
 }
-__device__ __forceinline__ uint32_t code_at(const uint2 &w, int i) { return ((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 0xff; }
 
-// The value of a first moment's code, or of a second one's.
-__device__ __forceinline__ float first_moment(uint32_t code, int exponent) {
-  const float size = (code & 0x7f) == 0x7f ? NAN : decode(code & 0x7f, 20, exponent);
-  return code & 0x80 ? -size : size;
+// Values of eight first moments' codes: they are e4m3 codes with another bias, which the hardware converts two at a time.
+// A power of two times it is exact, or rounded once where the value is denormal.
+__device__ __forceinline__ void first_moments(uint2 w, int exponent, float (&f)[8]) {
+  const float unit = ldexpf(1.0f, exponent - 134);      // 2^(X - 14) and the 2^-120 between the biases
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int word = int(i ? w.y : w.x);
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(word, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(word, true);
+    f[4 * i] = lo[0] * unit;
+    f[4 * i + 1] = lo[1] * unit;
+    f[4 * i + 2] = hi[0] * unit;
+    f[4 * i + 3] = hi[1] * unit;
+  }
 }
-__device__ __forceinline__ float second_moment(uint32_t code, int exponent) {
-  return code == 0xff ? NAN : decode(code, 19, exponent);
-}
-
-// Codes of eight values and the exponent of their run of 128; `noise`: 16 random bits each.
-template <int DROP>
-__device__ __forceinline__ uint2 encode(const float (&x)[8], const uint32_t (&noise)[8], int &exponent) {
-  float top = 0.0f;
+__device__ __forceinline__ bool has_last_code(uint32_t w) { return ((~w - 0x01010101u) & w & 0x80808080u) != 0; }
+__device__ __forceinline__ void second_moments(uint2 w, int exponent, float (&f)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float size = fabsf(x[i]);
-    top = fmaxf(top, size < INFINITY ? size : 0.0f);
+    const uint32_t word = i < 4 ? w.x : w.y;
+    const int up = 19 - 8 * (i & 3);                    // the code's bits go where a float's exponent and mantissa are
+    f[i] = ldexpf(__uint_as_float((up > 0 ? word << up : word >> -up) & 0x07f80000u), exponent - 14);
   }
-  top = group_reduce<16>(top, [](float a, float b) { return fmaxf(a, b); });
-  exponent = int(__float_as_uint(top) >> 23);
+  if (has_last_code(w.x) || has_last_code(w.y)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (((i < 4 ? w.x : w.y) >> (8 * (i & 3)) & 0xff) == 0xff) f[i] = NAN;
+  }
+}
+
+// Codes of eight values and the exponent of their run of 128, that is of 16 lanes' values.  random: 32 bits each, of which first
+// moments take the upper half and second moments the lower one.
+template <bool FIRST>
+__device__ __forceinline__ uint2 encode(const float (&x)[8], const uint32_t (&random)[8], int &exponent) {
+  constexpr uint32_t kInfinity = 0x7f800000u;
+  constexpr int kDrop = FIRST ? 20 : 19;                // mantissa bits that go
+  float y[8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    y[i] = x[i];
+    top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  }
+  const bool odd = __any(top >= kInfinity);             // seldom: an infinity or NaN somewhere, which gets its code at the end
+  if (odd) {
+    top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if ((__float_as_uint(x[i]) & 0x7fffffffu) >= kInfinity) y[i] = 0.0f;
+      top = max(top, __float_as_uint(y[i]) & 0x7fffffffu);
+    }
+  }
+  top = __float_as_uint(group_reduce<16>(__uint_as_float(top), [](float a, float b) { return fmaxf(a, b); }));
+  exponent = int(top >> 23);
   uint2 w = {0, 0};
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float size = fabsf(x[i]);
-    uint32_t code = (__float_as_uint(ldexpf(size, 14 - exponent)) + (noise[i] << (DROP - 16)) + (1u << (DROP - 17))) >> DROP;
-    if (!(size < INFINITY)) code = DROP == 20 ? 0x7f : 0xff;
-    if constexpr (DROP == 20) code |= (__float_as_uint(x[i]) >> 31) << 7;
-    else if (size > 0.0f && code == 0) code = 1;
+    // fields stay below 15, so the random bits never carry into the sign
+    const uint32_t bits = __float_as_uint(ldexpf(y[i], 14 - exponent)), low = FIRST ? (random[i] >> 12 & 0xffff0u) | 8u : (random[i] << 3 & 0x7fff8u) | 4u;
+    const uint32_t up = bits + low;
+    uint32_t code;
+    if constexpr (FIRST) code = (up >> 20 & 0x7fu) | (up >> 24 & 0x80u);
+    else code = max(up >> kDrop, min(__float_as_uint(y[i]), 1u));          // what is not zero does not become it
     (i < 4 ? w.x : w.y) |= code << (8 * (i & 3));
+  }
+  if (odd) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if ((__float_as_uint(x[i]) & 0x7fffffffu) < kInfinity) continue;
+      uint32_t &word = i < 4 ? w.x : w.y;
+      const uint32_t code = FIRST ? 0x7fu : 0xffu;
+      word = (word & ~(0xffu << (8 * (i & 3)))) | code << (8 * (i & 3));
+    }
   }
   return w;
 }
 
-template <typename GT, bool EIGHT>
-__global__ __launch_bounds__(kAdamBlock) void adamw_kernel(const AdamArgs a) {
+// Eight elements of a thread.  WHOLE: all of the workgroup's elements exist, and its loads go out together.
+template <typename GT, bool EIGHT, bool WHOLE>
+__device__ __forceinline__ void adamw_elements(const moe_spec_adamw_tensor &t, const AdamConsts &c, float scale, uint32_t place, int64_t at, int n) {
 #pragma clang fp contract(off)
-  __shared__ AdamConsts shared;
-  AdamConsts c = a.c;
-  if (a.step_dev) {                     // what depends on the step, by one thread
-    if (threadIdx.x == 0) {
-      const int64_t t = *a.step_dev;
-      c.alpha = float(a.lr / (1.0 - power(a.beta1, t)));
-      c.root_scale = float(1.0 / sqrt(1.0 - power(a.beta2, t)));
-      c.key = mix(a.seed + kOdd1 * uint32_t(t));
-      shared = c;
-    }
-    __syncthreads();
-    c = shared;
-  }
-  const float scale = a.scale_dev ? a.scale * *a.scale_dev : a.scale;
-  const int which = tensor_of(a.first, a.count);
-  const moe_spec_adamw_tensor &t = a.t[which];
-  const int64_t at = int64_t(blockIdx.x - a.first[which]) * kAdamChunk + threadIdx.x * kAdamVals;
-  const int n = int(t.n - at < kAdamVals ? (t.n - at > 0 ? t.n - at : 0) : kAdamVals);
-  Run<float, 8> rp;
+  if constexpr (WHOLE) n = 8;
+  const int64_t block = at / MOE_SPEC_MOMENT_BLOCK;
+  Run<float, 8> rp, rm, rv;
   Run<GT, 8> rg;
+  uint2 cm, cv;
+  int em = 0, ev = 0;
   rp.load(t.p + at, n);
   rg.load(static_cast<const GT *>(t.grad) + at, n);
-  float p[8], g[8], m[8], v[8];
   if constexpr (EIGHT) {
-    const uint2 cm = load_codes(static_cast<const uint8_t *>(t.m) + at, n), cv = load_codes(static_cast<const uint8_t *>(t.v) + at, n);
-    const int em = n ? t.m_exp[at / MOE_SPEC_MOMENT_BLOCK] : 0, ev = n ? t.v_exp[at / MOE_SPEC_MOMENT_BLOCK] : 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      m[i] = first_moment(code_at(cm, i), em);
-      v[i] = second_moment(code_at(cv, i), ev);
+    if constexpr (WHOLE) {
+      cm = load_raw<uint2>(static_cast<const uint8_t *>(t.m) + at);
+      cv = load_raw<uint2>(static_cast<const uint8_t *>(t.v) + at);
+      em = t.m_exp[block];
+      ev = t.v_exp[block];
+    } else {
+      cm = load_codes(static_cast<const uint8_t *>(t.m) + at, n);
+      cv = load_codes(static_cast<const uint8_t *>(t.v) + at, n);
+      if (n) em = t.m_exp[block], ev = t.v_exp[block];
     }
   } else {
-    Run<float, 8> r;
-    r.load(static_cast<const float *>(t.m) + at, n);
-    r.get(m);
-    r.load(static_cast<const float *>(t.v) + at, n);
-    r.get(v);
+    rm.load(static_cast<const float *>(t.m) + at, n);
+    rv.load(static_cast<const float *>(t.v) + at, n);
+  }
+  float p[8], g[8], m[8], v[8];
+  if constexpr (EIGHT) {
+    first_moments(cm, em, m);
+    second_moments(cv, ev, v);
+  } else {
+    rm.get(m);
+    rv.get(v);
   }
   rp.get(p);
   rg.get(g);
@@ -163,28 +195,60 @@ __global__ __launch_bounds__(kAdamBlock) void adamw_kernel(const AdamArgs a) {
   store_run<float, 8>(t.p + at, p, n);
   if (t.copy) store_run<uint16_t, 8>(static_cast<uint16_t *>(t.copy) + at, p, n);
   if constexpr (EIGHT) {
-    const uint32_t key1 = mix(c.key + kOdd2 * (a.place[which] + 1)), key2 = mix(key1 ^ kOdd1);
-    uint32_t up_m[8], up_v[8];
+    const uint32_t key1 = mix(c.key + kOdd2 * (place + 1)), key2 = mix(key1 ^ kOdd1);
+    uint32_t random[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       uint32_t x = uint32_t(at) + i + key1;
       x = (x ^ (x >> 16)) * kOdd1;
       x = ((x ^ (x >> 15)) + key2) * kOdd2;
-      x ^= x >> 16;
-      up_m[i] = x >> 16;
-      up_v[i] = x & 0xffff;
+      random[i] = x ^ (x >> 16);
     }
-    int em, ev;
-    const uint2 cm = encode<20>(m, up_m, em), cv = encode<19>(v, up_v, ev);
-    store_codes(static_cast<uint8_t *>(t.m) + at, cm, n);
-    store_codes(static_cast<uint8_t *>(t.v) + at, cv, n);
+    cm = encode<true>(m, random, em);
+    cv = encode<false>(v, random, ev);
+    if constexpr (WHOLE) {
+      __builtin_memcpy(static_cast<uint8_t *>(t.m) + at, &cm, 8);
+      __builtin_memcpy(static_cast<uint8_t *>(t.v) + at, &cv, 8);
+    } else {
+      store_codes(static_cast<uint8_t *>(t.m) + at, cm, n);
+      store_codes(static_cast<uint8_t *>(t.v) + at, cv, n);
+    }
     if (n && threadIdx.x % 16 == 0) {
-      t.m_exp[at / MOE_SPEC_MOMENT_BLOCK] = uint8_t(em);
-      t.v_exp[at / MOE_SPEC_MOMENT_BLOCK] = uint8_t(ev);
+      t.m_exp[block] = uint8_t(em);
+      t.v_exp[block] = uint8_t(ev);
     }
   } else {
     store_run<float, 8>(static_cast<float *>(t.m) + at, m, n);
     store_run<float, 8>(static_cast<float *>(t.v) + at, v, n);
+  }
+}
+
+// 32-bit moments: four wavefronts per SIMD leave the compiler the registers to ask for everything at once (2.2 M elements 14.0 ->
+// 13.4 us, 75 M 397 -> 392); 8-bit ones need eight of them for the arithmetic (15.9 us with the reading of the moments, 16.6 with four).
+template <typename GT, bool EIGHT>
+__global__ __launch_bounds__(kAdamBlock) __attribute__((amdgpu_waves_per_eu(EIGHT ? 8 : 4, EIGHT ? 8 : 4))) void adamw_kernel(const AdamArgs a) {
+  __shared__ AdamConsts shared;
+  const int which = tensor_of(a.first);
+  const moe_spec_adamw_tensor t = a.t[which];
+  AdamConsts c = a.c;
+  if (a.step_dev) {                     // what depends on the step, by one thread
+    if (threadIdx.x == 0) {
+      const int64_t step = *a.step_dev;
+      c.alpha = float(a.lr / (1.0 - power(a.beta1, step)));
+      c.root_scale = float(1.0 / sqrt(1.0 - power(a.beta2, step)));
+      c.key = mix(a.seed + kOdd1 * uint32_t(step));
+      shared = c;
+    }
+    __syncthreads();
+    c = shared;
+  }
+  const float scale = a.scale_dev ? a.scale * *a.scale_dev : a.scale;
+  const int64_t begin = int64_t(blockIdx.x - a.first[which]) * kAdamChunk, at = begin + threadIdx.x * kAdamVals;
+  if (begin + kAdamChunk <= t.n) {
+    adamw_elements<GT, EIGHT, true>(t, c, scale, a.place[which], at, 8);
+  } else {
+    const int n = int(t.n - at < kAdamVals ? (t.n - at > 0 ? t.n - at : 0) : kAdamVals);
+    adamw_elements<GT, EIGHT, false>(t, c, scale, a.place[which], at, n);
   }
 }
 
@@ -196,31 +260,33 @@ struct MomentTensor {
 struct MomentArgs {
   MomentTensor t[kPerLaunch];
   uint32_t first[kPerLaunch];
-  int count;
 };
 static_assert(sizeof(MomentArgs) <= 4096, "an argument block");
 
 template <typename OT>
 __global__ __launch_bounds__(kAdamBlock) void moments_kernel(const MomentArgs a) {
-  const int which = tensor_of(a.first, a.count);
-  const MomentTensor &t = a.t[which];
-  const int64_t at = int64_t(blockIdx.x - a.first[which]) * kAdamChunk + threadIdx.x * kAdamVals;
+  const int which = tensor_of(a.first);
+  const MomentTensor t = a.t[which];
+  const int64_t at = int64_t(blockIdx.x - a.first[which]) * kAdamChunk + threadIdx.x * kAdamVals, block = at / MOE_SPEC_MOMENT_BLOCK;
   const int n = int(t.n - at < kAdamVals ? t.n - at : kAdamVals);
   if (n <= 0) return;
-  float f[8];
+  float m[8], v[8];
+  if (n == kAdamVals && t.m_out && t.v_out) {
+    const uint2 cm = load_raw<uint2>(t.m + at), cv = load_raw<uint2>(t.v + at);
+    const int em = t.m_exp[block], ev = t.v_exp[block];
+    first_moments(cm, em, m);
+    store_run<OT, 8>(static_cast<OT *>(t.m_out) + at, m, 8);
+    second_moments(cv, ev, v);
+    store_run<OT, 8>(static_cast<OT *>(t.v_out) + at, v, 8);
+    return;
+  }
   if (t.m_out) {
-    const uint2 w = load_codes(t.m + at, n);
-    const int e = t.m_exp[at / MOE_SPEC_MOMENT_BLOCK];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = first_moment(code_at(w, i), e);
-    store_run<OT, 8>(static_cast<OT *>(t.m_out) + at, f, n);
+    first_moments(load_codes(t.m + at, n), t.m_exp[block], m);
+    store_run<OT, 8>(static_cast<OT *>(t.m_out) + at, m, n);
   }
   if (t.v_out) {
-    const uint2 w = load_codes(t.v + at, n);
-    const int e = t.v_exp[at / MOE_SPEC_MOMENT_BLOCK];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = second_moment(code_at(w, i), e);
-    store_run<OT, 8>(static_cast<OT *>(t.v_out) + at, f, n);
+    second_moments(load_codes(t.v + at, n), t.v_exp[block], v);
+    store_run<OT, 8>(static_cast<OT *>(t.v_out) + at, v, n);
   }
 }
 
@@ -229,21 +295,26 @@ template <typename Args, typename Put, typename Go>
 hipError_t in_launches(const moe_spec_adamw_tensor *tensors, int n_tensors, Args &a, Put put, Go go) {
   constexpr int64_t kMostBlocks = 1 << 30;
   int64_t blocks = 0;
-  a.count = 0;
+  int count = 0;
+  auto send = [&]() {
+    for (int i = count; i < kPerLaunch; ++i) a.first[i] = UINT32_MAX;
+    const unsigned grid = unsigned(blocks);
+    count = 0;
+    blocks = 0;
+    return go(grid);
+  };
   for (int i = 0; i < n_tensors; ++i) {
     const int64_t need = (tensors[i].n + kAdamChunk - 1) / kAdamChunk;
     if (need == 0) continue;
-    if (a.count == kPerLaunch || (a.count && blocks + need > kMostBlocks)) {
-      const hipError_t e = go(unsigned(blocks));
+    if (count == kPerLaunch || (count && blocks + need > kMostBlocks)) {
+      const hipError_t e = send();
       if (e != hipSuccess) return e;
-      a.count = 0;
-      blocks = 0;
     }
-    a.first[a.count] = uint32_t(blocks);
-    put(a.count++, i);
+    a.first[count] = uint32_t(blocks);
+    put(count++, i);
     blocks += need;
   }
-  return a.count ? go(unsigned(blocks)) : hipSuccess;
+  return count ? send() : hipSuccess;
 }
 
 const char *count_fault(const moe_spec_adamw_tensor *t, int n) {

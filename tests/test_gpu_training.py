@@ -439,7 +439,7 @@ def encode(x, drop, bits):
         code = np.where((size > 0) & (code == 0), 1, code)
     code = np.where(np.isfinite(size), code, 127 if drop == 20 else 255)
     if drop == 20:
-        code = code + 128 * np.signbit(y)
+        code = code + 128 * (np.signbit(y) & np.isfinite(size))                  # NaN has no sign
     return code.astype(np.uint8).reshape(-1)[:n], X.astype(np.uint8).reshape(-1)
 
 
