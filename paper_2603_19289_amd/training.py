@@ -268,3 +268,76 @@ class AdamW:
         pointers = lambda out: None if out is None else (C.c_void_p * len(out))(*[t.data_ptr() for t in out])  # noqa: E731
         _queue(self.device, M.lib().moe_spec_adamw_read_moments, self._desc, len(self._desc), _TYPES[dtype], pointers(m_out), pointers(v_out))
         return m_out, v_out
+
+
+class EstimatorTrainer:
+    """Distils the expert estimator (paper: Appendix A) from the routers it stands in for.
+
+    weights: the estimator's tables under the names that Engine and workload.make_estimator use (proj, layer_emb, ffn_in,
+    ffn_out, ln_gain, ln_bias, head), as numpy arrays in storage format or as tensors on the GPU.  Tensors are trained in place:
+    given an Engine's own (`engine.est`), its predictions follow the training, as its context reads the same memory; the caller
+    keeps the engine's stream and the training stream apart in time.  bfloat16 tables have float32 masters here and are the
+    copies that AdamW writes; products then take bfloat16 operands and add up in float32, in the library that torch
+    calls for plain matrix products, and what lies between them is bfloat16 too.  LayerNorm, losses and AdamW are this library's."""
+
+    NAMES = ("proj", "layer_emb", "ffn_in", "ffn_out", "ln_gain", "ln_bias", "head")
+
+    def __init__(self, weights: dict, *, lr: float = 1e-3, balance_coef: float = 0.0, ln_eps: float = 1e-5, device="cuda:0", **adamw):
+        from .engine import _np_to_torch_storage
+        to = lambda v: v if isinstance(v, torch.Tensor) else _np_to_torch_storage(v).to(device)  # noqa: E731
+        self.weights = {k: to(weights[k]) for k in self.NAMES}
+        self.dtype = self.weights["proj"].dtype
+        masters = {k: (v if v.dtype == torch.float32 else v.float()) for k, v in self.weights.items()}
+        self.optimizer = AdamW([masters[k] for k in self.NAMES], lr=lr, copies=[
+            self.weights[k] if self.weights[k] is not masters[k] else None for k in self.NAMES], **adamw)
+        self.balance_coef, self.ln_eps = balance_coef, ln_eps
+
+    @torch.no_grad()
+    def gradients(self, layers: Sequence[int], signal: torch.Tensor, teacher: torch.Tensor, ids: Optional[torch.Tensor] = None,
+                  valid: Optional[torch.Tensor] = None):
+        """Losses and gradients for the predicting signals [n, T, H] of n different layers and the logits [n, T, E] that the
+        next layers' routers gave -> (dict of loss, balance, counts; dict of gradients).  ids: the experts that these
+        routers chose, int32 [n, T, k], for the balance loss and the counts.  valid: [n, T], 0 for padding."""
+        n, tokens, hidden = signal.shape
+        if len(set(layers)) != n or len(layers) != n:
+            raise ValueError("a layer of its own for each of the signals is needed")
+        w = self.weights
+        flat = lambda t: None if t is None else t.reshape(n * tokens, *t.shape[2:])  # noqa: E731
+        at = torch.as_tensor(list(layers), device=signal.device)
+        x = flat(signal).to(self.dtype)
+        u = (torch.mm(x, w["proj"].T).view(n, tokens, -1) + w["layer_emb"][at][:, None]).reshape(n * tokens, -1)
+        h = torch.mm(u, w["ffn_in"].T)
+        gate = torch.sigmoid(h)
+        act = h * gate
+        v = u + torch.mm(act, w["ffn_out"].T)
+        y, mean, rstd = layernorm_forward(v, w["ln_gain"], w["ln_bias"], self.ln_eps)
+        z = torch.mm(y, w["head"].T)
+        mask = flat(valid)
+        loss, dz = distill_loss(z, flat(teacher), valid=mask)
+        out = {"loss": loss}
+        if ids is not None:
+            out["balance"], out["counts"], extra = balance_loss(z, flat(ids), coef=self.balance_coef, valid=mask,
+                                                                grad=self.balance_coef != 0.0)
+            if extra is not None:
+                dz = dz + extra
+        g = {"head": torch.mm(dz.T, y)}
+        dv, g["ln_gain"], g["ln_bias"] = layernorm_backward(torch.mm(dz, w["head"]), v, mean, rstd, w["ln_gain"])
+        g["ffn_out"] = torch.mm(dv.T, act)
+        dh = torch.mm(dv, w["ffn_out"]) * (gate * (1.0 + h * (1.0 - gate)))
+        g["ffn_in"] = torch.mm(dh.T, u)
+        du = dv + torch.mm(dh, w["ffn_in"])
+        g["proj"] = torch.mm(du.T, x)
+        g["layer_emb"] = torch.zeros(w["layer_emb"].shape, device=signal.device)
+        g["layer_emb"][at] = du.view(n, tokens, -1).sum(1, dtype=torch.float32)
+        return out, g
+
+    def step(self, layers, signal, teacher, ids=None, valid=None, *, grad_scale=1.0) -> dict:
+        """One training step; returns the losses (and counts) from before it."""
+        out, g = self.gradients(layers, signal, teacher, ids, valid)
+        self.optimizer.step([g[k].float() for k in self.NAMES], grad_scale=grad_scale)
+        return out
+
+    def numpy_weights(self) -> dict:
+        """The weights in storage format, for a new Engine or a file (bfloat16 as uint16 bit patterns)."""
+        return {k: (v.view(torch.int16).cpu().numpy().view("uint16") if v.dtype == torch.bfloat16 else v.cpu().numpy())
+                for k, v in self.weights.items()}

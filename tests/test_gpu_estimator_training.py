@@ -1,0 +1,108 @@
+"""The estimator's training path: its gradients against a 64-bit reverse pass of the same formulas, and what it trains as the
+estimator that an engine predicts with."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import moe_oracle as O
+from paper_2603_19289_amd import workload as W
+from tests.helpers import build, small_workload
+
+pytestmark = pytest.mark.gpu
+
+NAMES = ("proj", "layer_emb", "ffn_in", "ffn_out", "ln_gain", "ln_bias", "head")
+
+
+def batch(wl, n, tokens, seed):
+    g = torch.Generator().manual_seed(seed)
+    signal = torch.randn(n, tokens, wl.hidden, generator=g)
+    teacher = 1.5 * torch.randn(n, tokens, wl.n_experts, generator=g)
+    ids = teacher.topk(wl.top_k, -1).indices.to(torch.int32)
+    valid = torch.rand(n, tokens, generator=g) < 0.8
+    return signal, teacher, ids, valid
+
+
+def decoded(est):
+    return {k: torch.from_numpy(O.decode_weights(v) if v.dtype == np.uint16 else v.astype(np.float64)) for k, v in est.items()}
+
+
+def reverse_pass(est, layers, signal, teacher, ids, valid, coef):
+    """Losses and gradients in 64 bits, by torch's differentiation of elementary operations."""
+    w = {k: v.clone().requires_grad_() for k, v in decoded(est).items()}
+    n, tokens, _ = signal.shape
+    u = signal.double() @ w["proj"].T + w["layer_emb"][list(layers)][:, None]
+    h = u @ w["ffn_in"].T
+    v = u + (h * torch.sigmoid(h)) @ w["ffn_out"].T
+    c = v - v.mean(-1, keepdim=True)
+    y = c / torch.sqrt((c * c).mean(-1, keepdim=True) + 1e-5) * w["ln_gain"] + w["ln_bias"]
+    z = y @ w["head"].T
+    live = valid.double()
+    p, log_q = torch.softmax(teacher.double(), -1), z - torch.logsumexp(z, -1, keepdim=True)
+    loss = ((p * (p.log() - log_q)).sum(-1) * live).sum() / live.sum()
+    counts = torch.bincount(ids[valid].reshape(-1).long(), minlength=z.shape[-1])
+    f = counts.double() / live.sum() / ids.shape[-1]
+    balance = coef * z.shape[-1] * (f * (log_q.exp() * live[..., None]).sum((0, 1)) / live.sum()).sum()
+    (loss + balance).backward()
+    return loss.item(), balance.item(), counts, {k: t.grad for k, t in w.items()}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_equal_those_of_a_64_bit_reverse_pass(dtype):
+    """Relative to the largest gradient of a table.  float32: six products of at most 264 terms one after the other, each off by at
+    most 264 u of its terms' magnitudes, which are below 20 times what they add up to here: 6 * 264 * 20 * 2^-24 = 2e-3.  bfloat16: ten
+    roundings of 2^-8 on the way to any gradient, not all of one sign: their sum, 4e-2."""
+    from paper_2603_19289_amd import training as T
+    wl = small_workload(name="training", n_layers=5, hidden=264, n_experts=12, top_k=3, inter=200, dtype=dtype, batch=1, tokens=1, slots=6, seed=5)
+    est = W.make_estimator(wl, m=3, n=2)
+    layers = [3, 0, 2]
+    signal, teacher, ids, valid = batch(wl, 3, 37, 1)
+    trainer = T.EstimatorTrainer(est, balance_coef=0.1)
+    out, grads = trainer.gradients(layers, signal.cuda(), teacher.cuda(), ids.cuda(), valid.cuda())
+    loss, balance, counts, want = reverse_pass(est, layers, signal, teacher, ids, valid, 0.1)
+    tol = 2e-3 if dtype == "f32" else 4e-2
+    assert abs(out["loss"].item() - loss) < tol * loss and abs(out["balance"].item() - balance) < tol * balance
+    assert torch.equal(out["counts"].cpu().long(), counts)
+    for k in NAMES:
+        off = (grads[k].cpu().double() - want[k]).abs().max() / want[k].abs().max()
+        assert off < tol, (k, off)
+    assert not grads["layer_emb"][[1, 4]].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("state", ["f32", "f8"])
+def test_an_engine_predicts_with_what_is_trained_in_its_memory(dtype, state):
+    """The engine's own tables are trained in place between decode steps; its predictions are the oracle's with the trained tables."""
+    from paper_2603_19289_amd import training as T
+    from paper_2603_19289_amd.engine import engine_for
+    wl = small_workload(name="training", n_layers=4, hidden=264, n_experts=12, top_k=3, inter=200, dtype=dtype, batch=3, tokens=1, slots=9, seed=6)
+    res, ex, model = build(wl, "random")
+    est = W.make_estimator(wl, m=3, n=2)
+    eng = engine_for(wl, O.MODE_SPECULATIVE, res, ex, estimator=est)
+    try:
+        trainer = T.EstimatorTrainer(eng.est, lr=0.02, state=state, seed=1)
+        for step in range(3):
+            signal, teacher, ids, valid = (t.cuda() for t in batch(wl, 2, 50, 10 + step))
+            trainer.step([step, 3], signal, teacher, ids, valid)
+        torch.cuda.synchronize()
+        trained = trainer.numpy_weights()
+        for k in NAMES:
+            now = eng.est[k].view(torch.int16).cpu().numpy().view(np.uint16) if eng.est[k].dtype == torch.bfloat16 else eng.est[k].cpu().numpy()
+            assert np.array_equal(now, trained[k]) and not np.array_equal(trained[k], est[k]), k
+        x0, eps = W.make_inputs(wl)
+        advance = lambda t, l, r, o: W.advance_residual(wl, r, o, eps[t, l])  # noqa: E731
+        trace = {}
+        for name, weights in (("trained", trained), ("before", est)):
+            orc = O.MoEOracle(model, O.MODE_SPECULATIVE, wl.slots, estimator=O.Estimator(**weights), estimator_layers=range(wl.n_layers))
+            trace[name] = O.run_tokens(orc, x0, advance)
+        eng.begin_token()
+        for l in range(wl.n_layers):
+            r, want = trace["trained"][0][l]
+            _, got = eng.layer_step(l, torch.from_numpy(r.astype(np.float32)).cuda(), want_ids=True)
+            torch.cuda.synchronize()
+            assert np.array_equal(got["exec_ids"].cpu().numpy(), want.exec_ids), l
+            if l + 1 < wl.n_layers:
+                assert np.array_equal(got["next_ids"].cpu().numpy(), trace["trained"][0][l + 1][1].exec_ids), l
+        first = trace["before"][0][1][1].exec_ids
+        assert not np.array_equal(first, trace["trained"][0][1][1].exec_ids)     # training did change what is predicted
+    finally:
+        eng.close()
