@@ -71,6 +71,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 __device__ __forceinline__ uint16_t to_bf16(float x) { return uint16_t(pack_bf16(x, 0.0f)); }
 
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(uint16_t x) { return __uint_as_float(uint32_t(x) << 16); }
 template <typename WT> __device__ __forceinline__ WT from_float(float x);
 template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <> __device__ __forceinline__ uint16_t from_float<uint16_t>(float x) { return to_bf16(x); }

@@ -178,6 +178,36 @@ __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock)) void norm_forward_ke
   }
 }
 
+// Column sums of few rows: sixteen columns a workgroup, the rows over its threads, straight from dy and x.  These workgroups run
+// beside those that form dx, in the same launch.
+constexpr int kDirectCols = 16;
+template <typename WT, int BLOCK>
+__device__ __forceinline__ void direct_columns(const NormBackwardArgs &a, int index) {
+  constexpr int kSlices = BLOCK / kDirectCols;
+  __shared__ float part[2][kSlices][kDirectCols + 1];
+  const int lane = threadIdx.x % kDirectCols, slice = threadIdx.x / kDirectCols;
+  const int col = index * kDirectCols + lane, from = col < a.cols ? col : a.cols - 1;
+  float dgain = 0.0f, dbias = 0.0f;
+#pragma unroll 8
+  for (int64_t row = slice; row < a.rows; row += kSlices) {
+    const float x = to_float(static_cast<const WT *>(a.x)[row * a.x_stride + from]);
+    const float dy = to_float(static_cast<const WT *>(a.dy)[row * a.dy_stride + from]);
+    dgain += dy * ((x - a.mean[row]) * a.rstd[row]);
+    dbias += dy;
+  }
+  part[0][slice][lane] = dgain;
+  part[1][slice][lane] = dbias;
+  __syncthreads();
+  if (threadIdx.x < 2 * kDirectCols) {
+    const int which = threadIdx.x / kDirectCols;
+    float *out = which ? a.dbias : a.dgain;
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kSlices; ++i) sum += part[which][i][lane];
+    if (out && col < a.cols) out[col] = float(sum);
+  }
+}
+
 // One row after the other as above; the column sums of a workgroup's rows stay in registers and go out once, to its place in
 // the workspace, where norm_columns_kernel adds up the workgroups'.  No atomics: the order of the sums is fixed.
 template <typename WT, int LANES, int C, bool RAGGED>
@@ -185,6 +215,10 @@ __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock2)) void norm_backward_
   using S = Shape<WT, LANES, C>;
   constexpr int V = S::V;
   __shared__ float place[2][2 * S::kBlock2 / kWave];
+  if (int(blockIdx.x) >= a.blocks) {
+    direct_columns<WT, S::kBlock2>(a, blockIdx.x - a.blocks);
+    return;
+  }
   const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
   int turn = 0;
   float gain[C][V], dgain[C][V], dbias[C][V];
@@ -194,7 +228,7 @@ __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock2)) void norm_backward_
 #pragma unroll
     for (int i = 0; i < V; ++i) dgain[c][i] = dbias[c][i] = 0.0f;
   }
-  const int64_t step = int64_t(gridDim.x) * S::kRows2;
+  const int64_t step = int64_t(a.blocks) * S::kRows2;
   Run<WT, V> next_x[C], next_dy[C];
   float next_mean, next_rstd;
   auto fetch = [&](int64_t row) {
@@ -345,16 +379,21 @@ hipError_t forward(hipStream_t stream, NormForwardArgs &a) {
   });
 }
 
+// Few rows: the column sums are formed beside dx, from dy and x once more, which then come out of a cache.  Measured in us, beside dx /
+// in a launch of its own, bf16: 16 x 512 2.3 / 4.8, 256 x 512 2.8 / 5.2, 512 x 2048 6.0 / 8.8, 512 x 8192 18.4 / 18.8, 1024 x 64 4.2 / 5.7,
+// 1024 x 2048 9.8 / 13.2, 1024 x 8192 32 / 20, 2048 x 64 6.4 / 5.7, 2048 x 512 12.0 / 6.1.
+bool columns_beside(int64_t rows, int cols) { return rows <= 1024 && rows * cols <= (4 << 20); }
+
 template <typename WT>
 hipError_t backward(hipStream_t stream, NormBackwardArgs &a) {
+  const bool direct = (a.dgain || a.dbias) && !a.partial;
   return with_shape<WT>(a.cols, [&](auto shape) {
     using S = decltype(shape);
     a.blocks = blocks_for(a.rows, S::kRows2, kBackwardWaves * kWave / S::kBlock2);
-    if (a.blocks) {
-      const hipError_t e = a.cols % S::V ? launch(norm_backward_kernel<WT, S::kLanes, S::kChunks, true>, a.blocks, S::kBlock2, stream, a)
-                                         : launch(norm_backward_kernel<WT, S::kLanes, S::kChunks, false>, a.blocks, S::kBlock2, stream, a);
-      if (e != hipSuccess) return e;
-    }
+    const unsigned grid = a.blocks + (direct ? (a.cols + kDirectCols - 1) / kDirectCols : 0);
+    const hipError_t e = a.cols % S::V ? launch(norm_backward_kernel<WT, S::kLanes, S::kChunks, true>, grid, S::kBlock2, stream, a)
+                                       : launch(norm_backward_kernel<WT, S::kLanes, S::kChunks, false>, grid, S::kBlock2, stream, a);
+    if (e != hipSuccess) return e;
     if (!a.partial) return hipSuccess;
     return launch(norm_columns_kernel, (2 * a.ld + 31) / 32, 32 * kSlices, stream, a);
   });
@@ -392,6 +431,7 @@ extern "C" int moe_spec_layernorm_forward(void *stream, int dtype, const void *x
 
 extern "C" size_t moe_spec_layernorm_backward_workspace_bytes(int64_t rows, int cols) {
   if (rows < 0 || rows > MOE_SPEC_TRAIN_MAX_ROWS || cols < 1 || cols > MOE_SPEC_TRAIN_MAX_COLS) return 0;
+  if (columns_beside(rows, cols)) return 0;
   return size_t(blocks_for(rows, 1, kMaxBlocks)) * 2 * padded(cols) * sizeof(float);
 }
 
@@ -423,7 +463,7 @@ extern "C" int moe_spec_layernorm_backward(void *stream, int dtype, const void *
   NormBackwardArgs a = {dy, x, mean, rstd, gain, dx, dgain, dbias, nullptr, dy_stride, x_stride, dx_stride, rows, cols,
                         padded(cols), 0, 1.0f / float(cols)};
   if (columns) {
-    a.partial = static_cast<float *>(workspace);
+    if (need) a.partial = static_cast<float *>(workspace);
     if (rows == 0) {                    // nothing to add up: the column kernel writes zeros
       const hipError_t e = launch(norm_columns_kernel, (2 * a.ld + 31) / 32, 32 * kSlices, s, a);
       return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "layernorm_backward: %s", hipGetErrorString(e));

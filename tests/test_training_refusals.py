@@ -40,9 +40,9 @@ def test_no_rows_need_no_pointers():
 
 
 def ln_backward(**kw):
-    a = dict(stream=None, dtype=M.F32, dy=ADDR, dy_stride=64, x=ADDR * 2, x_stride=64, rows=4, cols=64, mean=ADDR, rstd=ADDR,
+    a = dict(stream=None, dtype=M.F32, dy=ADDR, dy_stride=64, x=ADDR * 2, x_stride=64, rows=4000, cols=64, mean=ADDR, rstd=ADDR,
              gain=ADDR, dx=ADDR * 3, dx_stride=64, dgain=ADDR, dbias=ADDR, workspace=ADDR,
-             workspace_bytes=M.moe_spec_layernorm_backward_workspace_bytes(4, 64))
+             workspace_bytes=M.moe_spec_layernorm_backward_workspace_bytes(4000, 64))
     a.update(kw)
     return M.lib().moe_spec_layernorm_backward(*a.values())
 
@@ -63,7 +63,7 @@ def test_layernorm_backward_asked_for_nothing_does_nothing():
 def test_workspace_sizes():
     size = M.moe_spec_layernorm_backward_workspace_bytes
     assert size(-1, 64) == size(4, 0) == size(4, 8193) == size(1 << 31, 64) == 0
-    assert size(0, 64) == 0 < size(1, 64) <= size(100, 64) <= size(100, 65)
+    assert size(0, 64) == size(100, 64) == 0 < size(2000, 64) <= size(4000, 64) <= size(4000, 65)       # few rows need none
     assert M.moe_spec_distill_loss_workspace_bytes(4, 257) == M.moe_spec_distill_loss_workspace_bytes(-1, 8) == 0
     assert M.moe_spec_balance_loss_workspace_bytes(4, 8, 17) == M.moe_spec_balance_loss_workspace_bytes(4, 8, 0) == 0
     assert M.moe_spec_balance_loss_workspace_bytes(100000, 256, 16) > M.moe_spec_distill_loss_workspace_bytes(100000, 256) > 0
