@@ -90,7 +90,7 @@ int moe_spec_balance_loss(void *stream, int dtype, const void *logits, int64_t l
  * float_with_bits(code << 20 or code << 19) * 2^(X - 14).  The largest has exponent field 14; the last code (127 / 255) is
  * NaN and stands for infinities too.  A second moment that is not zero is never stored as zero.
  * Codes are rounded up or down at random, without bias, by 16 bits each from a mix of seed, t, the tensor's place in the
- * call and the element's in the tensor.  To nearest would not do: with beta2 = 0.999 a step moves v by about a thousandth,
+ * call and the lower 32 bits of the element's in the tensor.  To nearest would not do: with beta2 = 0.999 a step moves v by about a thousandth,
  * half a step of the code is 1.6 to 3 %, and v would stand still.  The price is noise: a step that moves v by d < h, h the
  * code's step, does so with variance d h, so at beta2 = 0.999 and normally distributed gradients v wanders about its 32-bit
  * value with a relative standard deviation of about 0.15 (0.07 for the square root, which divides); m with one of 0.09
@@ -110,14 +110,14 @@ typedef struct {
 typedef struct {
   double lr, beta1, beta2, eps, weight_decay, grad_scale;
   int64_t step;                   /* t >= 1, unless step_dev is given */
-  const int64_t *step_dev;        /* dev, or NULL: where the kernels read t, for captured graphs (the caller advances it) */
+  const int64_t *step_dev;        /* dev, or NULL: where the kernels read t (below 1: 1), for captured graphs; the caller advances it */
   const float *grad_scale_dev;    /* dev, or NULL: a second factor of the gradients (a clipping factor, a loss scale) */
   uint32_t seed;
   int32_t grad_dtype;             /* MOE_SPEC_F32 | MOE_SPEC_BF16 */
   int32_t moments;                /* MOE_SPEC_MOMENTS_* */
 } moe_spec_adamw_config;
 
-/* tensors: host [n_tensors], read before the call returns. */
+/* tensors: host [n_tensors], read before the call returns; no two of them may share memory that is updated. */
 int moe_spec_adamw_step(void *stream, const moe_spec_adamw_tensor *tensors, int n_tensors, const moe_spec_adamw_config *cfg);
 
 /* The values of 8-bit moments (p, grad and copy are not looked at): m_out[i], v_out[i] dev [n] in out_dtype (bfloat16 holds

@@ -233,7 +233,7 @@ __global__ __launch_bounds__(kAdamBlock) __attribute__((amdgpu_waves_per_eu(EIGH
   AdamConsts c = a.c;
   if (a.step_dev) {                     // what depends on the step, by one thread
     if (threadIdx.x == 0) {
-      const int64_t step = *a.step_dev;
+      const int64_t step = *a.step_dev > 1 ? *a.step_dev : 1;
       c.alpha = float(a.lr / (1.0 - power(a.beta1, step)));
       c.root_scale = float(1.0 / sqrt(1.0 - power(a.beta2, step)));
       c.key = mix(a.seed + kOdd1 * uint32_t(step));

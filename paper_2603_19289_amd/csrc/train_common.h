@@ -49,7 +49,8 @@ inline const char *matrix_fault(const void *p, int64_t stride, int64_t rows, int
   if (rows == 0) return nullptr;
   if (!p) return "is null";
   if (misaligned(p, elem)) return "is not aligned to its elements";
-  if (stride < (output ? cols : 0) && rows > 1) return output ? "has a row stride below its row length" : "has a negative row stride";
+  if (rows == 1) return nullptr;
+  if (stride < (output ? cols : 0)) return output ? "has a row stride below its row length" : "has a negative row stride";
   if (stride > (int64_t(1) << 31)) return "has a row stride above 2^31";
   return nullptr;
 }

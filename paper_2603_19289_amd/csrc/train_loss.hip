@@ -22,6 +22,7 @@ namespace {
 constexpr int kLossBlock = 256, kLossBlocks = 1536, kVals = 8, kFinishBlock = 512;
 constexpr int kCountBlock = 1024, kCountBlocks = 64;
 constexpr int kOneBlock = 1024, kOneBlockRounds = 2;     // rows that one workgroup deals with in so many rounds: one launch
+constexpr float kLog2E = 1.442695040888963f, kLn2 = 0.693147180559945f;
 
 struct LossArgs {
   const void *z, *teacher;              // z: the student's logits, or the router's
@@ -47,7 +48,8 @@ struct Max { __device__ __forceinline__ float operator()(float a, float b) const
 
 // Adds the choices of the valid rows from `row` on, `step` apart, to hist, and the number of those rows to hist[bins].  A thread
 // takes two rows at a time, whose loads go out together: without a condition (behind the end: the last row's), so that none is
-// waited for before the others are out.
+// waited for before the others are out.  (Loads behind conditions: 10.7 us for 131072 rows x 8 choices, these 6.7.  What it takes
+// goes down with the workgroups, 3 us less for 64 of them than for 32, and what the loss kernel takes to add theirs up goes up.)
 template <int UNITS>                    // four choices each
 __device__ __forceinline__ int count_rows(const LossArgs &a, int64_t row, int64_t step, int *hist) {
   constexpr int kAhead = 2;
@@ -236,7 +238,6 @@ __global__ __launch_bounds__(BLOCK) void loss_kernel(const LossArgs a) {
           grad[i] = nothing ? 0.0f : (grad[i] * inv_z - p[i]) * scale;
         }
         cross = group_sum<G>(cross);
-        constexpr float kLn2 = 0.693147180559945f;
         result = cross * a.inv_tau + kLn2 * ((empty ? 0.0f : __builtin_amdgcn_logf(sum_z)) - __builtin_amdgcn_logf(sum_t));
         if (nothing) result = 0.0f;
       } else {
@@ -371,8 +372,9 @@ extern "C" int moe_spec_distill_loss(void *stream, int student_dtype, const void
                                      int64_t grad_stride, void *workspace, size_t workspace_bytes) {
   if (!known_type(student_dtype) || !known_type(teacher_dtype)) return train_fail(MOE_SPEC_EINVAL, "distill_loss: unknown dtype");
   if (!sizes_fit(rows, n_experts)) return train_fail(MOE_SPEC_EINVAL, "distill_loss: rows or n_experts out of range");
-  if (!(temperature > 0.0f) || !(1.0f / temperature > 0.0f) || !(1.0f / temperature < INFINITY))
-    return train_fail(MOE_SPEC_EINVAL, "distill_loss: temperature must be positive and finite, and so its reciprocal");
+  const float to_log2 = kLog2E / temperature;
+  if (!(temperature > 0.0f) || !(1.0f / temperature > 0.0f) || !(to_log2 < INFINITY))
+    return train_fail(MOE_SPEC_EINVAL, "distill_loss: temperature must be positive and finite, and so 1.5 times its reciprocal");
   if (const char *why = matrix_fault(student, student_stride, rows, n_experts, size_of(student_dtype), false))
     return train_fail(MOE_SPEC_EINVAL, "distill_loss: student %s", why);
   if (const char *why = matrix_fault(teacher, teacher_stride, rows, n_experts, size_of(teacher_dtype), false))
@@ -389,7 +391,7 @@ extern "C" int moe_spec_distill_loss(void *stream, int student_dtype, const void
   LossArgs a = {};
   a.z = student; a.teacher = teacher; a.grad = grad; a.valid = valid; a.loss = loss;
   a.z_stride = student_stride; a.teacher_stride = teacher_stride; a.grad_stride = grad_stride; a.rows = rows;
-  a.experts = n_experts; a.inv_tau = 1.0f / temperature; a.to_log2 = 1.442695040888963f / temperature;
+  a.experts = n_experts; a.inv_tau = 1.0f / temperature; a.to_log2 = to_log2;
   a.partial = static_cast<double *>(workspace);
   if (workspace) a.counted = reinterpret_cast<int *>(static_cast<char *>(workspace) + partial_bytes());
   hipError_t e;
@@ -408,7 +410,7 @@ extern "C" int moe_spec_balance_loss(void *stream, int dtype, const void *logits
   if (!sizes_fit(rows, n_experts)) return train_fail(MOE_SPEC_EINVAL, "balance_loss: rows or n_experts out of range");
   if (top_k < 1 || top_k > MOE_SPEC_MAX_TOP_K || rows * top_k > INT32_MAX)
     return train_fail(MOE_SPEC_EINVAL, "balance_loss: top_k must be 1 to %d and rows * top_k below 2^31", MOE_SPEC_MAX_TOP_K);
-  if (!(coef == coef)) return train_fail(MOE_SPEC_EINVAL, "balance_loss: coef is no number");
+  if (!(fabsf(coef) < INFINITY)) return train_fail(MOE_SPEC_EINVAL, "balance_loss: coef is not finite");
   if (const char *why = matrix_fault(logits, logits_stride, rows, n_experts, size_of(dtype), false))
     return train_fail(MOE_SPEC_EINVAL, "balance_loss: logits %s", why);
   if (const char *why = matrix_fault(ids, ids_stride, rows, top_k, 4, false)) return train_fail(MOE_SPEC_EINVAL, "balance_loss: ids %s", why);
@@ -424,7 +426,7 @@ extern "C" int moe_spec_balance_loss(void *stream, int dtype, const void *logits
   LossArgs a = {};
   a.z = logits; a.grad = grad; a.valid = valid; a.ids = ids; a.loss = loss; a.counts = counts;
   a.z_stride = logits_stride; a.grad_stride = grad_stride; a.ids_stride = ids_stride; a.rows = rows;
-  a.experts = a.bins = n_experts; a.top_k = top_k; a.coef = coef; a.inv_tau = 1.0f; a.to_log2 = 1.442695040888963f;
+  a.experts = a.bins = n_experts; a.top_k = top_k; a.coef = coef; a.inv_tau = 1.0f; a.to_log2 = kLog2E;
   a.partial = static_cast<double *>(workspace);
   if (workspace) a.counted = reinterpret_cast<int *>(static_cast<char *>(workspace) + partial_bytes());
   const hipError_t e = dtype == MOE_SPEC_BF16 ? run_loss<uint16_t, void>(s, a) : run_loss<float, void>(s, a);

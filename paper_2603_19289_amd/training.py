@@ -3,7 +3,7 @@ include/moe_spec_train.h.  Torch supplies memory and streams; the operators are 
 
 Every function queues its kernels on the current stream of its tensors' device and returns tensors that are valid in that
 stream's order.  Gradients are results of explicit calls (a loss returns its own, `layernorm_backward` takes one): nothing here
-records or reads an autograd graph.  All calls can be captured into a graph."""
+records or reads an autograd graph.  The functions and AdamW's calls can be captured into a graph."""
 from __future__ import annotations
 
 import ctypes as C
@@ -298,10 +298,10 @@ class EstimatorTrainer:
         """Losses and gradients for the predicting signals [n, T, H] of n different layers and the logits [n, T, E] that the
         next layers' routers gave -> (dict of loss, balance, counts; dict of gradients).  ids: the experts that these
         routers chose, int32 [n, T, k], for the balance loss and the counts.  valid: [n, T], 0 for padding."""
-        n, tokens, hidden = signal.shape
-        if len(set(layers)) != n or len(layers) != n:
-            raise ValueError("a layer of its own for each of the signals is needed")
+        n, tokens, _ = signal.shape
         w = self.weights
+        if len(set(layers)) != n or len(layers) != n or not all(0 <= l < w["layer_emb"].shape[0] for l in layers):
+            raise ValueError("a layer of its own for each of the signals is needed")
         flat = lambda t: None if t is None else t.reshape(n * tokens, *t.shape[2:])  # noqa: E731
         at = torch.as_tensor(list(layers), device=signal.device)
         x = flat(signal).to(self.dtype)

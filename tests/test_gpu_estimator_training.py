@@ -66,6 +66,9 @@ def test_gradients_equal_those_of_a_64_bit_reverse_pass(dtype):
         off = (grads[k].cpu().double() - want[k]).abs().max() / want[k].abs().max()
         assert off < tol, (k, off)
     assert not grads["layer_emb"][[1, 4]].any()
+    for bad in ([0, 0, 1], [0, 1], [0, 1, 5], [0, 1, -1]):                   # refused before anything is looked up
+        with pytest.raises(ValueError):
+            trainer.gradients(bad, signal.cuda(), teacher.cuda(), ids.cuda(), valid.cuda())
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -407,11 +407,11 @@ def mix(x):
     return x ^ (x >> 16)
 
 
-def noise(seed, step, place, n):
-    """32 random bits for each element of the tensor at a place of the call."""
+def noise(seed, step, place, n, first=0):
+    """32 random bits for n elements, from `first` on, of the tensor at a place of the call."""
     key1 = mix(mix(seed + ODD1 * step) + ODD2 * (place + 1))
     key2 = mix(key1 ^ ODD1)
-    x = (np.arange(n, dtype=np.uint64) + np.uint64(key1)) & np.uint64(0xffffffff)
+    x = (np.arange(first, first + n, dtype=np.uint64) + np.uint64(key1)) & np.uint64(0xffffffff)
     x = ((x ^ (x >> np.uint64(16))) * np.uint64(ODD1)) & np.uint64(0xffffffff)
     x = (((x ^ (x >> np.uint64(15))) + np.uint64(key2)) * np.uint64(ODD2)) & np.uint64(0xffffffff)
     return (x ^ (x >> np.uint64(16))).astype(np.uint32)
@@ -641,6 +641,66 @@ def test_adamw_odd_addresses_and_missing_gradients():
         T.AdamW([dev[0], dev[0]], lr=1e-3)
     with pytest.raises(ValueError):
         T.AdamW([dev[0]], lr=1e-3, states=dict(m=[dev[0]], v=[dev[1], dev[1]]))
+
+
+def test_adamw_step_number_and_scale_on_the_gpu():
+    """From tensors as from numbers, bit for bit; a step number below 1 is 1."""
+    from paper_2603_19289_amd import training as T
+    params, grads = adam_case([700], 3, "f32")
+    results = []
+    for number, scale in ((7, 0.5), (torch.tensor([7], device="cuda"), torch.tensor([0.5], device="cuda")), (1, 0.5), (torch.tensor([-3], device="cuda"), 0.5)):
+        p = on_gpu(params[0])
+        opt = T.AdamW([p], lr=1e-3, state="f8", seed=2)
+        opt.step([on_gpu(grads[0][0])], step=number, grad_scale=scale)
+        results.append([p, *(t[0] for t in opt.states().values())])
+    for a, b in ((0, 1), (2, 3)):
+        assert all(torch.equal(x, y) for x, y in zip(results[a], results[b]))
+    assert not torch.equal(results[0][1], results[2][1])
+
+
+# ------------------------------------------------------------------------------------------------ far apart
+def test_rows_that_are_far_apart():
+    """Element offsets beyond 2^31 and byte offsets beyond 2^32: views of a large buffer against the same rows close together."""
+    from paper_2603_19289_amd import training as T
+    rows, stride = 4, 1 << 30
+    far = torch.empty(3 * stride + 4096, dtype=torch.bfloat16, device="cuda")
+    views = [far.as_strided((rows, 700), (stride, 1), at) for at in (1, 1001, 2003)]
+    x, dy, gain, bias = (on_gpu(t) for t in ln_inputs(rows, 700, "bf16", 12))
+    views[0].copy_(x), views[1].copy_(dy)
+    y, mean, rstd = T.layernorm_forward(views[0], gain, bias, out=views[2])
+    want = T.layernorm_forward(x, gain, bias)
+    assert torch.equal(y, want[0]) and torch.equal(mean, want[1]) and torch.equal(rstd, want[2])
+    for a, b in zip(T.layernorm_backward(views[1], views[0], mean, rstd, gain), T.layernorm_backward(dy, x, mean, rstd, gain)):
+        assert torch.equal(a, b)
+    t, s, _, _ = logits(rows, 40, 12)
+    t, s = on_gpu(t, torch.bfloat16), on_gpu(s, torch.bfloat16)
+    vt, vs = views[0][:, :40], views[1][:, :40]
+    vt.copy_(t), vs.copy_(s)
+    for a, b in zip(T.distill_loss(vs, vt), T.distill_loss(s, t)):
+        assert torch.equal(a, b)
+    ids = far.view(torch.int32).as_strided((rows, 3), (stride // 2, 1), 1800)
+    ids.copy_(torch.tensor([[0, 1, 2], [3, 39, 5], [7, 7, 8], [9, 10, 0]], dtype=torch.int32))
+    for a, b in zip(T.balance_loss(vs, ids), T.balance_loss(s, ids.contiguous())):
+        assert torch.equal(a, b)
+
+
+def test_adamw_tensor_of_more_than_2_to_the_31_elements():
+    """The last elements of a long tensor, 8-bit moments: by the written formulas with their own places in the random numbers."""
+    from paper_2603_19289_amd import training as T
+    n, tail = (1 << 31) + 4096 + 5, 128 * 3 + 5
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    end = torch.randn(tail, generator=rng(1)).to(torch.bfloat16)
+    g[-tail:] = on_gpu(end)
+    opt = T.AdamW([p], lr=1e-3, state="f8", seed=21)
+    opt.step([g])
+    zero = np.zeros(tail, F)
+    q, m, v = adam_float(zero, end.float().numpy(), zero, zero, 1e-3, 0.9, 0.999, 1e-8, 0.01, 1)
+    r = noise(21, 1, 0, tail, first=n - tail)
+    held = opt.states()
+    for key, x, drop, bits in (("m", m, 20, r >> 16), ("v", v, 19, r & 0xffff)):
+        code, exponent = encode(x, drop, bits)
+        assert np.array_equal(held[key][0][-tail:].cpu().numpy(), code) and np.array_equal(held[key + "_exp"][0][-4:].cpu().numpy(), exponent)
+    assert np.array_equal(p[-tail:].cpu().numpy(), q) and not p[:n - tail].any() and not held["m"][0][:n - tail].any()
 
 
 # ------------------------------------------------------------------------------------------------ together

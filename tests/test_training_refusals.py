@@ -81,7 +81,7 @@ def distill(**kw):
 @pytest.mark.parametrize("bad,word", [(dict(student_dtype=3), "dtype"), (dict(teacher_dtype=-1), "dtype"), (dict(rows=-1), "rows"),
                                       (dict(n_experts=0), "n_experts"), (dict(n_experts=257), "n_experts"), (dict(temperature=0.0), "temperature"),
                                       (dict(temperature=-1.0), "temperature"), (dict(temperature=float("inf")), "temperature"),
-                                      (dict(temperature=float("nan")), "temperature"), (dict(temperature=1e-45), "temperature"),
+                                      (dict(temperature=float("nan")), "temperature"), (dict(temperature=1e-45), "temperature"), (dict(temperature=3.5e-39), "temperature"),
                                       (dict(student=None), "student is null"), (dict(teacher=ADDR + 1), "teacher is not aligned"),
                                       (dict(grad_stride=31), "grad"), (dict(grad=ADDR, grad_stride=64), "another stride"),
                                       (dict(grad=ADDR * 2), "teacher"), (dict(loss=None), "loss"), (dict(workspace=None), "workspace"),
@@ -98,7 +98,7 @@ def balance(**kw):
 
 
 @pytest.mark.parametrize("bad,word", [(dict(dtype=2), "dtype"), (dict(rows=-1), "rows"), (dict(n_experts=300), "n_experts"), (dict(top_k=0), "top_k"),
-                                      (dict(top_k=17), "top_k"), (dict(rows=(1 << 31) // 4), "rows * top_k"), (dict(coef=float("nan")), "coef"),
+                                      (dict(top_k=17), "top_k"), (dict(rows=(1 << 31) // 4), "rows * top_k"), (dict(coef=float("nan")), "coef"), (dict(coef=float("inf")), "coef"),
                                       (dict(logits=None), "logits is null"), (dict(ids=None), "ids is null"), (dict(ids=ADDR + 2), "ids is not aligned"),
                                       (dict(grad=ADDR, grad_stride=40), "another stride"), (dict(counts=None), "counts"), (dict(loss=ADDR + 1), "loss"),
                                       (dict(workspace_bytes=64), "workspace")])
@@ -153,3 +153,13 @@ def test_torch_layer_refuses_tensors_it_does_not_take():
         T.AdamW([], lr=1e-3)
     with pytest.raises(ValueError):
         T.AdamW([x], lr=1e-3, state="int4")
+
+
+def test_the_header_is_c():
+    """The declarations compile as C99 by themselves."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-fsyntax-only", "-x", "c", os.path.join(root, "include", "moe_spec_train.h")],
+                          capture_output=True, text=True)
+    assert done.returncode == 0, done.stderr
