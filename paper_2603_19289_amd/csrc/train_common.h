@@ -98,6 +98,18 @@ struct Run {
       }
     }
   }
+  // All N of them, or `fill` where there are none: nothing that is loaded is looked at here.
+  __device__ __forceinline__ void load_if(bool there, const WT *p, WT fill) {
+    WT e[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) e[i] = fill;
+#pragma unroll
+    for (int r = 0; r < R; ++r) __builtin_memcpy(&raw[r], e, sizeof(Raw));
+    if (there) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) raw[r] = load_raw<Raw>(p + r * V);
+    }
+  }
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int r = 0; r < R; ++r) raw[r] = Raw{};

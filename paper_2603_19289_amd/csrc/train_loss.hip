@@ -133,18 +133,27 @@ __global__ __launch_bounds__(BLOCK) void loss_kernel(const LossArgs a) {
   }
   Run<ST, kVals> next_z;
   Run<Teacher, kVals> next_t;
-  const int64_t step = int64_t(gridDim.x) * kRows;
+  const int64_t step = int64_t(gridDim.x) * kRows, row0 = int64_t(blockIdx.x) * kRows + slot;
+  const ST *from_z = static_cast<const ST *>(a.z) + row0 * a.z_stride + col;
+  const Teacher *from_t = static_cast<const Teacher *>(a.teacher) + row0 * a.teacher_stride + col;
+  ST *to = static_cast<ST *>(a.grad) + row0 * a.grad_stride + col;
   auto mask = [&](int64_t row) { return int(a.mask[(row < a.rows ? row : a.rows - 1) * a.mask_stride]); };
-  auto fetch = [&](int64_t row, bool live) {
-    const int here = live ? count : 0;                  // rows that do not count are not read
-    next_z.load(static_cast<const ST *>(a.z) + row * a.z_stride + col, here, lowest<ST>());
-    if constexpr (kDistill) next_t.load(static_cast<const Teacher *>(a.teacher) + row * a.teacher_stride + col, here, lowest<Teacher>());
+  auto fetch = [&](bool live) {         // the next of the rows, which lie a step apart
+    if (a.experts >= kVals) {           // eight values or, of rows that do not count, none
+      next_z.load_if(live && count, from_z, lowest<ST>());
+      if constexpr (kDistill) next_t.load_if(live && count, from_t, lowest<Teacher>());
+    } else {
+      next_z.load(from_z, live ? count : 0, lowest<ST>());
+      if constexpr (kDistill) next_t.load(from_t, live ? count : 0, lowest<Teacher>());
+    }
+    from_z += step * a.z_stride;
+    if constexpr (kDistill) from_t += step * a.teacher_stride;
   };
   double sum = 0.0;
-  int64_t row = int64_t(blockIdx.x) * kRows + slot;
+  int64_t row = row0;
   int ahead = mask(row + step);
   bool live = row < a.rows && (mask(row) || !a.valid);
-  fetch(row, live);
+  fetch(live);
 
   __shared__ int total[padded_bins(MOE_SPEC_MAX_EXPERTS)];
   const bool counting = a.bins || a.valid;
@@ -201,7 +210,7 @@ __global__ __launch_bounds__(BLOCK) void loss_kernel(const LossArgs a) {
     }
     const bool counts = live;
     live = row + step < a.rows && (ahead || !a.valid);
-    fetch(row + step, live);
+    fetch(live);
     ahead = mask(row + 2 * step);
 #pragma unroll
     for (int i = 0; i < kVals; ++i) grad[i] = 0.0f;
@@ -228,18 +237,21 @@ __global__ __launch_bounds__(BLOCK) void loss_kernel(const LossArgs a) {
         }
         sum_z = group_sum<G>(sum_z);
         sum_t = group_sum<G>(sum_t);
-        const bool nothing = sum_t == 0.0f || !counts;                     // the teacher's row is masked out whole
-        const bool empty = sum_z == 0.0f;                                  // the student's is
-        const float inv_z = nothing || empty ? 0.0f : __builtin_amdgcn_rcpf(sum_z), inv_t = nothing ? 0.0f : __builtin_amdgcn_rcpf(sum_t);
+        const bool empty = sum_z == 0.0f;                                  // the student's row is masked out whole
+        const float inv_t = sum_t == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum_t), over_z = empty ? 0.0f : __builtin_amdgcn_rcpf(sum_z) * scale;
 #pragma unroll
         for (int i = 0; i < kVals; ++i) {
           p[i] *= inv_t;
           cross += p[i] == 0.0f ? 0.0f : p[i] * (t[i] - z[i]);             // 0 log 0 = 0
-          grad[i] = nothing ? 0.0f : (grad[i] * inv_z - p[i]) * scale;
+          grad[i] = grad[i] * over_z - p[i] * scale;
         }
         cross = group_sum<G>(cross);
         result = cross * a.inv_tau + kLn2 * ((empty ? 0.0f : __builtin_amdgcn_logf(sum_z)) - __builtin_amdgcn_logf(sum_t));
-        if (nothing) result = 0.0f;
+        if (sum_t == 0.0f || !counts) {                                    // nothing to teach, the teacher's row is masked out whole
+          result = 0.0f;
+#pragma unroll
+          for (int i = 0; i < kVals; ++i) grad[i] = 0.0f;
+        }
       } else {
         float top = -INFINITY;
 #pragma unroll
@@ -255,16 +267,14 @@ __global__ __launch_bounds__(BLOCK) void loss_kernel(const LossArgs a) {
         }
         total_e = group_sum<G>(total_e);
         inner = group_sum<G>(inner);
-        const bool nothing = total_e == 0.0f || !counts;
-        const float inv = nothing ? 0.0f : __builtin_amdgcn_rcpf(total_e);
-        result = nothing ? 0.0f : inner * inv;
+        const float inv = total_e == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(total_e), over = inv * scale;
+        result = inner * inv;           // a row that does not count holds minus infinities: zeros from here on
 #pragma unroll
-        for (int i = 0; i < kVals; ++i) grad[i] = nothing ? 0.0f : z[i] * inv * (f[i] - result) * scale;
+        for (int i = 0; i < kVals; ++i) grad[i] = z[i] * ((f[i] - result) * over);
       }
       if (lane == 0) sum += double(result);
     }
     if (a.grad && row < a.rows && count) {
-      ST *to = static_cast<ST *>(a.grad) + row * a.grad_stride + col;
       if (!skip) {
         store_run<ST, kVals>(to, grad, count);
       } else {
@@ -272,6 +282,7 @@ __global__ __launch_bounds__(BLOCK) void loss_kernel(const LossArgs a) {
         for (int i = 1; i < kVals; ++i) if (i >= skip) to[i] = from_float<ST>(grad[i]);
       }
     }
+    to += step * a.grad_stride;
   }
   sum = block_sum<BLOCK>(sum) * double(kDistill ? share : scale);
   if (threadIdx.x == 0) {
