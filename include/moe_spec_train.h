@@ -121,7 +121,7 @@ typedef struct {
 int moe_spec_adamw_step(void *stream, const moe_spec_adamw_tensor *tensors, int n_tensors, const moe_spec_adamw_config *cfg);
 
 /* The values of 8-bit moments (p, grad and copy are not looked at): m_out[i], v_out[i] dev [n] in out_dtype (bfloat16 holds
- * them exactly), host arrays of n_tensors pointers; either array may be NULL. */
+ * all from 2^-120 on exactly), host arrays of n_tensors pointers; either array may be NULL. */
 int moe_spec_adamw_read_moments(void *stream, const moe_spec_adamw_tensor *tensors, int n_tensors, int out_dtype,
                                 void *const *m_out, void *const *v_out);
 

@@ -177,6 +177,7 @@ class AdamW:
             raise ValueError("a tensor is named twice")
         self._held, self._at = [t for t in (*self.params, *self.copies) if t is not None], None
         self._desc = (M.AdamWTensor * len(self.params))()
+        self._entries = list(self._desc)                       # views of the table's entries
         self._config = M.AdamWConfig(seed=self.seed, moments=M.MOMENTS_8BIT if eight else M.MOMENTS_32BIT)
         self._describe()
 
@@ -194,7 +195,7 @@ class AdamW:
         if at == self._at:
             return
         s = self._states
-        for i, (d, p) in enumerate(zip(self._desc, self.params)):
+        for i, (d, p) in enumerate(zip(self._entries, self.params)):
             d.p, d.m, d.v = p.data_ptr(), s["m"][i].data_ptr(), s["v"][i].data_ptr()
             if self.state == "f8":
                 d.m_exp, d.v_exp = s["m_exp"][i].data_ptr(), s["v_exp"][i].data_ptr()
@@ -218,12 +219,16 @@ class AdamW:
         read it from, which a captured graph needs.  grad_scale: a factor of the gradients, a number or a float32 tensor on the GPU."""
         if len(grads) != len(self.params):
             raise ValueError("as many gradients as parameters are needed")
-        dtype = next((g.dtype for g in grads if g is not None), torch.float32)
+        dtype = torch.float32
+        for g in grads:
+            if g is not None:
+                dtype = g.dtype
+                break
         if dtype not in _TYPES:
             raise ValueError("gradients must be float32 or bfloat16")
         self._describe()
         dev = self.device
-        for d, n, g in zip(self._desc, self._sizes, grads):
+        for d, n, g in zip(self._entries, self._sizes, grads):
             if g is None:
                 d.n = 0
                 continue
@@ -249,21 +254,24 @@ class AdamW:
             self.steps = c.step
 
     def read_moments(self, m_out: Optional[List[torch.Tensor]] = None, v_out: Optional[List[torch.Tensor]] = None):
-        """The values of 8-bit moments, into float32 or bfloat16 tensors (bfloat16 holds them exactly) or new float32 ones
-        -> (m, v)."""
+        """The values of 8-bit moments, into float32 or bfloat16 tensors (which hold all of them from 2^-120 on exactly) or new
+        float32 ones -> (m, v)."""
         if self.state != "f8":
             raise ValueError("32-bit moments are tensors of their own: states()")
         if m_out is None and v_out is None:
             m_out, v_out = ([torch.empty_like(p) for p in self.params] for _ in range(2))
-        given = [t for out in (m_out, v_out) if out is not None for t in out]
-        dtype = given[0].dtype
-        if dtype not in _TYPES or any(out is not None and len(out) != len(self.params) for out in (m_out, v_out)):
-            raise ValueError("a float32 or bfloat16 tensor for each parameter is needed")
+        if any(out is not None and len(out) != len(self.params) for out in (m_out, v_out)):
+            raise ValueError("a tensor for each parameter is needed")
+        dtype = (m_out if m_out is not None else v_out)[0].dtype
+        if dtype not in _TYPES:
+            raise ValueError("moments are read as float32 or bfloat16")
+        dev = self.device
         for out in (m_out, v_out):
-            for t, p in zip(out or (), self.params):
-                self._tensor(t, "an output", dtype, p.numel())
+            for t, n in zip(out or (), self._sizes):
+                if t.dtype != dtype or t.numel() != n or t.device != dev or not t.is_contiguous():
+                    self._tensor(t, "an output", dtype, n)
         self._describe()
-        for d, n in zip(self._desc, self._sizes):
+        for d, n in zip(self._entries, self._sizes):
             d.n = n
         pointers = lambda out: None if out is None else (C.c_void_p * len(out))(*[t.data_ptr() for t in out])  # noqa: E731
         _queue(self.device, M.lib().moe_spec_adamw_read_moments, self._desc, len(self._desc), _TYPES[dtype], pointers(m_out), pointers(v_out))
