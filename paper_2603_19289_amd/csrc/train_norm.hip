@@ -299,8 +299,19 @@ __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock2)) void norm_backward_
       }
     }
   float *out = a.partial + size_t(blockIdx.x) * 2 * a.ld;
-  // then the rows of the workgroup, one of the two sums after the other
   constexpr int kParts = S::kBlock2 / (LANES < kWave ? kWave : LANES);
+  if constexpr (kParts == 1) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const Place<V, RAGGED> at(c * LANES + lane, a.cols);
+      if (at.used) {                    // ends within ld; a length below V leaves room for V
+        store_run<float, V>(out + at.col, dgain[c], V);
+        store_run<float, V>(out + a.ld + at.col, dbias[c], V);
+      }
+    }
+    return;
+  }
+  // then the rows of the workgroup, one of the two sums after the other
   __shared__ float sums[kParts][LANES * C * V];
   const int part = threadIdx.x / (LANES < kWave ? kWave : LANES);
 #pragma unroll
