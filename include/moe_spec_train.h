@@ -12,15 +12,15 @@
  *
  * Every call queues kernels on `stream` (a hipStream_t) and returns; it allocates nothing, waits for nothing and keeps no
  * state, so it can be captured into a HIP graph.  "dev" pointers are memory of the stream's device, which need not be the
- * current one.  Tensors are row-major: the last dimension is contiguous, rows are `*_stride` elements apart.  An output's
+ * current one (the null stream's is).  Tensors are row-major: the last dimension is contiguous, rows are `*_stride` elements apart.  An output's
  * stride is at least its row length; an input's may be anything from 0 (one row for all) on.  Pointers need the alignment of
  * their elements and no more.  Outputs must not overlap inputs, except where an in-place form is named.  The same inputs
  * give the same bits: no atomics on floating-point values.  Values are bfloat16 or float (MOE_SPEC_BF16, MOE_SPEC_F32);
  * statistics, sums and moments are held in float or wider, and what goes out as bfloat16 is rounded once, to nearest even.
  *
  * Calls that need scratch take a workspace (dev, 16-byte aligned) of at least the bytes that the matching function names (0 for
- * small sizes: NULL will do; also 0 for sizes that the call refuses);
- * nothing in it has to be set and nothing is kept in it, but two calls that may run at the same time need two.
+ * small sizes: NULL will do; also 0 for sizes that the call refuses).  Nothing in it has to be set and nothing is kept in it,
+ * but two calls, or replays of two graphs, that may run at the same time need two.
  *
  * Returns 0 (MOE_SPEC_OK), MOE_SPEC_EINVAL for arguments it refuses (nothing has been queued then) or MOE_SPEC_EHIP;
  * moe_spec_train_last_error gives the reason of the calling thread's last failure.  Nothing throws or aborts. */
@@ -90,7 +90,8 @@ int moe_spec_balance_loss(void *stream, int dtype, const void *logits, int64_t l
  * float_with_bits(code << 20 or code << 19) * 2^(X - 14).  The largest has exponent field 14; the last code (127 / 255) is
  * NaN and stands for infinities too.  A second moment that is not zero is never stored as zero.
  * Codes are rounded up or down at random, without bias, by 16 bits each from a mix of seed, t, the tensor's place in the
- * call and the lower 32 bits of the element's in the tensor.  To nearest would not do: with beta2 = 0.999 a step moves v by about a thousandth,
+ * call and the lower 32 bits of the element's in the tensor.
+ * To nearest would not do: with beta2 = 0.999 a step moves v by about a thousandth,
  * half a step of the code is 1.6 to 3 %, and v would stand still.  The price is noise: a step that moves v by d < h, h the
  * code's step, does so with variance d h, so at beta2 = 0.999 and normally distributed gradients v wanders about its 32-bit
  * value with a relative standard deviation of about 0.15 (0.07 for the square root, which divides); m with one of 0.09
@@ -110,7 +111,8 @@ typedef struct {
 typedef struct {
   double lr, beta1, beta2, eps, weight_decay, grad_scale;
   int64_t step;                   /* t >= 1, unless step_dev is given */
-  const int64_t *step_dev;        /* dev, or NULL: where the kernels read t (below 1: 1), for captured graphs; the caller advances it */
+  const int64_t *step_dev;        /* dev, or NULL: where the kernels read t (below 1: 1), for captured graphs; the caller
+                                     advances it */
   const float *grad_scale_dev;    /* dev, or NULL: a second factor of the gradients (a clipping factor, a loss scale) */
   uint32_t seed;
   int32_t grad_dtype;             /* MOE_SPEC_F32 | MOE_SPEC_BF16 */

@@ -19,9 +19,13 @@
 namespace moe_spec {
 namespace {
 
+// Workgroups: 131072 rows of 128 experts with 1024 / 1536 / 2048 / 4096 of them 27.7 / 27.4 / 28.9 / 30.5 us (distillation).
 constexpr int kLossBlock = 256, kLossBlocks = 1536, kVals = 8, kFinishBlock = 512;
 constexpr int kCountBlock = 1024, kCountBlocks = 64;
-constexpr int kOneBlock = 1024, kOneBlockRounds = 2;     // rows that one workgroup deals with in so many rounds: one launch
+// Rows that one workgroup deals with in so many rounds take one launch.  A round is some 2 us of one compute unit's arithmetic, the
+// two launches saved some 2.5 us each: 301 rows of 32 experts, two rounds 5.2 us, 200 rows of 128 experts, four rounds 12.3 us, in
+// launches 7.7.
+constexpr int kOneBlock = 1024, kOneBlockRounds = 2;
 constexpr float kLog2E = 1.442695040888963f, kLn2 = 0.693147180559945f;
 
 struct LossArgs {

@@ -2,7 +2,7 @@
 include/moe_spec_train.h.  Torch supplies memory and streams; the operators are the library's kernels.
 
 Every function queues its kernels on the current stream of its tensors' device and returns tensors that are valid in that
-stream's order.  Gradients are results of explicit calls (a loss returns its own, `layernorm_backward` takes one): nothing here
+stream's order; tensors of another stream are the caller's to order and to keep, as with torch's own operations.  Gradients are results of explicit calls (a loss returns its own, `layernorm_backward` takes one): nothing here
 records or reads an autograd graph.  The functions and AdamW's calls can be captured into a graph."""
 from __future__ import annotations
 

@@ -163,3 +163,17 @@ def test_the_header_is_c():
     done = subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-fsyntax-only", "-x", "c", os.path.join(root, "include", "moe_spec_train.h")],
                           capture_output=True, text=True)
     assert done.returncode == 0, done.stderr
+
+
+def test_the_reason_of_a_failure_is_the_calling_threads():
+    import threading
+    refused(ln_forward(cols=0), "cols")
+    seen = []
+
+    def other():
+        seen.append(M.lib().moe_spec_train_last_error())
+        refused(distill(temperature=-1.0), "temperature")
+    t = threading.Thread(target=other)
+    t.start()
+    t.join()
+    assert seen == [b""] and b"cols" in M.lib().moe_spec_train_last_error()
