@@ -121,7 +121,7 @@ def test_layernorm_backward_against_differences():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("cols", [40, 720, 2880])
+@pytest.mark.parametrize("cols", [5, 40, 97, 720, 1023, 2049, 2880, 4101])
 def test_layernorm_strided_odd_and_in_place(cols, dtype):
     """Rows of a wider matrix that begin at odd elements, no gain or bias, one row for all, y over x; what lies between the rows
     and behind the last one stays."""
@@ -367,12 +367,12 @@ def test_losses_without_rows_or_valid_rows():
         assert loss.item() == 0.0 and not counts.any() and not grad.any()
 
 
-@pytest.mark.parametrize("experts", [30, 128])
-def test_losses_strided_odd_and_in_place(experts):
-    """Views of wider matrices at odd elements and odd mask addresses; the gradient over the student's logits (C entry)."""
+@pytest.mark.parametrize("rows", [333, 9000])
+@pytest.mark.parametrize("experts", [5, 30, 128])
+def test_losses_strided_odd_and_in_place(experts, rows):
+    """Views of wider matrices at odd elements and odd mask addresses; gradients over the logits themselves (C entries)."""
     from paper_2603_19289_amd import moe_spec as M
     from paper_2603_19289_amd import training as T
-    rows = 333
     t, s, valid, g = logits(rows, experts, 8)
     s = s.to(torch.bfloat16)
     ids = torch.rand(rows, experts, generator=g).topk(3, 1).indices.to(torch.int32)
@@ -388,10 +388,18 @@ def test_losses_strided_odd_and_in_place(experts):
     for a, b in zip(T.balance_loss(vs, vi, valid=vv), T.balance_loss(on_gpu(s), on_gpu(ids), valid=on_gpu(valid))):
         assert torch.equal(a, b)
     need = M.moe_spec_distill_loss_workspace_bytes(rows, experts)
-    space, loss = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty((), device="cuda")
+    space, loss = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda"), torch.empty((), device="cuda")
     M.moe_spec_distill_loss(torch.cuda.current_stream().cuda_stream, M.BF16, vs.data_ptr(), vs.stride(0), M.F32, vt.data_ptr(), vt.stride(0),
                             rows, experts, 1.0, vv.data_ptr(), loss.data_ptr(), vs.data_ptr(), vs.stride(0), space.data_ptr(), need)
     assert torch.equal(loss, plain[0]) and torch.equal(vs, plain[1])
+    vs.copy_(on_gpu(s))
+    want = T.balance_loss(vs, vi, valid=vv, coef=0.5)
+    need = M.moe_spec_balance_loss_workspace_bytes(rows, experts, 3)
+    space, counts = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda"), torch.empty(experts, dtype=torch.int32, device="cuda")
+    M.moe_spec_balance_loss(torch.cuda.current_stream().cuda_stream, M.BF16, vs.data_ptr(), vs.stride(0), rows, experts, vi.data_ptr(),
+                            vi.stride(0), 3, 0.5, vv.data_ptr(), loss.data_ptr(), counts.data_ptr(), vs.data_ptr(), vs.stride(0),
+                            space.data_ptr(), need)
+    assert torch.equal(loss, want[0]) and torch.equal(counts, want[1]) and torch.equal(vs, want[2])
     assert not wide_s[:, :3].any() and not wide_s[:, 3 + experts:].any()
 
 
