@@ -19,9 +19,10 @@
 namespace moe_spec {
 namespace {
 
-// Workgroups: 131072 rows of 128 experts with 1024 / 1536 / 2048 / 4096 of them 27.7 / 27.4 / 28.9 / 30.5 us (distillation).
-constexpr int kLossBlock = 256, kLossBlocks = 1536, kVals = 8, kFinishBlock = 512;
-constexpr int kCountBlock = 1024, kCountBlocks = 64;
+// Workgroups that walk over the rows, 24 wavefronts a compute unit: 131072 rows of 128 experts with 16 / 24 / 32 / 64 of them 27.7 / 27.4 /
+// 28.9 / 30.5 us (distillation).  512 threads rather than 256: half as many workgroups add up what was counted (balance 24.1 -> 23.3 us).
+constexpr int kLossBlock = 512, kLossBlocks = 768, kVals = 8, kFinishBlock = 256;
+constexpr int kCountBlock = 512, kCountBlocks = 128;
 // Rows that one workgroup deals with in so many rounds take one launch.  A round is some 2 us of one compute unit's arithmetic, the
 // two launches saved some 2.5 us each: 301 rows of 32 experts, two rounds 5.2 us, 200 rows of 128 experts, four rounds 12.3 us, in
 // launches 7.7.
@@ -52,8 +53,9 @@ struct Max { __device__ __forceinline__ float operator()(float a, float b) const
 
 // Adds the choices of the valid rows from `row` on, `step` apart, to hist, and the number of those rows to hist[bins].  A thread
 // takes two rows at a time, whose loads go out together: without a condition (behind the end: the last row's), so that none is
-// waited for before the others are out.  (Loads behind conditions: 10.7 us for 131072 rows x 8 choices, these 6.7.  What it takes
-// goes down with the workgroups, 3 us less for 64 of them than for 32, and what the loss kernel takes to add theirs up goes up.)
+// waited for before the others are out.  (Loads behind conditions: 10.7 us for 131072 rows x 8 choices, these 6.7.)  A compute unit
+// streams some 30 GB/s, so more workgroups count faster, and the loss kernel's add up what more of them left: the balance loss of
+// 131072 rows takes 27.9 us with 32 of 1024 threads, 23.3 with 64, 22.9 with 128, 22.4 with 128 of 512 threads, 22.6 with 256.
 template <int UNITS>                    // four choices each
 __device__ __forceinline__ int count_rows(const LossArgs &a, int64_t row, int64_t step, int *hist) {
   constexpr int kAhead = 2;
