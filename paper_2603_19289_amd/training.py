@@ -310,9 +310,14 @@ class EstimatorTrainer:
         w = self.weights
         if len(set(layers)) != n or len(layers) != n or not all(0 <= l < w["layer_emb"].shape[0] for l in layers):
             raise ValueError("a layer of its own for each of the signals is needed")
+        if any(t is not None and t.shape[:2] != (n, tokens) for t in (teacher, ids, valid)):
+            raise ValueError("teacher, ids and valid must have the layers and tokens of the signal")
         flat = lambda t: None if t is None else t.reshape(n * tokens, *t.shape[2:])  # noqa: E731
         at = torch.as_tensor(list(layers), device=signal.device)
-        x = flat(signal).to(self.dtype)
+        x, mask = flat(signal).to(self.dtype), flat(valid)
+        if mask is not None:                  # chosen, not multiplied: zero times what padding holds need not be zero in a product
+            _mask(mask, n * tokens, x.device)
+            x = x.masked_fill((mask == 0)[:, None], 0.0)
         u = (torch.mm(x, w["proj"].T).view(n, tokens, -1) + w["layer_emb"][at][:, None]).reshape(n * tokens, -1)
         h = torch.mm(u, w["ffn_in"].T)
         gate = torch.sigmoid(h)
@@ -320,7 +325,6 @@ class EstimatorTrainer:
         v = u + torch.mm(act, w["ffn_out"].T)
         y, mean, rstd = layernorm_forward(v, w["ln_gain"], w["ln_bias"], self.ln_eps)
         z = torch.mm(y, w["head"].T)
-        mask = flat(valid)
         loss, dz = distill_loss(z, flat(teacher), valid=mask)
         out = {"loss": loss}
         if ids is not None:

@@ -109,3 +109,29 @@ def test_an_engine_predicts_with_what_is_trained_in_its_memory(dtype, state):
         assert not np.array_equal(first, trace["trained"][0][1][1].exec_ids)     # training did change what is predicted
     finally:
         eng.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_padding_counts_for_nothing_whatever_it_holds(dtype):
+    """NaN, infinities and the type's largest values in the signal and the logits of rows that do not count: the bits of zeros there,
+    in the losses, in every gradient and in the tables after a step."""
+    from paper_2603_19289_amd import training as T
+    wl = small_workload(name="training", n_layers=5, hidden=264, n_experts=12, top_k=3, inter=200, dtype=dtype, batch=1, tokens=1, slots=6, seed=5)
+    est = W.make_estimator(wl, m=3, n=2)
+    signal, teacher, ids, valid = (t.cuda() for t in batch(wl, 3, 37, 1))
+    valid[1] = False                                      # a layer of padding only
+    want = None
+    for junk in (0.0, float("nan"), float("inf"), -float("inf"), torch.finfo(torch.float32).max):
+        trainer = T.EstimatorTrainer(est, balance_coef=0.1, state="f8")
+        fill = lambda t: torch.where(valid[..., None], t, torch.full_like(t, junk))  # noqa: E731
+        for mask in (valid, valid.to(torch.uint8)):
+            out, grads = trainer.gradients([3, 0, 2], fill(signal), fill(teacher), ids, mask)
+            now = [*out.values(), *(grads[k] for k in NAMES)]
+            want = want or now
+            assert all(torch.isfinite(t).all() for t in now), junk
+            assert all(torch.equal(a, b) for a, b in zip(now, want)), junk
+        trainer.step([3, 0, 2], fill(signal), fill(teacher), ids, valid)
+        assert all(torch.isfinite(t).all() for t in trainer.weights.values()), junk
+    for bad in (valid[:2], valid.float(), valid[..., None]):
+        with pytest.raises(ValueError):
+            trainer.gradients([3, 0, 2], signal, teacher, ids, bad)
