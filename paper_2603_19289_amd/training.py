@@ -7,12 +7,17 @@ records or reads an autograd graph.  The functions and AdamW's calls can be capt
 from __future__ import annotations
 
 import ctypes as C
+from array import array
+from operator import attrgetter
 from typing import List, Optional, Sequence
 
 import torch
 
 from . import moe_spec as M
 
+# what is asked of every tensor of a list, by map
+_NUMEL, _CONTIGUOUS, _DEVICE, _ADDRESS, _DTYPE = (torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.get_device, torch.Tensor.data_ptr,
+                                                  attrgetter("dtype"))
 _TYPES = {torch.float32: M.F32, torch.bfloat16: M.BF16}
 
 
@@ -172,27 +177,33 @@ class AdamW:
         self._states = {k: list(states[k]) for k in (("m", "v", "m_exp", "v_exp") if eight else ("m", "v"))}
         if any(len(t) != len(self.params) for t in (*self._states.values(), self.copies)):
             raise ValueError("as many moments and copies as parameters are needed")
-        written = [t for t in (*self.params, *self.copies, *(t for k in self._states.values() for t in k)) if t is not None and t.numel()]
-        if len({t.data_ptr() for t in written}) < len(written):
-            raise ValueError("a tensor is named twice")
-        self._held, self._at = [t for t in (*self.params, *self.copies) if t is not None], None
+        self._moments = [t for k in self._states.values() for t in k]
+        self._held = [t for t in (*self._moments, *self.params, *self.copies) if t is not None]
+        self._at = self._at_moments = None
         self._desc = (M.AdamWTensor * len(self.params))()
         self._entries = list(self._desc)                       # views of the table's entries
+        self._whole = False                                    # whether each entry's n is its tensor's
         self._config = M.AdamWConfig(seed=self.seed, moments=M.MOMENTS_8BIT if eight else M.MOMENTS_32BIT)
-        self._describe()
+        self._describe(self._held)
 
     def _tensor(self, t, name, dtype, n):
         if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.device or not t.is_cuda:
             raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} values on the parameters' GPU")
 
+    def _tensors(self, tensors, name, dtype, sizes):
+        """_tensor of each of them."""
+        if not (list(map(_NUMEL, tensors)) == sizes and all(map(_CONTIGUOUS, tensors)) and set(map(_DTYPE, tensors)) == {dtype}
+                and set(map(_DEVICE, tensors)) == {self.device.index}):
+            for t, n in zip(tensors, sizes):
+                self._tensor(t, name, dtype, n)
+
     def states(self) -> dict:
         """The moments: m and v, with 8 bits their codes and m_exp and v_exp."""
         return {k: list(t) for k, t in self._states.items()}
 
-    def _describe(self):
-        """The tensors' table for the library; made anew where a tensor has got other storage since."""
-        at = [t.data_ptr() for t in self._held]
-        if at == self._at:
+    def _describe(self, held):
+        """The tensors' table for the library; made anew where one of those that a call needs has got other storage since."""
+        if list(map(_ADDRESS, held)) == (self._at if held is self._held else self._at_moments):
             return
         s = self._states
         for i, (d, p) in enumerate(zip(self._entries, self.params)):
@@ -201,7 +212,7 @@ class AdamW:
                 d.m_exp, d.v_exp = s["m_exp"][i].data_ptr(), s["v_exp"][i].data_ptr()
             d.copy = self.copies[i].data_ptr() if self.copies[i] is not None else None
         self._check()
-        self._at = at
+        self._at, self._at_moments = list(map(_ADDRESS, self._held)), list(map(_ADDRESS, self._moments))
 
     def _check(self):
         eight = self.state == "f8"
@@ -212,6 +223,15 @@ class AdamW:
                 self._tensor(t[i], k, held, -(-p.numel() // M.MOMENT_BLOCK) if k.endswith("exp") else p.numel())
             if self.copies[i] is not None:
                 self._tensor(self.copies[i], "a copy", torch.bfloat16, p.numel())
+        written = [t.data_ptr() for t in self._held if t.numel()]
+        if len(set(written)) < len(written):
+            raise ValueError("a tensor is named twice")
+
+    def _all_whole(self):
+        if not self._whole:
+            for d, n in zip(self._entries, self._sizes):
+                d.n = n
+            self._whole = True
 
     def step(self, grads: Sequence[Optional[torch.Tensor]], *, step=None, grad_scale=1.0):
         """One step with a gradient for each parameter, all float32 or all bfloat16; a parameter whose gradient is None stays as
@@ -219,22 +239,24 @@ class AdamW:
         read it from, which a captured graph needs.  grad_scale: a factor of the gradients, a number or a float32 tensor on the GPU."""
         if len(grads) != len(self.params):
             raise ValueError("as many gradients as parameters are needed")
-        dtype = torch.float32
-        for g in grads:
-            if g is not None:
-                dtype = g.dtype
-                break
+        given = [g for g in grads if g is not None]
+        dtype = given[0].dtype if given else torch.float32
         if dtype not in _TYPES:
             raise ValueError("gradients must be float32 or bfloat16")
-        self._describe()
-        dev = self.device
-        for d, n, g in zip(self._entries, self._sizes, grads):
-            if g is None:
-                d.n = 0
-                continue
-            if g.dtype != dtype or g.numel() != n or g.device != dev or not g.is_contiguous():
-                self._tensor(g, "a gradient", dtype, n)
-            d.n, d.grad = n, g.data_ptr()
+        all_given = len(given) == len(grads)
+        self._tensors(given, "a gradient", dtype, self._sizes if all_given else [n for n, g in zip(self._sizes, grads) if g is not None])
+        self._describe(self._held)
+        self._all_whole()
+        if all_given:
+            for d, at in zip(self._entries, map(_ADDRESS, grads)):
+                d.grad = at
+        else:
+            self._whole = False
+            for d, g in zip(self._entries, grads):
+                if g is None:
+                    d.n = 0
+                else:
+                    d.grad = g.data_ptr()
         c = self._config
         c.lr, (c.beta1, c.beta2), c.eps, c.weight_decay, c.grad_dtype = self.lr, self.betas, self.eps, self.weight_decay, _TYPES[dtype]
         c.step_dev = c.grad_scale_dev = None
@@ -249,7 +271,7 @@ class AdamW:
             c.step_dev = step.data_ptr()
         else:
             c.step = self.steps + 1 if step is None else step
-        _queue(dev, M.lib().moe_spec_adamw_step, self._desc, len(self._desc), C.byref(c))
+        _queue(self.device, M.lib().moe_spec_adamw_step, self._desc, len(self._desc), C.byref(c))
         if not isinstance(step, torch.Tensor):
             self.steps = c.step
 
@@ -265,16 +287,14 @@ class AdamW:
         dtype = (m_out if m_out is not None else v_out)[0].dtype
         if dtype not in _TYPES:
             raise ValueError("moments are read as float32 or bfloat16")
-        dev = self.device
-        for out in (m_out, v_out):
-            for t, n in zip(out or (), self._sizes):
-                if t.dtype != dtype or t.numel() != n or t.device != dev or not t.is_contiguous():
-                    self._tensor(t, "an output", dtype, n)
-        self._describe()
-        for d, n in zip(self._entries, self._sizes):
-            d.n = n
-        pointers = lambda out: None if out is None else (C.c_void_p * len(out))(*[t.data_ptr() for t in out])  # noqa: E731
-        _queue(self.device, M.lib().moe_spec_adamw_read_moments, self._desc, len(self._desc), _TYPES[dtype], pointers(m_out), pointers(v_out))
+        given = [out for out in (m_out, v_out) if out is not None]
+        outs = [t for out in given for t in out]
+        self._tensors(outs, "an output", dtype, self._sizes * len(given))
+        self._describe(self._moments)
+        self._all_whole()
+        at = (C.c_void_p * len(self._sizes) * len(given)).from_buffer(array("Q", map(_ADDRESS, outs)))
+        _queue(self.device, M.lib().moe_spec_adamw_read_moments, self._desc, len(self._desc), _TYPES[dtype],
+               at[0] if m_out is not None else None, at[-1] if v_out is not None else None)
         return m_out, v_out
 
 

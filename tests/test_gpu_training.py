@@ -667,6 +667,25 @@ def test_adamw_step_number_and_scale_on_the_gpu():
     assert not torch.equal(results[0][1], results[2][1])
 
 
+@pytest.mark.parametrize("state", ["f32", "f8"])
+def test_adamw_goes_on_with_moments_that_were_put_in_its_tensors(state):
+    """`data` of a moment replaced, as a program that loads a checkpoint does: the next step reads and writes the new memory, and
+    leaves what was there before."""
+    from paper_2603_19289_amd import training as T
+    params, grads = adam_case([700, 130], 3, "f32")
+    grads = [[on_gpu(g) for g in gs] for gs in grads]
+    one = T.AdamW([on_gpu(p) for p in params], lr=1e-3, state=state, seed=2)
+    one.step(grads[0])
+    saved = {k: [t.clone() for t in ts] for k, ts in one.states().items()}
+    two = T.AdamW([p.clone() for p in one.params], lr=1e-3, state=state, seed=2, steps=1)
+    for key, ts in two.states().items():
+        for t, loaded in zip(ts, saved[key]):
+            t.data = loaded.clone()
+    one.step(grads[1]), two.step(grads[1])
+    for a, b in zip((*one.params, *(t for ts in one.states().values() for t in ts)), (*two.params, *(t for ts in two.states().values() for t in ts))):
+        assert torch.equal(a, b)
+
+
 # ------------------------------------------------------------------------------------------------ far apart
 def test_rows_that_are_far_apart():
     """Element offsets beyond 2^31 and byte offsets beyond 2^32: views of a large buffer against the same rows close together."""
