@@ -330,6 +330,8 @@ class EstimatorTrainer:
         w = self.weights
         if len(set(layers)) != n or len(layers) != n or not all(0 <= l < w["layer_emb"].shape[0] for l in layers):
             raise ValueError("a layer of its own for each of the signals is needed")
+        if ids is None and self.balance_coef != 0.0:
+            raise ValueError("the balance term needs choices to count: ids, or a balance_coef of 0")
         if any(t is not None and t.shape[:2] != (n, tokens) for t in (teacher, ids, valid)):
             raise ValueError("teacher, ids and valid must have the layers and tokens of the signal")
         flat = lambda t: None if t is None else t.reshape(n * tokens, *t.shape[2:])  # noqa: E731

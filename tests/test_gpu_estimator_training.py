@@ -135,3 +135,17 @@ def test_padding_counts_for_nothing_whatever_it_holds(dtype):
     for bad in (valid[:2], valid.float(), valid[..., None]):
         with pytest.raises(ValueError):
             trainer.gradients([3, 0, 2], signal, teacher, ids, bad)
+
+
+def test_a_balance_term_without_choices_is_refused():
+    from paper_2603_19289_amd import training as T
+    wl = small_workload(name="training", n_layers=5, hidden=264, n_experts=12, top_k=3, inter=200, dtype="f32", batch=1, tokens=1, slots=6, seed=5)
+    signal, teacher, _, valid = (t.cuda() for t in batch(wl, 3, 37, 1))
+    trainer = T.EstimatorTrainer(W.make_estimator(wl, m=3, n=2), balance_coef=0.1)
+    before = {k: t.clone() for k, t in trainer.weights.items()}
+    for call in (trainer.gradients, trainer.step):
+        with pytest.raises(ValueError):
+            call([3, 0, 2], signal, teacher, None, valid)
+    assert all(torch.equal(before[k], t) for k, t in trainer.weights.items())
+    trainer.balance_coef = 0.0
+    assert "balance" not in trainer.step([3, 0, 2], signal, teacher, None, valid)
