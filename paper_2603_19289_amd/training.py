@@ -298,6 +298,11 @@ class AdamW:
         return m_out, v_out
 
 
+def _choices(z: torch.Tensor, k: int) -> torch.Tensor:
+    """The k largest of each row, among equals those of the lowest index: int32 [rows, k]."""
+    return torch.sort(z, dim=1, descending=True, stable=True).indices[:, :k].to(torch.int32)
+
+
 class EstimatorTrainer:
     """Distils the expert estimator (paper: Appendix A) from the routers it stands in for.
 
@@ -306,11 +311,15 @@ class EstimatorTrainer:
     given an Engine's own (`engine.est`), its predictions follow the training, as its context reads the same memory; the caller
     keeps the engine's stream and the training stream apart in time.  bfloat16 tables have float32 masters here and are the
     copies that AdamW writes; products then take bfloat16 operands and add up in float32, in the library that torch
-    calls for plain matrix products, and what lies between them is bfloat16 too.  LayerNorm, losses and AdamW are this library's."""
+    calls for plain matrix products, and what lies between them is bfloat16 too.  LayerNorm, losses and AdamW are this library's.
+
+    balance_coef: weight of a balance loss over the estimator's own predictions, against its collapse on a few experts.  top_k: how
+    many experts it predicts for a token, which that loss counts."""
 
     NAMES = ("proj", "layer_emb", "ffn_in", "ffn_out", "ln_gain", "ln_bias", "head")
 
-    def __init__(self, weights: dict, *, lr: float = 1e-3, balance_coef: float = 0.0, ln_eps: float = 1e-5, device="cuda:0", **adamw):
+    def __init__(self, weights: dict, *, lr: float = 1e-3, balance_coef: float = 0.0, top_k: Optional[int] = None, ln_eps: float = 1e-5,
+                 device="cuda:0", **adamw):
         from .engine import _np_to_torch_storage
         to = lambda v: v if isinstance(v, torch.Tensor) else _np_to_torch_storage(v).to(device)  # noqa: E731
         self.weights = {k: to(weights[k]) for k in self.NAMES}
@@ -318,20 +327,25 @@ class EstimatorTrainer:
         masters = {k: (v if v.dtype == torch.float32 else v.float()) for k, v in self.weights.items()}
         self.optimizer = AdamW([masters[k] for k in self.NAMES], lr=lr, copies=[
             self.weights[k] if self.weights[k] is not masters[k] else None for k in self.NAMES], **adamw)
-        self.balance_coef, self.ln_eps = balance_coef, ln_eps
+        if top_k is not None and not 1 <= top_k <= self.weights["head"].shape[0]:
+            raise ValueError("top_k must be between 1 and the number of experts")
+        self.balance_coef, self.top_k, self.ln_eps = balance_coef, top_k, ln_eps
 
     @torch.no_grad()
     def gradients(self, layers: Sequence[int], signal: torch.Tensor, teacher: torch.Tensor, ids: Optional[torch.Tensor] = None,
                   valid: Optional[torch.Tensor] = None):
         """Losses and gradients for the predicting signals [n, T, H] of n different layers and the logits [n, T, E] that the
-        next layers' routers gave -> (dict of loss, balance, counts; dict of gradients).  ids: the experts that these
-        routers chose, int32 [n, T, k], for the balance loss and the counts.  valid: [n, T], 0 for padding."""
+        next layers' routers gave -> (dict of loss, balance, counts; dict of gradients).  The balance loss and the counts are of
+        the experts that the estimator chooses: the top_k largest of its logits, or ids, int32 [n, T, k], where the caller has its
+        choices already.  (Not the routers' choices: against those the loss would push the estimator away from what it is
+        to predict, and where they are balanced it would not push at all.)  valid: [n, T], 0 for padding, which counts for
+        nothing whatever it holds."""
         n, tokens, _ = signal.shape
         w = self.weights
         if len(set(layers)) != n or len(layers) != n or not all(0 <= l < w["layer_emb"].shape[0] for l in layers):
             raise ValueError("a layer of its own for each of the signals is needed")
-        if ids is None and self.balance_coef != 0.0:
-            raise ValueError("the balance term needs choices to count: ids, or a balance_coef of 0")
+        if ids is None and self.top_k is None and self.balance_coef != 0.0:
+            raise ValueError("the balance term needs choices to count: top_k or ids, or a balance_coef of 0")
         if any(t is not None and t.shape[:2] != (n, tokens) for t in (teacher, ids, valid)):
             raise ValueError("teacher, ids and valid must have the layers and tokens of the signal")
         flat = lambda t: None if t is None else t.reshape(n * tokens, *t.shape[2:])  # noqa: E731
@@ -349,8 +363,9 @@ class EstimatorTrainer:
         z = torch.mm(y, w["head"].T)
         loss, dz = distill_loss(z, flat(teacher), valid=mask)
         out = {"loss": loss}
-        if ids is not None:
-            out["balance"], out["counts"], extra = balance_loss(z, flat(ids), coef=self.balance_coef, valid=mask,
+        if ids is not None or self.top_k is not None:
+            chosen = flat(ids) if ids is not None else _choices(z, self.top_k)
+            out["balance"], out["counts"], extra = balance_loss(z, chosen, coef=self.balance_coef, valid=mask,
                                                                 grad=self.balance_coef != 0.0)
             if extra is not None:
                 dz = dz + extra

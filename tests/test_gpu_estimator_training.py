@@ -149,3 +149,52 @@ def test_a_balance_term_without_choices_is_refused():
     assert all(torch.equal(before[k], t) for k, t in trainer.weights.items())
     trainer.balance_coef = 0.0
     assert "balance" not in trainer.step([3, 0, 2], signal, teacher, None, valid)
+
+
+def logits_of(est, layers, signal):
+    """The estimator's logits in 64 bits."""
+    w = decoded(est)
+    u = signal.double() @ w["proj"].T + w["layer_emb"][list(layers)][:, None]
+    h = u @ w["ffn_in"].T
+    v = u + (h * torch.sigmoid(h)) @ w["ffn_out"].T
+    c = v - v.mean(-1, keepdim=True)
+    return (c / torch.sqrt((c * c).mean(-1, keepdim=True) + 1e-5) * w["ln_gain"] + w["ln_bias"]) @ w["head"].T
+
+
+def collapsed(est):
+    """Weights that give expert 0 the largest logit whatever the signal: its row of the head lies along the bias that all outputs share."""
+    bias = 0.4 * np.random.default_rng(3).standard_normal(len(est["ln_bias"])).astype(np.float32)
+    head = est["head"].copy()
+    head[0] = 0.3 * bias
+    return {**est, "ln_gain": 0.05 * est["ln_gain"], "ln_bias": bias, "head": head}
+
+
+@pytest.mark.parametrize("fallen", [False, True])
+def test_the_balance_term_is_of_the_estimators_own_choices(fallen):
+    """Under balanced routers: f of the top-k of the estimator's logits in the loss, the counts and every gradient, by the 64-bit
+    reverse pass with those choices.  No row's choice hangs on rounding: four products of at most 264 terms move z by at most 4 * 264 *
+    2^-24 of their terms' magnitudes, which are below 5 times the largest logit: 3e-4 of that."""
+    from paper_2603_19289_amd import training as T
+    wl = small_workload(name="training", n_layers=5, hidden=264, n_experts=12, top_k=3, inter=200, dtype="f32", batch=1, tokens=1, slots=6, seed=5)
+    est = W.make_estimator(wl, m=3, n=2)
+    est = collapsed(est) if fallen else est
+    layers = [3, 0, 2]
+    signal, teacher, _, valid = batch(wl, 3, 37, 1)
+    teacher[:] = 0.0
+    z = logits_of(est, layers, signal)
+    ranked, chosen = z.sort(-1, descending=True)
+    assert (ranked[..., 2] - ranked[..., 3]).min() > 3e-4 * z.abs().max()      # in 64 bits, before anything runs
+    trainer = T.EstimatorTrainer(est, balance_coef=0.1, top_k=3)
+    out, grads = trainer.gradients(layers, signal.cuda(), teacher.cuda(), valid=valid.cuda())
+    loss, balance, counts, want = reverse_pass(est, layers, signal, teacher, chosen[..., :3], valid, 0.1)
+    assert torch.equal(out["counts"].cpu().long(), counts) and (not fallen or counts[0] == valid.sum())
+    assert abs(out["loss"].item() - loss) < 2e-3 * loss and abs(out["balance"].item() - balance) < 2e-3 * balance
+    for k in NAMES:
+        assert (grads[k].cpu().double() - want[k]).abs().max() < 2e-3 * want[k].abs().max(), k
+    without = T.EstimatorTrainer(est, top_k=3).gradients(layers, signal.cuda(), teacher.cuda(), valid=valid.cuda())
+    assert torch.equal(without[0]["counts"], out["counts"])
+    if fallen:                                             # it is pushed: by more than rounding, in the head's row of expert 0
+        assert (grads["head"][0] - without[1]["head"][0]).abs().max() > 0.01 * without[1]["head"].abs().max()
+    for bad in (0, 13):
+        with pytest.raises(ValueError):
+            T.EstimatorTrainer(est, top_k=bad)

@@ -52,3 +52,11 @@ def test_adamw_refuses_a_tensor_that_comes_to_lie_on_another(calls):
     for _ in range(2):
         with pytest.raises(ValueError):
             opt.step([torch.zeros(30)] * 2)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_choices_among_equal_logits_are_those_of_the_lowest_index(dtype):
+    z = torch.tensor([[1.0, 3.0, 3.0, 0.0, 3.0], [2.0] * 5, [float("-inf")] * 5, [0.0, 1.0, -1.0, 1.0, 5.0]], dtype=dtype)
+    got = T._choices(z, 3)
+    assert got.dtype == torch.int32 and got.stride(1) == 1
+    assert got.tolist() == [[1, 2, 4], [0, 1, 2], [0, 1, 2], [4, 1, 3]]
