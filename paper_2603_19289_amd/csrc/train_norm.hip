@@ -261,10 +261,11 @@ __global__ __launch_bounds__((Shape<WT, LANES, C>::kBlock2)) void norm_backward_
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const Place<V, RAGGED> at(c * LANES + lane, a.cols);
+      const float centre = at.used ? mean : 0.0f;      // behind the last column h is zero, not mean * rstd, which may be infinite
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float dy = w[c][i];       // zero behind the last column and the last row
-        h[c][i] = (h[c][i] - mean) * rstd;
+        h[c][i] = (h[c][i] - centre) * rstd;
         dgain[c][i] += dy * h[c][i];
         dbias[c][i] += dy;
         w[c][i] = dy * gain[c][i];

@@ -161,6 +161,26 @@ def test_layernorm_rows_that_are_constant_or_not_finite():
     assert torch.isfinite(dx[fine]).all() and not torch.isfinite(dx[2:5]).any() and torch.isnan(dgain).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(3, 1), (3, 4), (3, 5), (5, 36), (1030, 40), (4, 520), (3, 1023), (2, 1030), (2, 2049), (2, 4100), (2, 8184)])
+def test_layernorm_backward_of_rows_far_from_zero(rows, cols, dtype):
+    """Constant rows whose mean times rstd is beyond float: h is zero, so dx = rstd (w - mean w), dgain is zero and all is finite.  The last
+    row is ordinary.  Bounds: the sum of w as above, depth 30 and a product; three operations."""
+    from paper_2603_19289_amd import training as T
+    x, dy, gain, _ = ln_inputs(rows, cols, dtype, 5 * cols + rows)
+    x[:-1] = torch.tensor(1e38).to(TYPES[dtype])
+    mean = x.double().mean(1).float()
+    rstd = torch.full((rows,), 316.0)
+    mean[-1], rstd[-1] = 0.0, 1.0
+    dx, dgain, dbias = T.layernorm_backward(on_gpu(dy), on_gpu(x), on_gpu(mean), on_gpu(rstd), on_gpu(gain))
+    w = dy.double() * gain.double()
+    c1 = w.mean(1, keepdim=True)
+    want = 316.0 * (w - c1)[:-1]
+    close(dx[:-1], want, 316.0 * (32 * U * w.abs().mean(1, keepdim=True) + 4 * U * (w.abs() + c1.abs()))[:-1] + half(TYPES[dtype]) * want.abs() * 1.01, "dx")
+    assert torch.isfinite(dx).all() and torch.isfinite(dbias).all()
+    close(dgain, dy[-1].double() * x[-1].double(), 2 * U * (dy[-1].double() * x[-1].double()).abs(), "dgain")
+
+
 def test_layernorm_without_rows_and_partial_outputs():
     from paper_2603_19289_amd import training as T
     x = torch.empty(0, 48, device="cuda")
