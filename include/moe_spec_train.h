@@ -61,7 +61,8 @@ int moe_spec_layernorm_backward(void *stream, int dtype, const void *dy, int64_t
  * `student` itself with the same stride.
  * A logit of minus infinity has probability zero.  Where the teacher's is, nothing is added to the loss; a row whose
  * teacher has no other logits teaches nothing: loss and gradient zero (it counts in the mean).  Where only the student's is,
- * the loss is infinite and the gradient finite.  Any other logit that is no finite number makes the loss and that row's
+ * the loss is infinite, however small the teacher's probability, and the gradient finite; a difference between logits of a
+ * row that float cannot hold counts as infinite.  Any other logit that is no finite number makes the loss and that row's
  * gradient NaN, and no other row's. */
 size_t moe_spec_distill_loss_workspace_bytes(int64_t rows, int n_experts);
 int moe_spec_distill_loss(void *stream, int student_dtype, const void *student, int64_t student_stride, int teacher_dtype,

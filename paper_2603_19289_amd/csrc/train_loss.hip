@@ -233,7 +233,7 @@ __global__ __launch_bounds__(BLOCK) void loss_kernel(const LossArgs a) {
         top_t = group_reduce<G>(top_t, Max());
         if (top_z == -INFINITY) top_z = 0.0f;
         if (top_t == -INFINITY) top_t = 0.0f;
-        float sum_z = 0.0f, sum_t = 0.0f, cross = 0.0f, p[kVals];
+        float sum_z = 0.0f, sum_t = 0.0f, cross = 0.0f, apart = 0.0f, p[kVals];
 #pragma unroll
         for (int i = 0; i < kVals; ++i) {
           z[i] -= top_z;
@@ -249,8 +249,10 @@ __global__ __launch_bounds__(BLOCK) void loss_kernel(const LossArgs a) {
         for (int i = 0; i < kVals; ++i) {
           p[i] *= inv_t;
           cross += p[i] == 0.0f ? 0.0f : p[i] * (t[i] - z[i]);             // 0 log 0 = 0
+          apart = fmaxf(apart, t[i] - z[i]);                               // both minus infinity: NaN, which fmaxf passes over
           grad[i] = grad[i] * over_z - p[i] * scale;
         }
+        if (apart == INFINITY) cross = INFINITY;                           // the student's alone is, however small p is
         cross = group_sum<G>(cross);
         result = cross * a.inv_tau + kLn2 * ((empty ? 0.0f : __builtin_amdgcn_logf(sum_z)) - __builtin_amdgcn_logf(sum_t));
         if (sum_t == 0.0f || !counts) {                                    // nothing to teach, the teacher's row is masked out whole

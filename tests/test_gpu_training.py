@@ -371,6 +371,27 @@ def test_losses_with_masked_and_non_finite_logits(dtype):
     assert math.isnan(loss.item()) and torch.isnan(grad[3]).all() and torch.isfinite(grad[[0, 1, 2, 4, 5, 6, 7, 8]]).all()
 
 
+@pytest.mark.parametrize("experts", [2, 7, 20, 128, 250])
+@pytest.mark.parametrize("rows", [3, 5000])
+def test_an_expert_that_only_the_student_rules_out_makes_the_loss_infinite(rows, experts):
+    """Also where the teacher's probability is below what float holds; not in rows that do not count, nor where the teacher rules it
+    out too or alone."""
+    from paper_2603_19289_amd import training as T
+    t, s, _, _ = logits(rows, experts, 3)
+    for below in (50.0, 100.0, 1000.0, 1e30):
+        a, b = t.clone(), s.clone()
+        a[1, experts - 1], b[1, experts - 1] = -below, -math.inf
+        loss, grad = T.distill_loss(on_gpu(b), on_gpu(a))
+        assert loss.item() == math.inf and torch.isfinite(grad).all(), below
+        valid = torch.ones(rows, dtype=torch.bool)
+        valid[1] = False
+        assert math.isfinite(T.distill_loss(on_gpu(b), on_gpu(a), valid=on_gpu(valid))[0].item())
+        a[1, experts - 1] = -math.inf
+        assert math.isfinite(T.distill_loss(on_gpu(b), on_gpu(a))[0].item())
+        b[1, experts - 1] = 0.5
+        assert math.isfinite(T.distill_loss(on_gpu(b), on_gpu(a))[0].item())
+
+
 def test_losses_without_rows_or_valid_rows():
     from paper_2603_19289_amd import training as T
     z = torch.empty(0, 8, device="cuda")
