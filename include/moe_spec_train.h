@@ -39,6 +39,7 @@ extern "C" {
 #define MOE_SPEC_TRAIN_MAX_COLS 8192          /* widest row of LayerNorm */
 #define MOE_SPEC_TRAIN_MAX_ROWS 0x7fffffff
 #define MOE_SPEC_TRAIN_MAX_TENSORS 65536      /* of one AdamW call */
+#define MOE_SPEC_ADAMW_MAX_ELEMENTS 34359736320  /* of one of its tensors: what the threads of a launch, below 2^32, take */
 
 /* LayerNorm (Appendix A: the estimator's last step before its head).  x, y dev [rows, cols]; gain, bias dev [cols] float or
  * NULL (ones, zeros); mean, rstd dev [rows] float or NULL: the row's mean and 1 / sqrt(variance + eps), which the backward

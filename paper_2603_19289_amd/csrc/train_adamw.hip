@@ -11,13 +11,13 @@
 // random bits below the last one that is kept rounds up with the probability of what is cut off.  One rounding an operation
 // (no contraction), IEEE division and root: parameters, moments and codes are those of the formulas in float, bit for bit.
 #include "train_common.h"
+#include "train_rules.h"
 
 #include <math.h>
 
 namespace moe_spec {
 namespace {
 
-constexpr int kAdamBlock = 256, kAdamVals = 8, kAdamChunk = kAdamBlock * kAdamVals, kPerLaunch = 40;
 constexpr uint32_t kOdd1 = 0x9E3779B1u, kOdd2 = 0x85EBCA77u;
 static_assert(MOE_SPEC_MOMENT_BLOCK == 16 * kAdamVals, "a run of a moment block is a row of 16 lanes");
 
@@ -290,37 +290,15 @@ __global__ __launch_bounds__(kAdamBlock) void moments_kernel(const MomentArgs a)
   }
 }
 
-// Deals the tensors to launches: as many as an argument block holds and as workgroups fit a grid.  `put` fills in one.
-template <typename Args, typename Put, typename Go>
-hipError_t in_launches(const moe_spec_adamw_tensor *tensors, int n_tensors, Args &a, Put put, Go go) {
-  constexpr int64_t kMostBlocks = 1 << 30;
-  int64_t blocks = 0;
-  int count = 0;
-  auto send = [&]() {
-    for (int i = count; i < kPerLaunch; ++i) a.first[i] = UINT32_MAX;
-    const unsigned grid = unsigned(blocks);
-    count = 0;
-    blocks = 0;
-    return go(grid);
-  };
-  for (int i = 0; i < n_tensors; ++i) {
-    const int64_t need = (tensors[i].n + kAdamChunk - 1) / kAdamChunk;
-    if (need == 0) continue;
-    if (count == kPerLaunch || (count && blocks + need > kMostBlocks)) {
-      const hipError_t e = send();
-      if (e != hipSuccess) return e;
-    }
-    a.first[count] = uint32_t(blocks);
-    put(count++, i);
-    blocks += need;
-  }
-  return count ? send() : hipSuccess;
+// Closes the list of a launch's first workgroups.
+void no_more(uint32_t (&first)[kPerLaunch], int count) {
+  for (int i = count; i < kPerLaunch; ++i) first[i] = UINT32_MAX;
 }
 
 const char *count_fault(const moe_spec_adamw_tensor *t, int n) {
   if (n < 0 || n > MOE_SPEC_TRAIN_MAX_TENSORS) return "a number of tensors out of range";
   if (n && !t) return "tensors is null";
-  for (int i = 0; i < n; ++i) if (t[i].n < 0 || t[i].n > (int64_t(1) << 40)) return "a tensor's n is out of range";
+  for (int i = 0; i < n; ++i) if (t[i].n < 0 || t[i].n > MOE_SPEC_ADAMW_MAX_ELEMENTS) return "a tensor's n is out of range";
   return nullptr;
 }
 
@@ -373,7 +351,12 @@ extern "C" int moe_spec_adamw_step(void *stream, const moe_spec_adamw_tensor *te
   a.step_dev = cfg->step_dev; a.scale_dev = cfg->grad_scale_dev; a.scale = float(cfg->grad_scale);
   a.seed = cfg->seed;
   const bool bf16 = cfg->grad_dtype == MOE_SPEC_BF16;
-  const hipError_t e = in_launches(tensors, n_tensors, a, [&](int slot, int i) { a.t[slot] = tensors[i]; a.place[slot] = uint32_t(i); }, [&](unsigned blocks) {
+  const hipError_t e = in_launches(tensors, n_tensors, [&](int slot, int i, uint32_t first) {
+    a.t[slot] = tensors[i];
+    a.place[slot] = uint32_t(i);
+    a.first[slot] = first;
+  }, [&](int count, unsigned blocks) {
+    no_more(a.first, count);
     if (eight) return bf16 ? launch(adamw_kernel<uint16_t, true>, blocks, kAdamBlock, s, a) : launch(adamw_kernel<float, true>, blocks, kAdamBlock, s, a);
     return bf16 ? launch(adamw_kernel<uint16_t, false>, blocks, kAdamBlock, s, a) : launch(adamw_kernel<float, false>, blocks, kAdamBlock, s, a);
   });
@@ -397,11 +380,13 @@ extern "C" int moe_spec_adamw_read_moments(void *stream, const moe_spec_adamw_te
   const OnDeviceOf on(s);
   if (on.error() != hipSuccess) return train_fail(MOE_SPEC_EHIP, "adamw_read_moments: %s", hipGetErrorString(on.error()));
   MomentArgs a;
-  const hipError_t e = in_launches(tensors, n_tensors, a, [&](int slot, int i) {
+  const hipError_t e = in_launches(tensors, n_tensors, [&](int slot, int i, uint32_t first) {
     const moe_spec_adamw_tensor &t = tensors[i];
     a.t[slot] = {static_cast<const uint8_t *>(t.m), static_cast<const uint8_t *>(t.v), t.m_exp, t.v_exp,
                  m_out ? m_out[i] : nullptr, v_out ? v_out[i] : nullptr, t.n};
-  }, [&](unsigned blocks) {
+    a.first[slot] = first;
+  }, [&](int count, unsigned blocks) {
+    no_more(a.first, count);
     return out_dtype == MOE_SPEC_BF16 ? launch(moments_kernel<uint16_t>, blocks, kAdamBlock, s, a) : launch(moments_kernel<float>, blocks, kAdamBlock, s, a);
   });
   return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "adamw_read_moments: %s", hipGetErrorString(e));

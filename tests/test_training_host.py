@@ -1,5 +1,8 @@
 """What training.py does on the host, on a machine without a GPU: calls into the library are recorded instead of made, and the checks that
 tensors lie on a GPU are left out."""
+import os
+import subprocess
+
 import pytest
 import torch
 
@@ -60,3 +63,52 @@ def test_choices_among_equal_logits_are_those_of_the_lowest_index(dtype):
     got = T._choices(z, 3)
     assert got.dtype == torch.int32 and got.stride(1) == 1
     assert got.tolist() == [[1, 2, 4], [0, 1, 2], [0, 1, 2], [4, 1, 3]]
+
+
+DEALING = r"""
+#include <cstdio>
+#include <vector>
+#include "train_rules.h"
+using namespace moe_spec;
+int main() {
+  int bad = 0;
+  const int64_t most = MOE_SPEC_ADAMW_MAX_ELEMENTS;
+  const int64_t lists[][4] = {{0, 1, 2048, 2049}, {most, most, 1, most}, {most / 2, most / 2, 4096, most}, {1, most, 1, 0},
+                              {most - 2048, 2048, 1, 5}, {most - 2048, 2049, 1, 5}, {0, 0, 0, 0}, {5, 0, 0, 7}};
+  for (auto &sizes : lists) for (int n : {0, 1, 4, 39, 40, 41, 80, 81, 300}) {
+    std::vector<moe_spec_adamw_tensor> t(n);
+    for (int i = 0; i < n; ++i) t[i].n = sizes[i % 4];
+    int next = 0, slots = 0, launches = 0;
+    int64_t blocks = 0;
+    bool ok = true;
+    in_launches(t.data(), n, [&](int slot, int i, uint32_t first) {
+      while (next < i && t[next].n == 0) ++next;              // what lies between has no elements
+      ok = ok && slot == slots++ && i == next++ && t[i].n > 0 && int64_t(first) == blocks;
+      blocks += (t[i].n + kAdamChunk - 1) / kAdamChunk;
+    }, [&](int count, unsigned grid) {
+      ok = ok && count == slots && count >= 1 && count <= kPerLaunch && int64_t(grid) == blocks && uint64_t(grid) * kAdamBlock < (uint64_t(1) << 32);
+      slots = 0;
+      blocks = 0;
+      ++launches;
+      return 0;
+    });
+    while (next < n && t[next].n == 0) ++next;
+    if ((!ok || next != n || slots) && ++bad <= 20) std::printf("n %d, first %lld: %d launches, next %d\n", n, (long long)sizes[0], launches, next);
+    int calls = 0;
+    const int e = in_launches(t.data(), n, [](int, int, uint32_t) {}, [&](int, unsigned) { return ++calls == 2 ? 7 : 0; });
+    if ((launches >= 2 ? e != 7 || calls != 2 : e != 0 || calls != launches) && ++bad <= 20) std::printf("n %d: status %d after %d calls\n", n, e, calls);
+  }
+  return bad ? 1 : 0;
+}
+"""
+
+
+def test_adamw_tensors_are_dealt_to_launches_that_fit(tmp_path):
+    """Every tensor that has elements is in exactly one launch, in order, its workgroups behind those of the tensors before it; a
+    launch has at most an argument block's tensors and fewer than 2^32 threads; one that fails ends the call."""
+    src, exe = tmp_path / "deal.cpp", tmp_path / "deal"
+    src.write_text(DEALING)
+    csrc = os.path.join(os.path.dirname(M.__file__), "csrc")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", csrc, str(src), "-o", str(exe)], check=True)
+    done = subprocess.run([str(exe)], capture_output=True, text=True, timeout=120)
+    assert done.returncode == 0, done.stdout[-2000:]

@@ -177,3 +177,18 @@ def test_the_reason_of_a_failure_is_the_calling_threads():
     t.start()
     t.join()
     assert seen == [b""] and b"cols" in M.lib().moe_spec_train_last_error()
+
+
+MOST = (2 ** 24 - 1) * 2048                       # elements of an AdamW tensor: a launch has fewer than 2^32 threads, 256 a workgroup
+
+
+@pytest.mark.parametrize("n", [MOST + 1, 1 << 35, 1 << 40])
+def test_adamw_refuses_a_tensor_that_no_launch_can_take(n):
+    refused(adamw(tensor=dict(n=n)), "adamw_step", "n is out")
+    arr = (M.AdamWTensor * 2)(M.AdamWTensor(n=5, m=ADDR, m_exp=ADDR), M.AdamWTensor(n=n, m=ADDR, m_exp=ADDR))
+    refused(M.lib().moe_spec_adamw_read_moments(None, arr, 2, M.BF16, (C.c_void_p * 2)(ADDR, ADDR), None), "read_moments", "n is out")
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="meant for a machine without a GPU")
+def test_adamw_takes_the_longest_tensor_that_it_names():
+    assert adamw(tensor=dict(n=MOST)) == M.EHIP
