@@ -2,8 +2,10 @@
 include/moe_spec_train.h.  Torch supplies memory and streams; the operators are the library's kernels.
 
 Every function queues its kernels on the current stream of its tensors' device and returns tensors that are valid in that
-stream's order; tensors of another stream are the caller's to order and to keep, as with torch's own operations.  Gradients are results of explicit calls (a loss returns its own, `layernorm_backward` takes one): nothing here
-records or reads an autograd graph.  The functions and AdamW's calls can be captured into a graph."""
+stream's order; tensors of another stream are the caller's to order and to keep, as with torch's own operations.  Gradients are
+results of explicit calls (a loss returns its own, `layernorm_backward` takes one): nothing here records or reads an autograd
+graph, and results have none.  What is written in place (`out`, AdamW's parameters and copies) counts as changed for graphs that have
+kept it: their backward pass raises torch's error, as after torch's own operations.  The functions and AdamW's calls can be captured into a graph."""
 from __future__ import annotations
 
 import ctypes as C
@@ -12,6 +14,7 @@ from operator import attrgetter
 from typing import List, Optional, Sequence
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import moe_spec as M
 
@@ -66,14 +69,19 @@ def layernorm_forward(x: torch.Tensor, gain: Optional[torch.Tensor] = None, bias
     dtype = _rows(x, "x")
     rows, cols = x.shape
     dev = x.device
-    if out is None:
+    given = out is not None
+    if not given:
         out = x.new_empty((rows, cols))
     elif _rows(out, "out", x) != dtype:
         raise ValueError("out must have the type of x")
+    elif out.requires_grad and torch.is_grad_enabled():
+        raise ValueError("out requires a gradient, and what is written there would not be in its graph")
     mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind(0)
     at = mean.data_ptr()
     _queue(dev, M.lib().moe_spec_layernorm_forward, dtype, x.data_ptr(), x.stride(0), rows, cols, _vector(gain, "gain", cols, dev),
            _vector(bias, "bias", cols, dev), eps, out.data_ptr(), out.stride(0), at, at + 4 * rows)
+    if given:
+        increment_version(out)
     return out, mean, rstd
 
 
@@ -178,7 +186,8 @@ class AdamW:
         if any(len(t) != len(self.params) for t in (*self._states.values(), self.copies)):
             raise ValueError("as many moments and copies as parameters are needed")
         self._moments = [t for k in self._states.values() for t in k]
-        self._held = [t for t in (*self._moments, *self.params, *self.copies) if t is not None]
+        self._written = [t for t in (*self.params, *self.copies) if t is not None]
+        self._held = [*self._moments, *self._written]
         self._at = self._at_moments = None
         self._desc = (M.AdamWTensor * len(self.params))()
         self._entries = list(self._desc)                       # views of the table's entries
@@ -274,6 +283,8 @@ class AdamW:
         _queue(self.device, M.lib().moe_spec_adamw_step, self._desc, len(self._desc), C.byref(c))
         if not isinstance(step, torch.Tensor):
             self.steps = c.step
+        increment_version(self._written if all_given else [t for i, g in enumerate(grads) if g is not None
+                                                           for t in (self.params[i], self.copies[i]) if t is not None])
 
     def read_moments(self, m_out: Optional[List[torch.Tensor]] = None, v_out: Optional[List[torch.Tensor]] = None):
         """The values of 8-bit moments, into float32 or bfloat16 tensors (which hold all of them from 2^-120 on exactly) or new

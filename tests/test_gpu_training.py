@@ -727,6 +727,48 @@ def test_adamw_goes_on_with_moments_that_were_put_in_its_tensors(state):
         assert torch.equal(a, b)
 
 
+# ------------------------------------------------------------------------------------------------ beside autograd
+def test_tensors_written_in_place_count_as_changed_for_graphs_that_kept_them():
+    """A backward pass over what was overwritten raises torch's error instead of giving gradients of other values; what was not written
+    does not count as changed."""
+    from paper_2603_19289_amd import training as T
+    a = torch.randn(3, 8, device="cuda", requires_grad=True)
+    v = 2 * a
+    square = (v * v).sum()                                 # keeps v
+    T.layernorm_forward(v.detach())
+    square.backward(retain_graph=True)
+    T.layernorm_forward(v.detach(), out=v.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        square.backward()
+    for t in (a, v):
+        with pytest.raises(ValueError):
+            T.layernorm_forward(t, out=t)
+    with torch.no_grad():
+        T.layernorm_forward(v, out=v)
+
+    for state in ("f32", "f8"):
+        p, q = (torch.randn(8, device="cuda", requires_grad=True) for _ in range(2))
+        copy = p.detach().to(torch.bfloat16).requires_grad_()
+        opt = T.AdamW([p, q], lr=0.1, state=state, copies=[copy, None])
+        g = torch.ones(8, device="cuda")
+        losses = [(t * t).sum() for t in (p, q, copy)]
+        opt.step([g, None])
+        losses[1].backward()                               # q had no gradient
+        for loss in (losses[0], losses[2]):
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                loss.backward()
+        loss = (q * q).sum()
+        opt.step([g, g])
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    # a gradient that a loss returned goes into a graph of torch's
+    w = torch.randn(5, 8, device="cuda", requires_grad=True)
+    z = torch.randn(4, 5, device="cuda") @ w
+    _, dz = T.distill_loss(z, torch.randn(4, 8, device="cuda"))
+    z.backward(dz)
+    assert not dz.requires_grad and torch.isfinite(w.grad).all()
+
+
 # ------------------------------------------------------------------------------------------------ far apart
 def test_rows_that_are_far_apart():
     """Element offsets beyond 2^31 and byte offsets beyond 2^32: views of a large buffer against the same rows close together."""
