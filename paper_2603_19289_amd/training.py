@@ -325,17 +325,30 @@ class EstimatorTrainer:
     calls for plain matrix products, and what lies between them is bfloat16 too.  LayerNorm, losses and AdamW are this library's.
 
     balance_coef: weight of a balance loss over the estimator's own predictions, against its collapse on a few experts.  top_k: how
-    many experts it predicts for a token, which that loss counts."""
+    many experts it predicts for a token, which that loss counts.
+
+    masters: the float32 tables of a training to go on with, as `masters()` gave them, to which weights are set; used in place where
+    weights are bfloat16.  Together with the moments (states, steps and seed, as AdamW takes them) the steps go on as if they had
+    never stopped; from bfloat16 weights alone they go on from rounded tables."""
 
     NAMES = ("proj", "layer_emb", "ffn_in", "ffn_out", "ln_gain", "ln_bias", "head")
 
     def __init__(self, weights: dict, *, lr: float = 1e-3, balance_coef: float = 0.0, top_k: Optional[int] = None, ln_eps: float = 1e-5,
-                 device="cuda:0", **adamw):
+                 masters: Optional[dict] = None, device="cuda:0", **adamw):
         from .engine import _np_to_torch_storage
         to = lambda v: v if isinstance(v, torch.Tensor) else _np_to_torch_storage(v).to(device)  # noqa: E731
         self.weights = {k: to(weights[k]) for k in self.NAMES}
         self.dtype = self.weights["proj"].dtype
-        masters = {k: (v if v.dtype == torch.float32 else v.float()) for k, v in self.weights.items()}
+        if masters is None:
+            masters = {k: (v if v.dtype == torch.float32 else v.float()) for k, v in self.weights.items()}
+        else:
+            masters = {k: to(masters[k]) for k in self.NAMES}
+            if any(m.dtype != torch.float32 or m.shape != self.weights[k].shape for k, m in masters.items()):
+                raise ValueError("masters must be float32 tables of the weights' shapes")
+            with torch.no_grad():
+                for k, v in self.weights.items():
+                    v.copy_(masters[k])
+            masters = {k: (v if v.dtype == torch.float32 else masters[k]) for k, v in self.weights.items()}
         self.optimizer = AdamW([masters[k] for k in self.NAMES], lr=lr, copies=[
             self.weights[k] if self.weights[k] is not masters[k] else None for k in self.NAMES], **adamw)
         if top_k is not None and not 1 <= top_k <= self.weights["head"].shape[0]:
@@ -396,6 +409,10 @@ class EstimatorTrainer:
         out, g = self.gradients(layers, signal, teacher, ids, valid)
         self.optimizer.step([g[k].float() for k in self.NAMES], grad_scale=grad_scale)
         return out
+
+    def masters(self) -> dict:
+        """The float32 tables that are trained: weights itself where those are float32."""
+        return dict(zip(self.NAMES, self.optimizer.params))
 
     def numpy_weights(self) -> dict:
         """The weights in storage format, for a new Engine or a file (bfloat16 as uint16 bit patterns)."""

@@ -198,3 +198,34 @@ def test_the_balance_term_is_of_the_estimators_own_choices(fallen):
     for bad in (0, 13):
         with pytest.raises(ValueError):
             T.EstimatorTrainer(est, top_k=bad)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("state", ["f32", "f8"])
+def test_training_that_is_resumed_goes_on_as_if_it_had_not_stopped(dtype, state):
+    """Masters, moments and the step's number through host memory into a new trainer: the bits of the one that went on."""
+    from paper_2603_19289_amd import training as T
+    wl = small_workload(name="training", n_layers=5, hidden=264, n_experts=12, top_k=3, inter=200, dtype=dtype, batch=1, tokens=1, slots=6, seed=5)
+    est = W.make_estimator(wl, m=3, n=2)
+    steps = [tuple(t.cuda() for t in batch(wl, 3, 37, s)) for s in range(4)]
+    whole = T.EstimatorTrainer(est, lr=1e-3, state=state, seed=4)
+    for signal, teacher, _, valid in steps[:2]:
+        whole.step([3, 0, 2], signal, teacher, valid=valid)
+    saved = {k: t.cpu().clone() for k, t in whole.masters().items()}
+    moments = {k: [t.cpu().clone() for t in ts] for k, ts in whole.optimizer.states().items()}
+    weights, number = whole.numpy_weights(), whole.optimizer.steps
+    for signal, teacher, _, valid in steps[2:]:
+        whole.step([3, 0, 2], signal, teacher, valid=valid)
+    resumed = T.EstimatorTrainer(weights, lr=1e-3, state=state, seed=4, masters={k: t.cuda() for k, t in saved.items()},
+                                 states={k: [t.cuda() for t in ts] for k, ts in moments.items()}, steps=number)
+    assert all(np.array_equal(weights[k], v) for k, v in resumed.numpy_weights().items())
+    for signal, teacher, _, valid in steps[2:]:
+        resumed.step([3, 0, 2], signal, teacher, valid=valid)
+    for a, b in ((whole.masters(), resumed.masters()), (whole.weights, resumed.weights)):
+        assert all(torch.equal(a[k], b[k]) for k in NAMES)
+    for k, ts in whole.optimizer.states().items():
+        assert all(torch.equal(a, b) for a, b in zip(ts, resumed.optimizer.states()[k]))
+    with pytest.raises(ValueError):
+        T.EstimatorTrainer(est, masters={**{k: t.cuda() for k, t in saved.items()}, "head": saved["head"][:, 1:].cuda()})
+    with pytest.raises(ValueError):
+        T.EstimatorTrainer(est, masters={k: t.cuda().to(torch.float16) for k, t in saved.items()})
