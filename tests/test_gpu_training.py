@@ -445,6 +445,175 @@ def test_losses_strided_odd_and_in_place(experts, rows):
     assert not wide_s[:, :3].any() and not wide_s[:, 3 + experts:].any()
 
 
+# ------------------------------------------------------------------------------------------------ long walks
+def constant(source, name):
+    """A number of a kernel file, which says how many rows a launch takes at a time."""
+    import os
+    import re
+
+    from paper_2603_19289_amd import moe_spec as M
+    text = open(os.path.join(os.path.dirname(M.__file__), "csrc", source)).read()
+    return int(re.search(rf"constexpr int [^;]*\b{name} = (\d+)", text).group(1))
+
+
+def norm_lanes(cols, dtype):
+    """Lanes of a LayerNorm row and 16-byte chunks of a lane."""
+    per = 4 if dtype == "f32" else 8
+    for lanes in (8, 16, 32, 64):
+        if -(-cols // per) <= lanes:
+            return lanes, 1
+    return next(n for n, most in ((64, 1024), (128, 2048), (256, 4096), (512, 8192)) if cols <= most), 16 // per
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(140003, 40), (40000, 250), (12500, 600), (12500, 720), (6200, 1500), (3100, 4096), (3101, 2880), (1600, 8191), (1600, 8192)])
+def test_layernorm_forward_walks_over_many_rows(rows, cols, dtype):
+    """Three rows or more for each place of the launch, so that rows which were fetched ahead and sums in either place of LDS follow one
+    another; also over its input, between odd strides."""
+    from paper_2603_19289_amd import training as T
+    lanes, chunks = norm_lanes(cols, dtype)
+    assert rows > 2 * (2 if chunks == 1 else 1) * constant("train_norm.hip", "kForwardWaves") * 64 // lanes
+    x, _, gain, bias = ln_inputs(rows, cols, dtype, rows + cols, offset=0.5)
+    dx, dg, db = on_gpu(x), on_gpu(gain), on_gpu(bias)
+    got = T.layernorm_forward(dx, dg, db, 1e-5)
+    ln_forward_checks(x, gain, bias, 1e-5, got, dtype, f"{rows}x{cols}")
+    wide = torch.full((rows, cols + 3), 9.0, dtype=TYPES[dtype], device="cuda")
+    wide[:, 1:1 + cols] = dx
+    again = T.layernorm_forward(wide[:, 1:1 + cols], dg, db, 1e-5, out=wide[:, 1:1 + cols])
+    for a, b in zip(got, again):
+        assert torch.equal(a, b)
+    assert (wide[:, 0] == 9.0).all() and (wide[:, 1 + cols:] == 9.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(70001, 60), (17000, 200), (7000, 720), (1030, 1025), (1500, 2047), (3300, 2048), (1100, 2880), (1700, 4096),
+                                       (1100, 4101), (600, 8192), (1300, 8191)])
+def test_layernorm_backward_through_the_workspace(rows, cols, dtype):
+    """Rows of one to eight wavefronts, ragged and whole, whose column sums go through the workspace; either weight's gradient alone, and
+    dx alone, have the same bits.  Bounds as above: a lane adds up at most rows / 256 + 1 rows."""
+    from paper_2603_19289_amd import moe_spec as M
+    from paper_2603_19289_amd import training as T
+    need = M.moe_spec_layernorm_backward_workspace_bytes(rows, cols)
+    assert need > 0
+    x, dy, gain, _ = ln_inputs(rows, cols, dtype, rows * 3 + cols)
+    xd, d = x.double(), dy.double()
+    mean = xd.mean(1).float()
+    rstd = (1.0 / torch.sqrt((xd - mean.double()[:, None]).square().mean(1) + 1e-5)).float()
+    args = [on_gpu(t) for t in (dy, x, mean, rstd, gain)]
+    dx, dgain, dbias = T.layernorm_backward(*args)
+    r = rstd.double()[:, None]
+    h = (xd - mean.double()[:, None]) * r
+    w = d * gain.double()
+    c1, c2 = w.mean(1, keepdim=True), (w * h).mean(1, keepdim=True)
+    want = r * (w - c1 - h * c2)
+    terms = 36 * U * (w.abs().mean(1, keepdim=True) + h.abs() * (w * h).abs().mean(1, keepdim=True)) + 8 * U * (w.abs() + c1.abs() + (h * c2).abs())
+    close(dx, want, r * terms + half(TYPES[dtype]) * want.abs() * 1.01 + 2 * U * want.abs(), "dx")
+    depth = rows / 256 + 20
+    close(dgain, (d * h).sum(0), depth * U * (d * h).abs().sum(0), "dgain")
+    close(dbias, d.sum(0), depth * U * d.abs().sum(0), "dbias")
+    assert torch.equal(T.layernorm_backward(*args, weight_grads=False)[0], dx)
+    space = torch.empty(need, dtype=torch.uint8, device="cuda")
+    stream, number = torch.cuda.current_stream().cuda_stream, M.F32 if dtype == "f32" else M.BF16
+    for first in (True, False):
+        out = torch.full((cols + 1,), 7.0, device="cuda")
+        M.moe_spec_layernorm_backward(stream, number, args[0].data_ptr(), cols, args[1].data_ptr(), cols, rows, cols, args[2].data_ptr(),
+                                      args[3].data_ptr(), args[4].data_ptr(), None, 0, out.data_ptr() if first else None,
+                                      None if first else out.data_ptr(), space.data_ptr(), need)
+        assert torch.equal(out[:cols], dgain if first else dbias) and out[cols] == 7.0
+
+
+def padded_runs(rows, g):
+    """A mask with padding of all lengths: runs of 1 to 700 rows that count and that do not, in turn."""
+    valid, at, live = torch.zeros(rows, dtype=torch.bool), 0, True
+    while at < rows:
+        n = int(torch.randint(1, 700, (1,), generator=g))
+        valid[at:at + n] = live
+        at, live = at + n, not live
+    return valid
+
+
+WALKS = [(900007, 7), (400003, 16), (80003, 125), (60001, 256)]
+
+
+def assert_walks(rows, experts):
+    lanes = 1
+    while lanes * 8 < experts:
+        lanes *= 2
+    assert rows > 2 * constant("train_loss.hip", "kLossBlocks") * (constant("train_loss.hip", "kLossBlock") // lanes)
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("rows,experts", WALKS)
+def test_distill_loss_walks_over_many_rows(rows, experts, masked):
+    """Three rows or more for each place of the launch, with runs of padding full of NaN; the gradient over the logits, between odd strides,
+    has the same bits."""
+    from paper_2603_19289_amd import moe_spec as M
+    from paper_2603_19289_amd import training as T
+    assert_walks(rows, experts)
+    t, s, _, g = logits(rows, experts, rows + experts)
+    s = s.to(torch.bfloat16)
+    valid = padded_runs(rows, g) if masked else None
+    dirty_s, dirty_t, mask = on_gpu(s), on_gpu(t), None
+    if masked:
+        mask = on_gpu(valid)
+        dirty_s[~mask], dirty_t[~mask] = math.nan, math.nan
+    loss, grad = T.distill_loss(dirty_s, dirty_t, temperature=1.5, valid=mask)
+    want, dz, off, off_dz = kl_oracle(s, t, 1.5, valid)
+    close(loss, want, off, "loss")
+    close(grad, dz, off_dz + half(s.dtype) * dz.abs() * 1.01 + 1e-40, "gradient")
+    assert not masked or not grad[~mask].any()
+    wide = torch.zeros(rows, experts + 3, dtype=torch.bfloat16, device="cuda")
+    inner = wide[:, 1:1 + experts]
+    inner.copy_(dirty_s)
+    need = M.moe_spec_distill_loss_workspace_bytes(rows, experts)
+    space, again = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty((), device="cuda")
+    M.moe_spec_distill_loss(torch.cuda.current_stream().cuda_stream, M.BF16, inner.data_ptr(), inner.stride(0), M.F32, dirty_t.data_ptr(),
+                            experts, rows, experts, 1.5, mask.data_ptr() if masked else None, again.data_ptr(), inner.data_ptr(), inner.stride(0),
+                            space.data_ptr(), need)
+    assert torch.equal(again, loss) and torch.equal(inner, grad) and not wide[:, 0].any() and not wide[:, 1 + experts:].any()
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("rows,experts", WALKS)
+def test_balance_loss_walks_over_many_rows(rows, experts, masked):
+    """As above; the longest has rows enough for the counting workgroups to go round as well."""
+    from paper_2603_19289_amd import training as T
+    assert_walks(rows, experts)
+    assert rows != WALKS[0][0] or rows > 2 * 2 * constant("train_loss.hip", "kCountBlocks") * constant("train_loss.hip", "kCountBlock")
+    z, _, _, g = logits(rows, experts, rows + experts + 1)
+    k = min(experts, 1 + rows % 8)
+    ids = torch.rand(rows, experts, generator=g).topk(k, 1).indices.to(torch.int32)
+    valid = padded_runs(rows, g) if masked else None
+    dirty, mask = on_gpu(z), None
+    if masked:
+        mask = on_gpu(valid)
+        dirty[~mask] = math.nan
+    loss, counts, grad = T.balance_loss(dirty, on_gpu(ids), coef=0.03, valid=mask)
+    want, want_counts, dz, off, off_dz = balance_oracle(z, ids, 0.03, valid)
+    assert torch.equal(counts.cpu().long(), want_counts)
+    close(loss, want, off, "loss")
+    close(grad, dz, off_dz + U * dz.abs() * 1.01 + 1e-40, "gradient")
+    assert not masked or not grad[~mask].any()
+
+
+@pytest.mark.parametrize("k", [8, 9, 12, 15, 16])
+@pytest.mark.parametrize("rows", [1, 100, 5003, 140001])
+def test_balance_loss_of_many_choices(rows, k):
+    """More choices than eight, in one workgroup and in launches, ids close together and in wider rows at odd addresses."""
+    from paper_2603_19289_amd import training as T
+    experts = 40
+    z, _, valid, g = logits(rows, experts, rows + k)
+    ids = torch.rand(rows, experts, generator=g).topk(k, 1).indices.to(torch.int32)
+    wide = torch.full((rows, k + 5), 3, dtype=torch.int32, device="cuda")
+    wide[:, 1:1 + k] = on_gpu(ids)
+    want, want_counts, dz, off, off_dz = balance_oracle(z, ids, 0.03, valid)
+    for chosen in (on_gpu(ids), wide[:, 1:1 + k]):
+        loss, counts, grad = T.balance_loss(on_gpu(z), chosen, coef=0.03, valid=on_gpu(valid))
+        assert torch.equal(counts.cpu().long(), want_counts)
+        close(loss, want, off, "loss")
+        close(grad, dz, off_dz + U * dz.abs() * 1.01 + 1e-40, "gradient")
+
+
 # ------------------------------------------------------------------------------------------------ AdamW
 F = np.float32
 ODD1, ODD2 = 0x9E3779B1, 0x85EBCA77
@@ -875,6 +1044,47 @@ def test_a_captured_training_step_equals_an_eager_one(state):
         for a, b, c in zip(captured.held(), eager.held(), plain.held()):
             assert torch.equal(a, b) and torch.equal(a, c), replay
     assert captured.counter.item() == 5
+
+
+def test_captured_operators_of_several_launches():
+    """Sizes that take workspaces: replays on new inputs, with eager work between them, equal the eager results; two captures have
+    workspaces of their own and may run at the same time."""
+    from paper_2603_19289_amd import moe_spec as M
+    from paper_2603_19289_amd import training as T
+    x, dy, gain, bias = (on_gpu(t) for t in ln_inputs(3001, 720, "bf16", 16))
+    t, s, valid, g = logits(20001, 100, 16)
+    ids = on_gpu(torch.rand(20001, 100, generator=g).topk(9, 1).indices.to(torch.int32))
+    t, s, valid = on_gpu(t), on_gpu(s), on_gpu(valid)
+    assert M.moe_spec_layernorm_backward_workspace_bytes(3001, 720) and M.moe_spec_balance_loss_workspace_bytes(20001, 100, 9)
+
+    def every():
+        y, mean, rstd = T.layernorm_forward(x, gain, bias)
+        return (y, *T.layernorm_backward(dy, x, mean, rstd, gain), *T.distill_loss(s, t, valid=valid), *T.balance_loss(s, ids, valid=valid))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        every()
+    torch.cuda.current_stream().wait_stream(side)
+    captures = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = every()
+        captures.append((graph, out))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for replay in range(3):
+        x.add_(0.125), s.mul_(0.75)
+        valid.copy_(valid.roll(17))
+        want = every()
+        for stream, (graph, _) in zip(streams, captures):
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for _, out in captures:
+            for a, b in zip(out, want):
+                assert torch.equal(a, b), replay
 
 
 def test_operators_on_another_stream_and_two_at_once():
