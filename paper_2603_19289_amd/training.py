@@ -373,12 +373,13 @@ class EstimatorTrainer:
         if any(t is not None and t.shape[:2] != (n, tokens) for t in (teacher, ids, valid)):
             raise ValueError("teacher, ids and valid must have the layers and tokens of the signal")
         flat = lambda t: None if t is None else t.reshape(n * tokens, *t.shape[2:])  # noqa: E731
-        at = torch.as_tensor(list(layers), device=signal.device)
+        at = torch.as_tensor(list(layers), dtype=torch.long, device=signal.device)
         x, mask = flat(signal).to(self.dtype), flat(valid)
         if mask is not None:                  # chosen, not multiplied: zero times what padding holds need not be zero in a product
             _mask(mask, n * tokens, x.device)
             x = x.masked_fill((mask == 0)[:, None], 0.0)
-        u = (torch.mm(x, w["proj"].T).view(n, tokens, -1) + w["layer_emb"][at][:, None]).reshape(n * tokens, -1)
+        latent = w["proj"].shape[0]
+        u = (torch.mm(x, w["proj"].T).view(n, tokens, latent) + w["layer_emb"][at][:, None]).view(n * tokens, latent)
         h = torch.mm(u, w["ffn_in"].T)
         gate = torch.sigmoid(h)
         act = h * gate
@@ -401,7 +402,7 @@ class EstimatorTrainer:
         du = dv + torch.mm(dh, w["ffn_in"])
         g["proj"] = torch.mm(du.T, x)
         g["layer_emb"] = torch.zeros(w["layer_emb"].shape, device=signal.device)
-        g["layer_emb"][at] = du.view(n, tokens, -1).sum(1, dtype=torch.float32)
+        g["layer_emb"][at] = du.view(n, tokens, latent).sum(1, dtype=torch.float32)
         return out, g
 
     def step(self, layers, signal, teacher, ids=None, valid=None, *, grad_scale=1.0) -> dict:

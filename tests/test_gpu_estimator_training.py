@@ -229,3 +229,21 @@ def test_training_that_is_resumed_goes_on_as_if_it_had_not_stopped(dtype, state)
         T.EstimatorTrainer(est, masters={**{k: t.cuda() for k, t in saved.items()}, "head": saved["head"][:, 1:].cuda()})
     with pytest.raises(ValueError):
         T.EstimatorTrainer(est, masters={k: t.cuda().to(torch.float16) for k, t in saved.items()})
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,tokens", [(3, 0), (0, 5), (1, 1)])
+def test_batches_of_nothing_and_of_one_token(n, tokens, dtype):
+    """Without rows: losses, counts and gradients of zero; one row: finite ones."""
+    from paper_2603_19289_amd import training as T
+    wl = small_workload(name="training", n_layers=5, hidden=264, n_experts=12, top_k=3, inter=200, dtype=dtype, batch=1, tokens=1, slots=6, seed=5)
+    signal, teacher, _, valid = (t.cuda() for t in batch(wl, n, tokens, 1))
+    trainer = T.EstimatorTrainer(W.make_estimator(wl, m=3, n=2), balance_coef=0.1, top_k=3)
+    for mask in (None, valid):
+        out, grads = trainer.gradients(range(n), signal, teacher, valid=mask)
+        assert all(grads[k].shape == trainer.weights[k].shape and torch.isfinite(grads[k]).all() for k in NAMES)
+        if n * tokens == 0:
+            assert out["loss"].item() == out["balance"].item() == 0.0 and not out["counts"].any()
+            assert not any(g.any() for g in grads.values())
+    trainer.step(range(n), signal, teacher, valid=valid)
+    assert all(torch.isfinite(t).all() for t in trainer.weights.values())
