@@ -366,6 +366,7 @@ class EstimatorTrainer:
         nothing whatever it holds."""
         n, tokens, _ = signal.shape
         w = self.weights
+        layers = [int(l) for l in layers]     # a tensor's elements are no equal members of a set
         if len(set(layers)) != n or len(layers) != n or not all(0 <= l < w["layer_emb"].shape[0] for l in layers):
             raise ValueError("a layer of its own for each of the signals is needed")
         if ids is None and self.top_k is None and self.balance_coef != 0.0:
@@ -373,7 +374,7 @@ class EstimatorTrainer:
         if any(t is not None and t.shape[:2] != (n, tokens) for t in (teacher, ids, valid)):
             raise ValueError("teacher, ids and valid must have the layers and tokens of the signal")
         flat = lambda t: None if t is None else t.reshape(n * tokens, *t.shape[2:])  # noqa: E731
-        at = torch.as_tensor(list(layers), dtype=torch.long, device=signal.device)
+        at = torch.as_tensor(layers, dtype=torch.long, device=signal.device)
         x, mask = flat(signal).to(self.dtype), flat(valid)
         if mask is not None:                  # chosen, not multiplied: zero times what padding holds need not be zero in a product
             _mask(mask, n * tokens, x.device)

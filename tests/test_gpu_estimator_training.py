@@ -247,3 +247,17 @@ def test_batches_of_nothing_and_of_one_token(n, tokens, dtype):
             assert not any(g.any() for g in grads.values())
     trainer.step(range(n), signal, teacher, valid=valid)
     assert all(torch.isfinite(t).all() for t in trainer.weights.values())
+
+
+def test_layers_named_by_a_tensor():
+    """As by a list; the same one twice is refused, as only one of its gradients would be kept."""
+    from paper_2603_19289_amd import training as T
+    wl = small_workload(name="training", n_layers=5, hidden=264, n_experts=12, top_k=3, inter=200, dtype="f32", batch=1, tokens=1, slots=6, seed=5)
+    signal, teacher, _, valid = (t.cuda() for t in batch(wl, 2, 9, 1))
+    trainer = T.EstimatorTrainer(W.make_estimator(wl, m=3, n=2))
+    want = trainer.gradients([3, 0], signal, teacher, valid=valid)[1]
+    for layers in (torch.tensor([3, 0]), torch.tensor([3, 0], device="cuda"), np.array([3, 0])):
+        got = trainer.gradients(layers, signal, teacher, valid=valid)[1]
+        assert all(torch.equal(got[k], want[k]) for k in NAMES)
+        with pytest.raises(ValueError):
+            trainer.gradients(layers * 0, signal, teacher, valid=valid)
