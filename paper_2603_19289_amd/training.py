@@ -293,19 +293,19 @@ class AdamW:
             raise ValueError("32-bit moments are tensors of their own: states()")
         if m_out is None and v_out is None:
             m_out, v_out = ([torch.empty_like(p) for p in self.params] for _ in range(2))
-        if any(out is not None and len(out) != len(self.params) for out in (m_out, v_out)):
+        n = len(self.params)
+        if (m_out is not None and len(m_out) != n) or (v_out is not None and len(v_out) != n):
             raise ValueError("a tensor for each parameter is needed")
-        dtype = (m_out if m_out is not None else v_out)[0].dtype
+        outs = [*(m_out or ()), *(v_out or ())]
+        dtype = outs[0].dtype
         if dtype not in _TYPES:
             raise ValueError("moments are read as float32 or bfloat16")
-        given = [out for out in (m_out, v_out) if out is not None]
-        outs = [t for out in given for t in out]
-        self._tensors(outs, "an output", dtype, self._sizes * len(given))
+        self._tensors(outs, "an output", dtype, self._sizes * (len(outs) // n))
         self._describe(self._moments)
         self._all_whole()
-        at = (C.c_void_p * len(self._sizes) * len(given)).from_buffer(array("Q", map(_ADDRESS, outs)))
-        _queue(self.device, M.lib().moe_spec_adamw_read_moments, self._desc, len(self._desc), _TYPES[dtype],
-               at[0] if m_out is not None else None, at[-1] if v_out is not None else None)
+        at = (C.c_void_p * n * (len(outs) // n)).from_buffer(array("Q", map(_ADDRESS, outs)))
+        _queue(self.device, M.lib().moe_spec_adamw_read_moments, self._desc, n, _TYPES[dtype], at[0] if m_out is not None else None,
+               at[-1] if v_out is not None else None)
         return m_out, v_out
 
 

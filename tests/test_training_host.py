@@ -112,3 +112,20 @@ def test_adamw_tensors_are_dealt_to_launches_that_fit(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", csrc, str(src), "-o", str(exe)], check=True)
     done = subprocess.run([str(exe)], capture_output=True, text=True, timeout=120)
     assert done.returncode == 0, done.stdout[-2000:]
+
+
+def test_moments_are_read_into_the_tensors_that_are_named(monkeypatch):
+    """One list of outputs, the other or both: the addresses that the library gets, and a list of the wrong length."""
+    got = []
+    monkeypatch.setattr(T, "_queue", lambda dev, call, desc, n, dtype, m, v: got.append([None if a is None else list(a) for a in (m, v)]))
+    monkeypatch.setattr(T.AdamW, "_tensor", lambda *a: None)
+    sizes = (300, 40, 7)
+    opt = T.AdamW([torch.zeros(n) for n in sizes], lr=1e-3, state="f8")
+    m, v = ([torch.zeros(n, dtype=torch.bfloat16) for n in sizes] for _ in range(2))
+    at = lambda out: [t.data_ptr() for t in out]  # noqa: E731
+    assert opt.read_moments(m, v) == (m, v) and opt.read_moments(m) == (m, None) and opt.read_moments(v_out=tuple(v)) == (None, tuple(v))
+    new = opt.read_moments()
+    assert got == [[at(m), at(v)], [at(m), None], [None, at(v)], [at(new[0]), at(new[1])]]
+    for bad in ((m[:2], v + v[:1]), (m[:2], None), (None, [])):
+        with pytest.raises(ValueError):
+            opt.read_moments(*bad)
