@@ -1,10 +1,10 @@
 // AdamW over many tensors in as few launches as their pointers fit into.
 //   m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2;  p = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
-// Bound by memory: 24 bytes an element and the gradient with 32-bit moments, 12 with 8-bit ones (75 M elements, bf16 gradients and
-// copies: 5.4 TB/s either way, what a large copy reaches); some 75 vector instructions an element with 8-bit moments, which is
-// two thirds of that time.  Eight elements a thread, 2048 a workgroup; which tensor a workgroup works on it finds in the
+// Bound by memory: 24 bytes an element and the gradient with 32-bit moments, 12 with 8-bit ones.  75 M elements, bf16 gradients and
+// copies: 393 us, 5.4 TB/s, what a large copy reaches, and 243 us, 5.0 TB/s: 96 vector instructions an element with 8-bit moments, whose
+// issue is four fifths of that time.  Eight elements a thread, 2048 a workgroup; which tensor a workgroup works on it finds in the
 // launch's argument block, so that nothing has to be copied to the device first and a captured launch carries its tensors with
-// it: 40 of them, which is what 4 KB hold.
+// it: 40 of them, 3 KB of the 4 KB that an argument block may have (55 would fit; not compared).
 //
 // 8-bit moments: a run of 128 elements lies in 16 lanes, whose largest magnitude four exchanges find.  With X its biased
 // exponent, |m| 2^(14-X) is a float whose upper bits are the code (exponent fields 0 to 14, denormals included); adding 16

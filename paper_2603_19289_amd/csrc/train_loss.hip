@@ -9,8 +9,9 @@
 //
 // Bound by memory: logits are read once, gradients written once; the gradient's factors (n, f) come first, from the mask and
 // the ids, which are a few per cent of the bytes.  A row lies in the registers of a group of 1 to 32 lanes, eight
-// values each.  Exponentials go through the hardware's 2^x: its argument x log2 e is rounded to float, which moves exp(x) by
-// |x| 2^-24 relative, so by at most 0.37 * 2^-24 of the row's largest term.  One reciprocal and one logarithm a row are the
+// values each.  Exponentials go through the hardware's 2^x (a unit in its last place).  Its argument, x log2 e with x a logit less
+// the row's largest over tau, has four roundings: the difference, log2 e, its quotient by tau and their product.  They move exp(x) by up to
+// 4 |x| 2^-24 relative, so by at most 4 * 0.37 * 2^-24 of the row's largest term.  One reciprocal and one logarithm a row are the
 // hardware's too (a unit in the last place).  Row results are added up in double.
 #include "train_common.h"
 
@@ -53,9 +54,10 @@ struct Max { __device__ __forceinline__ float operator()(float a, float b) const
 
 // Adds the choices of the valid rows from `row` on, `step` apart, to hist, and the number of those rows to hist[bins].  A thread
 // takes two rows at a time, whose loads go out together: without a condition (behind the end: the last row's), so that none is
-// waited for before the others are out.  (Loads behind conditions: 10.7 us for 131072 rows x 8 choices, these 6.7.)  A compute unit
-// streams some 30 GB/s, so more workgroups count faster, and the loss kernel's add up what more of them left: the balance loss of
-// 131072 rows takes 27.9 us with 32 of 1024 threads, 23.3 with 64, 22.9 with 128, 22.4 with 128 of 512 threads, 22.6 with 256.
+// waited for before the others are out.  (Loads behind conditions: 10.7 us for 131072 rows x 8 choices, these 6.7.)  More
+// workgroups count faster, and the loss kernel's add up what more of them left: the balance loss of 131072 rows takes 27.9 us with 32 of
+// 1024 threads, 23.3 with 64, 22.9 with 128, 22.4 with 128 of 512 threads, 22.6 with 256.  The launch takes 5 us for 4.3 MB, of which a
+// bare launch is some 2; what the other 3 are is not known (not contention: counters for groups of lanes changed nothing).
 template <int UNITS>                    // four choices each
 __device__ __forceinline__ int count_rows(const LossArgs &a, int64_t row, int64_t step, int *hist) {
   constexpr int kAhead = 2;

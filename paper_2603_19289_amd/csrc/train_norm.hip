@@ -3,7 +3,7 @@
 //   w = dy * gain, h = (x - mean) * rstd:  dx = rstd * (w - mean(w) - h * mean(w h)),  dgain = sum_rows dy h,  dbias = sum_rows dy
 // Both are bound by memory: x is read once and y written once, dy and x read once and dx written once.  A row stays in
 // registers between its loads and its stores, so the variance is taken about the mean that is already known (no sums of
-// squares that cancel).
+// squares that cancel).  Means are sums times 1 / cols, rounded to float: one rounding more than a division.
 //
 // Lanes: a row has as many as there are 16-byte chunks in it, a power of two up to 64 (several rows share a wavefront), and
 // beyond one chunk each up to 16 values a lane in up to eight wavefronts.  16 values keep the gains, the backward pass's two
@@ -393,7 +393,9 @@ hipError_t forward(hipStream_t stream, NormForwardArgs &a) {
 
 // Few rows: the column sums are formed beside dx, from dy and x once more, which then come out of a cache.  Measured in us, beside dx /
 // in a launch of its own, bf16: 16 x 512 2.3 / 4.8, 256 x 512 2.8 / 5.2, 512 x 2048 6.0 / 8.8, 512 x 8192 18.4 / 18.8, 1024 x 64 4.2 / 5.7,
-// 1024 x 2048 9.8 / 13.2, 1024 x 8192 32 / 20, 2048 x 64 6.4 / 5.7, 2048 x 512 12.0 / 6.1.
+// 1024 x 2048 9.8 / 13.2, 1024 x 4096 15.1 / 18.1, 1024 x 8192 32 / 20, 2048 x 64 6.4 / 5.7, 2048 x 512 12.0 / 6.1.  float32 reads twice as much:
+// 16 x 512 2.7 / 5.5, 256 x 512 2.9 / 5.7, 512 x 2048 6.5 / 10.1, 1024 x 1024 8.2 / 8.0, 1024 x 2048 11.2 / 14.5, but 1024 x 4096 19.1 / 16.5 and
+// 512 x 8192 21.4 / 17.0: between 2 M and 4 M values the rule costs it up to a quarter.
 bool columns_beside(int64_t rows, int cols) { return rows <= 1024 && rows * cols <= (4 << 20); }
 
 template <typename WT>

@@ -322,7 +322,10 @@ class EstimatorTrainer:
     given an Engine's own (`engine.est`), its predictions follow the training, as its context reads the same memory; the caller
     keeps the engine's stream and the training stream apart in time.  bfloat16 tables have float32 masters here and are the
     copies that AdamW writes; products then take bfloat16 operands and add up in float32, in the library that torch
-    calls for plain matrix products, and what lies between them is bfloat16 too.  LayerNorm, losses and AdamW are this library's.
+    calls for plain matrix products, and what lies between them is bfloat16 too: the feed-forward's values and all gradients that pass
+    through it, each table's gradient (widened for AdamW, which takes one type a call), the two losses' gradients before and after they are
+    added, and the logits, so that choices between nearly equal ones may differ from an engine's, which are float32.  LayerNorm, losses and
+    AdamW are this library's.
 
     balance_coef: weight of a balance loss over the estimator's own predictions, against its collapse on a few experts.  top_k: how
     many experts it predicts for a token, which that loss counts.
