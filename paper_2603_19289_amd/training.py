@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 from array import array
-from operator import attrgetter
+from operator import attrgetter, index
 from typing import List, Optional, Sequence
 
 import torch
@@ -369,7 +369,7 @@ class EstimatorTrainer:
         nothing whatever it holds."""
         n, tokens, _ = signal.shape
         w = self.weights
-        layers = [int(l) for l in layers]     # a tensor's elements are no equal members of a set
+        layers = [index(l) for l in layers]     # a tensor's elements are no equal members of a set
         if len(set(layers)) != n or len(layers) != n or not all(0 <= l < w["layer_emb"].shape[0] for l in layers):
             raise ValueError("a layer of its own for each of the signals is needed")
         if ids is None and self.top_k is None and self.balance_coef != 0.0:

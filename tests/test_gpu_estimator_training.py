@@ -261,3 +261,5 @@ def test_layers_named_by_a_tensor():
         assert all(torch.equal(got[k], want[k]) for k in NAMES)
         with pytest.raises(ValueError):
             trainer.gradients(layers * 0, signal, teacher, valid=valid)
+    with pytest.raises(TypeError):
+        trainer.gradients([0.5, 1.5], signal, teacher, valid=valid)
