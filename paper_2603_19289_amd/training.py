@@ -381,7 +381,7 @@ class EstimatorTrainer:
         x, mask = flat(signal).to(self.dtype), flat(valid)
         if mask is not None:                  # chosen, not multiplied: zero times what padding holds need not be zero in a product
             _mask(mask, n * tokens, x.device)
-            x = x.masked_fill((mask == 0)[:, None], 0.0)
+            x = torch.where(mask.bool()[:, None], x, 0.0)
         latent = w["proj"].shape[0]
         u = (torch.mm(x, w["proj"].T).view(n, tokens, latent) + w["layer_emb"][at][:, None]).view(n * tokens, latent)
         h = torch.mm(u, w["ffn_in"].T)
