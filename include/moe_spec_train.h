@@ -39,6 +39,8 @@ extern "C" {
 #define MOE_SPEC_TRAIN_MAX_COLS 8192          /* widest row of LayerNorm */
 #define MOE_SPEC_TRAIN_MAX_ROWS 0x7fffffff
 #define MOE_SPEC_TRAIN_MAX_TENSORS 65536      /* of one AdamW call */
+#define MOE_SPEC_TRAIN_MAX_FEATURES 65536     /* rows or columns of an expert's matrix, of a matrix that is orthogonalised */
+#define MOE_SPEC_MUON_MAX_ELEMENTS 4294967296 /* of one stack of matrices */
 #define MOE_SPEC_ADAMW_MAX_ELEMENTS 34359736320  /* of one of its tensors: what the threads of a launch, below 2^32, take */
 
 /* LayerNorm (Appendix A: the estimator's last step before its head).  x, y dev [rows, cols]; gain, bias dev [cols] float or
@@ -128,6 +130,71 @@ int moe_spec_adamw_step(void *stream, const moe_spec_adamw_tensor *tensors, int 
  * all from 2^-120 on exactly), host arrays of n_tensors pointers; either array may be NULL. */
 int moe_spec_adamw_read_moments(void *stream, const moe_spec_adamw_tensor *tensors, int n_tensors, int out_dtype,
                                 void *const *m_out, void *const *v_out);
+
+/* Products of rows that are sorted by expert with the experts' matrices, for training a layer's experts (and for serving them
+ * where all weights are on the device).  Group e is the rows from the largest of ends[0 .. e) to the largest of ends[0 .. e],
+ * each taken between 0 and rows: ends is usually the running sum of the experts' row counts, a group may be empty, and
+ * whatever ends holds, nothing outside of the matrices is touched.
+ *   y_r = W_e x_r      transpose = 0: x dev [rows, k] -> y dev [rows, n]
+ *   y_r = W_e^T x_r    transpose = 1: x dev [rows, n] -> y dev [rows, k], the gradient with respect to the other form's x
+ * w dev: n_experts matrices [n, k] (1 <= n_experts <= MOE_SPEC_MAX_EXPERTS), w_stride elements between their rows and
+ * w_expert_stride between matrices (gate and up rows of expert blocks are one such matrix, as the pool has them); x and w of type dtype, y of
+ * out_dtype.  ends dev [n_experts].  Rows of y behind the last group are set to zero.  Sums are float, in an order that sizes and
+ * groups alone decide. */
+int moe_spec_grouped_product(void *stream, int dtype, const void *x, int64_t x_stride, int64_t rows, const void *w, int64_t w_stride,
+                             int64_t w_expert_stride, int n_experts, int n, int k, const int32_t *ends, int transpose, int out_dtype,
+                             void *y, int64_t y_stride);
+
+/* Gradient of the matrices: dw dev, n_experts matrices [n, k] of out_dtype, dw_e = sum over the group's rows of dy_r x_r^T, written, not
+ * added to; zeros for an expert without rows.  dy dev [rows, n], x dev [rows, k], groups as above. */
+int moe_spec_grouped_weight_grad(void *stream, int dtype, const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int64_t rows,
+                                 int n_experts, int n, int k, const int32_t *ends, int out_dtype, void *dw, int64_t dw_stride,
+                                 int64_t dw_expert_stride);
+
+/* The experts' gated activation: a dev [rows, 2 cols] holds gate and up, h dev [rows, cols] = weight_r silu(gate) up.
+ * weight dev [rows] float or NULL (ones): the mixing weight of each row, if it is to be applied here.
+ * Backward: da dev [rows, 2 cols]; dweight dev [rows] float or NULL. */
+int moe_spec_swiglu_forward(void *stream, int dtype, const void *a, int64_t a_stride, int64_t rows, int cols, const float *weight,
+                            void *h, int64_t h_stride);
+int moe_spec_swiglu_backward(void *stream, int dtype, const void *dh, int64_t dh_stride, const void *a, int64_t a_stride, int64_t rows,
+                             int cols, const float *weight, void *da, int64_t da_stride, float *dweight);
+
+/* Orthogonalised matrices.  X = g / |g|_F (Frobenius norm, in double), then `iterations` times
+ *   X <- a X + (b A + c A A) X,  A = X X^T (or X^T X, where that is smaller)
+ * with (a, b, c) = coefficients, which pushes every singular value towards one; 3.4445, -4.7750, 2.0315 and five iterations bring
+ * those above a hundredth of the norm to between 0.7 and 1.2.  g dev: count matrices [rows, cols] of type dtype, g_stride elements
+ * between rows, g_matrix_stride between matrices; out dev, the same in bfloat16.  A matrix of zeros stays one; one that holds
+ * what is not finite becomes NaN, and no other.  The iterates are float16: the result is off by 0.1 to 0.3 % of its norm where singular
+ * values differ by less than a hundred, and a direction whose singular value is below some 2^-12 of the norm is mostly rounding. */
+size_t moe_spec_orthogonalise_workspace_bytes(int64_t count, int rows, int cols);
+int moe_spec_orthogonalise(void *stream, int dtype, const void *g, int64_t g_matrix_stride, int64_t g_stride, int64_t count, int rows,
+                           int cols, const double *coefficients, int iterations, void *out, int64_t out_matrix_stride, int64_t out_stride,
+                           void *workspace, size_t workspace_bytes);
+
+/* A step for matrices with that update (Muon).  With g = grad_scale * grad and O the function above, without its last rounding:
+ *   m = momentum m + g;  u = g + momentum m (nesterov) or m
+ *   p = p (1 - lr weight_decay) - lr update_rms sqrt(max(rows, cols)) O(u)
+ * so that an update's root mean square is about lr update_rms whatever the size (0.2 is what AdamW's usually is). */
+typedef struct {
+  float *p;                       /* dev [count, rows, cols], updated */
+  const void *grad;               /* dev, the same in grad_dtype */
+  float *m;                       /* dev, the same; updated; zeros before the first step */
+  void *copy;                     /* dev, the same in bfloat16, or NULL */
+  int64_t count;
+  int32_t rows, cols;
+} moe_spec_muon_tensor;
+
+typedef struct {
+  double lr, momentum, weight_decay, update_rms, grad_scale;
+  double coefficients[3];
+  const float *grad_scale_dev;    /* dev, or NULL: a second factor of the gradients */
+  int32_t iterations, nesterov, grad_dtype;
+} moe_spec_muon_config;
+
+/* tensors: host [n_tensors], read before the call returns; no two of them may share memory that is updated. */
+size_t moe_spec_muon_workspace_bytes(const moe_spec_muon_tensor *tensors, int n_tensors);
+int moe_spec_muon_step(void *stream, const moe_spec_muon_tensor *tensors, int n_tensors, const moe_spec_muon_config *cfg, void *workspace,
+                       size_t workspace_bytes);
 
 /* Text of the calling thread's last failure among the calls above. */
 const char *moe_spec_train_last_error(void);

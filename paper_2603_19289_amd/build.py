@@ -8,7 +8,7 @@ LIB = os.path.join(HERE, "libmoe_spec.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["csrc/moe_spec.cpp", "csrc/route_kernels.hip", "csrc/fused_kernels.hip", "csrc/expert_kernels.hip",
            "csrc/estimator_kernels.hip", "csrc/synth.hip", "csrc/train.cpp", "csrc/train_norm.hip", "csrc/train_loss.hip",
-           "csrc/train_adamw.hip"]
+           "csrc/train_adamw.hip", "csrc/train_grouped.hip", "csrc/train_gated.hip", "csrc/train_muon.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]

@@ -1,0 +1,293 @@
+// Products of rows grouped by expert with the experts' matrices:
+//   y_r = W_e x_r, or W_e^T x_r,  for the rows r of expert e        (grouped_kernel: tiles of rows of one expert each)
+//   dW_e = sum_{r of e} dy_r x_r^T                                  (weight_grad_kernel: tiles of one expert's matrix each)
+// Which expert a workgroup works for it finds in `ends` itself, a wavefront's scan over at most 256 words, so that nothing has to be known on
+// the host and a captured call follows other groups.
+#include "f32_tiles.h"
+
+namespace moe_spec {
+namespace {
+
+// ---- groups -------------------------------------------------------------------------------------------------
+// Group e is the rows [max of ends before e, max of ends up to e), both within [0, rows]: whatever ends holds, groups do not overlap and
+// lie inside the matrix.
+__device__ __forceinline__ int wave_max(int v) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v = max(v, __shfl_xor(v, d));
+  return v;
+}
+
+struct RowTile {
+  int expert;                  // n_experts: rows behind the last group; -1: none
+  int row0, rows;              // of all rows
+  int tile_n;
+};
+
+// Which tile of at most BM rows of one expert, and of which columns, this workgroup takes.  Consecutive workgroups go to the eight
+// dies in turn; each die gets a run of tiles, columns first, so that those that read the same rows and weights share an L2.
+template <int BM>
+__device__ __forceinline__ RowTile row_tile(const int32_t *ends, int n_experts, int rows, int tiles_n) {
+  const int lane = threadIdx.x & 63;
+  int end[4], count[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int e = 4 * lane + i;
+    end[i] = e < n_experts ? min(max(ends[e], 0), rows) : 0;
+    if (i) end[i] = max(end[i], end[i - 1]);
+  }
+  int before = end[3];                                   // inclusive running maximum over the lanes, then exclusive
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int v = __shfl_up(before, d);
+    if (lane >= d) before = max(before, v);
+  }
+  const int last = __shfl(before, 63);
+  before = __shfl_up(before, 1);
+  if (lane == 0) before = 0;
+  int sum = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    end[i] = max(end[i], before);
+    count[i] = (end[i] - (i ? end[i - 1] : before) + BM - 1) / BM;
+    sum += count[i];
+  }
+  int upto = sum;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int v = __shfl_up(upto, d);
+    if (lane >= d) upto += v;
+  }
+  const int tiles = __shfl(upto, 63), all = tiles + (rows - last + BM - 1) / BM;
+  const int64_t total = int64_t(all) * tiles_n, share = (total + 7) / 8, slot = blockIdx.x / 8, logical = blockIdx.x % 8 * share + slot;
+  RowTile t{-1, 0, 0, 0};
+  if (slot >= share || logical >= total) return t;
+  const int at = int(logical / tiles_n);
+  t.tile_n = int(logical % tiles_n);
+  if (at >= tiles) {
+    t.expert = n_experts;
+    t.row0 = last + (at - tiles) * BM;
+    t.rows = min(BM, rows - t.row0);
+    return t;
+  }
+  const int who = __popcll(__ballot(upto <= at));        // the lane whose experts have it
+  int from = upto - sum, expert = -1, row0 = 0, n = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int begin = i ? end[i - 1] : before;
+    if (at >= from && at < from + count[i]) {
+      expert = 4 * lane + i;
+      row0 = begin + (at - from) * BM;
+      n = min(BM, end[i] - row0);
+    }
+    from += count[i];
+  }
+  t.expert = __builtin_amdgcn_readfirstlane(__shfl(expert, who));
+  t.row0 = __builtin_amdgcn_readfirstlane(__shfl(row0, who));
+  t.rows = __builtin_amdgcn_readfirstlane(__shfl(n, who));
+  return t;
+}
+
+// ---- y = x W^T, y = x W ----------------------------------------------------------------------------------------
+struct GroupedArgs {
+  const void *x, *w;
+  void *y;
+  const int32_t *ends;
+  int64_t x_stride, w_stride, w_expert, y_stride, k;
+  int rows, n_experts, n, tiles_n, out_bf16;
+};
+
+// A wavefront's part of a tile into a row-major matrix.
+template <typename OT, int FM, int FN>
+__device__ __forceinline__ void store_tile(OT *p, int64_t stride, const f32x4_t (&acc)[FM][FN], int row, int col, int rows, int cols) {
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int f = 0; f < FM; ++f) {
+    const int r = row + 16 * f + i;
+    if (r >= rows) continue;
+    OT *q = p + int64_t(r) * stride;
+#pragma unroll
+    for (int h = 0; h < FN; ++h) {
+      const int c = col + 16 * h + 4 * g;
+      store4(q + c, acc[f][h], cols - c);
+    }
+  }
+}
+
+template <typename P, int BM, int BN, int WM, int WN, typename Elem>
+__device__ __forceinline__ void grouped_tile(const GroupedArgs &a, char *lds, bool w_imajor) {
+  const RowTile t = row_tile<BM>(a.ends, a.n_experts, a.rows, a.tiles_n);
+  if (t.expert < 0) return;
+  const int col0 = t.tile_n * BN, cols = min(BN, a.n - col0), wave = threadIdx.x >> 6;
+  P p;
+  const bool behind = t.expert == a.n_experts;
+  const Elem *w = static_cast<const Elem *>(a.w) + (behind ? 0 : t.expert * a.w_expert) + (w_imajor ? int64_t(col0) : col0 * a.w_stride);
+  p.run(lds, static_cast<const Elem *>(a.x) + t.row0 * a.x_stride, a.x_stride, t.rows, w, a.w_stride, cols, behind ? 0 : a.k);
+  const int row = wave / WN * (BM / WM), col = wave % WN * (BN / WN);
+  const int64_t at = t.row0 * a.y_stride + col0;
+  if (a.out_bf16) store_tile(static_cast<uint16_t *>(a.y) + at, a.y_stride, p.acc, row, col, t.rows, cols);
+  else store_tile(static_cast<float *>(a.y) + at, a.y_stride, p.acc, row, col, t.rows, cols);
+}
+
+template <int BM, int BN, int WM, int WN, bool W_IMAJOR, bool WHOLE16>
+__global__ __launch_bounds__(WM *WN * 64) void grouped_kernel(const GroupedArgs a) {
+  using P = TileProduct<Bf16, BM, BN, WM, WN, false, W_IMAJOR, WHOLE16>;
+  __shared__ __attribute__((aligned(16))) char lds[P::kLds];
+  grouped_tile<P, BM, BN, WM, WN, uint16_t>(a, lds, W_IMAJOR);
+}
+
+template <int BM, int BN, int WM, int WN, bool W_IMAJOR>
+__global__ __launch_bounds__(WM *WN * 64) void grouped_f32_kernel(const GroupedArgs a) {
+  using P = TileProductF32<BM, BN, WM, WN, false, W_IMAJOR>;
+  __shared__ __attribute__((aligned(16))) char lds[P::kLds];
+  grouped_tile<P, BM, BN, WM, WN, float>(a, lds, W_IMAJOR);
+}
+
+// ---- dW = dy^T x -------------------------------------------------------------------------------------------------
+struct WeightGradArgs {
+  const void *dy, *x;
+  void *dw;
+  const int32_t *ends;
+  int64_t dy_stride, x_stride, dw_stride, dw_expert;
+  int rows, n_experts, n, k, tiles_n, tiles_k, out_bf16;
+};
+
+template <typename P, int BM, int BN, int WM, int WN, typename Elem>
+__device__ __forceinline__ void weight_grad_tile(const WeightGradArgs &a, char *lds) {
+  const int per = a.tiles_n * a.tiles_k;
+  const int64_t total = int64_t(per) * a.n_experts, share = (total + 7) / 8, slot = blockIdx.x / 8, logical = blockIdx.x % 8 * share + slot;
+  if (slot >= share || logical >= total) return;
+  const int expert = int(logical / per), tile = int(logical % per), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = 0;
+  for (int e = lane; e < expert; e += 64) before = max(before, a.ends[e]);
+  const int begin = __builtin_amdgcn_readfirstlane(min(wave_max(before), a.rows));
+  const int end = __builtin_amdgcn_readfirstlane(min(max(a.ends[expert], begin), a.rows));
+  const int row0 = tile / a.tiles_k * BM, col0 = tile % a.tiles_k * BN, rows = min(BM, a.n - row0), cols = min(BN, a.k - col0);
+  P p;
+  p.run(lds, static_cast<const Elem *>(a.dy) + begin * a.dy_stride + row0, a.dy_stride, rows,
+        static_cast<const Elem *>(a.x) + begin * a.x_stride + col0, a.x_stride, cols, end - begin);
+  const int row = wave / WN * (BM / WM), col = wave % WN * (BN / WN);
+  const int64_t at = expert * a.dw_expert + row0 * a.dw_stride + col0;
+  if (a.out_bf16) store_tile(static_cast<uint16_t *>(a.dw) + at, a.dw_stride, p.acc, row, col, rows, cols);
+  else store_tile(static_cast<float *>(a.dw) + at, a.dw_stride, p.acc, row, col, rows, cols);
+}
+
+template <int BM, int BN, int WM, int WN, bool WHOLE16>
+__global__ __launch_bounds__(WM *WN * 64) void weight_grad_kernel(const WeightGradArgs a) {
+  using P = TileProduct<Bf16, BM, BN, WM, WN, true, true, WHOLE16>;
+  __shared__ __attribute__((aligned(16))) char lds[P::kLds];
+  weight_grad_tile<P, BM, BN, WM, WN, uint16_t>(a, lds);
+}
+
+template <int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN * 64) void weight_grad_f32_kernel(const WeightGradArgs a) {
+  using P = TileProductF32<BM, BN, WM, WN, true, true>;
+  __shared__ __attribute__((aligned(16))) char lds[P::kLds];
+  weight_grad_tile<P, BM, BN, WM, WN, float>(a, lds);
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------
+constexpr int64_t kMostExpertStride = int64_t(1) << 40;
+inline int64_t tiles_of(int64_t n, int tile) { return (n + tile - 1) / tile; }
+inline bool whole16(const void *p, int64_t stride) { return !misaligned(p, 16) && stride % 8 == 0; }
+
+// Workgroups of a launch of `threads` each, or 0 where a launch cannot have so many.
+inline unsigned grid_of(int64_t tiles, int threads) {
+  const int64_t grid = (tiles + 7) / 8 * 8;
+  return grid * threads < (int64_t(1) << 32) ? unsigned(grid) : 0;
+}
+
+// Most tiles of BM rows that any groups of these rows come to: one begun per group and the rows behind them.
+inline int64_t row_tiles(int64_t rows, int n_experts, int tile) {
+  const int64_t most = rows / tile + n_experts + 1;
+  return most < rows ? most : rows;
+}
+
+const char *sizes_fault(int64_t rows, int n_experts, int n, int k) {
+  if (rows < 0 || rows > MOE_SPEC_TRAIN_MAX_ROWS) return "rows must be between 0 and 2^31 - 1";
+  if (n_experts < 1 || n_experts > MOE_SPEC_MAX_EXPERTS) return "n_experts must be between 1 and 256";
+  if (n < 1 || n > MOE_SPEC_TRAIN_MAX_FEATURES || k < 1 || k > MOE_SPEC_TRAIN_MAX_FEATURES) return "n and k must be between 1 and 65536";
+  return nullptr;
+}
+
+// A kernel and the tile that it takes.
+template <typename Args>
+struct Choice {
+  void (*kernel)(Args);
+  int bm, bn, threads;
+};
+template <int BM, int BN, int WM, int WN, bool W_IMAJOR, bool WHOLE16>
+Choice<GroupedArgs> grouped_choice() { return {grouped_kernel<BM, BN, WM, WN, W_IMAJOR, WHOLE16>, BM, BN, WM * WN * 64}; }
+template <int BM, int BN, int WM, int WN, bool W_IMAJOR>
+Choice<GroupedArgs> grouped_f32_choice() { return {grouped_f32_kernel<BM, BN, WM, WN, W_IMAJOR>, BM, BN, WM * WN * 64}; }
+
+template <bool W_IMAJOR, bool WHOLE16>
+Choice<GroupedArgs> choose_grouped(const GroupedArgs &) { return grouped_choice<128, 128, 2, 2, W_IMAJOR, WHOLE16>(); }
+
+}  // namespace
+}  // namespace moe_spec
+
+using namespace moe_spec;
+
+extern "C" int moe_spec_grouped_product(void *stream, int dtype, const void *x, int64_t x_stride, int64_t rows, const void *w, int64_t w_stride,
+                                        int64_t w_expert_stride, int n_experts, int n, int k, const int32_t *ends, int transpose,
+                                        int out_dtype, void *y, int64_t y_stride) {
+  if (!known_type(dtype)) return train_fail(MOE_SPEC_EINVAL, "grouped_product: unknown dtype %d", dtype);
+  if (!known_type(out_dtype)) return train_fail(MOE_SPEC_EINVAL, "grouped_product: unknown out_dtype %d", out_dtype);
+  if (const char *why = sizes_fault(rows, n_experts, n, k)) return train_fail(MOE_SPEC_EINVAL, "grouped_product: %s", why);
+  const int in = transpose ? n : k, out = transpose ? k : n, elem = size_of(dtype);
+  if (rows == 0) return MOE_SPEC_OK;
+  if (const char *why = matrix_fault(x, x_stride, rows, in, elem, false)) return train_fail(MOE_SPEC_EINVAL, "grouped_product: x %s", why);
+  if (const char *why = matrix_fault(w, w_stride, n, k, elem, false)) return train_fail(MOE_SPEC_EINVAL, "grouped_product: w %s", why);
+  if (const char *why = matrix_fault(y, y_stride, rows, out, size_of(out_dtype), true)) return train_fail(MOE_SPEC_EINVAL, "grouped_product: y %s", why);
+  if (n_experts > 1 && (w_expert_stride < 0 || w_expert_stride > kMostExpertStride))
+    return train_fail(MOE_SPEC_EINVAL, "grouped_product: w_expert_stride must be between 0 and 2^40");
+  if (!ends || misaligned(ends, 4)) return train_fail(MOE_SPEC_EINVAL, "grouped_product: ends is null or not aligned to its elements");
+  if (y == x || y == w) return train_fail(MOE_SPEC_EINVAL, "grouped_product: y must not be x or w");
+  if (rows == 1) x_stride = in, y_stride = out;         // strides that are never taken are not looked at
+  if (n == 1) w_stride = k;
+  if (n_experts == 1) w_expert_stride = 0;
+  GroupedArgs a{x, w, y, ends, x_stride, w_stride, w_expert_stride, y_stride, in, int(rows), n_experts, out, 0, out_dtype == MOE_SPEC_BF16};
+  const bool whole = whole16(x, x_stride) && whole16(w, w_stride) && w_expert_stride % 8 == 0 && in % 8 == 0 && (!transpose || out % 8 == 0);
+  const Choice<GroupedArgs> c = dtype == MOE_SPEC_F32 ? (transpose ? grouped_f32_choice<64, 64, 2, 2, true>() : grouped_f32_choice<64, 64, 2, 2, false>())
+                                : transpose           ? (whole ? choose_grouped<true, true>(a) : choose_grouped<true, false>(a))
+                                                      : (whole ? choose_grouped<false, true>(a) : choose_grouped<false, false>(a));
+  a.tiles_n = int(tiles_of(out, c.bn));
+  const unsigned grid = grid_of(row_tiles(rows, n_experts, c.bm) * a.tiles_n, c.threads);
+  if (!grid) return train_fail(MOE_SPEC_EINVAL, "grouped_product: more rows and columns than one launch can take");
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const OnDeviceOf on(s);
+  const hipError_t e = on.error() == hipSuccess ? launch(c.kernel, grid, c.threads, s, a) : on.error();
+  return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "grouped_product: %s", hipGetErrorString(e));
+}
+
+extern "C" int moe_spec_grouped_weight_grad(void *stream, int dtype, const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
+                                            int64_t rows, int n_experts, int n, int k, const int32_t *ends, int out_dtype, void *dw,
+                                            int64_t dw_stride, int64_t dw_expert_stride) {
+  if (!known_type(dtype)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: unknown dtype %d", dtype);
+  if (!known_type(out_dtype)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: unknown out_dtype %d", out_dtype);
+  if (const char *why = sizes_fault(rows, n_experts, n, k)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: %s", why);
+  const int elem = size_of(dtype);
+  if (const char *why = matrix_fault(dy, dy_stride, rows, n, elem, false)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: dy %s", why);
+  if (const char *why = matrix_fault(x, x_stride, rows, k, elem, false)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: x %s", why);
+  if (const char *why = matrix_fault(dw, dw_stride, n, k, size_of(out_dtype), true)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: dw %s", why);
+  if (n == 1) dw_stride = k;
+  if (n_experts > 1 && (dw_expert_stride < (n - 1) * dw_stride + k || dw_expert_stride > kMostExpertStride))
+    return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: dw_expert_stride is below a matrix or above 2^40");
+  if (!ends || misaligned(ends, 4)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: ends is null or not aligned to its elements");
+  if (rows && (dw == dy || dw == x)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: dw must not be dy or x");
+  if (rows <= 1) dy_stride = n, x_stride = k;
+  if (n_experts == 1) dw_expert_stride = 0;
+  WeightGradArgs a{dy, x, dw, ends, dy_stride, x_stride, dw_stride, dw_expert_stride, int(rows), n_experts, n, k, 0, 0, out_dtype == MOE_SPEC_BF16};
+  const bool whole = whole16(dy, dy_stride) && whole16(x, x_stride) && n % 8 == 0 && k % 8 == 0;
+  const Choice<WeightGradArgs> c = dtype == MOE_SPEC_F32 ? Choice<WeightGradArgs>{weight_grad_f32_kernel<64, 64, 2, 2>, 64, 64, 256}
+                                   : whole               ? Choice<WeightGradArgs>{weight_grad_kernel<128, 128, 2, 2, true>, 128, 128, 256}
+                                                         : Choice<WeightGradArgs>{weight_grad_kernel<128, 128, 2, 2, false>, 128, 128, 256};
+  a.tiles_n = int(tiles_of(n, c.bm));
+  a.tiles_k = int(tiles_of(k, c.bn));
+  const unsigned grid = grid_of(int64_t(n_experts) * a.tiles_n * a.tiles_k, c.threads);
+  if (!grid) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: more experts' values than one launch can take");
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const OnDeviceOf on(s);
+  const hipError_t e = on.error() == hipSuccess ? launch(c.kernel, grid, c.threads, s, a) : on.error();
+  return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "grouped_weight_grad: %s", hipGetErrorString(e));
+}

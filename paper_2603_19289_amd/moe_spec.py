@@ -16,6 +16,7 @@ F32, BF16 = 0, 1
 COPY_DMA, COPY_KERNEL, COPY_DMA2 = 0, 1, 2
 STATIC_SCRATCH_BYTES = 8 << 20
 MOMENTS_32BIT, MOMENTS_8BIT, MOMENT_BLOCK = 0, 1, 128
+MAX_EXPERTS = 256
 
 
 class Config(C.Structure):
@@ -63,6 +64,17 @@ class AdamWConfig(C.Structure):
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
                 ("weight_decay", C.c_double), ("grad_scale", C.c_double), ("step", C.c_int64), ("step_dev", C.c_void_p),
                 ("grad_scale_dev", C.c_void_p), ("seed", C.c_uint32), ("grad_dtype", C.c_int32), ("moments", C.c_int32)]
+
+
+class MuonTensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("copy", C.c_void_p), ("count", C.c_int64),
+                ("rows", C.c_int32), ("cols", C.c_int32)]
+
+
+class MuonConfig(C.Structure):
+    _fields_ = [("lr", C.c_double), ("momentum", C.c_double), ("weight_decay", C.c_double), ("update_rms", C.c_double),
+                ("grad_scale", C.c_double), ("coefficients", C.c_double * 3), ("grad_scale_dev", C.c_void_p),
+                ("iterations", C.c_int32), ("nesterov", C.c_int32), ("grad_dtype", C.c_int32)]
 
 
 class MoeSpecError(RuntimeError):
@@ -119,6 +131,16 @@ def lib():
         L.moe_spec_balance_loss.argtypes = [vp, i32, vp, i64, i64, i32, vp, i64, i32, f32, vp, vp, vp, vp, i64, vp, sz]
         L.moe_spec_adamw_step.argtypes = [vp, C.POINTER(AdamWTensor), i32, C.POINTER(AdamWConfig)]
         L.moe_spec_adamw_read_moments.argtypes = [vp, C.POINTER(AdamWTensor), i32, i32, C.POINTER(vp), C.POINTER(vp)]
+        L.moe_spec_grouped_product.argtypes = [vp, i32, vp, i64, i64, vp, i64, i64, i32, i32, i32, vp, i32, i32, vp, i64]
+        L.moe_spec_grouped_weight_grad.argtypes = [vp, i32, vp, i64, vp, i64, i64, i32, i32, i32, vp, i32, vp, i64, i64]
+        L.moe_spec_swiglu_forward.argtypes = [vp, i32, vp, i64, i64, i32, vp, vp, i64]
+        L.moe_spec_swiglu_backward.argtypes = [vp, i32, vp, i64, vp, i64, i64, i32, vp, vp, i64, vp]
+        L.moe_spec_orthogonalise_workspace_bytes.argtypes = [i64, i32, i32]
+        L.moe_spec_orthogonalise_workspace_bytes.restype = sz
+        L.moe_spec_orthogonalise.argtypes = [vp, i32, vp, i64, i64, i64, i32, i32, C.POINTER(C.c_double), i32, vp, i64, i64, vp, sz]
+        L.moe_spec_muon_workspace_bytes.argtypes = [C.POINTER(MuonTensor), i32]
+        L.moe_spec_muon_workspace_bytes.restype = sz
+        L.moe_spec_muon_step.argtypes = [vp, C.POINTER(MuonTensor), i32, C.POINTER(MuonConfig), vp, sz]
         L.moe_spec_train_last_error.restype = C.c_char_p
         _lib = L
     return _lib
@@ -264,3 +286,41 @@ def moe_spec_adamw_step(stream, tensors, n_tensors, cfg: AdamWConfig):
 
 def moe_spec_adamw_read_moments(stream, tensors, n_tensors, out_dtype, m_out, v_out):
     _check_train(lib().moe_spec_adamw_read_moments(stream, tensors, n_tensors, out_dtype, m_out, v_out))
+
+
+def moe_spec_grouped_product(stream, dtype, x, x_stride, rows, w, w_stride, w_expert_stride, n_experts, n, k, ends, transpose, out_dtype, y,
+                             y_stride):
+    _check_train(lib().moe_spec_grouped_product(stream, dtype, x, x_stride, rows, w, w_stride, w_expert_stride, n_experts, n, k, ends,
+                                                transpose, out_dtype, y, y_stride))
+
+
+def moe_spec_grouped_weight_grad(stream, dtype, dy, dy_stride, x, x_stride, rows, n_experts, n, k, ends, out_dtype, dw, dw_stride,
+                                 dw_expert_stride):
+    _check_train(lib().moe_spec_grouped_weight_grad(stream, dtype, dy, dy_stride, x, x_stride, rows, n_experts, n, k, ends, out_dtype, dw,
+                                                    dw_stride, dw_expert_stride))
+
+
+def moe_spec_swiglu_forward(stream, dtype, a, a_stride, rows, cols, weight, h, h_stride):
+    _check_train(lib().moe_spec_swiglu_forward(stream, dtype, a, a_stride, rows, cols, weight, h, h_stride))
+
+
+def moe_spec_swiglu_backward(stream, dtype, dh, dh_stride, a, a_stride, rows, cols, weight, da, da_stride, dweight):
+    _check_train(lib().moe_spec_swiglu_backward(stream, dtype, dh, dh_stride, a, a_stride, rows, cols, weight, da, da_stride, dweight))
+
+
+def moe_spec_orthogonalise_workspace_bytes(count, rows, cols) -> int:
+    return lib().moe_spec_orthogonalise_workspace_bytes(count, rows, cols)
+
+
+def moe_spec_orthogonalise(stream, dtype, g, g_matrix_stride, g_stride, count, rows, cols, coefficients, iterations, out, out_matrix_stride,
+                           out_stride, workspace, workspace_bytes):
+    _check_train(lib().moe_spec_orthogonalise(stream, dtype, g, g_matrix_stride, g_stride, count, rows, cols, (C.c_double * 3)(*coefficients),
+                                              iterations, out, out_matrix_stride, out_stride, workspace, workspace_bytes))
+
+
+def moe_spec_muon_workspace_bytes(tensors, n_tensors) -> int:
+    return lib().moe_spec_muon_workspace_bytes(tensors, n_tensors)
+
+
+def moe_spec_muon_step(stream, tensors, n_tensors, cfg: MuonConfig, workspace, workspace_bytes):
+    _check_train(lib().moe_spec_muon_step(stream, tensors, n_tensors, C.byref(cfg), workspace, workspace_bytes))

@@ -309,6 +309,207 @@ class AdamW:
         return m_out, v_out
 
 
+def _out(out: Optional[torch.Tensor], name: str, shape, dtype: torch.dtype, like: torch.Tensor) -> torch.Tensor:
+    """The tensor that a result goes to: a new one, or the given one."""
+    if out is None:
+        return like.new_empty(shape, dtype=dtype)
+    if out.shape != shape or out.dtype != dtype or out.device != like.device or (out.stride(-1) != 1 and out.shape[-1] > 1):
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {like.device} whose rows are contiguous")
+    if out.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, and what is written there would not be in its graph")
+    return out
+
+
+def _groups(ends: torch.Tensor, experts: int, dev: torch.device):
+    if not 1 <= experts <= M.MAX_EXPERTS:
+        raise ValueError(f"between 1 and {M.MAX_EXPERTS} experts are taken")
+    return _vector(ends, "ends", experts, dev, torch.int32)
+
+
+def grouped_product(x: torch.Tensor, w: torch.Tensor, ends: torch.Tensor, *, transpose: bool = False,
+                    dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Products of rows that are sorted by expert with the experts' matrices w [experts, n, k]: w_e x_r for x [rows, k] -> [rows, n],
+    or w_e^T x_r for x [rows, n] -> [rows, k] with transpose, the gradient with respect to the other form's x.  Expert e has the
+    rows from ends[e - 1] (0 for the first) to ends[e], ends int32 [experts] on the GPU; rows behind the last become zero.
+    x and w are both float32 or both bfloat16, rows and matrices may be strided (a part of larger expert blocks, one row for all);
+    dtype: the result's type, x's own if left out."""
+    t = _rows(x, "x")
+    if w.dim() != 3 or w.dtype != x.dtype or w.device != x.device or (w.stride(2) != 1 and w.shape[2] > 1):
+        raise ValueError("w must be a three-dimensional tensor of the type and on the device of x, whose rows are contiguous")
+    experts, n, k = w.shape
+    if x.shape[1] != (n if transpose else k):
+        raise ValueError(f"x must have {n if transpose else k} columns")
+    kind = x.dtype if dtype is None else dtype
+    if kind not in _TYPES:
+        raise ValueError("results are float32 or bfloat16")
+    at = _groups(ends, experts, x.device)
+    given = out is not None
+    out = _out(out, "out", (x.shape[0], k if transpose else n), kind, x)
+    _queue(x.device, M.lib().moe_spec_grouped_product, t, x.data_ptr(), x.stride(0), x.shape[0], w.data_ptr(), w.stride(1), w.stride(0),
+           experts, n, k, at, bool(transpose), _TYPES[kind], out.data_ptr(), out.stride(0))
+    if given:
+        increment_version(out)
+    return out
+
+
+def grouped_weight_grad(dy: torch.Tensor, x: torch.Tensor, ends: torch.Tensor, *, dtype: Optional[torch.dtype] = None,
+                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradients of the experts' matrices, [experts, n, k]: the sum of dy_r x_r^T over each expert's rows, for dy [rows, n] and
+    x [rows, k] sorted by expert as for grouped_product; zeros for an expert without rows.  dtype: the result's type, x's own if left
+    out.  out: where it goes, for instance a part of larger blocks."""
+    t = _rows(x, "x")
+    if _rows(dy, "dy") != t or dy.device != x.device or dy.shape[0] != x.shape[0]:
+        raise ValueError("dy must have the type, the device and the rows of x")
+    kind = x.dtype if dtype is None else dtype
+    if kind not in _TYPES:
+        raise ValueError("results are float32 or bfloat16")
+    experts, n, k = ends.numel(), dy.shape[1], x.shape[1]
+    at = _groups(ends, experts, x.device)
+    given = out is not None
+    out = _out(out, "out", (experts, n, k), kind, x)
+    _queue(x.device, M.lib().moe_spec_grouped_weight_grad, t, dy.data_ptr(), dy.stride(0), x.data_ptr(), x.stride(0), x.shape[0], experts,
+           n, k, at, _TYPES[kind], out.data_ptr(), out.stride(1), out.stride(0))
+    if given:
+        increment_version(out)
+    return out
+
+
+def _gate_up(a: torch.Tensor):
+    t = _rows(a, "a")
+    if a.shape[1] % 2 or a.shape[1] == 0:
+        raise ValueError("a must hold as many columns of the gate as of the up projection")
+    return t, a.shape[0], a.shape[1] // 2
+
+
+def swiglu_forward(a: torch.Tensor, weight: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The experts' activation, silu(gate) * up for a [rows, 2 cols] = gate | up -> [rows, cols].  weight: float32 [rows] or None, a
+    factor of each row: the mixing weights may be applied here, as the down projection is linear."""
+    t, rows, cols = _gate_up(a)
+    h = a.new_empty((rows, cols))
+    _queue(a.device, M.lib().moe_spec_swiglu_forward, t, a.data_ptr(), a.stride(0), rows, cols, _vector(weight, "weight", rows, a.device),
+           h.data_ptr(), cols)
+    return h
+
+
+def swiglu_backward(dh: torch.Tensor, a: torch.Tensor, weight: Optional[torch.Tensor] = None):
+    """Gradients of swiglu_forward for dh [rows, cols] -> (da [rows, 2 cols], dweight float32 [rows], None without a weight)."""
+    t, rows, cols = _gate_up(a)
+    if _rows(dh, "dh") != t or dh.shape != (rows, cols) or dh.device != a.device:
+        raise ValueError("dh must have the type, the device and the rows of a, and half its columns")
+    da = a.new_empty((rows, 2 * cols))
+    dweight = None if weight is None else a.new_empty(rows, dtype=torch.float32)
+    _queue(a.device, M.lib().moe_spec_swiglu_backward, t, dh.data_ptr(), dh.stride(0), a.data_ptr(), a.stride(0), rows, cols,
+           _vector(weight, "weight", rows, a.device), da.data_ptr(), 2 * cols, None if weight is None else dweight.data_ptr())
+    return da, dweight
+
+
+ORTHOGONALISE = (3.4445, -4.7750, 2.0315)          # coefficients of its iteration
+
+
+def orthogonalise(g: torch.Tensor, *, iterations: int = 5, coefficients=ORTHOGONALISE, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Matrices [rows, cols] or stacks of them [count, rows, cols], float32 or bfloat16, with their singular values pushed towards one
+    -> bfloat16, of g's shape.  Formula and accuracy are in include/moe_spec_train.h."""
+    dtype = _TYPES.get(g.dtype)
+    if dtype is None or g.dim() not in (2, 3) or not g.is_cuda or (g.stride(-1) != 1 and g.shape[-1] > 1):
+        raise ValueError("g must be a float32 or bfloat16 matrix on a GPU, or a stack of them, whose rows are contiguous")
+    given = out is not None
+    out = _out(out, "out", g.shape, torch.bfloat16, g)
+    count, (rows, cols) = (g.shape[0] if g.dim() == 3 else 1), g.shape[-2:]
+    lib = M.lib()
+    need = lib.moe_spec_orthogonalise_workspace_bytes(count, rows, cols)
+    space = g.new_empty(need, dtype=torch.uint8) if need else None
+    _queue(g.device, lib.moe_spec_orthogonalise, dtype, g.data_ptr(), g.stride(0) if g.dim() == 3 else 0, g.stride(-2), count, rows, cols,
+           (C.c_double * 3)(*coefficients), iterations, out.data_ptr(), out.stride(0) if g.dim() == 3 else 0, out.stride(-2),
+           space.data_ptr() if need else None, need)
+    if given:
+        increment_version(out)
+    return out
+
+
+class Muon:
+    """Momentum with orthogonalised updates for float32 matrices [rows, cols] and stacks of them [count, rows, cols], such as experts'
+    weights, in one call; embeddings, heads and vectors are AdamW's.  Holds the tensors and their momenta; the settings may be
+    changed between steps.  A captured step keeps those it was captured with; grad_scale it reads anew where it is a tensor.
+
+    update_rms: the root mean square of an update at lr = 1.  copies: bfloat16 tensors (or None in places) that get the updated
+    parameters, rounded.  states: momenta to go on with, as `states()` gave them; used in place."""
+
+    def __init__(self, params: Sequence[torch.Tensor], *, lr: float, momentum: float = 0.95, nesterov: bool = True,
+                 weight_decay: float = 0.01, update_rms: float = 0.2, iterations: int = 5, coefficients=ORTHOGONALISE,
+                 copies: Optional[Sequence[Optional[torch.Tensor]]] = None, states: Optional[dict] = None):
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("no parameters")
+        self.lr, self.momentum, self.nesterov, self.weight_decay = lr, momentum, nesterov, weight_decay
+        self.update_rms, self.iterations, self.coefficients = update_rms, iterations, tuple(coefficients)
+        self.device = self.params[0].device
+        self.copies = list(copies) if copies is not None else [None] * len(self.params)
+        self._m = list(states["m"]) if states is not None else [torch.zeros_like(p, memory_format=torch.contiguous_format) for p in self.params]
+        if len(self._m) != len(self.params) or len(self.copies) != len(self.params):
+            raise ValueError("as many momenta and copies as parameters are needed")
+        self._shapes = [tuple(p.shape) for p in self.params]
+        if any(len(s) not in (2, 3) for s in self._shapes):
+            raise ValueError("parameters must be matrices or stacks of matrices")
+        self._held = [t for t in (*self.params, *self._m, *self.copies) if t is not None]
+        self._at = None
+        self._desc = (M.MuonTensor * len(self.params))()
+        self._describe()
+
+    def states(self) -> dict:
+        """The momenta."""
+        return {"m": list(self._m)}
+
+    def _tensor(self, t, name, dtype, shape):
+        if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.device or not t.is_cuda:
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on the parameters' GPU")
+
+    def _describe(self):
+        """The tensors' table for the library; made anew where one of them has got other storage since."""
+        at = list(map(_ADDRESS, self._held))
+        if at == self._at:
+            return
+        for d, p, m, c, shape in zip(self._desc, self.params, self._m, self.copies, self._shapes):
+            self._tensor(p, "a parameter", torch.float32, shape)
+            self._tensor(m, "a momentum", torch.float32, shape)
+            if c is not None:
+                self._tensor(c, "a copy", torch.bfloat16, shape)
+            d.p, d.m, d.copy = p.data_ptr(), m.data_ptr(), None if c is None else c.data_ptr()
+            d.rows, d.cols = shape[-2:]
+        written = [t.data_ptr() for t in self._held if t.numel()]
+        if len(set(written)) < len(written):
+            raise ValueError("a tensor is named twice")
+        self._at = at
+
+    def step(self, grads: Sequence[Optional[torch.Tensor]], *, grad_scale=1.0):
+        """One step with a gradient for each parameter, all float32 or all bfloat16; a parameter whose gradient is None stays as it
+        is.  grad_scale: a factor of the gradients, a number or a float32 tensor on the GPU."""
+        if len(grads) != len(self.params):
+            raise ValueError("as many gradients as parameters are needed")
+        dtype = next((g.dtype for g in grads if g is not None), torch.float32)
+        if dtype not in _TYPES:
+            raise ValueError("gradients must be float32 or bfloat16")
+        self._describe()
+        for d, g, shape in zip(self._desc, grads, self._shapes):
+            if g is None:
+                d.count = 0
+            else:
+                self._tensor(g, "a gradient", dtype, shape)
+                d.grad, d.count = g.data_ptr(), shape[0] if len(shape) == 3 else 1
+        c = M.MuonConfig(lr=self.lr, momentum=self.momentum, weight_decay=self.weight_decay, update_rms=self.update_rms, grad_scale=1.0,
+                         coefficients=self.coefficients, iterations=self.iterations, nesterov=bool(self.nesterov), grad_dtype=_TYPES[dtype])
+        if isinstance(grad_scale, torch.Tensor):
+            if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.device != self.device:
+                raise ValueError("grad_scale must be a number or one float32 value on the parameters' GPU")
+            c.grad_scale_dev = grad_scale.data_ptr()
+        else:
+            c.grad_scale = grad_scale
+        lib = M.lib()
+        need = lib.moe_spec_muon_workspace_bytes(self._desc, len(self._desc))
+        space = self.params[0].new_empty(need, dtype=torch.uint8) if need else None
+        _queue(self.device, lib.moe_spec_muon_step, self._desc, len(self._desc), C.byref(c), space.data_ptr() if need else None, need)
+        increment_version([t for p, m, q, g in zip(self.params, self._m, self.copies, grads) if g is not None for t in (p, m, q) if t is not None])
+
+
 def _choices(z: torch.Tensor, k: int) -> torch.Tensor:
     """The k largest of each row, among equals those of the lowest index: int32 [rows, k]."""
     return torch.sort(z, dim=1, descending=True, stable=True).indices[:, :k].to(torch.int32)
