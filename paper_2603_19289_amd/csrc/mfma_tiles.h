@@ -6,7 +6,6 @@
 // i-major one by two transposing reads of 8.  LDS is swizzled so that either read meets every bank once:
 //   k-major: rows of 128 bytes, the 16-byte chunk c of row r at place c ^ (r / 2 % 8)  (16 rows of a fragment, one chunk each)
 //   i-major: 32-byte granules, granule q of row k at place q ^ f(k)  (32 lanes read rows {0..3, 8..11} + 4 h of a fragment's 32)
-// The next 64 columns are on their way into the other half of LDS while the matrix instructions work on this one.
 #pragma once
 #include <type_traits>
 
@@ -32,70 +31,89 @@ struct F16 {
 };
 
 constexpr int kTileK = 64;
-__device__ const uint4 kZeroChunk = {0, 0, 0, 0};      // what lies outside a tile is read from here
-
 using LdsPtr = __attribute__((address_space(3))) char *;
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return uint32_t(reinterpret_cast<uintptr_t>((LdsPtr)p)); }
 
-// 16 bytes a lane from global memory to LDS at base + 16 lane; base is the wavefront's.  Written as an instruction, since the compiler
-// would wait for it before every later LDS read, whichever half that reads; it has no output register.  lds_loads_done() and a
-// barrier come before the first read.
-__device__ __forceinline__ void load_to_lds(const void *from, uint32_t base) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(base) : "memory");
+// 16 bytes a lane from memory to LDS at base + 16 lane (base is the wavefront's), through a buffer descriptor: what lies outside of its
+// bounds arrives as zeros.  Written as an instruction, since the compiler would wait for it before every later LDS read, whichever
+// half that reads; it has no output register.  lds_loads_done() and a barrier come before the first read.
+typedef __attribute__((ext_vector_type(4))) uint32_t Buffer;
+__device__ __forceinline__ void load_to_lds(Buffer from, uint32_t offset, uint32_t base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(from), "s"(base) : "memory");
 }
-__device__ __forceinline__ void lds_loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Until at most LEFT of this wavefront's loads are on their way.
+template <int LEFT>
+__device__ __forceinline__ void lds_loads_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
 
-// An operand tile of ROWS x 64 (k-major) or 64 x ROWS (i-major) in LDS and the loads that fill it.
-// WHOLE16: addresses, row strides and extents are multiples of 16 bytes: a chunk lies inside the matrix or outside of it.
+constexpr uint32_t kOutside = 0xffffff00u;             // an offset that no descriptor here contains
+constexpr int64_t kMostTileStride = 1 << 22;           // elements; 256 rows of a tile then stay below 2^32 bytes
+
+// An operand tile of ROWS x 64 (k-major) or 64 x ROWS (i-major) in LDS, and the loads that fill it.
+// WHOLE16: straight to LDS.  Addresses, row strides and extents are multiples of 16 bytes (a chunk lies inside the matrix or outside of
+// it), rows do not overlap and lie at most kMostTileStride apart.  Otherwise: through registers, any stride and alignment.
 template <int ROWS, bool IMAJOR, bool WHOLE16, int THREADS>
 struct OperandTile {
   static constexpr int kBytes = ROWS * kTileK * 2, kChunks = ROWS * kTileK / 8, kEach = kChunks / THREADS;
-  static_assert(kChunks % THREADS == 0 && THREADS % 64 == 0 && ROWS % 64 == 0, "whole chunks for every thread");
-  const uint16_t *at[kEach];             // where this thread's chunks of the next step lie
-  bool in[kEach];                        // i-major: whether those columns exist
-  int64_t step;                          // elements from one step to the next
-  int rows;                              // rows of the tile that exist (at least one)
-  uint4 held[WHOLE16 ? 1 : kEach];
+  static constexpr int kAcross = IMAJOR ? ROWS / 8 : 8, kApart = THREADS / kAcross;      // chunks of a row; rows between a thread's chunks
+  static_assert(kChunks % THREADS == 0 && THREADS % 128 == 0 && ROWS % 64 == 0 && (!IMAJOR || kApart % 16 == 0), "a thread's chunks lie in one column");
 
   static __device__ __forceinline__ int granule_swizzle(int k) {
     return ROWS >= 128 ? (k & 3) | (k >> 1 & 4) : (k >> 1 & 1) | (k >> 2 & 2);
   }
   // Row (k-major: of the tile, i-major: k) and first column of the chunk that goes to place c.
-  static __device__ __forceinline__ int row_of(int c) { return IMAJOR ? c / (ROWS / 8) : c / 8; }
+  static __device__ __forceinline__ int row_of(int c) { return c / kAcross; }
   static __device__ __forceinline__ int column_of(int c) {
-    if constexpr (IMAJOR) {
-      const int place = c % (ROWS / 8), k = c / (ROWS / 8);
-      return (((place >> 1) ^ granule_swizzle(k)) << 4) | (place & 1) << 3;
-    } else {
-      return ((c % 8) ^ (c / 16 % 8)) * 8;
-    }
+    if constexpr (IMAJOR) return (((c % kAcross >> 1) ^ granule_swizzle(c / kAcross)) << 4) | (c & 1) << 3;
+    else return ((c % 8) ^ (c / 16 % 8)) * 8;
   }
+
+  Buffer from;                           // WHOLE16: the rest of the operand
+  uint32_t offset, row_bytes;            // this thread's first chunk; between rows
+  int64_t step;                          // from one step to the next, bytes or elements
+  const uint16_t *at[WHOLE16 ? 1 : kEach];
+  uint4 held[WHOLE16 ? 1 : kEach];
+  int rows, column;                      // rows of the tile that exist (at least one); this thread's column
+
   // origin: the element (0, 0) of the tile; ld: elements between rows of memory.
   __device__ __forceinline__ void begin(const uint16_t *origin, int64_t ld, int rows_, int tid) {
     rows = rows_;
+    column = column_of(tid);
     step = IMAJOR ? ld * kTileK : kTileK;
+    if constexpr (WHOLE16) {
+      const uint64_t p = reinterpret_cast<uint64_t>(origin);
+      row_bytes = uint32_t(ld) * 2;
+      from[0] = __builtin_amdgcn_readfirstlane(uint32_t(p));
+      from[1] = __builtin_amdgcn_readfirstlane(uint32_t(p >> 32));
+      from[2] = __builtin_amdgcn_readfirstlane(uint32_t(rows) * row_bytes);
+      from[3] = 0x00020000u;
+      offset = IMAJOR && column >= rows ? kOutside : row_of(tid) * row_bytes + column * 2;
+      step *= 2;
+    } else {
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      const int c = j * THREADS + tid, r = row_of(c), col = column_of(c);
-      if constexpr (IMAJOR) {
-        in[j] = col < rows;
-        at[j] = origin + int64_t(r) * ld + col;
-      } else {
-        at[j] = origin + int64_t(min(r, rows - 1)) * ld + col;
+      for (int j = 0; j < kEach; ++j) {
+        const int r = row_of(tid) + j * kApart;
+        at[j] = origin + int64_t(IMAJOR ? r : min(r, rows - 1)) * ld + column;
       }
     }
   }
-  // Asks for the next step; k_left: columns that are left (k-major), rows that are left (i-major).
+  // Asks for the next step, of which k_left (at most 64) columns (k-major) or rows of memory (i-major) exist.
   __device__ __forceinline__ void issue(uint32_t lds, int k_left, int tid) {
+    if constexpr (WHOLE16) {
+      if constexpr (IMAJOR) from[2] = uint32_t(k_left) * row_bytes;
+      const uint32_t mine = !IMAJOR && column >= k_left ? kOutside : offset;
+      const uint32_t base = __builtin_amdgcn_readfirstlane(lds + (tid & ~63) * 16);
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      const int c = j * THREADS + tid;
-      const int k = IMAJOR ? row_of(c) : column_of(c);
-      if constexpr (WHOLE16) {
-        const void *from = (k < k_left && (!IMAJOR || in[j])) ? static_cast<const void *>(at[j]) : &kZeroChunk;
-        load_to_lds(from, __builtin_amdgcn_readfirstlane(lds + (c & ~63) * 16));
-      } else {
-        const int n = IMAJOR ? (k < k_left ? rows - column_of(c) : 0) : k_left - k;
+      for (int j = 0; j < kEach; ++j) {
+        const uint32_t o = mine + j * kApart * row_bytes;
+        load_to_lds(from, j == 0 || mine != kOutside ? o : kOutside, base + j * THREADS * 16);
+      }
+      const uint64_t p = (uint64_t(from[1]) << 32 | from[0]) + uint64_t(step);
+      from[0] = uint32_t(p);
+      from[1] = uint32_t(p >> 32);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        const int n = IMAJOR ? (row_of(tid) + j * kApart < k_left ? rows - column : 0) : k_left - column;
         held[j] = uint4{0, 0, 0, 0};
         if (n >= 8) {
           held[j] = load_raw<uint4>(at[j]);
@@ -105,8 +123,8 @@ struct OperandTile {
           for (int i = 0; i < 7; ++i) if (i < n) e[i] = at[j][i];
           __builtin_memcpy(&held[j], e, 16);
         }
+        at[j] += step;
       }
-      at[j] += step;
     }
   }
   // Puts what issue() asked for where it said.
@@ -121,15 +139,14 @@ struct OperandTile {
   static __device__ __forceinline__ s16x8_t fragment(const char *lds, int row, int half, int lane) {
     const int i = lane & 15, g = lane >> 4;
     if constexpr (IMAJOR) {
-      const int k = half * 32 + g * 8 + (i >> 2);
-      const uint32_t at = lds_address(lds) + k * (ROWS * 2) + (((row >> 4) ^ granule_swizzle(k)) << 5) + (i & 3) * 8;
       using P = __attribute__((address_space(3))) s16x4_t *;
-      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<P>(at));
-      // four rows further on; their swizzle is the same where 128 or more rows need three bits, and otherwise differs in its second
-      const int k4 = k + 4;
-      const uint32_t at4 = lds_address(lds) + k4 * (ROWS * 2) + (((row >> 4) ^ granule_swizzle(k4)) << 5) + (i & 3) * 8;
-      const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<P>(at4));
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      s16x4_t part[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = half * 32 + g * 8 + h * 4 + (i >> 2);
+        part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<P>(lds_address(lds) + k * (ROWS * 2) + (((row >> 4) ^ granule_swizzle(k)) << 5) + (i & 3) * 8));
+      }
+      return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
       return *reinterpret_cast<const s16x8_t *>(lds + (row + i) * 128 + (((half * 4 + g) ^ (i >> 1)) << 4));
     }
@@ -152,24 +169,32 @@ struct TileProduct {
 #pragma unroll
       for (int h = 0; h < FN; ++h) acc[f][h] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   }
-  __device__ __forceinline__ void compute(const char *half, int wave, int lane) {
-    const int row = wave / WN * (BM / WM), col = wave % WN * (BN / WN);
+  // The operands of 32 columns: all of b, and half of a's rows.
+  static constexpr int FH = FM / 2;
+  static_assert(FM % 2 == 0, "two halves of rows");
+  static __device__ __forceinline__ void read_a(s16x8_t (&v)[FH], const char *half, int kk, int upper, int row, int lane) {
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      s16x8_t a[FM], b[FN];
+    for (int f = 0; f < FH; ++f) v[f] = A::fragment(half, row + 16 * (upper * FH + f), kk, lane);
+  }
+  static __device__ __forceinline__ void read_b(s16x8_t (&v)[FN], const char *half, int kk, int col, int lane) {
 #pragma unroll
-      for (int h = 0; h < FN; ++h) b[h] = B::fragment(half + A::kBytes, col + 16 * h, kk, lane);
+    for (int h = 0; h < FN; ++h) v[h] = B::fragment(half + A::kBytes, col + 16 * h, kk, lane);
+  }
+  template <int UPPER>
+  __device__ __forceinline__ void multiply(const s16x8_t (&a)[FH], const s16x8_t (&b)[FN]) {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int f = 0; f < FM; ++f) a[f] = A::fragment(half, row + 16 * f, kk, lane);
+    for (int f = 0; f < FH; ++f)
 #pragma unroll
-      for (int f = 0; f < FM; ++f)
-#pragma unroll
-        for (int h = 0; h < FN; ++h) acc[f][h] = Type::mfma(b[h], a[f], acc[f][h]);
-    }
+      for (int h = 0; h < FN; ++h) acc[UPPER * FH + f][h] = Type::mfma(b[h], a[f], acc[UPPER * FH + f][h]);
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
   }
   // a, b: the tile's first elements; K columns; rows and columns of the tile that exist.  Every thread of the workgroup calls it.
   __device__ __forceinline__ void run(char *lds, const uint16_t *a, int64_t lda, int a_rows, const uint16_t *b, int64_t ldb, int b_rows, int64_t K) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int row = wave / WN * (BM / WM), col = wave % WN * (BN / WN);
     const uint32_t base = lds_address(lds);
     clear();
     if (K <= 0) return;
@@ -177,41 +202,99 @@ struct TileProduct {
     B tb;
     ta.begin(a, lda, a_rows, tid);
     tb.begin(b, ldb, b_rows, tid);
-    const auto left = [](int64_t k) { return int(k < kTileK ? k : int64_t(kTileK)); };
-    ta.issue(base, left(K), tid);
-    tb.issue(base + A::kBytes, left(K), tid);
-    ta.land(lds, tid);
-    tb.land(lds + A::kBytes, tid);
-    lds_loads_done();
-    __syncthreads();
-    int now = 0;
-    for (int64_t k = K - kTileK;; k -= kTileK) {
-      const int next = now ^ kHalf;
-      if (k > 0) {
-        ta.issue(base + next, left(k), tid);
-        tb.issue(base + next + A::kBytes, left(k), tid);
-      }
-      compute(lds + now, wave, lane);
-      if (k <= 0) break;
-      ta.land(lds + next, tid);
-      tb.land(lds + next + A::kBytes, tid);
-      lds_loads_done();
+    const auto issue = [&](int half, int64_t k) {                  // the step that has k columns left
+      const int left = int(k < kTileK ? (k > 0 ? k : 0) : int64_t(kTileK));
+      ta.issue(base + half, left, tid);
+      tb.issue(base + half + A::kBytes, left, tid);
+    };
+    s16x8_t a0[FH], a1[FH], b0[FN], b1[FN];
+    if constexpr (WHOLE16) {
+      // Two steps are on their way or in LDS.  Each step is four runs of products; what the next run needs is read while one goes on.
+      // Before the last run all of a step has been read, and its half of LDS gets the step after next.  Steps behind the last are
+      // asked for and read too, as zeros, so that the loop has no branches.
+      issue(0, K);
+      issue(kHalf, K - kTileK);
+      lds_loads_done<A::kEach + B::kEach>();
       __syncthreads();
-      now = next;
+      read_b(b0, lds, 0, col, lane);
+      read_a(a0, lds, 0, 0, row, lane);
+      int now = 0;
+      for (int64_t k = K; k > 0; k -= kTileK) {
+        read_a(a1, lds + now, 0, 1, row, lane);
+        multiply<0>(a0, b0);
+        read_b(b1, lds + now, 1, col, lane);
+        read_a(a0, lds + now, 1, 0, row, lane);
+        multiply<1>(a1, b0);
+        read_a(a1, lds + now, 1, 1, row, lane);
+        multiply<0>(a0, b1);
+        lds_loads_done<0>();
+        __syncthreads();
+        now ^= kHalf;
+        read_b(b0, lds + now, 0, col, lane);
+        read_a(a0, lds + now, 0, 0, row, lane);
+        multiply<1>(a1, b1);
+        issue(now ^ kHalf, k - 2 * kTileK);
+      }
+      lds_loads_done<0>();                       // nothing may arrive once the workgroup has given its LDS back
+    } else {
+      issue(0, K);
+      int now = 0;
+      for (int64_t k = K; k > 0; k -= kTileK, now ^= kHalf) {
+        ta.land(lds + now, tid);
+        tb.land(lds + now + A::kBytes, tid);
+        __syncthreads();                         // one a step: what is written next is the half that was read before the last one
+        if (k > kTileK) issue(now ^ kHalf, k - kTileK);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          read_b(b0, lds + now, kk, col, lane);
+          read_a(a0, lds + now, kk, 0, row, lane);
+          read_a(a1, lds + now, kk, 1, row, lane);
+          multiply<0>(a0, b0);
+          multiply<1>(a1, b0);
+        }
+      }
     }
   }
 };
 
-// Four values of one row of a result, of which the first n exist.
-__device__ __forceinline__ void store4(uint16_t *p, f32x4_t v, int n) {
-  const uint2 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-  if (n >= 4) {
-    __builtin_memcpy(p, &w, 8);
-  } else {
+// A wavefront's part of a 16-bit result in LDS, row by row, so that it leaves in rows of 16 bytes a lane instead of 8 bytes of 16 rows.
+// The 16-byte chunk c of row r lies at place c ^ (r / 2 % chunks).
+template <int ROWS, int COLS>
+struct ResultTile {
+  static constexpr int kAcross = COLS / 8, kBytes = ROWS * COLS * 2, kEach = ROWS * kAcross / 64;
+  static __device__ __forceinline__ int place(int row, int chunk) { return row * (COLS * 2) + ((chunk ^ (row >> 1 & (kAcross - 1))) << 4); }
+  // Four columns from 16 h + 4 g on of row 16 f + i, as two words, from lane (i, g).
+  static __device__ __forceinline__ void put(char *lds, int f, int h, uint2 v, int lane) {
+    const int row = 16 * f + (lane & 15), col = 16 * h + 4 * (lane >> 4);
+    *reinterpret_cast<uint2 *>(lds + place(row, col >> 3) + (col & 4) * 2) = v;
+  }
+  static __device__ __forceinline__ uint4 chunk(const char *lds, int row, int c) { return *reinterpret_cast<const uint4 *>(lds + place(row, c)); }
+  // Eight rows from `row` on (a multiple of 8) of column `col` + lane % 16 (col a multiple of 16; row the same for 16 lanes).
+  static __device__ __forceinline__ uint4 column(const char *lds, int row, int col, int lane) {
+    using P = __attribute__((address_space(3))) s16x4_t *;
+    const int j = lane & 15, c = col + 4 * (j & 3);
+    uint2 v[2];
 #pragma unroll
-    for (int i = 0; i < 3; ++i) if (i < n) p[i] = uint16_t(i & 1 ? (i < 2 ? w.x : w.y) >> 16 : (i < 2 ? w.x : w.y));
+    for (int h = 0; h < 2; ++h)
+      v[h] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          reinterpret_cast<P>(lds_address(lds) + place(row + 4 * h + (j >> 2), c >> 3) + (c & 4) * 2)));
+    return uint4{v[0].x, v[0].y, v[1].x, v[1].y};
+  }
+};
+
+// Up to eight 16-bit values at p, of which n exist.
+__device__ __forceinline__ void store8(uint16_t *p, uint4 v, int n) {
+  if (n >= 8) {
+    __builtin_memcpy(p, &v, 16);
+  } else {
+    uint16_t e[8];
+    __builtin_memcpy(e, &v, 16);
+#pragma unroll
+    for (int i = 0; i < 7; ++i) if (i < n) p[i] = e[i];
   }
 }
+
+// Four values of one row of a result, of which the first n exist.
 __device__ __forceinline__ void store4(float *p, f32x4_t v, int n) {
   if (n >= 4) {
     __builtin_memcpy(p, &v, 16);

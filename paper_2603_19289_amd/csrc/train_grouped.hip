@@ -41,7 +41,7 @@ __device__ __forceinline__ RowTile row_tile(const int32_t *ends, int n_experts, 
     const int v = __shfl_up(before, d);
     if (lane >= d) before = max(before, v);
   }
-  const int last = __shfl(before, 63);
+  const int last = __builtin_amdgcn_readlane(before, 63);
   before = __shfl_up(before, 1);
   if (lane == 0) before = 0;
   int sum = 0;
@@ -57,7 +57,7 @@ __device__ __forceinline__ RowTile row_tile(const int32_t *ends, int n_experts, 
     const int v = __shfl_up(upto, d);
     if (lane >= d) upto += v;
   }
-  const int tiles = __shfl(upto, 63), all = tiles + (rows - last + BM - 1) / BM;
+  const int tiles = __builtin_amdgcn_readlane(upto, 63), all = tiles + (rows - last + BM - 1) / BM;
   const int64_t total = int64_t(all) * tiles_n, share = (total + 7) / 8, slot = blockIdx.x / 8, logical = blockIdx.x % 8 * share + slot;
   RowTile t{-1, 0, 0, 0};
   if (slot >= share || logical >= total) return t;
@@ -69,7 +69,7 @@ __device__ __forceinline__ RowTile row_tile(const int32_t *ends, int n_experts, 
     t.rows = min(BM, rows - t.row0);
     return t;
   }
-  const int who = __popcll(__ballot(upto <= at));        // the lane whose experts have it
+  const int who = __builtin_amdgcn_readfirstlane(__popcll(__ballot(upto <= at)));        // the lane whose experts have it
   int from = upto - sum, expert = -1, row0 = 0, n = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -81,9 +81,9 @@ __device__ __forceinline__ RowTile row_tile(const int32_t *ends, int n_experts, 
     }
     from += count[i];
   }
-  t.expert = __builtin_amdgcn_readfirstlane(__shfl(expert, who));
-  t.row0 = __builtin_amdgcn_readfirstlane(__shfl(row0, who));
-  t.rows = __builtin_amdgcn_readfirstlane(__shfl(n, who));
+  t.expert = __builtin_amdgcn_readlane(expert, who);
+  t.row0 = __builtin_amdgcn_readlane(row0, who);
+  t.rows = __builtin_amdgcn_readlane(n, who);
   return t;
 }
 
@@ -96,15 +96,31 @@ struct GroupedArgs {
   int rows, n_experts, n, tiles_n, out_bf16;
 };
 
-// A wavefront's part of a tile into a row-major matrix.
-template <typename OT, int FM, int FN>
-__device__ __forceinline__ void store_tile(OT *p, int64_t stride, const f32x4_t (&acc)[FM][FN], int row, int col, int rows, int cols) {
+// A wavefront's part of a tile into a row-major matrix p, whose rows and cols from (row, col) on exist; bfloat16 by way of its part of LDS.
+template <int WAVES, int FM, int FN>
+__device__ __forceinline__ void store_tile(void *out, int64_t at, int64_t stride, bool bf16, const f32x4_t (&acc)[FM][FN], char *lds, int row, int col,
+                                           int rows, int cols) {
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  if (bf16) {
+    using R = ResultTile<16 * FM, 16 * FN>;
+    char *mine = lds + (threadIdx.x >> 6) * R::kBytes;
+    __syncthreads();                             // the operands have been read by all
+#pragma unroll
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+      for (int h = 0; h < FN; ++h) R::put(mine, f, h, uint2{pack_bf16(acc[f][h][0], acc[f][h][1]), pack_bf16(acc[f][h][2], acc[f][h][3])}, lane);
+#pragma unroll
+    for (int q = 0; q < R::kEach; ++q) {
+      const int r = (q * 64 + lane) / R::kAcross, c = (q * 64 + lane) % R::kAcross;
+      if (row + r < rows) store8(static_cast<uint16_t *>(out) + at + int64_t(row + r) * stride + col + 8 * c, R::chunk(mine, r, c), cols - col - 8 * c);
+    }
+    return;
+  }
 #pragma unroll
   for (int f = 0; f < FM; ++f) {
     const int r = row + 16 * f + i;
     if (r >= rows) continue;
-    OT *q = p + int64_t(r) * stride;
+    float *q = static_cast<float *>(out) + at + int64_t(r) * stride;
 #pragma unroll
     for (int h = 0; h < FN; ++h) {
       const int c = col + 16 * h + 4 * g;
@@ -114,32 +130,37 @@ __device__ __forceinline__ void store_tile(OT *p, int64_t stride, const f32x4_t 
 }
 
 template <typename P, int BM, int BN, int WM, int WN, typename Elem>
-__device__ __forceinline__ void grouped_tile(const GroupedArgs &a, char *lds, bool w_imajor) {
-  const RowTile t = row_tile<BM>(a.ends, a.n_experts, a.rows, a.tiles_n);
-  if (t.expert < 0) return;
+__device__ __forceinline__ void grouped_tile(const GroupedArgs &a, const RowTile &t, char *lds, bool w_imajor) {
   const int col0 = t.tile_n * BN, cols = min(BN, a.n - col0), wave = threadIdx.x >> 6;
   P p;
   const bool behind = t.expert == a.n_experts;
   const Elem *w = static_cast<const Elem *>(a.w) + (behind ? 0 : t.expert * a.w_expert) + (w_imajor ? int64_t(col0) : col0 * a.w_stride);
   p.run(lds, static_cast<const Elem *>(a.x) + t.row0 * a.x_stride, a.x_stride, t.rows, w, a.w_stride, cols, behind ? 0 : a.k);
-  const int row = wave / WN * (BM / WM), col = wave % WN * (BN / WN);
-  const int64_t at = t.row0 * a.y_stride + col0;
-  if (a.out_bf16) store_tile(static_cast<uint16_t *>(a.y) + at, a.y_stride, p.acc, row, col, t.rows, cols);
-  else store_tile(static_cast<float *>(a.y) + at, a.y_stride, p.acc, row, col, t.rows, cols);
+  store_tile<WM * WN>(a.y, t.row0 * a.y_stride + col0, a.y_stride, a.out_bf16, p.acc, lds, wave / WN * (BM / WM), wave % WN * (BN / WN), t.rows, cols);
 }
 
+// Tiles of 256 rows whose expert has no more than 128 left are half the work as one of 128.
 template <int BM, int BN, int WM, int WN, bool W_IMAJOR, bool WHOLE16>
 __global__ __launch_bounds__(WM *WN * 64) void grouped_kernel(const GroupedArgs a) {
   using P = TileProduct<Bf16, BM, BN, WM, WN, false, W_IMAJOR, WHOLE16>;
   __shared__ __attribute__((aligned(16))) char lds[P::kLds];
-  grouped_tile<P, BM, BN, WM, WN, uint16_t>(a, lds, W_IMAJOR);
+  const RowTile t = row_tile<BM>(a.ends, a.n_experts, a.rows, a.tiles_n);
+  if (t.expert < 0) return;
+  if constexpr (BM == 256) {
+    if (t.rows <= BM / 2) {
+      grouped_tile<TileProduct<Bf16, BM / 2, BN, WM, WN, false, W_IMAJOR, WHOLE16>, BM / 2, BN, WM, WN, uint16_t>(a, t, lds, W_IMAJOR);
+      return;
+    }
+  }
+  grouped_tile<P, BM, BN, WM, WN, uint16_t>(a, t, lds, W_IMAJOR);
 }
 
 template <int BM, int BN, int WM, int WN, bool W_IMAJOR>
 __global__ __launch_bounds__(WM *WN * 64) void grouped_f32_kernel(const GroupedArgs a) {
   using P = TileProductF32<BM, BN, WM, WN, false, W_IMAJOR>;
   __shared__ __attribute__((aligned(16))) char lds[P::kLds];
-  grouped_tile<P, BM, BN, WM, WN, float>(a, lds, W_IMAJOR);
+  const RowTile t = row_tile<BM>(a.ends, a.n_experts, a.rows, a.tiles_n);
+  if (t.expert >= 0) grouped_tile<P, BM, BN, WM, WN, float>(a, t, lds, W_IMAJOR);
 }
 
 // ---- dW = dy^T x -------------------------------------------------------------------------------------------------
@@ -165,10 +186,8 @@ __device__ __forceinline__ void weight_grad_tile(const WeightGradArgs &a, char *
   P p;
   p.run(lds, static_cast<const Elem *>(a.dy) + begin * a.dy_stride + row0, a.dy_stride, rows,
         static_cast<const Elem *>(a.x) + begin * a.x_stride + col0, a.x_stride, cols, end - begin);
-  const int row = wave / WN * (BM / WM), col = wave % WN * (BN / WN);
-  const int64_t at = expert * a.dw_expert + row0 * a.dw_stride + col0;
-  if (a.out_bf16) store_tile(static_cast<uint16_t *>(a.dw) + at, a.dw_stride, p.acc, row, col, rows, cols);
-  else store_tile(static_cast<float *>(a.dw) + at, a.dw_stride, p.acc, row, col, rows, cols);
+  store_tile<WM * WN>(a.dw, expert * a.dw_expert + row0 * a.dw_stride + col0, a.dw_stride, a.out_bf16, p.acc, lds, wave / WN * (BM / WM),
+                      wave % WN * (BN / WN), rows, cols);
 }
 
 template <int BM, int BN, int WM, int WN, bool WHOLE16>
@@ -186,9 +205,13 @@ __global__ __launch_bounds__(WM *WN * 64) void weight_grad_f32_kernel(const Weig
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
+constexpr int kComputeUnits = 256;
 constexpr int64_t kMostExpertStride = int64_t(1) << 40;
 inline int64_t tiles_of(int64_t n, int tile) { return (n + tile - 1) / tile; }
-inline bool whole16(const void *p, int64_t stride) { return !misaligned(p, 16) && stride % 8 == 0; }
+// Whether rows of `width` values can travel straight to LDS.
+inline bool whole16(const void *p, int64_t stride, int width) {
+  return !misaligned(p, 16) && stride % 8 == 0 && width % 8 == 0 && stride >= width && stride <= kMostTileStride;
+}
 
 // Workgroups of a launch of `threads` each, or 0 where a launch cannot have so many.
 inline unsigned grid_of(int64_t tiles, int threads) {
@@ -220,8 +243,27 @@ Choice<GroupedArgs> grouped_choice() { return {grouped_kernel<BM, BN, WM, WN, W_
 template <int BM, int BN, int WM, int WN, bool W_IMAJOR>
 Choice<GroupedArgs> grouped_f32_choice() { return {grouped_f32_kernel<BM, BN, WM, WN, W_IMAJOR>, BM, BN, WM * WN * 64}; }
 
+// Large tiles need few reads for their products, small ones leave fewer places empty and more workgroups: the largest whose half
+// an expert's rows fill on average, and of which there are as many as compute units.
 template <bool W_IMAJOR, bool WHOLE16>
-Choice<GroupedArgs> choose_grouped(const GroupedArgs &) { return grouped_choice<128, 128, 2, 2, W_IMAJOR, WHOLE16>(); }
+Choice<GroupedArgs> choose_grouped(int64_t rows, int n_experts, int n) {
+  if constexpr (WHOLE16) {
+    const int64_t mean = rows / n_experts;
+    const auto tiles = [&](int bm, int bn) { return (mean < 1 ? rows : n_experts * tiles_of(mean, bm)) * tiles_of(n, bn); };
+    if (mean >= 128 && tiles(256, 256) >= kComputeUnits) return grouped_choice<256, 256, 2, 4, W_IMAJOR, WHOLE16>();
+    if (mean >= 12 && tiles(128, 128) >= kComputeUnits) return grouped_choice<128, 128, 2, 4, W_IMAJOR, WHOLE16>();
+    if (tiles(64, 128) >= kComputeUnits) return grouped_choice<64, 128, 2, 2, W_IMAJOR, WHOLE16>();
+    return grouped_choice<64, 64, 2, 2, W_IMAJOR, WHOLE16>();
+  }
+  return grouped_choice<128, 128, 2, 2, W_IMAJOR, WHOLE16>();
+}
+
+Choice<WeightGradArgs> choose_weight_grad(int n_experts, int n, int k) {
+  const auto tiles = [&](int b) { return n_experts * tiles_of(n, b) * tiles_of(k, b); };
+  if (tiles(256) >= kComputeUnits) return {weight_grad_kernel<256, 256, 2, 4, true>, 256, 256, 512};
+  if (tiles(128) >= kComputeUnits) return {weight_grad_kernel<128, 128, 2, 4, true>, 128, 128, 512};
+  return {weight_grad_kernel<64, 64, 2, 2, true>, 64, 64, 256};
+}
 
 }  // namespace
 }  // namespace moe_spec
@@ -247,10 +289,10 @@ extern "C" int moe_spec_grouped_product(void *stream, int dtype, const void *x, 
   if (n == 1) w_stride = k;
   if (n_experts == 1) w_expert_stride = 0;
   GroupedArgs a{x, w, y, ends, x_stride, w_stride, w_expert_stride, y_stride, in, int(rows), n_experts, out, 0, out_dtype == MOE_SPEC_BF16};
-  const bool whole = whole16(x, x_stride) && whole16(w, w_stride) && w_expert_stride % 8 == 0 && in % 8 == 0 && (!transpose || out % 8 == 0);
+  const bool whole = whole16(x, x_stride, in) && whole16(w, w_stride, k) && w_expert_stride % 8 == 0;
   const Choice<GroupedArgs> c = dtype == MOE_SPEC_F32 ? (transpose ? grouped_f32_choice<64, 64, 2, 2, true>() : grouped_f32_choice<64, 64, 2, 2, false>())
-                                : transpose           ? (whole ? choose_grouped<true, true>(a) : choose_grouped<true, false>(a))
-                                                      : (whole ? choose_grouped<false, true>(a) : choose_grouped<false, false>(a));
+                                : transpose           ? (whole ? choose_grouped<true, true>(rows, n_experts, out) : choose_grouped<true, false>(rows, n_experts, out))
+                                                      : (whole ? choose_grouped<false, true>(rows, n_experts, out) : choose_grouped<false, false>(rows, n_experts, out));
   a.tiles_n = int(tiles_of(out, c.bn));
   const unsigned grid = grid_of(row_tiles(rows, n_experts, c.bm) * a.tiles_n, c.threads);
   if (!grid) return train_fail(MOE_SPEC_EINVAL, "grouped_product: more rows and columns than one launch can take");
@@ -278,9 +320,9 @@ extern "C" int moe_spec_grouped_weight_grad(void *stream, int dtype, const void 
   if (rows <= 1) dy_stride = n, x_stride = k;
   if (n_experts == 1) dw_expert_stride = 0;
   WeightGradArgs a{dy, x, dw, ends, dy_stride, x_stride, dw_stride, dw_expert_stride, int(rows), n_experts, n, k, 0, 0, out_dtype == MOE_SPEC_BF16};
-  const bool whole = whole16(dy, dy_stride) && whole16(x, x_stride) && n % 8 == 0 && k % 8 == 0;
+  const bool whole = whole16(dy, dy_stride, n) && whole16(x, x_stride, k);
   const Choice<WeightGradArgs> c = dtype == MOE_SPEC_F32 ? Choice<WeightGradArgs>{weight_grad_f32_kernel<64, 64, 2, 2>, 64, 64, 256}
-                                   : whole               ? Choice<WeightGradArgs>{weight_grad_kernel<128, 128, 2, 2, true>, 128, 128, 256}
+                                   : whole               ? choose_weight_grad(n_experts, n, k)
                                                          : Choice<WeightGradArgs>{weight_grad_kernel<128, 128, 2, 2, false>, 128, 128, 256};
   a.tiles_n = int(tiles_of(n, c.bm));
   a.tiles_k = int(tiles_of(k, c.bn));

@@ -33,14 +33,15 @@ struct MuonArgs {
   uint32_t first[kPerMuonLaunch];        // a stack's first workgroup
   float mu, decay, rate, scale, ca, cb, cc;
   const float *scale_dev;
-  int nesterov, which, bf16, has_p;
+  uint32_t total;                        // workgroups that have a tile
+  int nesterov, which;
 };
 static_assert(sizeof(MuonArgs) <= 4096, "an argument block");
 
-__device__ __forceinline__ int stack_of(const uint32_t (&first)[kPerMuonLaunch]) {
+__device__ __forceinline__ int stack_of(const uint32_t (&first)[kPerMuonLaunch], uint32_t workgroup) {
   int which = -1;
 #pragma unroll
-  for (int i = 0; i < kPerMuonLaunch; ++i) which += first[i] <= blockIdx.x;
+  for (int i = 0; i < kPerMuonLaunch; ++i) which += first[i] <= workgroup;
   return which;
 }
 
@@ -70,7 +71,7 @@ __device__ __forceinline__ void direction8(const MuonArgs &a, const MuonStack &t
 template <typename GT>
 __global__ __launch_bounds__(kMuonBlock) void muon_begin_kernel(const MuonArgs a) {
 #pragma clang fp contract(off)
-  const int which = stack_of(a.first);
+  const int which = stack_of(a.first, blockIdx.x);
   const MuonStack &t = a.t[which];
   const uint32_t at = blockIdx.x - a.first[which];
   const int64_t matrix = at / t.slices;
@@ -135,7 +136,7 @@ __device__ __forceinline__ Normaliser normaliser(const MuonStack &t, int64_t mat
 template <typename GT>
 __global__ __launch_bounds__(kMuonBlock) void muon_normalise_kernel(const MuonArgs a) {
   __shared__ __attribute__((aligned(16))) uint16_t tile[kTurn][kTurn + 8];
-  const int which = stack_of(a.first);
+  const int which = stack_of(a.first, blockIdx.x);
   const MuonStack &t = a.t[which];
   const int across = (t.cols + kTurn - 1) / kTurn, down = (t.rows + kTurn - 1) / kTurn;
   const uint32_t at = blockIdx.x - a.first[which];
@@ -194,7 +195,7 @@ __device__ __forceinline__ void finish8(const MuonArgs &a, const MuonStack &t, i
 template <typename OT>
 __global__ __launch_bounds__(kMuonBlock) void muon_finish_kernel(const MuonArgs a) {
   __shared__ __attribute__((aligned(16))) uint16_t tile[kTurn][kTurn + 8];
-  const int which = stack_of(a.first);
+  const int which = stack_of(a.first, blockIdx.x);
   const MuonStack &t = a.t[which];
   const int across = (t.cols + kTurn - 1) / kTurn, down = (t.rows + kTurn - 1) / kTurn;
   const uint32_t at = blockIdx.x - a.first[which];
@@ -229,51 +230,83 @@ __global__ __launch_bounds__(kMuonBlock) void muon_finish_kernel(const MuonArgs 
   }
 }
 
-// One product for every matrix.  SQUARE: A = X X^T; POLYNOMIAL: B = a I + b A + c A A; APPLY: X' = B X.
+// One product for every matrix.  SQUARE: A = X X^T; POLYNOMIAL: B = a I + b A + c A A; APPLY: X' = B X.  A and B are symmetric: of them
+// only tiles on and below the diagonal are worked out, and written to both places.
 enum MuonProduct { SQUARE, POLYNOMIAL, APPLY };
 
-template <int BM, int BN, int WM, int WN, MuonProduct KIND>
+template <int TILE, int WM, int WN, MuonProduct KIND>
 __global__ __launch_bounds__(WM *WN * 64) void muon_product_kernel(const MuonArgs a) {
-  using P = TileProduct<F16, BM, BN, WM, WN, false, KIND == APPLY, true>;
+  constexpr bool SYMMETRIC = KIND != APPLY;
+  using P = TileProduct<F16, TILE, TILE, WM, WN, false, KIND == APPLY, true>;
+  using R = ResultTile<TILE / WM, TILE / WN>;
   __shared__ __attribute__((aligned(16))) char lds[P::kLds];
-  const int which = stack_of(a.first);
+  const uint32_t share = (a.total + 7) / 8, logical = blockIdx.x % 8 * share + blockIdx.x / 8;      // a die gets a run of tiles
+  if (blockIdx.x / 8 >= share || logical >= a.total) return;
+  const int which = stack_of(a.first, logical);
   const MuonStack &t = a.t[which];
-  const int cols = KIND == APPLY ? t.n : t.m, down = (t.m + BM - 1) / BM, across = (cols + BN - 1) / BN;
-  const uint32_t at = blockIdx.x - a.first[which];
-  const int64_t matrix = at / uint32_t(down * across);
-  const int tile = at % uint32_t(down * across), row0 = tile / across * BM, col0 = tile % across * BN;
+  const int cols = SYMMETRIC ? t.m : t.n, down = (t.m + TILE - 1) / TILE, across = (cols + TILE - 1) / TILE;
+  const uint32_t at = logical - a.first[which], per = SYMMETRIC ? down * (down + 1) / 2 : down * across;
+  const int64_t matrix = at / per;
+  const int tile = at % per;
+  int tile_row = tile / across, tile_col = tile % across;
+  if constexpr (SYMMETRIC) {
+    tile_row = int((sqrtf(8.0f * tile + 1.0f) - 1.0f) * 0.5f);
+    while (tile_row * (tile_row + 1) / 2 > tile) --tile_row;
+    while ((tile_row + 1) * (tile_row + 2) / 2 <= tile) ++tile_row;
+    tile_row = __builtin_amdgcn_readfirstlane(tile_row);
+    tile_col = tile - tile_row * (tile_row + 1) / 2;
+  }
+  const int row0 = tile_row * TILE, col0 = tile_col * TILE;
   const uint16_t *x = t.x[a.which] + matrix * t.m * t.ld_n, *ta = t.a + matrix * t.m * t.ld_m, *tb = t.b + matrix * t.m * t.ld_m;
   P p;
-  const int rows = min(BM, t.m - row0), some = min(BN, cols - col0);
+  const int rows = min(TILE, t.m - row0), some = min(TILE, cols - col0);
+  // X may have rows of 65536 values and A of as many: the strides that a tile takes at most
   if constexpr (KIND == SQUARE) p.run(lds, x + int64_t(row0) * t.ld_n, t.ld_n, rows, x + int64_t(col0) * t.ld_n, t.ld_n, some, t.n);
   if constexpr (KIND == POLYNOMIAL) p.run(lds, ta + int64_t(row0) * t.ld_m, t.ld_m, rows, ta + int64_t(col0) * t.ld_m, t.ld_m, some, t.m);
   if constexpr (KIND == APPLY) p.run(lds, tb + int64_t(row0) * t.ld_m, t.ld_m, rows, x + col0, t.ld_n, some, t.m);
-  const int ld = KIND == APPLY ? t.ld_n : t.ld_m;
+  const int ld = SYMMETRIC ? t.ld_m : t.ld_n;
   uint16_t *out = KIND == APPLY ? t.x[a.which ^ 1] + matrix * t.m * t.ld_n : (KIND == SQUARE ? t.a : t.b) + matrix * t.m * t.ld_m;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+  const int wave_row = row0 + wave / WN * (TILE / WM), wave_col = col0 + wave % WN * (TILE / WN);
+  char *mine = lds + wave * R::kBytes;
+  __syncthreads();                               // the operands have been read by all
 #pragma unroll
   for (int f = 0; f < P::FM; ++f) {
-    const int row = row0 + wave / WN * (BM / WM) + 16 * f + i;
-    if (row >= t.m) continue;
 #pragma unroll
     for (int h = 0; h < P::FN; ++h) {
-      const int col = col0 + wave % WN * (BN / WN) + 16 * h + 4 * g;
-      if (col >= ld) continue;                   // ld is a multiple of 8: all four or none
-      const int64_t to = int64_t(row) * ld + col;
+      const int row = wave_row + 16 * f + i, col = wave_col + 16 * h + 4 * g;
       float v[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) v[r] = p.acc[f][h][r] * (1.0f / kHeld);
       if constexpr (KIND == POLYNOMIAL) {
-        uint16_t e[4];
-        __builtin_memcpy(e, ta + to, 8);
+        uint16_t e[4] = {0, 0, 0, 0};
+        if (row < t.m && col < ld) __builtin_memcpy(e, ta + int64_t(row) * ld + col, 8);
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[r] = a.cb * from_f16(e[r]) + a.cc * v[r] + (col + r == row ? a.ca * kHeld : 0.0f);
       }
       uint16_t e[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) e[r] = col + r < cols ? to_f16(v[r]) : uint16_t(0);     // what fills up a row is zero
-      __builtin_memcpy(out + to, e, 8);
+      for (int r = 0; r < 4; ++r) e[r] = col + r < cols && row < t.m ? to_f16(v[r]) : uint16_t(0);     // what fills up a row is zero
+      uint2 w;
+      __builtin_memcpy(&w, e, 8);
+      R::put(mine, f, h, w, lane);
     }
+  }
+#pragma unroll
+  for (int q = 0; q < R::kEach; ++q) {
+    const int r = (q * 64 + lane) / R::kAcross, c = (q * 64 + lane) % R::kAcross, row = wave_row + r, col = wave_col + 8 * c;
+    if (row < t.m && col < ld) *reinterpret_cast<uint4 *>(out + int64_t(row) * ld + col) = R::chunk(mine, r, c);
+  }
+  if constexpr (SYMMETRIC) {
+    if (tile_row == tile_col) return;
+#pragma unroll
+    for (int r = 0; r < TILE / WM; r += 32)
+#pragma unroll
+      for (int c = 0; c < TILE / WN; c += 16) {
+        const uint4 v = R::column(mine, r + 8 * g, c, lane);
+        const int row = wave_col + c + i, col = wave_row + r + 8 * g;
+        if (row < cols && col < ld) *reinterpret_cast<uint4 *>(out + int64_t(row) * ld + col) = v;
+      }
   }
 }
 
@@ -305,14 +338,6 @@ char *place(MuonStack &t, char *at) {
   return at + 2 * x + 2 * a + round256(size_t(t.count) * t.slices * 8);
 }
 
-// Why a stack cannot be taken, or null.  Its values stay below 2^40 and every launch over it below 2^31 workgroups of 256.
-const char *stack_fault(int64_t count, int64_t rows, int64_t cols) {
-  if (count < 0 || rows < 0 || cols < 0) return "a negative size";
-  if (rows > MOE_SPEC_TRAIN_MAX_FEATURES || cols > MOE_SPEC_TRAIN_MAX_FEATURES) return "more than 65536 rows or columns";
-  if (count && rows && cols && count > MOE_SPEC_MUON_MAX_ELEMENTS / (rows * cols)) return "more than 2^32 values";
-  return nullptr;
-}
-
 const char *iteration_fault(const double *c, int iterations) {
   if (iterations < 1 || iterations > 64) return "iterations must be between 1 and 64";
   for (int i = 0; i < 3; ++i) if (!(fabs(c[i]) <= 16.0)) return "coefficients must lie between -16 and 16";
@@ -332,15 +357,40 @@ void firsts(MuonArgs &a, int n, Count workgroups, unsigned &grid) {
 inline int64_t tiles(int64_t n, int tile) { return (n + tile - 1) / tile; }
 inline int64_t begin_blocks(const MuonStack &t) { return t.count * t.slices; }
 inline int64_t turn_blocks(const MuonStack &t) { return t.count * tiles(t.rows, kTurn) * tiles(t.cols, kTurn); }
-constexpr int kMuonTile = 128;
-inline int64_t square_blocks(const MuonStack &t) { return t.count * tiles(t.m, kMuonTile) * tiles(t.m, kMuonTile); }
-inline int64_t apply_blocks(const MuonStack &t) { return t.count * tiles(t.m, kMuonTile) * tiles(t.n, kMuonTile); }
+inline int64_t square_blocks(const MuonStack &t, int tile) { return t.count * tiles(t.m, tile) * (tiles(t.m, tile) + 1) / 2; }
+inline int64_t apply_blocks(const MuonStack &t, int tile) { return t.count * tiles(t.m, tile) * tiles(t.n, tile); }
 // Most of them, of any launch over the stack.
 inline int64_t most_blocks(const MuonStack &t) {
   const int64_t b = begin_blocks(t), u = turn_blocks(t);
-  return b > u ? b : u;                                 // products have fewer: their tiles are four times as large
+  return b > u ? b : u;                                 // products have no more: their smallest tiles are as large
 }
 constexpr int64_t kMostMuonBlocks = (int64_t(1) << 32) / kMuonBlock - 1;
+
+// One product over n stacks, in the largest tiles of which there are as many as compute units.
+template <MuonProduct KIND>
+hipError_t run_product(MuonArgs &a, int n, hipStream_t s) {
+  int tile = 256;
+  const auto blocks = [&](const MuonStack &t) { return KIND == APPLY ? apply_blocks(t, tile) : square_blocks(t, tile); };
+  for (;; tile /= 2) {
+    firsts(a, n, blocks, a.total);
+    if (tile == 64 || a.total >= 256) break;
+  }
+  const unsigned grid = (a.total + 7) / 8 * 8;
+  if (tile == 256) return launch(muon_product_kernel<256, 2, 4, KIND>, grid, 512, s, a);
+  if (tile == 128) return launch(muon_product_kernel<128, 2, 4, KIND>, grid, 512, s, a);
+  return launch(muon_product_kernel<64, 2, 2, KIND>, grid, 256, s, a);
+}
+
+// Why a stack cannot be taken, or null.
+const char *stack_fault(int64_t count, int64_t rows, int64_t cols) {
+  if (count < 0 || rows < 0 || cols < 0) return "a negative size";
+  if (rows > MOE_SPEC_TRAIN_MAX_FEATURES || cols > MOE_SPEC_TRAIN_MAX_FEATURES) return "more than 65536 rows or columns";
+  if (count == 0 || rows == 0 || cols == 0) return nullptr;
+  if (count > MOE_SPEC_MUON_MAX_ELEMENTS / (rows * cols)) return "more than 2^32 values";
+  MuonStack t;
+  shape(t, count, int(rows), int(cols));
+  return most_blocks(t) > kMostMuonBlocks ? "more matrices than one launch can take" : nullptr;
+}
 
 hipError_t run_stacks(MuonArgs &a, int n, int iterations, bool grad_bf16, bool out_bf16, hipStream_t s) {
   unsigned grid;
@@ -350,18 +400,13 @@ hipError_t run_stacks(MuonArgs &a, int n, int iterations, bool grad_bf16, bool o
   if (e != hipSuccess) return e;
   firsts(a, n, turn_blocks, grid);
   e = grad_bf16 ? launch(muon_normalise_kernel<uint16_t>, grid, kMuonBlock, s, a) : launch(muon_normalise_kernel<float>, grid, kMuonBlock, s, a);
-  if (e != hipSuccess) return e;
-  for (int i = 0; i < iterations; ++i) {
+  for (int i = 0; i < iterations && e == hipSuccess; ++i) {
     a.which = i & 1;
-    firsts(a, n, square_blocks, grid);
-    e = launch(muon_product_kernel<kMuonTile, kMuonTile, 2, 2, SQUARE>, grid, 256, s, a);
-    if (e != hipSuccess) return e;
-    e = launch(muon_product_kernel<kMuonTile, kMuonTile, 2, 2, POLYNOMIAL>, grid, 256, s, a);
-    if (e != hipSuccess) return e;
-    firsts(a, n, apply_blocks, grid);
-    e = launch(muon_product_kernel<kMuonTile, kMuonTile, 2, 2, APPLY>, grid, 256, s, a);
-    if (e != hipSuccess) return e;
+    e = run_product<SQUARE>(a, n, s);
+    if (e == hipSuccess) e = run_product<POLYNOMIAL>(a, n, s);
+    if (e == hipSuccess) e = run_product<APPLY>(a, n, s);
   }
+  if (e != hipSuccess) return e;
   a.which = iterations & 1;
   firsts(a, n, turn_blocks, grid);
   return out_bf16 ? launch(muon_finish_kernel<uint16_t>, grid, kMuonBlock, s, a) : launch(muon_finish_kernel<float>, grid, kMuonBlock, s, a);

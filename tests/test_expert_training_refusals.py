@@ -93,7 +93,7 @@ def orthogonalise(**kw):
 
 
 @pytest.mark.parametrize("bad,word", [(dict(dtype=2), "dtype"), (dict(count=-1), "negative"), (dict(rows=-1), "negative"), (dict(cols=65537), "65536"),
-                                      (dict(count=1 << 40), "2^32"), (dict(coefficients=None), "coefficients"), (dict(coefficients=(C.c_double * 3)(NAN, 0, 0)), "coefficients"),
+                                      (dict(count=1 << 40), "2^32"), (dict(count=1 << 30, rows=1, cols=1, g_matrix_stride=1, out_matrix_stride=1), "one launch"), (dict(coefficients=None), "coefficients"), (dict(coefficients=(C.c_double * 3)(NAN, 0, 0)), "coefficients"),
                                       (dict(coefficients=(C.c_double * 3)(1, INF, 0)), "coefficients"), (dict(coefficients=(C.c_double * 3)(1, 0, -17)), "coefficients"),
                                       (dict(iterations=0), "iterations"), (dict(iterations=65), "iterations"), (dict(g=None), "g is null"), (dict(g=ADDR + 1), "g is not"),
                                       (dict(g_stride=-1), "g has"), (dict(g_matrix_stride=-1), "g's matrix"), (dict(out=None), "out is null"), (dict(out=ADDR + 1), "out is not"),
