@@ -147,9 +147,10 @@ int moe_spec_grouped_product(void *stream, int dtype, const void *x, int64_t x_s
 
 /* Gradient of the matrices: dw dev, n_experts matrices [n, k] of out_dtype, dw_e = sum over the group's rows of dy_r x_r^T, written, not
  * added to; zeros for an expert without rows.  dy dev [rows, n], x dev [rows, k], groups as above. */
+size_t moe_spec_grouped_weight_grad_workspace_bytes(int dtype, int64_t rows, int n_experts, int n, int k);
 int moe_spec_grouped_weight_grad(void *stream, int dtype, const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int64_t rows,
                                  int n_experts, int n, int k, const int32_t *ends, int out_dtype, void *dw, int64_t dw_stride,
-                                 int64_t dw_expert_stride);
+                                 int64_t dw_expert_stride, void *workspace, size_t workspace_bytes);
 
 /* The experts' gated activation: a dev [rows, 2 cols] holds gate and up, h dev [rows, cols] = weight_r silu(gate) up.
  * weight dev [rows] float or NULL (ones): the mixing weight of each row, if it is to be applied here.

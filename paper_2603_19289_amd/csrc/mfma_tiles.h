@@ -155,12 +155,14 @@ struct OperandTile {
 
 // The product of a tile of BM x BN by WM x WN wavefronts.  acc[f][h][r] of lane (i, g): row 16 f + i, column 16 h + 4 g + r of the
 // wavefront's part.
-template <typename Type, int BM, int BN, int WM, int WN, bool A_IMAJOR, bool B_IMAJOR, bool WHOLE16>
+// STEPS: how many steps of 64 columns are in LDS or on their way there.
+template <typename Type, int BM, int BN, int WM, int WN, bool A_IMAJOR, bool B_IMAJOR, bool WHOLE16, int STEPS = 2>
 struct TileProduct {
   static constexpr int kThreads = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
   using A = OperandTile<BM, A_IMAJOR, WHOLE16, kThreads>;
   using B = OperandTile<BN, B_IMAJOR, WHOLE16, kThreads>;
-  static constexpr int kHalf = A::kBytes + B::kBytes, kLds = 2 * kHalf;
+  static constexpr int kPart = A::kBytes + B::kBytes, kLds = STEPS * kPart;
+  static_assert(STEPS >= 2 && (WHOLE16 || STEPS == 2), "");
   f32x4_t acc[FM][FN];
 
   __device__ __forceinline__ void clear() {
@@ -172,13 +174,13 @@ struct TileProduct {
   // The operands of 32 columns: all of b, and half of a's rows.
   static constexpr int FH = FM / 2;
   static_assert(FM % 2 == 0, "two halves of rows");
-  static __device__ __forceinline__ void read_a(s16x8_t (&v)[FH], const char *half, int kk, int upper, int row, int lane) {
+  static __device__ __forceinline__ void read_a(s16x8_t (&v)[FH], const char *part, int kk, int upper, int row, int lane) {
 #pragma unroll
-    for (int f = 0; f < FH; ++f) v[f] = A::fragment(half, row + 16 * (upper * FH + f), kk, lane);
+    for (int f = 0; f < FH; ++f) v[f] = A::fragment(part, row + 16 * (upper * FH + f), kk, lane);
   }
-  static __device__ __forceinline__ void read_b(s16x8_t (&v)[FN], const char *half, int kk, int col, int lane) {
+  static __device__ __forceinline__ void read_b(s16x8_t (&v)[FN], const char *part, int kk, int col, int lane) {
 #pragma unroll
-    for (int h = 0; h < FN; ++h) v[h] = B::fragment(half + A::kBytes, col + 16 * h, kk, lane);
+    for (int h = 0; h < FN; ++h) v[h] = B::fragment(part + A::kBytes, col + 16 * h, kk, lane);
   }
   template <int UPPER>
   __device__ __forceinline__ void multiply(const s16x8_t (&a)[FH], const s16x8_t (&b)[FN]) {
@@ -202,19 +204,19 @@ struct TileProduct {
     B tb;
     ta.begin(a, lda, a_rows, tid);
     tb.begin(b, ldb, b_rows, tid);
-    const auto issue = [&](int half, int64_t k) {                  // the step that has k columns left
+    const auto issue = [&](int part, int64_t k) {                  // the step that has k columns left
       const int left = int(k < kTileK ? (k > 0 ? k : 0) : int64_t(kTileK));
-      ta.issue(base + half, left, tid);
-      tb.issue(base + half + A::kBytes, left, tid);
+      ta.issue(base + part, left, tid);
+      tb.issue(base + part + A::kBytes, left, tid);
     };
     s16x8_t a0[FH], a1[FH], b0[FN], b1[FN];
     if constexpr (WHOLE16) {
-      // Two steps are on their way or in LDS.  Each step is four runs of products; what the next run needs is read while one goes on.
-      // Before the last run all of a step has been read, and its half of LDS gets the step after next.  Steps behind the last are
-      // asked for and read too, as zeros, so that the loop has no branches.
-      issue(0, K);
-      issue(kHalf, K - kTileK);
-      lds_loads_done<A::kEach + B::kEach>();
+      // Each step is four runs of products; what the next run needs is read while one goes on.  Before the last run all of a step has
+      // been read, and its part of LDS gets the step that is STEPS further on.  Steps behind the last are asked for and read too, as zeros,
+      // so that the loop has no branches.
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) issue(i * kPart, K - i * kTileK);
+      lds_loads_done<(STEPS - 1) * (A::kEach + B::kEach)>();
       __syncthreads();
       read_b(b0, lds, 0, col, lane);
       read_a(a0, lds, 0, 0, row, lane);
@@ -227,23 +229,24 @@ struct TileProduct {
         multiply<1>(a1, b0);
         read_a(a1, lds + now, 1, 1, row, lane);
         multiply<0>(a0, b1);
-        lds_loads_done<0>();
+        lds_loads_done<(STEPS - 2) * (A::kEach + B::kEach)>();
         __syncthreads();
-        now ^= kHalf;
-        read_b(b0, lds + now, 0, col, lane);
-        read_a(a0, lds + now, 0, 0, row, lane);
+        const int next = now + kPart == kLds ? 0 : now + kPart;
+        read_b(b0, lds + next, 0, col, lane);
+        read_a(a0, lds + next, 0, 0, row, lane);
         multiply<1>(a1, b1);
-        issue(now ^ kHalf, k - 2 * kTileK);
+        issue(now, k - STEPS * kTileK);
+        now = next;
       }
       lds_loads_done<0>();                       // nothing may arrive once the workgroup has given its LDS back
     } else {
       issue(0, K);
       int now = 0;
-      for (int64_t k = K; k > 0; k -= kTileK, now ^= kHalf) {
+      for (int64_t k = K; k > 0; k -= kTileK, now ^= kPart) {
         ta.land(lds + now, tid);
         tb.land(lds + now + A::kBytes, tid);
         __syncthreads();                         // one a step: what is written next is the half that was read before the last one
-        if (k > kTileK) issue(now ^ kHalf, k - kTileK);
+        if (k > kTileK) issue(now ^ kPart, k - kTileK);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
           read_b(b0, lds + now, kk, col, lane);

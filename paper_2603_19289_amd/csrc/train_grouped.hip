@@ -140,9 +140,9 @@ __device__ __forceinline__ void grouped_tile(const GroupedArgs &a, const RowTile
 }
 
 // Tiles of 256 rows whose expert has no more than 128 left are half the work as one of 128.
-template <int BM, int BN, int WM, int WN, bool W_IMAJOR, bool WHOLE16>
+template <int BM, int BN, int WM, int WN, int STEPS, bool W_IMAJOR, bool WHOLE16>
 __global__ __launch_bounds__(WM *WN * 64) void grouped_kernel(const GroupedArgs a) {
-  using P = TileProduct<Bf16, BM, BN, WM, WN, false, W_IMAJOR, WHOLE16>;
+  using P = TileProduct<Bf16, BM, BN, WM, WN, false, W_IMAJOR, WHOLE16, STEPS>;
   __shared__ __attribute__((aligned(16))) char lds[P::kLds];
   const RowTile t = row_tile<BM>(a.ends, a.n_experts, a.rows, a.tiles_n);
   if (t.expert < 0) return;
@@ -153,6 +153,66 @@ __global__ __launch_bounds__(WM *WN * 64) void grouped_kernel(const GroupedArgs 
     }
   }
   grouped_tile<P, BM, BN, WM, WN, uint16_t>(a, t, lds, W_IMAJOR);
+}
+
+// A few rows, as one decoded token's choices: sixteen weight rows a workgroup, whose four wavefronts take every fourth run of columns (32 of
+// bfloat16, 16 of float) and ask for all they need of 2048 (1024) at once, straight into registers; the sums meet in LDS.  Up to 16 rows
+// of an expert share the weights.  Any stride and alignment.  8 rows of 8 of 128 matrices 1536 x 2048: 10.9 us, 4.6 TB/s; tiles of 64 x 128: 14.
+constexpr int kFewBlock = 256, kFewWaves = kFewBlock / 64, kFewDeep = 16;
+
+template <typename Elem>
+__global__ __launch_bounds__(kFewBlock) void grouped_few_kernel(const GroupedArgs a) {
+  constexpr int V = 16 / sizeof(Elem);
+  __shared__ f32x4_t part[kFewWaves][64];
+  const RowTile t = row_tile<16>(a.ends, a.n_experts, a.rows, a.tiles_n);
+  if (t.expert < 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+  const int col0 = t.tile_n * 16, K = t.expert == a.n_experts ? 0 : int(a.k);
+  const Elem *w = static_cast<const Elem *>(a.w) + (t.expert == a.n_experts ? 0 : t.expert * a.w_expert) + min(col0 + i, a.n - 1) * a.w_stride;
+  const Elem *x = static_cast<const Elem *>(a.x) + (t.row0 + int64_t(min(i, t.rows - 1))) * a.x_stride;
+  // V values of a row from column k on, zeros behind its end
+  const auto ask = [=](const Elem *row, int n) {
+    uint4 v = {0, 0, 0, 0};
+    if (n >= V) {
+      v = load_raw<uint4>(row);
+    } else if (n > 0) {
+      Elem e[V] = {};
+#pragma unroll
+      for (int j = 0; j < V - 1; ++j) if (j < n) e[j] = row[j];
+      __builtin_memcpy(&v, e, 16);
+    }
+    return v;
+  };
+  f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int first = (wave * 4 + g) * V; first - g * V < K; first += kFewWaves * kFewDeep * 4 * V) {
+    uint4 vw[kFewDeep], vx[kFewDeep];
+#pragma unroll
+    for (int d = 0; d < kFewDeep; ++d) {
+      const int k = first + d * kFewWaves * 4 * V;
+      vw[d] = ask(w + k, K - k);
+      vx[d] = ask(x + k, i < t.rows ? K - k : 0);
+    }
+#pragma unroll
+    for (int d = 0; d < kFewDeep; ++d) {
+      if constexpr (V == 8) {
+        acc = Bf16::mfma(__builtin_bit_cast(s16x8_t, vw[d]), __builtin_bit_cast(s16x8_t, vx[d]), acc);
+      } else {                                   // which four columns an instruction takes together does not matter
+        const f32x4_t fw = __builtin_bit_cast(f32x4_t, vw[d]), fx = __builtin_bit_cast(f32x4_t, vx[d]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[j], fx[j], acc, 0, 0, 0);
+      }
+    }
+  }
+  part[wave][lane] = acc;
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int v = 1; v < kFewWaves; ++v) acc += part[v][lane];
+  if (i >= t.rows) return;
+  const int64_t at = (t.row0 + int64_t(i)) * a.y_stride + col0 + 4 * g;
+  const int n = a.n - col0 - 4 * g;
+  if (a.out_bf16) store8(static_cast<uint16_t *>(a.y) + at, uint4{pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), 0, 0}, n < 4 ? n : 4);
+  else store4(static_cast<float *>(a.y) + at, acc, n);
 }
 
 template <int BM, int BN, int WM, int WN, bool W_IMAJOR>
@@ -170,29 +230,62 @@ struct WeightGradArgs {
   const int32_t *ends;
   int64_t dy_stride, x_stride, dw_stride, dw_expert;
   int rows, n_experts, n, k, tiles_n, tiles_k, out_bf16;
+  int parts;                   // of each expert's rows; more than one: sums of each go to `partial`
+  float *partial;              // [parts, n_experts, n, k]
 };
 
 template <typename P, int BM, int BN, int WM, int WN, typename Elem>
 __device__ __forceinline__ void weight_grad_tile(const WeightGradArgs &a, char *lds) {
   const int per = a.tiles_n * a.tiles_k;
-  const int64_t total = int64_t(per) * a.n_experts, share = (total + 7) / 8, slot = blockIdx.x / 8, logical = blockIdx.x % 8 * share + slot;
+  const int64_t total = int64_t(per) * a.n_experts * a.parts, share = (total + 7) / 8, slot = blockIdx.x / 8, logical = blockIdx.x % 8 * share + slot;
   if (slot >= share || logical >= total) return;
-  const int expert = int(logical / per), tile = int(logical % per), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int group = int(logical / per), tile = int(logical % per), expert = group / a.parts, part = group % a.parts;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int before = 0;
   for (int e = lane; e < expert; e += 64) before = max(before, a.ends[e]);
-  const int begin = __builtin_amdgcn_readfirstlane(min(wave_max(before), a.rows));
-  const int end = __builtin_amdgcn_readfirstlane(min(max(a.ends[expert], begin), a.rows));
+  int begin = __builtin_amdgcn_readfirstlane(min(wave_max(before), a.rows));
+  int end = __builtin_amdgcn_readfirstlane(min(max(a.ends[expert], begin), a.rows));
+  if (a.parts > 1) {                             // a part is a whole number of steps
+    const int64_t length = (int64_t(end - begin + kTileK - 1) / kTileK + a.parts - 1) / a.parts * kTileK;
+    const int64_t from = begin + part * length, to = from + length;
+    begin = int(from < end ? from : end);
+    end = int(to < end ? to : end);
+  }
   const int row0 = tile / a.tiles_k * BM, col0 = tile % a.tiles_k * BN, rows = min(BM, a.n - row0), cols = min(BN, a.k - col0);
   P p;
   p.run(lds, static_cast<const Elem *>(a.dy) + begin * a.dy_stride + row0, a.dy_stride, rows,
         static_cast<const Elem *>(a.x) + begin * a.x_stride + col0, a.x_stride, cols, end - begin);
-  store_tile<WM * WN>(a.dw, expert * a.dw_expert + row0 * a.dw_stride + col0, a.dw_stride, a.out_bf16, p.acc, lds, wave / WN * (BM / WM),
-                      wave % WN * (BN / WN), rows, cols);
+  const int row = wave / WN * (BM / WM), col = wave % WN * (BN / WN);
+  if (a.parts > 1) {
+    store_tile<WM * WN>(a.partial, ((int64_t(part) * a.n_experts + expert) * a.n + row0) * a.k + col0, a.k, false, p.acc, lds, row, col, rows, cols);
+  } else {
+    store_tile<WM * WN>(a.dw, expert * a.dw_expert + row0 * a.dw_stride + col0, a.dw_stride, a.out_bf16, p.acc, lds, row, col, rows, cols);
+  }
 }
 
-template <int BM, int BN, int WM, int WN, bool WHOLE16>
+// The parts' sums, in their order.
+__global__ __launch_bounds__(256) void weight_grad_join_kernel(const WeightGradArgs a) {
+  const int64_t across = (a.k + 3) / 4, at = int64_t(blockIdx.x) * 256 + threadIdx.x, row = at / across, matrix = int64_t(a.n_experts) * a.n * a.k;
+  if (row >= int64_t(a.n_experts) * a.n) return;
+  const int c = int(at % across) * 4, n = min(4, a.k - c);
+  f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int p = 0; p < a.parts; ++p) {
+    const float *from = a.partial + p * matrix + row * a.k + c;
+    if (n == 4) {
+      sum += load_raw<f32x4_t>(from);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 3; ++j) if (j < n) sum[j] += from[j];
+    }
+  }
+  const int64_t to = row / a.n * a.dw_expert + row % a.n * a.dw_stride + c;
+  if (a.out_bf16) store8(static_cast<uint16_t *>(a.dw) + to, uint4{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]), 0, 0}, n);
+  else store4(static_cast<float *>(a.dw) + to, sum, n);
+}
+
+template <int BM, int BN, int WM, int WN, int STEPS, bool WHOLE16>
 __global__ __launch_bounds__(WM *WN * 64) void weight_grad_kernel(const WeightGradArgs a) {
-  using P = TileProduct<Bf16, BM, BN, WM, WN, true, true, WHOLE16>;
+  using P = TileProduct<Bf16, BM, BN, WM, WN, true, true, WHOLE16, STEPS>;
   __shared__ __attribute__((aligned(16))) char lds[P::kLds];
   weight_grad_tile<P, BM, BN, WM, WN, uint16_t>(a, lds);
 }
@@ -238,31 +331,45 @@ struct Choice {
   void (*kernel)(Args);
   int bm, bn, threads;
 };
-template <int BM, int BN, int WM, int WN, bool W_IMAJOR, bool WHOLE16>
-Choice<GroupedArgs> grouped_choice() { return {grouped_kernel<BM, BN, WM, WN, W_IMAJOR, WHOLE16>, BM, BN, WM * WN * 64}; }
+template <int BM, int BN, int WM, int WN, int STEPS, bool W_IMAJOR, bool WHOLE16>
+Choice<GroupedArgs> grouped_choice() { return {grouped_kernel<BM, BN, WM, WN, STEPS, W_IMAJOR, WHOLE16>, BM, BN, WM * WN * 64}; }
 template <int BM, int BN, int WM, int WN, bool W_IMAJOR>
 Choice<GroupedArgs> grouped_f32_choice() { return {grouped_f32_kernel<BM, BN, WM, WN, W_IMAJOR>, BM, BN, WM * WN * 64}; }
 
-// Large tiles need few reads for their products, small ones leave fewer places empty and more workgroups: the largest whose half
-// an expert's rows fill on average, and of which there are as many as compute units.
+// Large tiles need few reads for their products, small ones leave fewer places empty and are more.  By rows an expert has on average,
+// where there are as many tiles as compute units: 256 x 256 from 128 rows on (128 matrices of 1536 x 2048, 256 rows each: 305 us, 128 x 128 325),
+// 128 x 128 from 48 (32 of 5760 x 2880, 64 rows each: 230 us; 64 x 128 271), otherwise 64 x 128 with three steps under way (12 rows each: 149 and
+// 186 us, 5.5 and 5.9 TB/s; 128 x 128 149 and 187; 8 matrices of 512 x 2048: 14 us, 128 x 128 24).
 template <bool W_IMAJOR, bool WHOLE16>
 Choice<GroupedArgs> choose_grouped(int64_t rows, int n_experts, int n) {
   if constexpr (WHOLE16) {
     const int64_t mean = rows / n_experts;
-    const auto tiles = [&](int bm, int bn) { return (mean < 1 ? rows : n_experts * tiles_of(mean, bm)) * tiles_of(n, bn); };
-    if (mean >= 128 && tiles(256, 256) >= kComputeUnits) return grouped_choice<256, 256, 2, 4, W_IMAJOR, WHOLE16>();
-    if (mean >= 12 && tiles(128, 128) >= kComputeUnits) return grouped_choice<128, 128, 2, 4, W_IMAJOR, WHOLE16>();
-    if (tiles(64, 128) >= kComputeUnits) return grouped_choice<64, 128, 2, 2, W_IMAJOR, WHOLE16>();
-    return grouped_choice<64, 64, 2, 2, W_IMAJOR, WHOLE16>();
+    const auto tiles = [&](int tile) { return n_experts * tiles_of(mean, tile) * tiles_of(n, tile); };
+    if (mean >= 128 && tiles(256) >= kComputeUnits) return grouped_choice<256, 256, 2, 4, 2, W_IMAJOR, WHOLE16>();
+    if (mean >= 48 && tiles(128) >= kComputeUnits) return grouped_choice<128, 128, 2, 4, 2, W_IMAJOR, WHOLE16>();
+    return grouped_choice<64, 128, 2, 4, 3, W_IMAJOR, WHOLE16>();
   }
-  return grouped_choice<128, 128, 2, 2, W_IMAJOR, WHOLE16>();
+  return grouped_choice<128, 128, 2, 2, 2, W_IMAJOR, WHOLE16>();
+}
+// Whether the kernel for few rows takes a product: up to 16 rows an expert, and up to 48 Mi weights to read.  Beyond that (16 rows of 1536 x 2048
+// bfloat16: 20.3 us, with tiles 20.8; 4 of 5760 x 2880: 31.8 and 28.3) its reads of 64 bytes a row are slower than those of the tiles.
+bool few_rows(int64_t rows, int n_experts, int n, int k) {
+  return rows <= 16 * int64_t(n_experts) && (rows < n_experts ? rows : n_experts) * int64_t(n) * k <= int64_t(48) << 20;
 }
 
-Choice<WeightGradArgs> choose_weight_grad(int n_experts, int n, int k) {
+// How a weight gradient is split: tiles of the matrices, and parts of each expert's rows where those alone leave half of the compute units
+// without work and the rows are many (192 of them for a part, three steps).  3 experts of 224 x 544, 11000 rows each: 149 -> 30 us; one of
+// 1024 x 1024, 8192 rows: 89 -> 34; but 8 of 1024 x 512, 2048 rows each, 256 tiles in two parts: 38 -> 41, so not there.
+struct WeightGradSplit { int tile, parts; };
+WeightGradSplit split_weight_grad(int dtype, bool whole, int64_t rows, int n_experts, int n, int k) {
   const auto tiles = [&](int b) { return n_experts * tiles_of(n, b) * tiles_of(k, b); };
-  if (tiles(256) >= kComputeUnits) return {weight_grad_kernel<256, 256, 2, 4, true>, 256, 256, 512};
-  if (tiles(128) >= kComputeUnits) return {weight_grad_kernel<128, 128, 2, 4, true>, 128, 128, 512};
-  return {weight_grad_kernel<64, 64, 2, 2, true>, 64, 64, 256};
+  const bool narrow = dtype == MOE_SPEC_F32 || (whole && n <= 64 && k <= 64);
+  if (!narrow && whole && tiles(256) >= kComputeUnits) return {256, 1};
+  const int tile = narrow ? 64 : 128;
+  int64_t parts = tiles(tile) > kComputeUnits / 2 ? 1 : 2 * kComputeUnits / tiles(tile);
+  const int64_t most = rows / n_experts / (3 * kTileK);
+  if (parts > most) parts = most;
+  return {tile, int(parts < 1 ? 1 : parts > 64 ? 64 : parts)};
 }
 
 }  // namespace
@@ -290,7 +397,9 @@ extern "C" int moe_spec_grouped_product(void *stream, int dtype, const void *x, 
   if (n_experts == 1) w_expert_stride = 0;
   GroupedArgs a{x, w, y, ends, x_stride, w_stride, w_expert_stride, y_stride, in, int(rows), n_experts, out, 0, out_dtype == MOE_SPEC_BF16};
   const bool whole = whole16(x, x_stride, in) && whole16(w, w_stride, k) && w_expert_stride % 8 == 0;
-  const Choice<GroupedArgs> c = dtype == MOE_SPEC_F32 ? (transpose ? grouped_f32_choice<64, 64, 2, 2, true>() : grouped_f32_choice<64, 64, 2, 2, false>())
+  const Choice<GroupedArgs> c = !transpose && few_rows(rows, n_experts, n, k)
+                                    ? Choice<GroupedArgs>{dtype == MOE_SPEC_F32 ? grouped_few_kernel<float> : grouped_few_kernel<uint16_t>, 16, 16, kFewBlock}
+                                : dtype == MOE_SPEC_F32 ? (transpose ? grouped_f32_choice<64, 64, 2, 2, true>() : grouped_f32_choice<64, 64, 2, 2, false>())
                                 : transpose           ? (whole ? choose_grouped<true, true>(rows, n_experts, out) : choose_grouped<true, false>(rows, n_experts, out))
                                                       : (whole ? choose_grouped<false, true>(rows, n_experts, out) : choose_grouped<false, false>(rows, n_experts, out));
   a.tiles_n = int(tiles_of(out, c.bn));
@@ -302,9 +411,15 @@ extern "C" int moe_spec_grouped_product(void *stream, int dtype, const void *x, 
   return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "grouped_product: %s", hipGetErrorString(e));
 }
 
+extern "C" size_t moe_spec_grouped_weight_grad_workspace_bytes(int dtype, int64_t rows, int n_experts, int n, int k) {
+  if (!known_type(dtype) || sizes_fault(rows, n_experts, n, k)) return 0;
+  const int parts = split_weight_grad(dtype, true, rows, n_experts, n, k).parts;
+  return parts > 1 ? size_t(parts) * n_experts * n * k * 4 : 0;
+}
+
 extern "C" int moe_spec_grouped_weight_grad(void *stream, int dtype, const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
                                             int64_t rows, int n_experts, int n, int k, const int32_t *ends, int out_dtype, void *dw,
-                                            int64_t dw_stride, int64_t dw_expert_stride) {
+                                            int64_t dw_stride, int64_t dw_expert_stride, void *workspace, size_t workspace_bytes) {
   if (!known_type(dtype)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: unknown dtype %d", dtype);
   if (!known_type(out_dtype)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: unknown out_dtype %d", out_dtype);
   if (const char *why = sizes_fault(rows, n_experts, n, k)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: %s", why);
@@ -319,17 +434,26 @@ extern "C" int moe_spec_grouped_weight_grad(void *stream, int dtype, const void 
   if (rows && (dw == dy || dw == x)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: dw must not be dy or x");
   if (rows <= 1) dy_stride = n, x_stride = k;
   if (n_experts == 1) dw_expert_stride = 0;
-  WeightGradArgs a{dy, x, dw, ends, dy_stride, x_stride, dw_stride, dw_expert_stride, int(rows), n_experts, n, k, 0, 0, out_dtype == MOE_SPEC_BF16};
   const bool whole = whole16(dy, dy_stride, n) && whole16(x, x_stride, k);
+  // the workspace is that of sixteen-byte rows, whatever these are, so that its size goes by sizes alone
+  const WeightGradSplit split = split_weight_grad(dtype, true, rows, n_experts, n, k);
+  const size_t need = moe_spec_grouped_weight_grad_workspace_bytes(dtype, rows, n_experts, n, k);
+  if (need && (!workspace || misaligned(workspace, 16) || workspace_bytes < need))
+    return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: the workspace is null, not aligned to 16 bytes or smaller than %zu bytes", need);
+  WeightGradArgs a{dy, x, dw, ends, dy_stride, x_stride, dw_stride, dw_expert_stride, int(rows), n_experts, n, k, 0, 0, out_dtype == MOE_SPEC_BF16, split.parts,
+                   static_cast<float *>(workspace)};
   const Choice<WeightGradArgs> c = dtype == MOE_SPEC_F32 ? Choice<WeightGradArgs>{weight_grad_f32_kernel<64, 64, 2, 2>, 64, 64, 256}
-                                   : whole               ? choose_weight_grad(n_experts, n, k)
-                                                         : Choice<WeightGradArgs>{weight_grad_kernel<128, 128, 2, 2, false>, 128, 128, 256};
+                                   : !whole              ? Choice<WeightGradArgs>{weight_grad_kernel<128, 128, 2, 2, 2, false>, 128, 128, 256}
+                                   : split.tile == 256   ? Choice<WeightGradArgs>{weight_grad_kernel<256, 256, 2, 4, 2, true>, 256, 256, 512}
+                                   : split.tile == 128   ? Choice<WeightGradArgs>{weight_grad_kernel<128, 128, 2, 4, 2, true>, 128, 128, 512}
+                                                         : Choice<WeightGradArgs>{weight_grad_kernel<64, 64, 2, 2, 4, true>, 64, 64, 256};
   a.tiles_n = int(tiles_of(n, c.bm));
   a.tiles_k = int(tiles_of(k, c.bn));
-  const unsigned grid = grid_of(int64_t(n_experts) * a.tiles_n * a.tiles_k, c.threads);
+  const unsigned grid = grid_of(int64_t(n_experts) * a.tiles_n * a.tiles_k * a.parts, c.threads);
   if (!grid) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: more experts' values than one launch can take");
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const OnDeviceOf on(s);
-  const hipError_t e = on.error() == hipSuccess ? launch(c.kernel, grid, c.threads, s, a) : on.error();
+  hipError_t e = on.error() == hipSuccess ? launch(c.kernel, grid, c.threads, s, a) : on.error();
+  if (e == hipSuccess && a.parts > 1) e = launch(weight_grad_join_kernel, unsigned((int64_t(n_experts) * n * tiles_of(k, 4) + 255) / 256), 256, s, a);
   return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "grouped_weight_grad: %s", hipGetErrorString(e));
 }

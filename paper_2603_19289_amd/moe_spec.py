@@ -132,7 +132,9 @@ def lib():
         L.moe_spec_adamw_step.argtypes = [vp, C.POINTER(AdamWTensor), i32, C.POINTER(AdamWConfig)]
         L.moe_spec_adamw_read_moments.argtypes = [vp, C.POINTER(AdamWTensor), i32, i32, C.POINTER(vp), C.POINTER(vp)]
         L.moe_spec_grouped_product.argtypes = [vp, i32, vp, i64, i64, vp, i64, i64, i32, i32, i32, vp, i32, i32, vp, i64]
-        L.moe_spec_grouped_weight_grad.argtypes = [vp, i32, vp, i64, vp, i64, i64, i32, i32, i32, vp, i32, vp, i64, i64]
+        L.moe_spec_grouped_weight_grad_workspace_bytes.argtypes = [i32, i64, i32, i32, i32]
+        L.moe_spec_grouped_weight_grad_workspace_bytes.restype = sz
+        L.moe_spec_grouped_weight_grad.argtypes = [vp, i32, vp, i64, vp, i64, i64, i32, i32, i32, vp, i32, vp, i64, i64, vp, sz]
         L.moe_spec_swiglu_forward.argtypes = [vp, i32, vp, i64, i64, i32, vp, vp, i64]
         L.moe_spec_swiglu_backward.argtypes = [vp, i32, vp, i64, vp, i64, i64, i32, vp, vp, i64, vp]
         L.moe_spec_orthogonalise_workspace_bytes.argtypes = [i64, i32, i32]
@@ -294,10 +296,14 @@ def moe_spec_grouped_product(stream, dtype, x, x_stride, rows, w, w_stride, w_ex
                                                 transpose, out_dtype, y, y_stride))
 
 
+def moe_spec_grouped_weight_grad_workspace_bytes(dtype, rows, n_experts, n, k) -> int:
+    return lib().moe_spec_grouped_weight_grad_workspace_bytes(dtype, rows, n_experts, n, k)
+
+
 def moe_spec_grouped_weight_grad(stream, dtype, dy, dy_stride, x, x_stride, rows, n_experts, n, k, ends, out_dtype, dw, dw_stride,
-                                 dw_expert_stride):
+                                 dw_expert_stride, workspace, workspace_bytes):
     _check_train(lib().moe_spec_grouped_weight_grad(stream, dtype, dy, dy_stride, x, x_stride, rows, n_experts, n, k, ends, out_dtype, dw,
-                                                    dw_stride, dw_expert_stride))
+                                                    dw_stride, dw_expert_stride, workspace, workspace_bytes))
 
 
 def moe_spec_swiglu_forward(stream, dtype, a, a_stride, rows, cols, weight, h, h_stride):

@@ -367,8 +367,11 @@ def grouped_weight_grad(dy: torch.Tensor, x: torch.Tensor, ends: torch.Tensor, *
     at = _groups(ends, experts, x.device)
     given = out is not None
     out = _out(out, "out", (experts, n, k), kind, x)
-    _queue(x.device, M.lib().moe_spec_grouped_weight_grad, t, dy.data_ptr(), dy.stride(0), x.data_ptr(), x.stride(0), x.shape[0], experts,
-           n, k, at, _TYPES[kind], out.data_ptr(), out.stride(1), out.stride(0))
+    lib = M.lib()
+    need = lib.moe_spec_grouped_weight_grad_workspace_bytes(t, x.shape[0], experts, n, k)
+    space = x.new_empty(need, dtype=torch.uint8) if need else None
+    _queue(x.device, lib.moe_spec_grouped_weight_grad, t, dy.data_ptr(), dy.stride(0), x.data_ptr(), x.stride(0), x.shape[0], experts,
+           n, k, at, _TYPES[kind], out.data_ptr(), out.stride(1), out.stride(0), space.data_ptr() if need else None, need)
     if given:
         increment_version(out)
     return out

@@ -37,7 +37,7 @@ def test_grouped_product_refuses(bad, word):
 
 def weight_grad(**kw):
     a = dict(stream=None, dtype=M.BF16, dy=ADDR, dy_stride=32, x=ADDR * 2, x_stride=64, rows=40, n_experts=4, n=32, k=64, ends=ADDR, out_dtype=M.F32,
-             dw=ADDR * 3, dw_stride=64, dw_expert_stride=32 * 64)
+             dw=ADDR * 3, dw_stride=64, dw_expert_stride=32 * 64, workspace=ADDR, workspace_bytes=1 << 30)
     a.update(kw)
     return M.lib().moe_spec_grouped_weight_grad(*a.values())
 
@@ -46,9 +46,20 @@ def weight_grad(**kw):
                                       (dict(n=65537), "n and k"), (dict(k=0), "n and k"), (dict(dy=None), "dy is null"), (dict(dy=ADDR + 1), "dy is not aligned"),
                                       (dict(x=None), "x is null"), (dict(x_stride=-1), "x has"), (dict(dw=None), "dw is null"), (dict(dw=ADDR * 3 + 2), "dw is not aligned"),
                                       (dict(dw_stride=63), "dw has"), (dict(dw_expert_stride=32 * 64 - 1), "dw_expert_stride"), (dict(dw=ADDR), "dw must not"),
-                                      (dict(ends=None), "ends")])
+                                      (dict(ends=None), "ends"), (dict(rows=4000, workspace=None), "workspace"), (dict(rows=4000, workspace=ADDR + 8), "workspace"),
+                                      (dict(rows=4000, workspace_bytes=8), "workspace")])
 def test_grouped_weight_grad_refuses(bad, word):
     refused(weight_grad(**bad), "grouped_weight_grad", word)
+
+
+def test_weight_grad_workspace():
+    size = M.moe_spec_grouped_weight_grad_workspace_bytes
+    for dtype in (M.F32, M.BF16):
+        assert size(dtype, -1, 4, 8, 8) == size(dtype, 4, 0, 8, 8) == size(dtype, 4, 257, 8, 8) == size(dtype, 4, 1, 0, 8) == size(dtype, 4, 1, 8, 65537) == 0
+        assert size(dtype, 0, 4, 32, 64) == size(dtype, 700, 4, 32, 64) == 0 and size(dtype, 100000, 128, 1536, 2048) == 0
+        assert size(dtype, 20000, 4, 32, 64) % (4 * 32 * 64 * 4) == 0 < size(dtype, 20000, 4, 32, 64) <= 64 * 4 * 32 * 64 * 4
+        assert weight_grad(dtype=dtype, dy=ADDR * 4, x=ADDR * 5, dw_stride=64, workspace=None, workspace_bytes=0, rows=-1) == M.EINVAL
+    assert size(7, 100000, 4, 32, 64) == 0
 
 
 def test_too_large_for_a_launch():

@@ -128,6 +128,22 @@ def test_larger_groups(case, dtype):
     assert not y[ends[-1]:].any() and not dx[ends[-1]:].any()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes,n,k", [([9000, 0, 5, 700], 40, 72), ([20000], 56, 24), ([3000, 6000], 200, 136), ([4000, 4100], 75, 33), ([12345, 1, 0], 9, 1)], ids=str)
+def test_weight_gradients_of_long_groups(sizes, n, k, dtype):
+    """Rows that are split among workgroups and whose sums are joined: whole numbers that float holds, equal whatever the order."""
+    from paper_2603_19289_amd import training as T
+    ends, rows, n, k = groups((sizes, n, k))
+    g = torch.Generator("cuda").manual_seed(rows)
+    t = TYPES[dtype]
+    dy, x = (torch.randint(-3, 4, s, generator=g, device="cuda").to(t) for s in ((rows + 3, n), (rows + 3, k)))
+    want = torch.stack([dy[b:f].double().t() @ x[b:f].double() for b, f in bounds(ends, rows)])
+    for kind in (torch.float32, torch.bfloat16):
+        out = torch.full((len(sizes), n, k + 5), 2.0, dtype=kind, device="cuda")
+        T.grouped_weight_grad(dy, x, i32(ends), dtype=kind, out=out[:, :, :k])
+        assert torch.equal(out[:, :, :k], want.to(kind)) and torch.all(out[:, :, k:] == 2.0)
+
+
 @pytest.mark.parametrize("dtype,rows,experts,n,k", [("f32", 333, 3, 130, 700), ("bf16", 333, 3, 136, 704), ("bf16", 50, 7, 96, 2048), ("bf16", 301, 2, 75, 333)])
 def test_products_of_any_values(dtype, rows, experts, n, k):
     """2 u for each term of a sum, and for float32 the products' own rounding; half a step of what goes out."""
