@@ -16,9 +16,11 @@ struct OperandTileF32 {
   int rows;
   float4 held[kEach];
 
-  __device__ __forceinline__ void begin(const float *origin, int64_t ld, int rows_, int tid) {
+  // Every second step from the step `first` on.
+  __device__ __forceinline__ void begin(const float *origin, int64_t ld, int rows_, int tid, int first) {
     rows = rows_;
-    step = IMAJOR ? ld * kStep : kStep;
+    step = (IMAJOR ? ld * kStep : kStep) * 2;
+    origin += first * (step / 2);
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
       const int c = j * THREADS + tid, r = c / kAcross, col = c % kAcross * 4;
@@ -60,7 +62,7 @@ struct TileProductF32 {
   static constexpr int kThreads = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
   using A = OperandTileF32<BM, A_IMAJOR, kThreads>;
   using B = OperandTileF32<BN, B_IMAJOR, kThreads>;
-  static constexpr int kLds = (A::kFloats + B::kFloats) * 4;
+  static constexpr int kPart = A::kFloats + B::kFloats, kLds = 2 * kPart * 4;
   f32x4_t acc[FM][FN];
 
   __device__ __forceinline__ void run(char *lds_bytes, const float *a, int64_t lda, int a_rows, const float *b, int64_t ldb, int b_rows, int64_t K) {
@@ -72,34 +74,39 @@ struct TileProductF32 {
 #pragma unroll
       for (int h = 0; h < FN; ++h) acc[f][h] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     if (K <= 0) return;
-    A ta;
-    B tb;
-    ta.begin(a, lda, a_rows, tid);
-    tb.begin(b, ldb, b_rows, tid);
-    const auto left = [](int64_t k) { return int(k < A::kStep ? k : int64_t(A::kStep)); };
-    ta.issue(left(K), tid);
-    tb.issue(left(K), tid);
-    for (int64_t k = K; k > 0; k -= A::kStep) {
-      ta.land(lds, tid);
-      tb.land(lds + A::kFloats, tid);
+    // two steps are on their way in registers, one is in LDS while another goes there: one barrier a step
+    A ta[2];
+    B tb[2];
+    const auto left = [](int64_t k) { return int(k < A::kStep ? (k > 0 ? k : 0) : int64_t(A::kStep)); };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      ta[i].begin(a, lda, a_rows, tid, i);
+      tb[i].begin(b, ldb, b_rows, tid, i);
+      ta[i].issue(left(K - i * A::kStep), tid);
+      tb[i].issue(left(K - i * A::kStep), tid);
+    }
+    const auto step = [&](int64_t k, A &now_a, B &now_b, float *part) {
+      now_a.land(part, tid);
+      now_b.land(part + A::kFloats, tid);
       __syncthreads();
-      if (k > A::kStep) {
-        ta.issue(left(k - A::kStep), tid);
-        tb.issue(left(k - A::kStep), tid);
-      }
+      now_a.issue(left(k - 2 * A::kStep), tid);
+      now_b.issue(left(k - 2 * A::kStep), tid);
 #pragma unroll
       for (int kk = 0; kk < A::kStep; kk += 4) {
         float va[FM], vb[FN];
 #pragma unroll
-        for (int f = 0; f < FM; ++f) va[f] = A::value(lds, row + 16 * f, kk, lane);
+        for (int f = 0; f < FM; ++f) va[f] = A::value(part, row + 16 * f, kk, lane);
 #pragma unroll
-        for (int h = 0; h < FN; ++h) vb[h] = B::value(lds + A::kFloats, col + 16 * h, kk, lane);
+        for (int h = 0; h < FN; ++h) vb[h] = B::value(part + A::kFloats, col + 16 * h, kk, lane);
 #pragma unroll
         for (int f = 0; f < FM; ++f)
 #pragma unroll
           for (int h = 0; h < FN; ++h) acc[f][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(vb[h], va[f], acc[f][h], 0, 0, 0);
       }
-      __syncthreads();
+    };
+    for (int64_t k = K; k > 0; k -= 2 * A::kStep) {
+      step(k, ta[0], tb[0], lds);
+      if (k > A::kStep) step(k - A::kStep, ta[1], tb[1], lds + kPart);
     }
   }
 };

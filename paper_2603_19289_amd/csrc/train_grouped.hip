@@ -234,12 +234,14 @@ struct WeightGradArgs {
   float *partial;              // [parts, n_experts, n, k]
 };
 
+// Each die gets an eighth of every expert's tiles (another one for each expert, where eighths differ), since experts differ in their rows: where dies
+// had experts of their own, the last one to finish kept the others waiting (65536 rows over 128 experts: DIEUS us).
 template <typename P, int BM, int BN, int WM, int WN, typename Elem>
 __device__ __forceinline__ void weight_grad_tile(const WeightGradArgs &a, char *lds) {
   const int per = a.tiles_n * a.tiles_k;
-  const int64_t total = int64_t(per) * a.n_experts * a.parts, share = (total + 7) / 8, slot = blockIdx.x / 8, logical = blockIdx.x % 8 * share + slot;
-  if (slot >= share || logical >= total) return;
-  const int group = int(logical / per), tile = int(logical % per), expert = group / a.parts, part = group % a.parts;
+  const unsigned most = (per + 7) / 8, slot = blockIdx.x / 8, group = slot / most, die = (blockIdx.x + group) % 8;
+  const int tile = int(int64_t(die) * per / 8 + slot % most), expert = group / a.parts, part = group % a.parts;
+  if (tile >= (int64_t(die) + 1) * per / 8) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int before = 0;
   for (int e = lane; e < expert; e += 64) before = max(before, a.ends[e]);
@@ -449,7 +451,7 @@ extern "C" int moe_spec_grouped_weight_grad(void *stream, int dtype, const void 
                                                          : Choice<WeightGradArgs>{weight_grad_kernel<64, 64, 2, 2, 4, true>, 64, 64, 256};
   a.tiles_n = int(tiles_of(n, c.bm));
   a.tiles_k = int(tiles_of(k, c.bn));
-  const unsigned grid = grid_of(int64_t(n_experts) * a.tiles_n * a.tiles_k * a.parts, c.threads);
+  const unsigned grid = grid_of(int64_t(n_experts) * a.parts * tiles_of(int64_t(a.tiles_n) * a.tiles_k, 8) * 8, c.threads);
   if (!grid) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: more experts' values than one launch can take");
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const OnDeviceOf on(s);

@@ -13,7 +13,7 @@
 namespace moe_spec {
 namespace {
 
-constexpr int kMuonBlock = 256, kPerMuonLaunch = 24, kSliceValues = 16384, kTurn = 64;
+constexpr int kMuonBlock = 256, kPerMuonLaunch = 24, kSliceValues = 4096, kTurn = 64;
 constexpr float kHeld = 64.0f;
 
 // A stack of matrices of one size.
@@ -45,27 +45,52 @@ __device__ __forceinline__ int stack_of(const uint32_t (&first)[kPerMuonLaunch],
   return which;
 }
 
-// Eight values of a gradient.
+// The gradient and the momentum of a chunk of eight values, where there is one.
 template <typename GT>
-__device__ __forceinline__ void gradient8(const MuonStack &t, int64_t matrix, int row, int c, int n, float (&g)[8]) {
-  Run<GT, 8> r;
-  r.load(static_cast<const GT *>(t.grad) + matrix * t.grad_matrix + row * t.grad_stride + c, n);
-  r.get(g);
-}
-
-// What is orthogonalised: the gradient, or the momentum with the gradient in it.  STEP: the momentum has been updated already.
-template <typename GT>
-__device__ __forceinline__ void direction8(const MuonArgs &a, const MuonStack &t, float scale, int64_t matrix, int row, int c, int n, float (&u)[8]) {
+struct Chunk {
+  Run<GT, 8> g;
+  Run<float, 8> m;
+  int row, col, n;                       // n: how many exist (at most eight count), none or less: no chunk
+  __device__ __forceinline__ int64_t at(const MuonStack &t, int64_t matrix) const { return (matrix * t.rows + row) * t.cols + col; }
+  __device__ __forceinline__ void load(const MuonStack &t, int64_t matrix) {
+    if (n <= 0) return;
+    g.load(static_cast<const GT *>(t.grad) + matrix * t.grad_matrix + row * t.grad_stride + col, n);
+    if (t.momentum) m.load(t.momentum + at(t, matrix), n);
+  }
+  // What is orthogonalised: the gradient, or the momentum (which is up to date) with the gradient in it.
+  __device__ __forceinline__ void direction(const MuonArgs &a, const MuonStack &t, float scale, float (&u)[8]) const {
 #pragma clang fp contract(off)
-  gradient8<GT>(t, matrix, row, c, n, u);
-  if (!t.momentum) return;
-  Run<float, 8> rm;
-  float m[8];
-  rm.load(t.momentum + matrix * t.rows * t.cols + int64_t(row) * t.cols + c, n);
-  rm.get(m);
+    g.get(u);
+    if (!t.momentum) return;
+    float v[8];
+    m.get(v);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) u[i] = a.nesterov ? u[i] * scale + m[i] * a.mu : m[i];
-}
+    for (int j = 0; j < 8; ++j) u[j] = a.nesterov ? u[j] * scale + v[j] * a.mu : v[j];
+  }
+};
+
+// A workgroup's part of a matrix that is gone through as it lies: whole rows, kAhead chunks a thread at a time.  Parts of 4096 values in two rounds of
+// loads at once stream at 4.4 (momentum), 4.8 (X_0) and 4.8 TB/s (result) over 75 M values and start small matrices on more compute units; parts of
+// 16384 at 4.0, 4.7 and 4.7, with one chunk at a time 4.7, 4.5 and 4.4.
+constexpr int kAhead = 2;
+struct Slice {
+  int64_t matrix;
+  int row0, chunks, across;
+  __device__ __forceinline__ Slice(const MuonStack &t, uint32_t at) {
+    matrix = at / uint32_t(t.slices);
+    const int slice = at % uint32_t(t.slices);
+    across = (t.cols + 7) / 8;
+    row0 = slice * t.slice_rows;
+    chunks = min(t.slice_rows, t.rows - row0) * across;
+  }
+  template <typename C>
+  __device__ __forceinline__ void place(C &c, int i, int cols) const {
+    const int r = i / across;
+    c.row = row0 + r;
+    c.col = (i - r * across) * 8;
+    c.n = i < chunks ? cols - c.col : 0;
+  }
+};
 
 // Momentum and sums of squares, a slice of a matrix's rows a workgroup.
 template <typename GT>
@@ -74,37 +99,42 @@ __global__ __launch_bounds__(kMuonBlock) void muon_begin_kernel(const MuonArgs a
   const int which = stack_of(a.first, blockIdx.x);
   const MuonStack &t = a.t[which];
   const uint32_t at = blockIdx.x - a.first[which];
-  const int64_t matrix = at / t.slices;
-  const int slice = at % t.slices, row0 = slice * t.slice_rows, rows = min(t.slice_rows, t.rows - row0), across = (t.cols + 7) / 8;
+  const Slice slice(t, at);
   const float scale = a.scale_dev ? a.scale * *a.scale_dev : a.scale;
   double sum = 0.0;
-  for (int i = threadIdx.x; i < rows * across; i += kMuonBlock) {
-    const int row = row0 + i / across, c = i % across * 8, n = t.cols - c;
-    float u[8];
-    gradient8<GT>(t, matrix, row, c, n, u);
-    if (t.momentum) {
-      float *m_at = t.momentum + matrix * t.rows * t.cols + int64_t(row) * t.cols + c;
-      Run<float, 8> rm;
-      float m[8];
-      rm.load(m_at, n);
-      rm.get(m);
+  for (int i = threadIdx.x; i < slice.chunks; i += kAhead * kMuonBlock) {
+    Chunk<GT> c[kAhead];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float g = u[j] * scale;
-        m[j] = m[j] * a.mu + g;
-        u[j] = a.nesterov ? g + m[j] * a.mu : m[j];
-      }
-      store_run<float, 8>(m_at, m, n);
+    for (int q = 0; q < kAhead; ++q) {
+      slice.place(c[q], i + q * kMuonBlock, t.cols);
+      c[q].load(t, slice.matrix);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) if (j < n) sum += double(u[j]) * double(u[j]);
+    for (int q = 0; q < kAhead; ++q) {
+      if (c[q].n <= 0) continue;
+      float u[8];
+      c[q].g.get(u);
+      if (t.momentum) {
+        float m[8];
+        c[q].m.get(m);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float g = u[j] * scale;
+          m[j] = m[j] * a.mu + g;
+          u[j] = a.nesterov ? g + m[j] * a.mu : m[j];
+        }
+        store_run<float, 8>(t.momentum + c[q].at(t, slice.matrix), m, c[q].n);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) if (j < c[q].n) sum += double(u[j]) * double(u[j]);
+    }
   }
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
   __shared__ double part[kMuonBlock / 64];
   if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) t.partial[matrix * t.slices + slice] = (part[0] + part[1]) + (part[2] + part[3]);
+  if (threadIdx.x == 0) t.partial[at] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
 __device__ __forceinline__ uint16_t to_f16(float v) { return __builtin_bit_cast(uint16_t, _Float16(v)); }
@@ -132,101 +162,157 @@ __device__ __forceinline__ Normaliser normaliser(const MuonStack &t, int64_t mat
   return {float(double(kHeld) / part), -exponent};
 }
 
-// X_0 as float16, laid on its side where the matrix is upright: tiles of 64 x 64 then go through LDS.
+// X_0 as float16.  A matrix that is not upright as it lies; an upright one is laid on its side, tiles of 64 x 64 through LDS.
+struct Turn {
+  int64_t matrix;
+  int row0, col0;
+  __device__ __forceinline__ Turn(const MuonStack &t, uint32_t at) {
+    const uint32_t across = (t.cols + kTurn - 1) / kTurn, down = (t.rows + kTurn - 1) / kTurn;
+    matrix = at / (across * down);
+    const int q = at % (across * down);
+    row0 = q / int(across) * kTurn;
+    col0 = q % int(across) * kTurn;
+  }
+};
+
 template <typename GT>
 __global__ __launch_bounds__(kMuonBlock) void muon_normalise_kernel(const MuonArgs a) {
   __shared__ __attribute__((aligned(16))) uint16_t tile[kTurn][kTurn + 8];
   const int which = stack_of(a.first, blockIdx.x);
   const MuonStack &t = a.t[which];
-  const int across = (t.cols + kTurn - 1) / kTurn, down = (t.rows + kTurn - 1) / kTurn;
   const uint32_t at = blockIdx.x - a.first[which];
-  const int64_t matrix = at / uint32_t(across * down);
-  const int q = at % uint32_t(across * down), row0 = q / across * kTurn, col0 = q % across * kTurn;
   const float scale = a.scale_dev ? a.scale * *a.scale_dev : a.scale;
-  const Normaliser normal = normaliser(t, matrix);
-  const bool upright = t.rows > t.cols;
-  uint16_t *x = t.x[0] + matrix * t.m * t.ld_n;
-#pragma unroll
-  for (int i = threadIdx.x; i < kTurn * kTurn / 8; i += kMuonBlock) {
-    const int r = i / (kTurn / 8), c = i % (kTurn / 8) * 8, row = row0 + r, col = col0 + c;
+  // eight values of X, zeros behind a row's last
+  const auto held = [&](const Normaliser &normal, const Chunk<GT> &c) {
+    uint16_t e[8];
     float u[8];
-    uint16_t e[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (row < t.rows && col < t.cols) {
-      direction8<GT>(a, t, scale, matrix, row, col, t.cols - col, u);
+    if (c.n > 0) c.direction(a, t, scale, u);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) e[j] = col + j < t.cols ? normal(u[j]) : uint16_t(0);
+    for (int j = 0; j < 8; ++j) e[j] = j < c.n ? normal(u[j]) : uint16_t(0);
+    uint4 v;
+    __builtin_memcpy(&v, e, 16);
+    return v;
+  };
+  if (t.rows <= t.cols) {
+    const Slice slice(t, at);
+    const Normaliser normal = normaliser(t, slice.matrix);
+    uint16_t *x = t.x[0] + slice.matrix * t.m * t.ld_n;
+    for (int i = threadIdx.x; i < slice.chunks; i += kAhead * kMuonBlock) {
+      Chunk<GT> c[kAhead];
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        slice.place(c[q], i + q * kMuonBlock, t.cols);
+        c[q].load(t, slice.matrix);
+      }
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q)
+        if (c[q].n > 0) *reinterpret_cast<uint4 *>(x + int64_t(c[q].row) * t.ld_n + c[q].col) = held(normal, c[q]);
     }
-    if (upright) __builtin_memcpy(&tile[r][c], e, 16);
-    else if (row < t.rows && col < t.ld_n) __builtin_memcpy(x + int64_t(row) * t.ld_n + col, e, 16);
+    return;
   }
-  if (!upright) return;
+  const Turn turn(t, at);
+  const Normaliser normal = normaliser(t, turn.matrix);
+  uint16_t *x = t.x[0] + turn.matrix * t.m * t.ld_n;
+  Chunk<GT> c[2];
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int i = threadIdx.x + q * kMuonBlock;
+    c[q].row = turn.row0 + i / (kTurn / 8);
+    c[q].col = turn.col0 + i % (kTurn / 8) * 8;
+    c[q].n = c[q].row < t.rows ? t.cols - c[q].col : 0;
+    c[q].load(t, turn.matrix);
+  }
+#pragma unroll
+  for (int q = 0; q < 2; ++q) *reinterpret_cast<uint4 *>(&tile[c[q].row - turn.row0][c[q].col - turn.col0]) = held(normal, c[q]);
   __syncthreads();
 #pragma unroll
-  for (int i = threadIdx.x; i < kTurn * kTurn / 8; i += kMuonBlock) {
-    const int c = i / (kTurn / 8), r = i % (kTurn / 8) * 8;              // a column of the matrix is a row of X
-    if (col0 + c >= t.cols || row0 + r >= t.ld_n) continue;
+  for (int q = 0; q < 2; ++q) {
+    const int i = threadIdx.x + q * kMuonBlock, across = i / (kTurn / 8), r = i % (kTurn / 8) * 8;      // a column of the matrix is a row of X
+    if (turn.col0 + across >= t.cols || turn.row0 + r >= t.ld_n) continue;
     uint16_t e[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = tile[r + j][c];
-    __builtin_memcpy(x + int64_t(col0 + c) * t.ld_n + row0 + r, e, 16);
+    for (int j = 0; j < 8; ++j) e[j] = tile[r + j][across];
+    __builtin_memcpy(x + int64_t(turn.col0 + across) * t.ld_n + turn.row0 + r, e, 16);
   }
 }
 
-// The result: p <- p decay - rate o and its copy, or o itself.
-template <typename OT>
-__device__ __forceinline__ void finish8(const MuonArgs &a, const MuonStack &t, int64_t matrix, int row, int c, int n, const float (&o)[8]) {
+// The result of eight values: p <- p decay - rate o and its copy, or o itself.
+struct Result {
+  Run<float, 8> p;
+  uint4 x;
+  int row, col, n;
+  __device__ __forceinline__ int64_t at(const MuonStack &t, int64_t matrix) const { return (matrix * t.rows + row) * t.cols + col; }
+  __device__ __forceinline__ void load(const MuonStack &t, int64_t matrix) {
+    if (n > 0 && t.p) p.load(t.p + at(t, matrix), n);
+  }
+  __device__ __forceinline__ void store(const MuonArgs &a, const MuonStack &t, int64_t matrix) const {
 #pragma clang fp contract(off)
-  if (t.p) {
-    float *p_at = t.p + matrix * t.rows * t.cols + int64_t(row) * t.cols + c;
-    Run<float, 8> rp;
-    float p[8];
-    rp.load(p_at, n);
-    rp.get(p);
-    const float rate = a.rate * sqrtf(float(t.n));
+    if (n <= 0) return;
+    uint16_t e[8];
+    __builtin_memcpy(e, &x, 16);
+    float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) p[j] = p[j] * a.decay - o[j] * rate;
-    store_run<float, 8>(p_at, p, n);
-    if (t.out) store_run<OT, 8>(static_cast<OT *>(t.out) + matrix * t.out_matrix + row * t.out_stride + c, p, n);
-  } else {
-    store_run<OT, 8>(static_cast<OT *>(t.out) + matrix * t.out_matrix + row * t.out_stride + c, o, n);
+    for (int j = 0; j < 8; ++j) v[j] = from_f16(e[j]) * (1.0f / kHeld);
+    if (t.p) {
+      float old[8];
+      p.get(old);
+      const float rate = a.rate * sqrtf(float(t.n));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = old[j] * a.decay - v[j] * rate;
+      store_run<float, 8>(t.p + at(t, matrix), v, n);
+    }
+    if (t.out) store_run<uint16_t, 8>(static_cast<uint16_t *>(t.out) + matrix * t.out_matrix + row * t.out_stride + col, v, n);
   }
-}
+};
 
-template <typename OT>
 __global__ __launch_bounds__(kMuonBlock) void muon_finish_kernel(const MuonArgs a) {
   __shared__ __attribute__((aligned(16))) uint16_t tile[kTurn][kTurn + 8];
   const int which = stack_of(a.first, blockIdx.x);
   const MuonStack &t = a.t[which];
-  const int across = (t.cols + kTurn - 1) / kTurn, down = (t.rows + kTurn - 1) / kTurn;
   const uint32_t at = blockIdx.x - a.first[which];
-  const int64_t matrix = at / uint32_t(across * down);
-  const int q = at % uint32_t(across * down), row0 = q / across * kTurn, col0 = q % across * kTurn;
-  const bool upright = t.rows > t.cols;
-  const uint16_t *x = t.x[a.which] + matrix * t.m * t.ld_n;
-  if (upright) {
+  if (t.rows <= t.cols) {
+    const Slice slice(t, at);
+    const uint16_t *x = t.x[a.which] + slice.matrix * t.m * t.ld_n;
+    for (int i = threadIdx.x; i < slice.chunks; i += kAhead * kMuonBlock) {
+      Result r[kAhead];
 #pragma unroll
-    for (int i = threadIdx.x; i < kTurn * kTurn / 8; i += kMuonBlock) {
-      const int c = i / (kTurn / 8), r = i % (kTurn / 8) * 8;
-      uint4 v = {0, 0, 0, 0};
-      if (col0 + c < t.cols && row0 + r < t.ld_n) v = load_raw<uint4>(x + int64_t(col0 + c) * t.ld_n + row0 + r);
-      uint16_t e[8];
-      __builtin_memcpy(e, &v, 16);
+      for (int q = 0; q < kAhead; ++q) {
+        slice.place(r[q], i + q * kMuonBlock, t.cols);
+        r[q].load(t, slice.matrix);
+        if (r[q].n > 0) r[q].x = *reinterpret_cast<const uint4 *>(x + int64_t(r[q].row) * t.ld_n + r[q].col);
+      }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) tile[r + j][c] = e[j];
+      for (int q = 0; q < kAhead; ++q) r[q].store(a, t, slice.matrix);
     }
-    __syncthreads();
+    return;
+  }
+  const Turn turn(t, at);
+  const uint16_t *x = t.x[a.which] + turn.matrix * t.m * t.ld_n;
+  Result r[2];
+  uint4 v[2];
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int i = threadIdx.x + q * kMuonBlock, across = i / (kTurn / 8), down = i % (kTurn / 8) * 8;
+    v[q] = uint4{0, 0, 0, 0};
+    if (turn.col0 + across < t.cols && turn.row0 + down < t.ld_n) v[q] = *reinterpret_cast<const uint4 *>(x + int64_t(turn.col0 + across) * t.ld_n + turn.row0 + down);
+    r[q].row = turn.row0 + i / (kTurn / 8);
+    r[q].col = turn.col0 + i % (kTurn / 8) * 8;
+    r[q].n = r[q].row < t.rows ? t.cols - r[q].col : 0;
+    r[q].load(t, turn.matrix);
   }
 #pragma unroll
-  for (int i = threadIdx.x; i < kTurn * kTurn / 8; i += kMuonBlock) {
-    const int r = i / (kTurn / 8), c = i % (kTurn / 8) * 8, row = row0 + r, col = col0 + c;
-    if (row >= t.rows || col >= t.cols) continue;
+  for (int q = 0; q < 2; ++q) {
+    const int i = threadIdx.x + q * kMuonBlock, across = i / (kTurn / 8), down = i % (kTurn / 8) * 8;
     uint16_t e[8];
-    if (upright) __builtin_memcpy(e, &tile[r][c], 16);
-    else __builtin_memcpy(e, x + int64_t(row) * t.ld_n + col, 16);
-    float o[8];
+    __builtin_memcpy(e, &v[q], 16);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = from_f16(e[j]) * (1.0f / kHeld);
-    finish8<OT>(a, t, matrix, row, col, t.cols - col, o);
+    for (int j = 0; j < 8; ++j) tile[down + j][across] = e[j];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    r[q].x = *reinterpret_cast<const uint4 *>(&tile[r[q].row - turn.row0][r[q].col - turn.col0]);
+    r[q].store(a, t, turn.matrix);
   }
 }
 
@@ -234,10 +320,10 @@ __global__ __launch_bounds__(kMuonBlock) void muon_finish_kernel(const MuonArgs 
 // only tiles on and below the diagonal are worked out, and written to both places.
 enum MuonProduct { SQUARE, POLYNOMIAL, APPLY };
 
-template <int TILE, int WM, int WN, MuonProduct KIND>
+template <int TILE, int WM, int WN, int STEPS, MuonProduct KIND>
 __global__ __launch_bounds__(WM *WN * 64) void muon_product_kernel(const MuonArgs a) {
   constexpr bool SYMMETRIC = KIND != APPLY;
-  using P = TileProduct<F16, TILE, TILE, WM, WN, false, KIND == APPLY, true>;
+  using P = TileProduct<F16, TILE, TILE, WM, WN, false, KIND == APPLY, true, STEPS>;
   using R = ResultTile<TILE / WM, TILE / WN>;
   __shared__ __attribute__((aligned(16))) char lds[P::kLds];
   const uint32_t share = (a.total + 7) / 8, logical = blockIdx.x % 8 * share + blockIdx.x / 8;      // a die gets a run of tiles
@@ -259,11 +345,10 @@ __global__ __launch_bounds__(WM *WN * 64) void muon_product_kernel(const MuonArg
   const int row0 = tile_row * TILE, col0 = tile_col * TILE;
   const uint16_t *x = t.x[a.which] + matrix * t.m * t.ld_n, *ta = t.a + matrix * t.m * t.ld_m, *tb = t.b + matrix * t.m * t.ld_m;
   P p;
-  const int rows = min(TILE, t.m - row0), some = min(TILE, cols - col0);
-  // X may have rows of 65536 values and A of as many: the strides that a tile takes at most
-  if constexpr (KIND == SQUARE) p.run(lds, x + int64_t(row0) * t.ld_n, t.ld_n, rows, x + int64_t(col0) * t.ld_n, t.ld_n, some, t.n);
-  if constexpr (KIND == POLYNOMIAL) p.run(lds, ta + int64_t(row0) * t.ld_m, t.ld_m, rows, ta + int64_t(col0) * t.ld_m, t.ld_m, some, t.m);
-  if constexpr (KIND == APPLY) p.run(lds, tb + int64_t(row0) * t.ld_m, t.ld_m, rows, x + col0, t.ld_n, some, t.m);
+  const int rows = min(TILE, t.m - row0), some = min(TILE, cols - col0), K = KIND == SQUARE ? t.n : t.m;
+  if constexpr (KIND == SQUARE) p.run(lds, x + int64_t(row0) * t.ld_n, t.ld_n, rows, x + int64_t(col0) * t.ld_n, t.ld_n, some, K);
+  if constexpr (KIND == POLYNOMIAL) p.run(lds, ta + int64_t(row0) * t.ld_m, t.ld_m, rows, ta + int64_t(col0) * t.ld_m, t.ld_m, some, K);
+  if constexpr (KIND == APPLY) p.run(lds, tb + int64_t(row0) * t.ld_m, t.ld_m, rows, x + col0, t.ld_n, some, K);
   const int ld = SYMMETRIC ? t.ld_m : t.ld_n;
   uint16_t *out = KIND == APPLY ? t.x[a.which ^ 1] + matrix * t.m * t.ld_n : (KIND == SQUARE ? t.a : t.b) + matrix * t.m * t.ld_m;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
@@ -356,29 +441,38 @@ void firsts(MuonArgs &a, int n, Count workgroups, unsigned &grid) {
 
 inline int64_t tiles(int64_t n, int tile) { return (n + tile - 1) / tile; }
 inline int64_t begin_blocks(const MuonStack &t) { return t.count * t.slices; }
-inline int64_t turn_blocks(const MuonStack &t) { return t.count * tiles(t.rows, kTurn) * tiles(t.cols, kTurn); }
+// Of the launches that bring X and take the result.
+inline int64_t turn_blocks(const MuonStack &t) {
+  return t.rows <= t.cols ? begin_blocks(t) : t.count * tiles(t.rows, kTurn) * tiles(t.cols, kTurn);
+}
 inline int64_t square_blocks(const MuonStack &t, int tile) { return t.count * tiles(t.m, tile) * (tiles(t.m, tile) + 1) / 2; }
 inline int64_t apply_blocks(const MuonStack &t, int tile) { return t.count * tiles(t.m, tile) * tiles(t.n, tile); }
 // Most of them, of any launch over the stack.
 inline int64_t most_blocks(const MuonStack &t) {
-  const int64_t b = begin_blocks(t), u = turn_blocks(t);
-  return b > u ? b : u;                                 // products have no more: their smallest tiles are as large
+  const int64_t b = begin_blocks(t), u = turn_blocks(t), p = apply_blocks(t, 64), s = square_blocks(t, 64);
+  const int64_t x = b > u ? b : u, y = p > s ? p : s;
+  return x > y ? x : y;
 }
 constexpr int64_t kMostMuonBlocks = (int64_t(1) << 32) / kMuonBlock - 1;
 
-// One product over n stacks, in the largest tiles of which there are as many as compute units.
+// One product over n stacks.  A compute unit holds one workgroup of 256 x 256 tiles, two of 128 x 128 or four of 64 x 64, which take about
+// 1 : 0.62 : 0.6 of the time for a round of them (256 x 256 tiles reach 1050 TFLOP/s, 128 x 128 820, 64 x 64 420): the tile whose rounds are done first.
 template <MuonProduct KIND>
 hipError_t run_product(MuonArgs &a, int n, hipStream_t s) {
-  int tile = 256;
+  int tile = 256, best = 256;
+  double least = 0.0;
   const auto blocks = [&](const MuonStack &t) { return KIND == APPLY ? apply_blocks(t, tile) : square_blocks(t, tile); };
-  for (;; tile /= 2) {
+  for (; tile >= 64; tile /= 2) {
     firsts(a, n, blocks, a.total);
-    if (tile == 64 || a.total >= 256) break;
+    const double time = tile == 256 ? (a.total + 255) / 256 : tile == 128 ? 0.62 * ((a.total + 511) / 512) : 0.6 * ((a.total + 1023) / 1024);
+    if (tile == 256 || time < least) best = tile, least = time;
   }
+  tile = best;
+  firsts(a, n, blocks, a.total);
   const unsigned grid = (a.total + 7) / 8 * 8;
-  if (tile == 256) return launch(muon_product_kernel<256, 2, 4, KIND>, grid, 512, s, a);
-  if (tile == 128) return launch(muon_product_kernel<128, 2, 4, KIND>, grid, 512, s, a);
-  return launch(muon_product_kernel<64, 2, 2, KIND>, grid, 256, s, a);
+  if (tile == 256) return launch(muon_product_kernel<256, 2, 4, 2, KIND>, grid, 512, s, a);
+  if (tile == 128) return launch(muon_product_kernel<128, 2, 4, 2, KIND>, grid, 512, s, a);
+  return launch(muon_product_kernel<64, 2, 2, 4, KIND>, grid, 256, s, a);
 }
 
 // Why a stack cannot be taken, or null.
@@ -392,7 +486,7 @@ const char *stack_fault(int64_t count, int64_t rows, int64_t cols) {
   return most_blocks(t) > kMostMuonBlocks ? "more matrices than one launch can take" : nullptr;
 }
 
-hipError_t run_stacks(MuonArgs &a, int n, int iterations, bool grad_bf16, bool out_bf16, hipStream_t s) {
+hipError_t run_stacks(MuonArgs &a, int n, int iterations, bool grad_bf16, hipStream_t s) {
   unsigned grid;
   hipError_t e;
   firsts(a, n, begin_blocks, grid);
@@ -409,7 +503,7 @@ hipError_t run_stacks(MuonArgs &a, int n, int iterations, bool grad_bf16, bool o
   if (e != hipSuccess) return e;
   a.which = iterations & 1;
   firsts(a, n, turn_blocks, grid);
-  return out_bf16 ? launch(muon_finish_kernel<uint16_t>, grid, kMuonBlock, s, a) : launch(muon_finish_kernel<float>, grid, kMuonBlock, s, a);
+  return launch(muon_finish_kernel, grid, kMuonBlock, s, a);
 }
 
 }  // namespace
@@ -475,7 +569,7 @@ extern "C" int moe_spec_muon_step(void *stream, const moe_spec_muon_tensor *tens
     MuonStack t{};
     shape(t, m.count, m.rows, m.cols);
     if (n == kPerMuonLaunch || (n && blocks + most_blocks(t) > kMostMuonBlocks)) {
-      e = run_stacks(a, n, cfg->iterations, cfg->grad_dtype == MOE_SPEC_BF16, true, s);
+      e = run_stacks(a, n, cfg->iterations, cfg->grad_dtype == MOE_SPEC_BF16, s);
       n = 0;
       blocks = 0;
     }
@@ -489,7 +583,7 @@ extern "C" int moe_spec_muon_step(void *stream, const moe_spec_muon_tensor *tens
     a.t[n++] = t;
     blocks += most_blocks(t);
   }
-  if (e == hipSuccess && n) e = run_stacks(a, n, cfg->iterations, cfg->grad_dtype == MOE_SPEC_BF16, true, s);
+  if (e == hipSuccess && n) e = run_stacks(a, n, cfg->iterations, cfg->grad_dtype == MOE_SPEC_BF16, s);
   return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "muon_step: %s", hipGetErrorString(e));
 }
 
@@ -534,6 +628,6 @@ extern "C" int moe_spec_orthogonalise(void *stream, int dtype, const void *g, in
   a.ca = float(coefficients[0]);
   a.cb = float(coefficients[1]);
   a.cc = float(coefficients[2]);
-  const hipError_t e = run_stacks(a, 1, iterations, dtype == MOE_SPEC_BF16, true, s);
+  const hipError_t e = run_stacks(a, 1, iterations, dtype == MOE_SPEC_BF16, s);
   return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "orthogonalise: %s", hipGetErrorString(e));
 }
