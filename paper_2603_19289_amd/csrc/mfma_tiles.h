@@ -210,8 +210,47 @@ struct TileProduct {
       tb.issue(base + part + A::kBytes, left, tid);
     };
     s16x8_t a0[FH], a1[FH], b0[FN], b1[FN];
-    if constexpr (WHOLE16) {
-      // Each step is four runs of products; what the next run needs is read while one goes on.  Before the last run all of a step has
+    if constexpr (WHOLE16 && FM == 2) {
+      // Small tiles, whose runs would be too short to cover a read: all that the next step needs is read while a step is multiplied.  Steps
+      // behind the last are asked for and read too, as zeros.
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) issue(i * kPart, K - i * kTileK);
+      s16x8_t va[2][2][FM], vb[2][2][FN];
+      const auto read = [&](s16x8_t (&x)[2][FM], s16x8_t (&y)[2][FN], int part) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+          for (int h = 0; h < FN; ++h) y[kk][h] = B::fragment(lds + part + A::kBytes, col + 16 * h, kk, lane);
+#pragma unroll
+          for (int f = 0; f < FM; ++f) x[kk][f] = A::fragment(lds + part, row + 16 * f, kk, lane);
+        }
+      };
+      lds_loads_done<(STEPS - 1) * (A::kEach + B::kEach)>();
+      __syncthreads();
+      read(va[0], vb[0], 0);
+      int now = 0;
+      for (int64_t k = K; k > 0; k -= 2 * kTileK) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          lds_loads_done<(STEPS - 2) * (A::kEach + B::kEach)>();
+          __syncthreads();                       // the next step is there, and this one has been read by all
+          const int next = now + kPart == kLds ? 0 : now + kPart;
+          read(va[i ^ 1], vb[i ^ 1], next);
+          issue(now, k - (STEPS + i) * kTileK);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int f = 0; f < FM; ++f)
+#pragma unroll
+              for (int h = 0; h < FN; ++h) acc[f][h] = Type::mfma(vb[i][kk][h], va[i][kk][f], acc[f][h]);
+          __builtin_amdgcn_sched_barrier(0);
+          now = next;
+        }
+      }
+      lds_loads_done<0>();                       // nothing may arrive once the workgroup has given its LDS back
+    } else if constexpr (WHOLE16) {
+      // Large tiles: each step is four runs of products; what the next run needs is read while one goes on.  Before the last run all of a step has
       // been read, and its part of LDS gets the step that is STEPS further on.  Steps behind the last are asked for and read too, as zeros,
       // so that the loop has no branches.
 #pragma unroll
