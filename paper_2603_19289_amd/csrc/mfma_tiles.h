@@ -324,6 +324,12 @@ struct ResultTile {
   }
 };
 
+// Sixteen bytes past the caches, to an address that has an element's alignment.
+__device__ __forceinline__ void store_past(void *p, uint4 v) {
+  typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
+  __builtin_nontemporal_store(Words{v.x, v.y, v.z, v.w}, static_cast<Words *>(p));
+}
+
 // Up to eight 16-bit values at p, of which n exist.
 __device__ __forceinline__ void store8(uint16_t *p, uint4 v, int n) {
   if (n >= 8) {

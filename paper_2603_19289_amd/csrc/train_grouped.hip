@@ -96,8 +96,9 @@ struct GroupedArgs {
   int rows, n_experts, n, tiles_n, out_bf16;
 };
 
-// A wavefront's part of a tile into a row-major matrix p, whose rows and cols from (row, col) on exist; bfloat16 by way of its part of LDS.
-template <int WAVES, int FM, int FN>
+// A wavefront's part of a tile into a row-major matrix, of which the tile's first `rows` rows and `cols` columns exist, from (row, col) on; bfloat16
+// by way of its part of LDS.  PAST: past the caches.
+template <bool PAST, int FM, int FN>
 __device__ __forceinline__ void store_tile(void *out, int64_t at, int64_t stride, bool bf16, const f32x4_t (&acc)[FM][FN], char *lds, int row, int col,
                                            int rows, int cols) {
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
@@ -112,7 +113,11 @@ __device__ __forceinline__ void store_tile(void *out, int64_t at, int64_t stride
 #pragma unroll
     for (int q = 0; q < R::kEach; ++q) {
       const int r = (q * 64 + lane) / R::kAcross, c = (q * 64 + lane) % R::kAcross;
-      if (row + r < rows) store8(static_cast<uint16_t *>(out) + at + int64_t(row + r) * stride + col + 8 * c, R::chunk(mine, r, c), cols - col - 8 * c);
+      uint16_t *to = static_cast<uint16_t *>(out) + at + int64_t(row + r) * stride + col + 8 * c;
+      const int n = cols - col - 8 * c;
+      if (row + r >= rows) continue;
+      if (PAST && n >= 8) store_past(to, R::chunk(mine, r, c));
+      else store8(to, R::chunk(mine, r, c), n);
     }
     return;
   }
@@ -124,7 +129,8 @@ __device__ __forceinline__ void store_tile(void *out, int64_t at, int64_t stride
 #pragma unroll
     for (int h = 0; h < FN; ++h) {
       const int c = col + 16 * h + 4 * g;
-      store4(q + c, acc[f][h], cols - c);
+      if (PAST && cols - c >= 4) store_past(q + c, __builtin_bit_cast(uint4, acc[f][h]));
+      else store4(q + c, acc[f][h], cols - c);
     }
   }
 }
@@ -136,7 +142,7 @@ __device__ __forceinline__ void grouped_tile(const GroupedArgs &a, const RowTile
   const bool behind = t.expert == a.n_experts;
   const Elem *w = static_cast<const Elem *>(a.w) + (behind ? 0 : t.expert * a.w_expert) + (w_imajor ? int64_t(col0) : col0 * a.w_stride);
   p.run(lds, static_cast<const Elem *>(a.x) + t.row0 * a.x_stride, a.x_stride, t.rows, w, a.w_stride, cols, behind ? 0 : a.k);
-  store_tile<WM * WN>(a.y, t.row0 * a.y_stride + col0, a.y_stride, a.out_bf16, p.acc, lds, wave / WN * (BM / WM), wave % WN * (BN / WN), t.rows, cols);
+  store_tile<false>(a.y, t.row0 * a.y_stride + col0, a.y_stride, a.out_bf16, p.acc, lds, wave / WN * (BM / WM), wave % WN * (BN / WN), t.rows, cols);
 }
 
 // Tiles of 256 rows whose expert has no more than 128 left are half the work as one of 128.
@@ -232,10 +238,11 @@ struct WeightGradArgs {
   int rows, n_experts, n, k, tiles_n, tiles_k, out_bf16;
   int parts;                   // of each expert's rows; more than one: sums of each go to `partial`
   float *partial;              // [parts, n_experts, n, k]
+  int past;                    // gradients that no cache would keep for who reads them go past the caches: 805 MB in 555 instead of 576 us
 };
 
 // Each die gets an eighth of every expert's tiles (another one for each expert, where eighths differ), since experts differ in their rows: where dies
-// had experts of their own, the last one to finish kept the others waiting (65536 rows over 128 experts: DIEUS us).
+// had experts of their own, the last one to finish kept the others waiting (65536 rows over 128 experts: 634 -> 570 us).
 template <typename P, int BM, int BN, int WM, int WN, typename Elem>
 __device__ __forceinline__ void weight_grad_tile(const WeightGradArgs &a, char *lds) {
   const int per = a.tiles_n * a.tiles_k;
@@ -259,9 +266,11 @@ __device__ __forceinline__ void weight_grad_tile(const WeightGradArgs &a, char *
         static_cast<const Elem *>(a.x) + begin * a.x_stride + col0, a.x_stride, cols, end - begin);
   const int row = wave / WN * (BM / WM), col = wave % WN * (BN / WN);
   if (a.parts > 1) {
-    store_tile<WM * WN>(a.partial, ((int64_t(part) * a.n_experts + expert) * a.n + row0) * a.k + col0, a.k, false, p.acc, lds, row, col, rows, cols);
+    store_tile<false>(a.partial, ((int64_t(part) * a.n_experts + expert) * a.n + row0) * a.k + col0, a.k, false, p.acc, lds, row, col, rows, cols);
+  } else if (a.past) {
+    store_tile<true>(a.dw, expert * a.dw_expert + row0 * a.dw_stride + col0, a.dw_stride, a.out_bf16, p.acc, lds, row, col, rows, cols);
   } else {
-    store_tile<WM * WN>(a.dw, expert * a.dw_expert + row0 * a.dw_stride + col0, a.dw_stride, a.out_bf16, p.acc, lds, row, col, rows, cols);
+    store_tile<false>(a.dw, expert * a.dw_expert + row0 * a.dw_stride + col0, a.dw_stride, a.out_bf16, p.acc, lds, row, col, rows, cols);
   }
 }
 
@@ -301,6 +310,7 @@ __global__ __launch_bounds__(WM *WN * 64) void weight_grad_f32_kernel(const Weig
 
 // ---- host ----------------------------------------------------------------------------------------------------------
 constexpr int kComputeUnits = 256;
+constexpr int64_t kCacheBytes = int64_t(256) << 20;     // memory-side
 constexpr int64_t kMostExpertStride = int64_t(1) << 40;
 inline int64_t tiles_of(int64_t n, int tile) { return (n + tile - 1) / tile; }
 // Whether rows of `width` values can travel straight to LDS.
@@ -443,7 +453,7 @@ extern "C" int moe_spec_grouped_weight_grad(void *stream, int dtype, const void 
   if (need && (!workspace || misaligned(workspace, 16) || workspace_bytes < need))
     return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: the workspace is null, not aligned to 16 bytes or smaller than %zu bytes", need);
   WeightGradArgs a{dy, x, dw, ends, dy_stride, x_stride, dw_stride, dw_expert_stride, int(rows), n_experts, n, k, 0, 0, out_dtype == MOE_SPEC_BF16, split.parts,
-                   static_cast<float *>(workspace)};
+                   static_cast<float *>(workspace), int64_t(n_experts) * n * k * size_of(out_dtype) > kCacheBytes};
   const Choice<WeightGradArgs> c = dtype == MOE_SPEC_F32 ? Choice<WeightGradArgs>{weight_grad_f32_kernel<64, 64, 2, 2>, 64, 64, 256}
                                    : !whole              ? Choice<WeightGradArgs>{weight_grad_kernel<128, 128, 2, 2, 2, false>, 128, 128, 256}
                                    : split.tile == 256   ? Choice<WeightGradArgs>{weight_grad_kernel<256, 256, 2, 4, 2, true>, 256, 256, 512}
