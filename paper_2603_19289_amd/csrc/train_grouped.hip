@@ -48,7 +48,8 @@ __device__ __forceinline__ RowTile row_tile(const int32_t *ends, int n_experts, 
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     end[i] = max(end[i], before);
-    count[i] = (end[i] - (i ? end[i - 1] : before) + BM - 1) / BM;
+    const int n = end[i] - (i ? end[i - 1] : before);
+    count[i] = n / BM + (n % BM != 0);
     sum += count[i];
   }
   int upto = sum;
@@ -57,7 +58,7 @@ __device__ __forceinline__ RowTile row_tile(const int32_t *ends, int n_experts, 
     const int v = __shfl_up(upto, d);
     if (lane >= d) upto += v;
   }
-  const int tiles = __builtin_amdgcn_readlane(upto, 63), all = tiles + (rows - last + BM - 1) / BM;
+  const int tiles = __builtin_amdgcn_readlane(upto, 63), all = tiles + (rows - last) / BM + ((rows - last) % BM != 0);
   const int64_t total = int64_t(all) * tiles_n, share = (total + 7) / 8, slot = blockIdx.x / 8, logical = blockIdx.x % 8 * share + slot;
   RowTile t{-1, 0, 0, 0};
   if (slot >= share || logical >= total) return t;
@@ -352,16 +353,16 @@ Choice<GroupedArgs> grouped_f32_choice() { return {grouped_f32_kernel<BM, BN, WM
 // where there are as many tiles as compute units: 256 x 256 from 128 rows on (128 matrices of 1536 x 2048, 256 rows each: 305 us, 128 x 128 325),
 // 128 x 128 from 48 (32 of 5760 x 2880, 64 rows each: 230 us; 64 x 128 271), otherwise 64 x 128 with three steps under way (12 rows each: 149 and
 // 186 us, 5.5 and 5.9 TB/s; 128 x 128 149 and 187; 8 matrices of 512 x 2048: 14 us, 128 x 128 24).
+// Through registers the same two smaller tiles (8 experts of 1001 x 1501, 500 rows each: 42 and 47 us; 16 of 333 x 777, 31 rows each: 18 and 15).
 template <bool W_IMAJOR, bool WHOLE16>
 Choice<GroupedArgs> choose_grouped(int64_t rows, int n_experts, int n) {
+  const int64_t mean = rows / n_experts;
+  const auto tiles = [&](int tile) { return n_experts * tiles_of(mean, tile) * tiles_of(n, tile); };
   if constexpr (WHOLE16) {
-    const int64_t mean = rows / n_experts;
-    const auto tiles = [&](int tile) { return n_experts * tiles_of(mean, tile) * tiles_of(n, tile); };
     if (mean >= 128 && tiles(256) >= kComputeUnits) return grouped_choice<256, 256, 2, 4, 2, W_IMAJOR, WHOLE16>();
-    if (mean >= 48 && tiles(128) >= kComputeUnits) return grouped_choice<128, 128, 2, 4, 2, W_IMAJOR, WHOLE16>();
-    return grouped_choice<64, 128, 2, 4, 3, W_IMAJOR, WHOLE16>();
   }
-  return grouped_choice<128, 128, 2, 2, 2, W_IMAJOR, WHOLE16>();
+  if (mean >= 48 && tiles(128) >= kComputeUnits) return grouped_choice<128, 128, 2, 4, 2, W_IMAJOR, WHOLE16>();
+  return grouped_choice<64, 128, 2, 4, WHOLE16 ? 3 : 2, W_IMAJOR, WHOLE16>();
 }
 // Whether the kernel for few rows takes a product: up to 16 rows an expert, and up to 48 Mi weights to read.  Beyond that (16 rows of 1536 x 2048
 // bfloat16: 20.3 us, with tiles 20.8; 4 of 5760 x 2880: 31.8 and 28.3) its reads of 64 bytes a row are slower than those of the tiles.
@@ -382,6 +383,12 @@ WeightGradSplit split_weight_grad(int dtype, bool whole, int64_t rows, int n_exp
   const int64_t most = rows / n_experts / (3 * kTileK);
   if (parts > most) parts = most;
   return {tile, int(parts < 1 ? 1 : parts > 64 ? 64 : parts)};
+}
+
+// Through registers: 99 experts of 72 x 218 9.6 us with 64 x 128, 12.7 with 128 x 128; 8 of 1001 x 1501, 4000 rows, 42 and 39.
+Choice<WeightGradArgs> staged_weight_grad(int n_experts, int n, int k) {
+  if (n_experts * tiles_of(n, 128) * tiles_of(k, 128) >= kComputeUnits) return {weight_grad_kernel<128, 128, 2, 4, 2, false>, 128, 128, 512};
+  return {weight_grad_kernel<64, 128, 2, 4, 2, false>, 64, 128, 512};
 }
 
 }  // namespace
@@ -411,7 +418,7 @@ extern "C" int moe_spec_grouped_product(void *stream, int dtype, const void *x, 
   const bool whole = whole16(x, x_stride, in) && whole16(w, w_stride, k) && w_expert_stride % 8 == 0;
   const Choice<GroupedArgs> c = !transpose && few_rows(rows, n_experts, n, k)
                                     ? Choice<GroupedArgs>{dtype == MOE_SPEC_F32 ? grouped_few_kernel<float> : grouped_few_kernel<uint16_t>, 16, 16, kFewBlock}
-                                : dtype == MOE_SPEC_F32 ? (transpose ? grouped_f32_choice<64, 64, 2, 2, true>() : grouped_f32_choice<64, 64, 2, 2, false>())
+                                : dtype == MOE_SPEC_F32 ? (transpose ? grouped_f32_choice<64, 64, 2, 4, true>() : grouped_f32_choice<64, 64, 2, 4, false>())
                                 : transpose           ? (whole ? choose_grouped<true, true>(rows, n_experts, out) : choose_grouped<true, false>(rows, n_experts, out))
                                                       : (whole ? choose_grouped<false, true>(rows, n_experts, out) : choose_grouped<false, false>(rows, n_experts, out));
   a.tiles_n = int(tiles_of(out, c.bn));
@@ -454,8 +461,8 @@ extern "C" int moe_spec_grouped_weight_grad(void *stream, int dtype, const void 
     return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: the workspace is null, not aligned to 16 bytes or smaller than %zu bytes", need);
   WeightGradArgs a{dy, x, dw, ends, dy_stride, x_stride, dw_stride, dw_expert_stride, int(rows), n_experts, n, k, 0, 0, out_dtype == MOE_SPEC_BF16, split.parts,
                    static_cast<float *>(workspace), int64_t(n_experts) * n * k * size_of(out_dtype) > kCacheBytes};
-  const Choice<WeightGradArgs> c = dtype == MOE_SPEC_F32 ? Choice<WeightGradArgs>{weight_grad_f32_kernel<64, 64, 2, 2>, 64, 64, 256}
-                                   : !whole              ? Choice<WeightGradArgs>{weight_grad_kernel<128, 128, 2, 2, 2, false>, 128, 128, 256}
+  const Choice<WeightGradArgs> c = dtype == MOE_SPEC_F32 ? Choice<WeightGradArgs>{weight_grad_f32_kernel<64, 64, 2, 4>, 64, 64, 512}
+                                   : !whole              ? staged_weight_grad(n_experts, n, k)
                                    : split.tile == 256   ? Choice<WeightGradArgs>{weight_grad_kernel<256, 256, 2, 4, 2, true>, 256, 256, 512}
                                    : split.tile == 128   ? Choice<WeightGradArgs>{weight_grad_kernel<128, 128, 2, 4, 2, true>, 128, 128, 512}
                                                          : Choice<WeightGradArgs>{weight_grad_kernel<64, 64, 2, 2, 4, true>, 64, 64, 256};
