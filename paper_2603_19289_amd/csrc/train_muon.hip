@@ -147,26 +147,28 @@ __global__ __launch_bounds__(kMuonBlock) void muon_begin_kernel(const MuonArgs<N
 __device__ __forceinline__ uint16_t to_f16(float v) { return __builtin_bit_cast(uint16_t, _Float16(v)); }
 __device__ __forceinline__ float from_f16(uint16_t v) { return float(__builtin_bit_cast(_Float16, v)); }
 
-// What makes 64 X_0 of a matrix's values: they are taken times 2^shift, which alone could leave float's range where they are tiny, and then
+// What makes X_0, or 64 X_0, of a matrix's values: they are taken times 2^shift, which alone could leave float's range where they are tiny, and then
 // times factor: zero where the matrix has only zeros, NaN where it holds what is not finite.
 struct Normaliser {
   float factor;
   int shift;
-  __device__ __forceinline__ uint16_t operator()(float u) const {
-    return factor > 0.0f ? to_f16(ldexpf(u, shift) * factor) : factor == 0.0f ? uint16_t(0) : uint16_t(0x7e00);
-  }
+  __device__ __forceinline__ float scaled(float u) const { return factor > 0.0f ? ldexpf(u, shift) * factor : factor == 0.0f ? 0.0f : NAN; }
 };
+// From a matrix's sum of squares.
+__device__ __forceinline__ Normaliser normaliser(double sum, float held) {
+  if (!(sum < double(INFINITY))) return {NAN, 0};
+  if (!(sum > 0.0)) return {0.0f, 0};
+  int exponent;
+  const double part = frexp(sqrt(sum), &exponent);
+  return {float(double(held) / part), -exponent};
+}
 __device__ __forceinline__ Normaliser normaliser(const MuonStack &t, int64_t matrix) {
   const int lane = threadIdx.x & 63;
   double sum = 0.0;
   for (int i = lane; i < t.slices; i += 64) sum += t.partial[matrix * t.slices + i];
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-  if (!(sum < double(INFINITY))) return {NAN, 0};
-  if (!(sum > 0.0)) return {0.0f, 0};
-  int exponent;
-  const double part = frexp(sqrt(sum), &exponent);
-  return {float(double(kHeld) / part), -exponent};
+  return normaliser(sum, kHeld);
 }
 
 // X_0 as float16.  A matrix that is not upright as it lies; an upright one is laid on its side, tiles of 64 x 64 through LDS.
@@ -195,7 +197,7 @@ __global__ __launch_bounds__(kMuonBlock) void muon_normalise_kernel(const MuonAr
     float u[8];
     if (c.n > 0) c.direction(a, t, scale, u);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = j < c.n ? normal(u[j]) : uint16_t(0);
+    for (int j = 0; j < 8; ++j) e[j] = j < c.n ? to_f16(normal.scaled(u[j])) : uint16_t(0);
     uint4 v;
     __builtin_memcpy(&v, e, 16);
     return v;
@@ -253,13 +255,16 @@ struct Result {
     if (n > 0 && t.p) p.load(t.p + at(t, matrix), n);
   }
   __device__ __forceinline__ void store(const MuonSettings &a, const MuonStack &t, int64_t matrix) const {
-#pragma clang fp contract(off)
-    if (n <= 0) return;
     uint16_t e[8];
     __builtin_memcpy(e, &x, 16);
     float v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = from_f16(e[j]) * (1.0f / kHeld);
+    store(a, t, matrix, v);
+  }
+  __device__ __forceinline__ void store(const MuonSettings &a, const MuonStack &t, int64_t matrix, float (&v)[8]) const {
+#pragma clang fp contract(off)
+    if (n <= 0) return;
     if (t.p) {
       float old[8];
       p.get(old);
@@ -330,6 +335,7 @@ enum MuonProduct { SQUARE, POLYNOMIAL, APPLY };
 
 template <int TILE, int WM, int WN, int STEPS, MuonProduct KIND, int N>
 __global__ __launch_bounds__(WM *WN * 64) void muon_product_kernel(const MuonArgs<N> a) {
+#pragma clang fp contract(off)                   // a matrix gets the same bits in every launch's company
   constexpr bool SYMMETRIC = KIND != APPLY;
   using P = TileProduct<F16, TILE, TILE, WM, WN, false, KIND == APPLY, true, STEPS>;
   using R = ResultTile<TILE / WM, TILE / WN>;
@@ -403,9 +409,146 @@ __global__ __launch_bounds__(WM *WN * 64) void muon_product_kernel(const MuonArg
   }
 }
 
+// ---- small matrices ----------------------------------------------------------------------------------------------
+// All of a step for a matrix that fits into LDS, in one workgroup and in float throughout: momentum, norm, the iteration by 16x16x4
+// instructions, result.  Up to 64 rows once it lies on its side.  X, A and B have rows of four times an odd number of floats, so that a fragment's
+// sixteen rows of four columns lie in banks of their own; rows and columns that fill them up are zeros and stay so.  is_small()
+// says which.
+constexpr int kSmallBlock = 1024, kSmallWaves = kSmallBlock / 64, kSmallRows = 64, kSmallFloats = 24576;       // of X
+constexpr int kSmallLd = 68, kSmallPartial = 16 * 256;
+inline __host__ __device__ int small_ld(int n) { return (n + 3) / 8 * 8 + 4; }        // the next four times an odd number
+
+template <typename GT, int N>
+__global__ __launch_bounds__(kSmallBlock) void muon_small_kernel(const MuonArgs<N> a, int iterations) {
+#pragma clang fp contract(off)
+  __shared__ float x[kSmallFloats], sa[kSmallRows * kSmallLd], sb[kSmallRows * kSmallLd], part[kSmallPartial];
+  __shared__ double sums[kSmallWaves];
+  const int which = stack_of(a.first, blockIdx.x);
+  const MuonStack &t = a.t[which];
+  const int64_t matrix = blockIdx.x - a.first[which];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
+  const int ld = small_ld(t.n), high = (t.m + 15) / 16, strips = (t.n + 15) / 16, across = (t.cols + 7) / 8, chunks = t.rows * across;
+  const bool upright = t.rows > t.cols;
+  const float scale = a.scale_dev ? a.scale * *a.scale_dev : a.scale;
+  for (int q = tid; q < high * 16 * ld; q += kSmallBlock) x[q] = 0.0f;
+  __syncthreads();
+  double sum = 0.0;
+  for (int q = tid; q < chunks; q += kSmallBlock) {
+    Chunk<GT> c;
+    c.row = q / across;
+    c.col = (q - c.row * across) * 8;
+    c.n = t.cols - c.col;
+    c.load(t, matrix);
+    float u[8];
+    c.g.get(u);
+    if (t.momentum) {
+      float m[8];
+      c.m.get(m);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float v = u[j] * scale;
+        m[j] = m[j] * a.mu + v;
+        u[j] = a.nesterov ? v + m[j] * a.mu : m[j];
+      }
+      store_run<float, 8>(t.momentum + c.at(t, matrix), m, c.n);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j >= c.n) continue;
+      sum += double(u[j]) * double(u[j]);
+      x[upright ? (c.col + j) * ld + c.row : c.row * ld + c.col + j] = u[j];
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < kSmallWaves; ++w) sum += sums[w];
+  const Normaliser normal = normaliser(sum, 1.0f);
+  for (int q = tid; q < high * 16 * ld; q += kSmallBlock) x[q] = normal.scaled(x[q]);
+  __syncthreads();
+
+  const int tiles = high * (high + 1) / 2, slices = kSmallWaves / tiles, steps = (t.n + 3) / 4, per = (steps + slices - 1) / slices;
+  // tile number -> its row and column, on and below the diagonal
+  const auto tile_row = [](int tile) { return tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3; };
+  for (int it = 0; it < iterations; ++it) {
+    if (wave < tiles * slices) {                 // A = X X^T, a slice of the columns a wavefront
+      const int tile = wave % tiles, slice = wave / tiles, r = tile_row(tile), c = tile - r * (r + 1) / 2;
+      f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+      const int from = slice * per, to = min(from + per, steps);
+      const float *xr = x + (16 * r + i) * ld + g, *xc = x + (16 * c + i) * ld + g;
+      for (int k = from; k < to; ++k) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(xr[4 * k], xc[4 * k], acc, 0, 0, 0);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) part[(slice * tiles + tile) * 256 + (4 * g + q) * 16 + i] = acc[q];
+    }
+    __syncthreads();
+    for (int q = tid; q < tiles * 256; q += kSmallBlock) {
+      const int tile = q / 256, r = tile_row(tile), c = tile - r * (r + 1) / 2, row = 16 * r + q % 256 / 16, col = 16 * c + q % 16;
+      float v = 0.0f;
+      for (int s = 0; s < slices; ++s) v += part[s * tiles * 256 + q];
+      sa[row * kSmallLd + col] = v;
+      if (r != c) sa[col * kSmallLd + row] = v;
+    }
+    __syncthreads();
+    for (int tile = wave; tile < tiles; tile += kSmallWaves) {        // B = a I + b A + c A A
+      const int r = tile_row(tile), c = tile - r * (r + 1) / 2;
+      f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+      const float *ar = sa + (16 * r + i) * kSmallLd + g, *ac = sa + (16 * c + i) * kSmallLd + g;
+      for (int k = 0; k < 4 * high; ++k) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(ar[4 * k], ac[4 * k], acc, 0, 0, 0);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int row = 16 * r + 4 * g + q, col = 16 * c + i;
+        const float v = a.cb * sa[row * kSmallLd + col] + a.cc * acc[q] + (row == col && row < t.m ? a.ca : 0.0f);
+        sb[row * kSmallLd + col] = v;
+        if (r != c) sb[col * kSmallLd + row] = v;
+      }
+    }
+    __syncthreads();
+    for (int strip = wave; strip < strips; strip += kSmallWaves) {    // X = B X, sixteen columns a wavefront, in place
+      float v[16];
+      const bool in = 16 * strip + i < ld;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] = k < 4 * high && in ? x[(4 * k + g) * ld + 16 * strip + i] : 0.0f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (r >= high) continue;
+        f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+          if (k < 4 * high) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(sb[(16 * r + i) * kSmallLd + 4 * k + g], v[k], acc, 0, 0, 0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) if (in) x[(16 * r + 4 * g + q) * ld + 16 * strip + i] = acc[q];
+      }
+    }
+    __syncthreads();
+  }
+
+  for (int q = tid; q < chunks; q += kSmallBlock) {
+    Result r;
+    r.row = q / across;
+    r.col = (q - r.row * across) * 8;
+    r.n = t.cols - r.col;
+    r.load(t, matrix);
+    float o[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = j < r.n ? x[upright ? (r.col + j) * ld + r.row : r.row * ld + r.col + j] : 0.0f;
+    r.store(a, t, matrix, o);
+  }
+}
+
 // ---- host ----------------------------------------------------------------------------------------------------------
 inline int round8(int n) { return (n + 7) / 8 * 8; }
 inline size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+// Whether a matrix is one workgroup's: it fits into LDS, and its products (16 rows squared times columns) are few enough for one compute unit.  In
+// microseconds, with one workgroup and with launches over many: 8 x 8 15 and 50, 305 x 11 23 and 65, 16 x 1500 55 and 83, 64 x 256 66 and 66,
+// 64 x 350 85 and 64.
+inline bool is_small(const MuonStack &t) {
+  const int high = (t.m + 15) / 16;
+  return t.m <= kSmallRows && high * 16 * small_ld(t.n) <= kSmallFloats && high * high * t.n <= 4096;
+}
 
 // Sizes of a stack and the workspace that it takes.
 size_t shape(MuonStack &t, int64_t count, int rows, int cols) {
@@ -419,6 +562,7 @@ size_t shape(MuonStack &t, int64_t count, int rows, int cols) {
   t.slice_rows = cols >= kSliceValues ? 1 : kSliceValues / cols;
   if (t.slice_rows > rows) t.slice_rows = rows;
   t.slices = (rows + t.slice_rows - 1) / t.slice_rows;
+  if (is_small(t)) return 0;
   return 2 * round256(size_t(count) * t.m * t.ld_n * 2) + 2 * round256(size_t(count) * t.m * t.ld_m * 2) + round256(size_t(count) * t.slices * 8);
 }
 char *place(MuonStack &t, char *at) {
@@ -457,6 +601,7 @@ inline int64_t square_blocks(const MuonStack &t, int tile) { return t.count * ti
 inline int64_t apply_blocks(const MuonStack &t, int tile) { return t.count * tiles(t.m, tile) * tiles(t.n, tile); }
 // Most of them, of any launch over the stack.
 inline int64_t most_blocks(const MuonStack &t) {
+  if (is_small(t)) return t.count * (kSmallBlock / kMuonBlock);
   const int64_t b = begin_blocks(t), u = turn_blocks(t), p = apply_blocks(t, 64), s = square_blocks(t, 64);
   const int64_t x = b > u ? b : u, y = p > s ? p : s;
   return x > y ? x : y;
@@ -516,13 +661,26 @@ hipError_t run_launches(MuonArgs<N> &a, int n, int iterations, bool grad_bf16, h
 }
 
 template <int N>
+hipError_t run_small(const MuonArgs<kPerMuonLaunch> &a, int n, int iterations, bool grad_bf16, hipStream_t s) {
+  MuonArgs<N> few{};
+  static_cast<MuonSettings &>(few) = a;
+  for (int i = 0; i < n; ++i) few.t[i] = a.t[i];
+  unsigned grid;
+  firsts(few, n, [](const MuonStack &t) { return t.count; }, grid);
+  void *args[] = {&few, &iterations};
+  const void *kernel = grad_bf16 ? reinterpret_cast<const void *>(muon_small_kernel<uint16_t, N>) : reinterpret_cast<const void *>(muon_small_kernel<float, N>);
+  return hipLaunchKernel(kernel, dim3(grid), dim3(kSmallBlock), args, 0, s);
+}
+
+template <int N>
 hipError_t run_few(const MuonArgs<kPerMuonLaunch> &a, int n, int iterations, bool grad_bf16, hipStream_t s) {
   MuonArgs<N> few{};
   static_cast<MuonSettings &>(few) = a;
   for (int i = 0; i < n; ++i) few.t[i] = a.t[i];
   return run_launches(few, n, iterations, grad_bf16, s);
 }
-hipError_t run_stacks(MuonArgs<kPerMuonLaunch> &a, int n, int iterations, bool grad_bf16, hipStream_t s) {
+hipError_t run_stacks(MuonArgs<kPerMuonLaunch> &a, int n, int iterations, bool grad_bf16, bool small, hipStream_t s) {
+  if (small) return n == 1 ? run_small<1>(a, n, iterations, grad_bf16, s) : run_small<kPerMuonLaunch>(a, n, iterations, grad_bf16, s);
   if (n == 1) return run_few<1>(a, n, iterations, grad_bf16, s);
   if (n <= 4) return run_few<4>(a, n, iterations, grad_bf16, s);
   return run_launches(a, n, iterations, grad_bf16, s);
@@ -565,9 +723,11 @@ extern "C" int moe_spec_muon_step(void *stream, const moe_spec_muon_tensor *tens
       return train_fail(MOE_SPEC_EINVAL, "muon_step: tensor %d has a pointer that is not aligned to its type", i);
   }
   const size_t need = moe_spec_muon_workspace_bytes(tensors, n_tensors);
-  if (need == 0) return MOE_SPEC_OK;
-  if (!workspace || misaligned(workspace, 16) || workspace_bytes < need)
+  if (need && (!workspace || misaligned(workspace, 16) || workspace_bytes < need))
     return train_fail(MOE_SPEC_EINVAL, "muon_step: the workspace is null, not aligned to 16 bytes or smaller than %zu bytes", need);
+  bool any = false;
+  for (int i = 0; i < n_tensors; ++i) any = any || (tensors[i].count && tensors[i].rows && tensors[i].cols);
+  if (!any) return MOE_SPEC_OK;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const OnDeviceOf on(s);
   if (on.error() != hipSuccess) return train_fail(MOE_SPEC_EHIP, "muon_step: %s", hipGetErrorString(on.error()));
@@ -581,31 +741,35 @@ extern "C" int moe_spec_muon_step(void *stream, const moe_spec_muon_tensor *tens
   a.cb = float(cfg->coefficients[1]);
   a.cc = float(cfg->coefficients[2]);
   a.nesterov = cfg->nesterov != 0;
+  const bool bf16 = cfg->grad_dtype == MOE_SPEC_BF16;
   char *at = static_cast<char *>(workspace);
-  int n = 0;
-  int64_t blocks = 0;
   hipError_t e = hipSuccess;
-  for (int i = 0; i < n_tensors && e == hipSuccess; ++i) {
-    const moe_spec_muon_tensor &m = tensors[i];
-    if (m.count == 0 || m.rows == 0 || m.cols == 0) continue;
-    MuonStack t{};
-    shape(t, m.count, m.rows, m.cols);
-    if (n == kPerMuonLaunch || (n && blocks + most_blocks(t) > kMostMuonBlocks)) {
-      e = run_stacks(a, n, cfg->iterations, cfg->grad_dtype == MOE_SPEC_BF16, s);
-      n = 0;
-      blocks = 0;
+  for (int small = 0; small < 2; ++small) {              // large matrices, then those that fit into a workgroup
+    int n = 0;
+    int64_t blocks = 0;
+    for (int i = 0; i < n_tensors && e == hipSuccess; ++i) {
+      const moe_spec_muon_tensor &m = tensors[i];
+      if (m.count == 0 || m.rows == 0 || m.cols == 0) continue;
+      MuonStack t{};
+      shape(t, m.count, m.rows, m.cols);
+      if (is_small(t) != bool(small)) continue;
+      if (n == kPerMuonLaunch || (n && blocks + most_blocks(t) > kMostMuonBlocks)) {
+        e = run_stacks(a, n, cfg->iterations, bf16, small, s);
+        n = 0;
+        blocks = 0;
+      }
+      if (!small) at = place(t, at);
+      t.p = m.p;
+      t.grad = m.grad;
+      t.momentum = m.m;
+      t.out = m.copy;
+      t.grad_stride = t.out_stride = m.cols;
+      t.grad_matrix = t.out_matrix = int64_t(m.rows) * m.cols;
+      a.t[n++] = t;
+      blocks += most_blocks(t);
     }
-    at = place(t, at);
-    t.p = m.p;
-    t.grad = m.grad;
-    t.momentum = m.m;
-    t.out = m.copy;
-    t.grad_stride = t.out_stride = m.cols;
-    t.grad_matrix = t.out_matrix = int64_t(m.rows) * m.cols;
-    a.t[n++] = t;
-    blocks += most_blocks(t);
+    if (e == hipSuccess && n) e = run_stacks(a, n, cfg->iterations, bf16, small, s);
   }
-  if (e == hipSuccess && n) e = run_stacks(a, n, cfg->iterations, cfg->grad_dtype == MOE_SPEC_BF16, s);
   return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "muon_step: %s", hipGetErrorString(e));
 }
 
@@ -634,12 +798,12 @@ extern "C" int moe_spec_orthogonalise(void *stream, int dtype, const void *g, in
   MuonArgs<kPerMuonLaunch> a{};
   MuonStack &t = a.t[0];
   const size_t need = shape(t, count, rows, cols);
-  if (!workspace || misaligned(workspace, 16) || workspace_bytes < need)
+  if (need && (!workspace || misaligned(workspace, 16) || workspace_bytes < need))
     return train_fail(MOE_SPEC_EINVAL, "orthogonalise: the workspace is null, not aligned to 16 bytes or smaller than %zu bytes", need);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const OnDeviceOf on(s);
   if (on.error() != hipSuccess) return train_fail(MOE_SPEC_EHIP, "orthogonalise: %s", hipGetErrorString(on.error()));
-  place(t, static_cast<char *>(workspace));
+  if (need) place(t, static_cast<char *>(workspace));
   t.grad = g;
   t.grad_stride = g_stride;
   t.grad_matrix = count > 1 ? g_matrix_stride : 0;
@@ -650,6 +814,6 @@ extern "C" int moe_spec_orthogonalise(void *stream, int dtype, const void *g, in
   a.ca = float(coefficients[0]);
   a.cb = float(coefficients[1]);
   a.cc = float(coefficients[2]);
-  const hipError_t e = run_stacks(a, 1, iterations, dtype == MOE_SPEC_BF16, s);
+  const hipError_t e = run_stacks(a, 1, iterations, dtype == MOE_SPEC_BF16, is_small(t), s);
   return e == hipSuccess ? MOE_SPEC_OK : train_fail(MOE_SPEC_EHIP, "orthogonalise: %s", hipGetErrorString(e));
 }

@@ -97,8 +97,8 @@ def test_swiglu_refuses_outputs():
 
 
 def orthogonalise(**kw):
-    a = dict(stream=None, dtype=M.F32, g=ADDR, g_matrix_stride=32 * 64, g_stride=64, count=3, rows=32, cols=64, coefficients=(C.c_double * 3)(1.5, -0.5, 0.0),
-             iterations=5, out=ADDR * 2, out_matrix_stride=32 * 64, out_stride=64, workspace=ADDR, workspace_bytes=1 << 30)
+    a = dict(stream=None, dtype=M.F32, g=ADDR, g_matrix_stride=80 * 96, g_stride=96, count=3, rows=80, cols=96, coefficients=(C.c_double * 3)(1.5, -0.5, 0.0),
+             iterations=5, out=ADDR * 2, out_matrix_stride=80 * 96, out_stride=96, workspace=ADDR, workspace_bytes=1 << 30)
     a.update(kw)
     return M.lib().moe_spec_orthogonalise(*a.values())
 
@@ -108,7 +108,7 @@ def orthogonalise(**kw):
                                       (dict(coefficients=(C.c_double * 3)(1, INF, 0)), "coefficients"), (dict(coefficients=(C.c_double * 3)(1, 0, -17)), "coefficients"),
                                       (dict(iterations=0), "iterations"), (dict(iterations=65), "iterations"), (dict(g=None), "g is null"), (dict(g=ADDR + 1), "g is not"),
                                       (dict(g_stride=-1), "g has"), (dict(g_matrix_stride=-1), "g's matrix"), (dict(out=None), "out is null"), (dict(out=ADDR + 1), "out is not"),
-                                      (dict(out_stride=63), "out has"), (dict(out_matrix_stride=100), "out's matrix"), (dict(out=ADDR), "out must not"),
+                                      (dict(out_stride=95), "out has"), (dict(out_matrix_stride=100), "out's matrix"), (dict(out=ADDR), "out must not"),
                                       (dict(workspace=None), "workspace"), (dict(workspace=ADDR + 8), "workspace"), (dict(workspace_bytes=1000), "workspace")])
 def test_orthogonalise_refuses(bad, word):
     refused(orthogonalise(**bad), "orthogonalise", word)
@@ -118,7 +118,7 @@ def muon(tensor=None, n=1, workspace=ADDR, workspace_bytes=1 << 30, null=False, 
     cfg = dict(lr=1e-3, momentum=0.9, weight_decay=0.0, update_rms=0.2, grad_scale=1.0, coefficients=(3.4445, -4.775, 2.0315), iterations=5, nesterov=1,
                grad_dtype=M.F32)
     cfg.update(kw)
-    t = dict(p=ADDR, grad=ADDR, m=ADDR, copy=ADDR, count=2, rows=16, cols=24)
+    t = dict(p=ADDR, grad=ADDR, m=ADDR, copy=ADDR, count=2, rows=160, cols=240)
     t.update(tensor or {})
     return M.lib().moe_spec_muon_step(None, None if null else (M.MuonTensor * 1)(M.MuonTensor(**t)), n, C.byref(M.MuonConfig(**cfg)), workspace, workspace_bytes)
 
@@ -140,7 +140,8 @@ def test_sizes_without_work_need_nothing():
     assert orthogonalise(count=0, g=None, out=None, workspace=None) == M.OK and orthogonalise(rows=0, g=None, out=None, workspace=None) == M.OK
     assert muon(tensor=dict(count=0, p=None), workspace=None, workspace_bytes=0) == M.OK and muon(n=0, null=True, workspace=None) == M.OK
     assert M.moe_spec_orthogonalise_workspace_bytes(0, 5, 5) == M.moe_spec_orthogonalise_workspace_bytes(1, 70000, 5) == 0
-    assert M.moe_spec_orthogonalise_workspace_bytes(2, 5, 5) >= M.moe_spec_orthogonalise_workspace_bytes(1, 5, 5) > 0
+    assert M.moe_spec_orthogonalise_workspace_bytes(2, 500, 5000) > M.moe_spec_orthogonalise_workspace_bytes(1, 500, 5000) > 0
+    assert M.moe_spec_orthogonalise_workspace_bytes(20, 5, 5) == 0 < M.moe_spec_orthogonalise_workspace_bytes(1, 65, 65)      # small ones need none
     assert M.lib().moe_spec_muon_step(None, None, 0, None, None, 0) == M.EINVAL
 
 
