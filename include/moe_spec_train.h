@@ -183,6 +183,7 @@ typedef struct {
   void *copy;                     /* dev, the same in bfloat16, or NULL */
   int64_t count;
   int32_t rows, cols;
+  int64_t copy_stride;            /* elements between the matrices of copy, such as those of expert blocks; 0: rows * cols */
 } moe_spec_muon_tensor;
 
 typedef struct {

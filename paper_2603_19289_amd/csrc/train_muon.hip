@@ -721,6 +721,8 @@ extern "C" int moe_spec_muon_step(void *stream, const moe_spec_muon_tensor *tens
     if (!m.p || !m.grad || !m.m) return train_fail(MOE_SPEC_EINVAL, "muon_step: tensor %d has a null pointer", i);
     if (misaligned(m.p, 4) || misaligned(m.m, 4) || misaligned(m.grad, size_of(cfg->grad_dtype)) || misaligned(m.copy, 2))
       return train_fail(MOE_SPEC_EINVAL, "muon_step: tensor %d has a pointer that is not aligned to its type", i);
+    if (m.copy_stride != 0 && (m.copy_stride < int64_t(m.rows) * m.cols || m.copy_stride > int64_t(1) << 40))
+      return train_fail(MOE_SPEC_EINVAL, "muon_step: tensor %d has a copy_stride below a matrix or above 2^40", i);
   }
   const size_t need = moe_spec_muon_workspace_bytes(tensors, n_tensors);
   if (need && (!workspace || misaligned(workspace, 16) || workspace_bytes < need))
@@ -764,7 +766,8 @@ extern "C" int moe_spec_muon_step(void *stream, const moe_spec_muon_tensor *tens
       t.momentum = m.m;
       t.out = m.copy;
       t.grad_stride = t.out_stride = m.cols;
-      t.grad_matrix = t.out_matrix = int64_t(m.rows) * m.cols;
+      t.grad_matrix = int64_t(m.rows) * m.cols;
+      t.out_matrix = m.copy_stride ? m.copy_stride : t.grad_matrix;
       a.t[n++] = t;
       blocks += most_blocks(t);
     }

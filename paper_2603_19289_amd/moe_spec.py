@@ -68,7 +68,7 @@ class AdamWConfig(C.Structure):
 
 class MuonTensor(C.Structure):
     _fields_ = [("p", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("copy", C.c_void_p), ("count", C.c_int64),
-                ("rows", C.c_int32), ("cols", C.c_int32)]
+                ("rows", C.c_int32), ("cols", C.c_int32), ("copy_stride", C.c_int64)]
 
 
 class MuonConfig(C.Structure):

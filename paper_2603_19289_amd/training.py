@@ -435,7 +435,7 @@ class Muon:
     changed between steps.  A captured step keeps those it was captured with; grad_scale it reads anew where it is a tensor.
 
     update_rms: the root mean square of an update at lr = 1.  copies: bfloat16 tensors (or None in places) that get the updated
-    parameters, rounded.  states: momenta to go on with, as `states()` gave them; used in place."""
+    parameters, rounded; a stack's may be a part of larger blocks, as an expert block holds gate, up and down.  states: momenta to go on with, as `states()` gave them; used in place."""
 
     def __init__(self, params: Sequence[torch.Tensor], *, lr: float, momentum: float = 0.95, nesterov: bool = True,
                  weight_decay: float = 0.01, update_rms: float = 0.2, iterations: int = 5, coefficients=ORTHOGONALISE,
@@ -468,16 +468,20 @@ class Muon:
 
     def _describe(self):
         """The tensors' table for the library; made anew where one of them has got other storage since."""
-        at = list(map(_ADDRESS, self._held))
+        at = [*map(_ADDRESS, self._held), *(c.stride() for c in self.copies if c is not None)]
         if at == self._at:
             return
         for d, p, m, c, shape in zip(self._desc, self.params, self._m, self.copies, self._shapes):
             self._tensor(p, "a parameter", torch.float32, shape)
             self._tensor(m, "a momentum", torch.float32, shape)
-            if c is not None:
-                self._tensor(c, "a copy", torch.bfloat16, shape)
-            d.p, d.m, d.copy = p.data_ptr(), m.data_ptr(), None if c is None else c.data_ptr()
+            d.p, d.m, d.copy, d.copy_stride = p.data_ptr(), m.data_ptr(), None if c is None else c.data_ptr(), 0
             d.rows, d.cols = shape[-2:]
+            if c is not None:
+                if len(shape) == 3 and tuple(c.shape) == shape and shape[0] > 1 and c.stride(0) > shape[1] * shape[2]:
+                    d.copy_stride, c = c.stride(0), c[0]                 # a part of larger blocks
+                    self._tensor(c, "a copy's matrix", torch.bfloat16, shape[1:])
+                else:
+                    self._tensor(c, "a copy", torch.bfloat16, shape)
         written = [t.data_ptr() for t in self._held if t.numel()]
         if len(set(written)) < len(written):
             raise ValueError("a tensor is named twice")

@@ -128,7 +128,7 @@ def muon(tensor=None, n=1, workspace=ADDR, workspace_bytes=1 << 30, null=False, 
                                       (dict(iterations=0), "iterations"), (dict(coefficients=(NAN, 0, 0)), "coefficients"), (dict(grad_scale_dev=ADDR + 1), "grad_scale_dev"),
                                       (dict(n=-1), "tensors"), (dict(n=65537), "tensors"), (dict(null=True), "tensors"), (dict(tensor=dict(count=-1)), "negative"),
                                       (dict(tensor=dict(rows=70000)), "65536"), (dict(tensor=dict(p=None)), "null"), (dict(tensor=dict(grad=None)), "null"), (dict(tensor=dict(m=None)), "null"),
-                                      (dict(tensor=dict(copy=ADDR + 1)), "aligned"), (dict(tensor=dict(m=ADDR + 2)), "aligned"), (dict(workspace=None), "workspace"),
+                                      (dict(tensor=dict(copy=ADDR + 1)), "aligned"), (dict(tensor=dict(copy_stride=160 * 240 - 1)), "copy_stride"), (dict(tensor=dict(copy_stride=-1)), "copy_stride"), (dict(tensor=dict(m=ADDR + 2)), "aligned"), (dict(workspace=None), "workspace"),
                                       (dict(workspace=ADDR + 4), "workspace"), (dict(workspace_bytes=64), "workspace")])
 def test_muon_step_refuses(bad, word):
     refused(muon(**bad), "muon_step", word)
@@ -205,6 +205,9 @@ def test_muon_follows_tensors_that_get_other_storage(recorded):
         m = opt.states()["m"]
         assert table() == [(p[0].data_ptr(), g[0].data_ptr(), m[0].data_ptr(), None, 3, 4, 5),
                            (p[1].data_ptr(), g[1].data_ptr(), m[1].data_ptr(), opt.copies[1].data_ptr(), 1, 6, 7)]
+    blocks = torch.zeros(3, 50, dtype=torch.bfloat16)
+    other = T.Muon([torch.zeros(3, 4, 5)], lr=0.1, copies=[blocks[:, 10:30].unflatten(1, (4, 5))])
+    assert other._desc[0].copy == blocks.data_ptr() + 20 and other._desc[0].copy_stride == 50
     opt.step([None, g[1]])
     assert [d[4] for d in table()] == [0, 1]
     p[0].data = opt.states()["m"][0].data

@@ -503,6 +503,20 @@ def test_muon_steps(grad, nesterov):
                 assert torch.equal(copies[i], p[i].to(torch.bfloat16))
 
 
+@pytest.mark.parametrize("rows,cols", [(24, 40), (72, 130), (130, 72)])
+def test_muon_copies_into_expert_blocks(rows, cols):
+    from paper_2603_19289_amd import training as T
+    blocks = torch.full((4, 3 * rows * cols + 5), 6.0, dtype=torch.bfloat16, device="cuda")
+    part = blocks[:, rows * cols:2 * rows * cols].unflatten(1, (rows, cols))
+    p = torch.randn(4, rows, cols, device="cuda")
+    T.Muon([p], lr=0.1, copies=[part]).step([torch.randn(4, rows, cols, device="cuda")])
+    assert torch.equal(part, p.to(torch.bfloat16))
+    part.fill_(6.0)
+    assert torch.all(blocks == 6.0)
+    with pytest.raises(ValueError):
+        T.Muon([p], lr=0.1, copies=[torch.zeros(4, cols, rows, dtype=torch.bfloat16, device="cuda").transpose(1, 2)])
+
+
 def test_muon_leaves_out_parameters_without_gradient():
     from paper_2603_19289_amd import training as T
     p = [torch.randn(8, 16, device="cuda") for _ in range(3)]
