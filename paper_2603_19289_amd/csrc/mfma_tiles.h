@@ -1,10 +1,11 @@
 // One output tile of a matrix product on the matrix cores, for 16-bit operands that lie either way in memory:
-//   C[m, n] = sum_k a(m, k) b(n, k),   acc in float, 16x16x32 instructions, K walked 64 at a time.
-// An operand is "k-major" (the 64 values of a row of the tile are contiguous) or "i-major" (the tile's rows are contiguous for each k, as
+//   C[m, n] = sum_k a(m, k) b(n, k),   acc in float, 16x16x32 instructions, K walked a step of 64 (or 32) at a time.
+// An operand is "k-major" (a step's values of a row of the tile are contiguous) or "i-major" (the tile's rows are contiguous for each k, as
 // a weight matrix is for the gradient of its input, and both operands are for the gradient of a weight matrix).  Both kinds travel
 // from global memory to LDS as they lie, 16 bytes a lane, without a register between; a k-major fragment is read as 16 bytes, an
 // i-major one by two transposing reads of 8.  LDS is swizzled so that either read meets every bank once:
-//   k-major: rows of 128 bytes, the 16-byte chunk c of row r at place c ^ (r / 2 % 8)  (16 rows of a fragment, one chunk each)
+//   k-major: rows of 128 bytes, the 16-byte chunk c of row r at place c ^ (r / 2 % 8)  (16 rows of a fragment, one chunk each); steps of 32:
+//            rows of 64 bytes, place c ^ (r / 4 % 4)
 //   i-major: 32-byte granules, granule q of row k at place q ^ f(k)  (32 lanes read rows {0..3, 8..11} + 4 h of a fragment's 32)
 #pragma once
 #include <type_traits>
@@ -30,7 +31,7 @@ struct F16 {
   }
 };
 
-constexpr int kTileK = 64;
+constexpr int kTileK = 64;               // of a usual step
 using LdsPtr = __attribute__((address_space(3))) char *;
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return uint32_t(reinterpret_cast<uintptr_t>((LdsPtr)p)); }
 
@@ -73,13 +74,13 @@ struct RowChunk {
   }
 };
 
-// An operand tile of ROWS x 64 (k-major) or 64 x ROWS (i-major) in LDS, and the loads that fill it.
+// An operand tile of ROWS x KS (k-major) or KS x ROWS (i-major) in LDS, and the loads that fill it.
 // WHOLE16: straight to LDS.  Addresses, row strides and extents are multiples of 16 bytes (a chunk lies inside the matrix or outside of
 // it), rows do not overlap and lie at most kMostTileStride apart.  Otherwise: through registers, any stride and alignment.
-template <int ROWS, bool IMAJOR, bool WHOLE16, int THREADS>
+template <int ROWS, bool IMAJOR, bool WHOLE16, int THREADS, int KS>
 struct OperandTile {
-  static constexpr int kBytes = ROWS * kTileK * 2, kChunks = ROWS * kTileK / 8, kEach = kChunks / THREADS;
-  static constexpr int kAcross = IMAJOR ? ROWS / 8 : 8, kApart = THREADS / kAcross;      // chunks of a row; rows between a thread's chunks
+  static constexpr int kBytes = ROWS * KS * 2, kChunks = ROWS * KS / 8, kEach = kChunks / THREADS;
+  static constexpr int kAcross = IMAJOR ? ROWS / 8 : KS / 8, kApart = THREADS / kAcross;      // chunks of a row; rows between a thread's chunks
   static_assert(kChunks % THREADS == 0 && THREADS % 128 == 0 && ROWS % 64 == 0 && (!IMAJOR || kApart % 16 == 0), "a thread's chunks lie in one column");
 
   static __device__ __forceinline__ int granule_swizzle(int k) {
@@ -89,7 +90,7 @@ struct OperandTile {
   static __device__ __forceinline__ int row_of(int c) { return c / kAcross; }
   static __device__ __forceinline__ int column_of(int c) {
     if constexpr (IMAJOR) return (((c % kAcross >> 1) ^ granule_swizzle(c / kAcross)) << 4) | (c & 1) << 3;
-    else return ((c % 8) ^ (c / 16 % 8)) * 8;
+    else return KS == 64 ? ((c % 8) ^ (c / 16 % 8)) * 8 : ((c % 4) ^ (c / 16 % 4)) * 8;
   }
 
   Buffer from;                           // WHOLE16: the rest of the operand
@@ -107,7 +108,7 @@ struct OperandTile {
     narrow = (IMAJOR ? rows : K) < 8;
     safe = origin;
     column = column_of(tid);
-    step = IMAJOR ? ld * kTileK : kTileK;
+    step = IMAJOR ? ld * KS : KS;
     if constexpr (WHOLE16) {
       const uint64_t p = reinterpret_cast<uint64_t>(origin);
       row_bytes = uint32_t(ld) * 2;
@@ -173,19 +174,20 @@ struct OperandTile {
       }
       return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      return *reinterpret_cast<const s16x8_t *>(lds + (row + i) * 128 + (((half * 4 + g) ^ (i >> 1)) << 4));
+      return *reinterpret_cast<const s16x8_t *>(lds + (row + i) * (KS * 2) + (KS == 64 ? ((half * 4 + g) ^ (i >> 1)) << 4 : (g ^ (i >> 2)) << 4));
     }
   }
 };
 
 // The product of a tile of BM x BN by WM x WN wavefronts.  acc[f][h][r] of lane (i, g): row 16 f + i, column 16 h + 4 g + r of the
 // wavefront's part.
-// STEPS: how many steps of 64 columns are in LDS or on their way there.
-template <typename Type, int BM, int BN, int WM, int WN, bool A_IMAJOR, bool B_IMAJOR, bool WHOLE16, int STEPS = 2>
+// STEPS: how many steps of KS columns are in LDS or on their way there.  8192 x 8192 x 2048, 256 x 256 tiles, k-major operands: two steps of 64
+// 250 us, four of 32 266; i-major ones 280 and 268.
+template <typename Type, int BM, int BN, int WM, int WN, bool A_IMAJOR, bool B_IMAJOR, bool WHOLE16, int STEPS = 2, int KS = 64>
 struct TileProduct {
   static constexpr int kThreads = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
-  using A = OperandTile<BM, A_IMAJOR, WHOLE16, kThreads>;
-  using B = OperandTile<BN, B_IMAJOR, WHOLE16, kThreads>;
+  using A = OperandTile<BM, A_IMAJOR, WHOLE16, kThreads, KS>;
+  using B = OperandTile<BN, B_IMAJOR, WHOLE16, kThreads, KS>;
   static constexpr int kPart = A::kBytes + B::kBytes, kLds = STEPS * kPart;
   static_assert(STEPS >= 2 && (WHOLE16 || STEPS == 2), "");
   f32x4_t acc[FM][FN];
@@ -230,7 +232,7 @@ struct TileProduct {
     ta.begin(a, lda, a_rows, K, tid);
     tb.begin(b, ldb, b_rows, K, tid);
     const auto issue = [&](int part, int64_t k) {                  // the step that has k columns left
-      const int left = int(k < kTileK ? (k > 0 ? k : 0) : int64_t(kTileK));
+      const int left = int(k < KS ? (k > 0 ? k : 0) : int64_t(KS));
       ta.issue(base + part, left, tid);
       tb.issue(base + part + A::kBytes, left, tid);
     };
@@ -272,6 +274,32 @@ struct TileProduct {
           __builtin_amdgcn_sched_barrier(0);
           now = next;
         }
+      }
+      lds_loads_done<0>();                       // nothing may arrive once the workgroup has given its LDS back
+    } else if constexpr (WHOLE16 && KS == 32) {
+      // As below, with two runs a step.
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) issue(i * kPart, K - i * KS);
+      lds_loads_done<(STEPS - 1) * (A::kEach + B::kEach)>();
+      __syncthreads();
+      read_b(b0, lds, 0, col, lane);
+      read_a(a0, lds, 0, 0, row, lane);
+      int now = 0;
+      const auto step = [&](int64_t k, const s16x8_t (&b)[FN], s16x8_t (&b_next)[FN]) {
+        read_a(a1, lds + now, 0, 1, row, lane);
+        multiply<0>(a0, b);
+        lds_loads_done<(STEPS - 2) * (A::kEach + B::kEach)>();
+        __syncthreads();
+        const int next = now + kPart == kLds ? 0 : now + kPart;
+        read_b(b_next, lds + next, 0, col, lane);
+        read_a(a0, lds + next, 0, 0, row, lane);
+        multiply<1>(a1, b);
+        issue(now, k - STEPS * KS);
+        now = next;
+      };
+      for (int64_t k = K; k > 0; k -= 2 * KS) {
+        step(k, b0, b1);
+        step(k - KS, b1, b0);
       }
       lds_loads_done<0>();                       // nothing may arrive once the workgroup has given its LDS back
     } else if constexpr (WHOLE16) {

@@ -312,9 +312,9 @@ __global__ __launch_bounds__(256) void weight_grad_join_kernel(const WeightGradA
   else store4(static_cast<float *>(a.dw) + to, sum, n);
 }
 
-template <int BM, int BN, int WM, int WN, int STEPS, bool WHOLE16>
+template <int BM, int BN, int WM, int WN, int STEPS, bool WHOLE16, int KS = 64>
 __global__ __launch_bounds__(WM *WN * 64) void weight_grad_kernel(const WeightGradArgs a) {
-  using P = TileProduct<Bf16, BM, BN, WM, WN, true, true, WHOLE16, STEPS>;
+  using P = TileProduct<Bf16, BM, BN, WM, WN, true, true, WHOLE16, STEPS, KS>;
   __shared__ __attribute__((aligned(16))) char lds[P::kLds];
   weight_grad_tile<P, BM, BN, WM, WN, uint16_t>(a, lds);
 }
@@ -387,6 +387,8 @@ bool few_rows(int64_t rows, int n_experts, int n, int k) {
   return rows <= 16 * int64_t(n_experts) && (rows < n_experts ? rows : n_experts) * int64_t(n) * k <= int64_t(48) << 20;
 }
 
+// Large tiles of weight gradients take four steps of 32 rows: an expert's rows are few steps, and the first arrives sooner (512 rows an expert, 128 of
+// 1536 x 2048: 562 -> 521 us).
 // How a weight gradient is split: tiles of the matrices, and parts of each expert's rows where those alone leave half of the compute units
 // without work and the rows are many (192 of them for a part, three steps).  3 experts of 224 x 544, 11000 rows each: 149 -> 30 us; one of
 // 1024 x 1024, 8192 rows: 89 -> 34; but 8 of 1024 x 512, 2048 rows each, 256 tiles in two parts: 38 -> 41, so not there.
@@ -480,7 +482,7 @@ extern "C" int moe_spec_grouped_weight_grad(void *stream, int dtype, const void 
                    static_cast<float *>(workspace), int64_t(n_experts) * n * k * size_of(out_dtype) > kCacheBytes};
   const Choice<WeightGradArgs> c = dtype == MOE_SPEC_F32 ? Choice<WeightGradArgs>{weight_grad_f32_kernel<64, 64, 2, 4>, 64, 64, 512}
                                    : !whole              ? staged_weight_grad(n_experts, n, k)
-                                   : split.tile == 256   ? Choice<WeightGradArgs>{weight_grad_kernel<256, 256, 2, 4, 2, true>, 256, 256, 512}
+                                   : split.tile == 256   ? Choice<WeightGradArgs>{weight_grad_kernel<256, 256, 2, 4, 4, true, 32>, 256, 256, 512}
                                    : split.tile == 128   ? Choice<WeightGradArgs>{weight_grad_kernel<128, 128, 2, 4, 2, true>, 128, 128, 512}
                                                          : Choice<WeightGradArgs>{weight_grad_kernel<64, 64, 2, 2, 4, true>, 64, 64, 256};
   a.tiles_n = int(tiles_of(n, c.bm));
