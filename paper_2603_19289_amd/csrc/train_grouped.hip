@@ -246,6 +246,63 @@ __global__ __launch_bounds__(WM *WN * 64) void grouped_f32_kernel(const GroupedA
   if (t.expert >= 0) grouped_tile<P, BM, BN, WM, WN, float>(a, t, lds, W_IMAJOR);
 }
 
+// The same for transposed float weights, whose rows lie along the result: a lane reads four columns of one of four rows of a step, a wavefront 64 columns of
+// the result, and each of four instructions takes one column of every lane.  Eight wavefronts take every eighth four rows, sixteen of them at
+// once.  One row each for 8 of 128 matrices 1536 x 2048: 19 us, with tiles 42; 32 rows 69 and 127.  (The same with bfloat16 widened
+// on the way was slower than its tiles: 23 and 14 for 8 of them.)
+constexpr int kFewTBlock = 512, kFewTWaves = kFewTBlock / 64, kFewTCols = 64;
+
+__global__ __launch_bounds__(kFewTBlock) void grouped_few_transposed_kernel(const GroupedArgs a) {
+  __shared__ f32x4_t part[kFewTWaves][4][64];
+  const RowTile t = row_tile<16>(a.ends, a.n_experts, a.rows, a.tiles_n);
+  if (t.expert < 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+  const int col0 = t.tile_n * kFewTCols, K = t.expert == a.n_experts ? 0 : int(a.k), mine = col0 + 4 * i, n = a.n - mine;
+  const float *w = static_cast<const float *>(a.w) + (t.expert == a.n_experts ? 0 : t.expert * a.w_expert) + mine;
+  const float *x = static_cast<const float *>(a.x) + (t.row0 + int64_t(min(i, t.rows - 1))) * a.x_stride;
+  f32x4_t acc[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  // rows of weights behind the last are the first one's, and count for nothing
+  const auto walk = [&](auto whole) {
+    for (int first = 4 * wave; first < K; first += kFewTWaves * kFewDeep * 4) {
+      Run<float, 4> vw[kFewDeep];
+      float vx[kFewDeep];
+#pragma unroll
+      for (int d = 0; d < kFewDeep; ++d) {
+        const int at = first + d * kFewTWaves * 4 + g, k = at < K ? at : 0;
+        vw[d].load(w + int64_t(k) * a.w_stride, decltype(whole)::value ? 4 : n);
+        vx[d] = x[k];
+      }
+#pragma unroll
+      for (int d = 0; d < kFewDeep; ++d) {
+        const bool in = first + d * kFewTWaves * 4 + g < K;
+        float f[4];
+        vw[d].get(f);
+        const float v = in && i < t.rows ? vx[d] : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? f[j] : 0.0f, v, acc[j], 0, 0, 0);
+      }
+    }
+  };
+  if (a.n - col0 >= kFewTCols) walk(std::true_type());
+  else walk(std::false_type());
+#pragma unroll
+  for (int j = 0; j < 4; ++j) part[wave][j][lane] = acc[j];
+  __syncthreads();
+  // lane (token i, g), value q of column set j: column col0 + 4 (4 g + q) + j
+  for (int q = threadIdx.x; q < t.rows * kFewTCols; q += kFewTBlock) {
+    const int row = q / kFewTCols, c = q % kFewTCols, from = c / 4;
+    float sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < kFewTWaves; ++v) sum += part[v][c % 4][from / 4 * 16 + row][from % 4];
+    if (col0 + c >= a.n) continue;
+    const int64_t to = (t.row0 + int64_t(row)) * a.y_stride + col0 + c;
+    if (a.out_bf16) static_cast<uint16_t *>(a.y)[to] = to_bf16(sum);
+    else static_cast<float *>(a.y)[to] = sum;
+  }
+}
+
 // ---- dW = dy^T x -------------------------------------------------------------------------------------------------
 struct WeightGradArgs {
   const void *dy, *x;
@@ -381,14 +438,20 @@ Choice<GroupedArgs> choose_grouped(int64_t rows, int n_experts, int n) {
   if (mean >= 48 && tiles(128) >= kComputeUnits) return grouped_choice<128, 128, 2, 4, 2, W_IMAJOR, WHOLE16>();
   return grouped_choice<64, 128, 2, 4, WHOLE16 ? 3 : 2, W_IMAJOR, WHOLE16>();
 }
-// Whether the kernel for few rows takes a product: up to 16 rows an expert, and up to 48 Mi weights to read.  Beyond that (16 rows of 1536 x 2048
-// bfloat16: 20.3 us, with tiles 20.8; 4 of 5760 x 2880: 31.8 and 28.3) its reads of 64 bytes a row are slower than those of the tiles.
-bool few_rows(int64_t rows, int n_experts, int n, int k) {
-  return rows <= 16 * int64_t(n_experts) && (rows < n_experts ? rows : n_experts) * int64_t(n) * k <= int64_t(48) << 20;
+// Whether a kernel for few rows takes a product: up to 16 rows an expert.
+//   bfloat16, not transposed: up to 48 Mi weights to read.  Beyond that (16 rows of 1536 x 2048: 20.3 us, with tiles 20.8; 4 of 5760 x 2880: 31.8
+//   and 28.3) its reads of 64 bytes a row are slower than those of the tiles.  Transposed: never.
+//   float, not transposed: the same, and up to 8 rows an expert of any size (32 rows over 128 of 1536 x 2048: 80 us, with tiles 127; 200 over 32 of
+//   2880 x 2880: 294 and 340; 400 over those of 2880 x 5760: 809 and 686).
+//   float, transposed: sums of at least 128 products (100 rows of 16 experts, 333 x 777: 9.4 us, with tiles 13.8; 128 rows over 128 of
+//   1536 x 2048: 166 and 299; but 20 rows of 16 experts, 64 x 64: 7.1 and 5.1).
+bool few_rows(int dtype, bool transpose, int64_t rows, int n_experts, int n, int k) {
+  if (rows > 16 * int64_t(n_experts)) return false;
+  if (transpose) return dtype == MOE_SPEC_F32 && n >= 128;
+  if (dtype == MOE_SPEC_F32 && rows <= 8 * int64_t(n_experts)) return true;
+  return (rows < n_experts ? rows : n_experts) * int64_t(n) * k <= int64_t(48) << 20;
 }
 
-// Large tiles of weight gradients take four steps of 32 rows: an expert's rows are few steps, and the first arrives sooner (512 rows an expert, 128 of
-// 1536 x 2048: 562 -> 521 us).
 // How a weight gradient is split: tiles of the matrices, and parts of each expert's rows where those alone leave half of the compute units
 // without work and the rows are many (192 of them for a part, three steps).  3 experts of 224 x 544, 11000 rows each: 149 -> 30 us; one of
 // 1024 x 1024, 8192 rows: 89 -> 34; but 8 of 1024 x 512, 2048 rows each, 256 tiles in two parts: 38 -> 41, so not there.
@@ -435,9 +498,10 @@ extern "C" int moe_spec_grouped_product(void *stream, int dtype, const void *x, 
   if (n_experts == 1) w_expert_stride = 0;
   GroupedArgs a{x, w, y, ends, x_stride, w_stride, w_expert_stride, y_stride, in, int(rows), n_experts, out, 0, out_dtype == MOE_SPEC_BF16};
   const bool whole = whole16(x, x_stride, in) && whole16(w, w_stride, k) && w_expert_stride % 8 == 0;
-  const Choice<GroupedArgs> c = !transpose && few_rows(rows, n_experts, n, k)
-                                    ? Choice<GroupedArgs>{dtype == MOE_SPEC_F32 ? grouped_few_kernel<float> : grouped_few_kernel<uint16_t>, 16, 16, kFewBlock}
-                                : dtype == MOE_SPEC_F32 ? (transpose ? grouped_f32_choice<64, 64, 2, 4, true>() : grouped_f32_choice<64, 64, 2, 4, false>())
+  const bool few = few_rows(dtype, transpose, rows, n_experts, n, k), wide = dtype == MOE_SPEC_F32;
+  const Choice<GroupedArgs> c = few && transpose ? Choice<GroupedArgs>{grouped_few_transposed_kernel, 16, kFewTCols, kFewTBlock}
+                                : few ? Choice<GroupedArgs>{wide ? grouped_few_kernel<float> : grouped_few_kernel<uint16_t>, 16, 16, kFewBlock}
+                                : wide ? (transpose ? grouped_f32_choice<64, 64, 2, 4, true>() : grouped_f32_choice<64, 64, 2, 4, false>())
                                 : transpose           ? (whole ? choose_grouped<true, true>(rows, n_experts, out) : choose_grouped<true, false>(rows, n_experts, out))
                                                       : (whole ? choose_grouped<false, true>(rows, n_experts, out) : choose_grouped<false, false>(rows, n_experts, out));
   a.tiles_n = int(tiles_of(out, c.bn));
@@ -480,6 +544,8 @@ extern "C" int moe_spec_grouped_weight_grad(void *stream, int dtype, const void 
     return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: the workspace is null, not aligned to 16 bytes or smaller than %zu bytes", need);
   WeightGradArgs a{dy, x, dw, ends, dy_stride, x_stride, dw_stride, dw_expert_stride, int(rows), n_experts, n, k, 0, 0, out_dtype == MOE_SPEC_BF16, split.parts,
                    static_cast<float *>(workspace), int64_t(n_experts) * n * k * size_of(out_dtype) > kCacheBytes};
+  // Large tiles take four steps of 32 rows: an expert's rows are few steps, and the first arrives sooner (512 rows an expert, 128 of
+  // 1536 x 2048: 562 -> 521 us).
   const Choice<WeightGradArgs> c = dtype == MOE_SPEC_F32 ? Choice<WeightGradArgs>{weight_grad_f32_kernel<64, 64, 2, 4>, 64, 64, 512}
                                    : !whole              ? staged_weight_grad(n_experts, n, k)
                                    : split.tile == 256   ? Choice<WeightGradArgs>{weight_grad_kernel<256, 256, 2, 4, 4, true, 32>, 256, 256, 512}

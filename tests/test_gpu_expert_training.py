@@ -62,7 +62,8 @@ def i32(ends):
 # sizes of the groups (rows behind the last: a final negative number), n, k
 GROUPS = [([1], 1, 1), ([0], 8, 8), ([5, 0, 3], 7, 9), ([64], 64, 64), ([130, 1, 0, 127, -9], 136, 200), ([17] * 5, 65, 63), ([0, 0, 300, 0], 256, 72),
           ([1] * 8 + [0] * 20, 96, 128), ([3, 200, 40, -1], 33, 257), ([129, 127], 128, 320), ([1] * 256, 24, 40), ([0] * 255 + [20], 16, 24),
-          ([2, 0] * 30, 40, 1030), ([600, 500], 260, 264), ([-4], 8, 16), ([9, 70, 5], 1, 70), ([9, 70, 5], 70, 1)]
+          ([2, 0] * 30, 40, 1030), ([600, 500], 260, 264), ([-4], 8, 16), ([9, 70, 5], 1, 70), ([9, 70, 5], 70, 1),
+          ([3, 0, 17, 1, -2], 300, 130), ([16, 1], 1031, 67), ([2, 5], 128, 3)]
 
 
 def groups(case):
