@@ -1,5 +1,6 @@
 // One output tile of a float32 matrix product on the matrix cores (16x16x4 instructions, float throughout), with the interface
-// of mfma_tiles.h.  K is walked 32 at a time; a tile goes through registers into LDS, where rows are padded so that the one value a
+// of mfma_tiles.h, for operands of any stride and alignment; those of whole 16-byte chunks take the tiles there (4096 rows, 8 experts of 1024 x 2048:
+// 168 us, these 201).  K is walked 32 at a time; a tile goes through registers into LDS, where rows are padded so that the one value a
 // lane needs per instruction lies in a bank of its own: k-major rows of 36 floats, i-major ones of ROWS + 16.
 #pragma once
 #include "mfma_tiles.h"

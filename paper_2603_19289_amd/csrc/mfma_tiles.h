@@ -1,11 +1,12 @@
-// One output tile of a matrix product on the matrix cores, for 16-bit operands that lie either way in memory:
-//   C[m, n] = sum_k a(m, k) b(n, k),   acc in float, 16x16x32 instructions, K walked a step of 64 (or 32) at a time.
+// One output tile of a matrix product on the matrix cores, for operands of 16 bits or of float that lie either way in memory:
+//   C[m, n] = sum_k a(m, k) b(n, k),   acc in float, 16x16x32 (16x16x4) instructions, K walked a step of 64 (or 32) at a time.
 // An operand is "k-major" (a step's values of a row of the tile are contiguous) or "i-major" (the tile's rows are contiguous for each k, as
 // a weight matrix is for the gradient of its input, and both operands are for the gradient of a weight matrix).  Both kinds travel
 // from global memory to LDS as they lie, 16 bytes a lane, without a register between; a k-major fragment is read as 16 bytes, an
-// i-major one by two transposing reads of 8.  LDS is swizzled so that either read meets every bank once:
+// i-major one by two transposing reads of 8 (float: four of 4, a row each).  LDS is swizzled so that either read meets every bank once:
 //   k-major: rows of 128 bytes, the 16-byte chunk c of row r at place c ^ (r / 2 % 8)  (16 rows of a fragment, one chunk each); steps of 32:
 //            rows of 64 bytes, place c ^ (r / 4 % 4)
+//   i-major, float: the 16-byte chunk c of row k at place c ^ (k & 12)  (16 lanes a row, of rows four apart)
 //   i-major: 32-byte granules, granule q of row k at place q ^ f(k)  (32 lanes read rows {0..3, 8..11} + 4 h of a fragment's 32)
 #pragma once
 #include <type_traits>
@@ -21,17 +22,31 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8v_t;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
 
 struct Bf16 {
+  using Elem = uint16_t;
+  static constexpr int kStep = 64;
   static __device__ __forceinline__ f32x4_t mfma(s16x8_t a, s16x8_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v_t, a), __builtin_bit_cast(bf16x8v_t, b), c, 0, 0, 0);
   }
 };
 struct F16 {
+  using Elem = uint16_t;
+  static constexpr int kStep = 64;
   static __device__ __forceinline__ f32x4_t mfma(s16x8_t a, s16x8_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
   }
 };
+// Sixteen columns: an operand's lane (i, g) holds columns 4 g .. 4 g + 3, one for each of four instructions.
+struct F32 {
+  using Elem = float;
+  static constexpr int kStep = 32;
+  static __device__ __forceinline__ f32x4_t mfma(s16x8_t a, s16x8_t b, f32x4_t c) {
+    const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, b);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+    return c;
+  }
+};
 
-constexpr int kTileK = 64;               // of a usual step
 using LdsPtr = __attribute__((address_space(3))) char *;
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return uint32_t(reinterpret_cast<uintptr_t>((LdsPtr)p)); }
 
@@ -47,7 +62,7 @@ template <int LEFT>
 __device__ __forceinline__ void lds_loads_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
 
 constexpr uint32_t kOutside = 0xffffff00u;             // an offset that no descriptor here contains
-constexpr int64_t kMostTileStride = 1 << 22;           // elements; 256 rows of a tile then stay below 2^32 bytes
+constexpr int64_t kMostTileStride = 1 << 22;           // elements; 256 rows of 16 bits (128 of float) then stay below 2^32 bytes
 
 // Sixteen bytes of a row by way of registers, of which the first n elements exist: asked for without a branch, which would hold up the next
 // request, at an address that lies in the row (a chunk that is cut off is moved back to end with it, one that does not exist becomes `safe`),
@@ -77,11 +92,12 @@ struct RowChunk {
 // An operand tile of ROWS x KS (k-major) or KS x ROWS (i-major) in LDS, and the loads that fill it.
 // WHOLE16: straight to LDS.  Addresses, row strides and extents are multiples of 16 bytes (a chunk lies inside the matrix or outside of
 // it), rows do not overlap and lie at most kMostTileStride apart.  Otherwise: through registers, any stride and alignment.
-template <int ROWS, bool IMAJOR, bool WHOLE16, int THREADS, int KS>
+template <typename Elem, int ROWS, bool IMAJOR, bool WHOLE16, int THREADS, int KS>
 struct OperandTile {
-  static constexpr int kBytes = ROWS * KS * 2, kChunks = ROWS * KS / 8, kEach = kChunks / THREADS;
-  static constexpr int kAcross = IMAJOR ? ROWS / 8 : KS / 8, kApart = THREADS / kAcross;      // chunks of a row; rows between a thread's chunks
+  static constexpr int kElem = sizeof(Elem), kOfChunk = 16 / kElem, kBytes = ROWS * KS * kElem, kChunks = kBytes / 16, kEach = kChunks / THREADS;
+  static constexpr int kAcross = (IMAJOR ? ROWS : KS) / kOfChunk, kApart = THREADS / kAcross;      // chunks of a row; rows between a thread's chunks
   static_assert(kChunks % THREADS == 0 && THREADS % 128 == 0 && ROWS % 64 == 0 && (!IMAJOR || kApart % 16 == 0), "a thread's chunks lie in one column");
+  static_assert(kElem == 2 || (WHOLE16 && KS == 32), "float: straight to LDS");
 
   static __device__ __forceinline__ int granule_swizzle(int k) {
     return ROWS >= 128 ? (k & 3) | (k >> 1 & 4) : (k >> 1 & 1) | (k >> 2 & 2);
@@ -89,21 +105,22 @@ struct OperandTile {
   // Row (k-major: of the tile, i-major: k) and first column of the chunk that goes to place c.
   static __device__ __forceinline__ int row_of(int c) { return c / kAcross; }
   static __device__ __forceinline__ int column_of(int c) {
-    if constexpr (IMAJOR) return (((c % kAcross >> 1) ^ granule_swizzle(c / kAcross)) << 4) | (c & 1) << 3;
-    else return KS == 64 ? ((c % 8) ^ (c / 16 % 8)) * 8 : ((c % 4) ^ (c / 16 % 4)) * 8;
+    if constexpr (IMAJOR && kElem == 4) return ((c % kAcross) ^ (c / kAcross & 12)) * 4;
+    else if constexpr (IMAJOR) return (((c % kAcross >> 1) ^ granule_swizzle(c / kAcross)) << 4) | (c & 1) << 3;
+    else return (kAcross == 8 ? (c % 8) ^ (c / 16 % 8) : (c % 4) ^ (c / 16 % 4)) * kOfChunk;
   }
 
   Buffer from;                           // WHOLE16: the rest of the operand
   uint32_t offset, row_bytes;            // this thread's first chunk; between rows
   int64_t step;                          // from one step to the next, bytes or elements
-  const uint16_t *at[WHOLE16 ? 1 : kEach], *safe;
+  const Elem *at[WHOLE16 ? 1 : kEach], *safe;
   uint4 held[WHOLE16 ? 1 : kEach];
   int rows, column;                      // rows of the tile that exist (at least one); this thread's column
   int k_held;                            // columns or rows of memory of the step that is held
   bool narrow;
 
   // origin: the element (0, 0) of the tile; ld: elements between rows of memory; K columns in all.
-  __device__ __forceinline__ void begin(const uint16_t *origin, int64_t ld, int rows_, int64_t K, int tid) {
+  __device__ __forceinline__ void begin(const Elem *origin, int64_t ld, int rows_, int64_t K, int tid) {
     rows = rows_;
     narrow = (IMAJOR ? rows : K) < 8;
     safe = origin;
@@ -111,13 +128,13 @@ struct OperandTile {
     step = IMAJOR ? ld * KS : KS;
     if constexpr (WHOLE16) {
       const uint64_t p = reinterpret_cast<uint64_t>(origin);
-      row_bytes = uint32_t(ld) * 2;
+      row_bytes = uint32_t(ld) * kElem;
       from[0] = __builtin_amdgcn_readfirstlane(uint32_t(p));
       from[1] = __builtin_amdgcn_readfirstlane(uint32_t(p >> 32));
       from[2] = __builtin_amdgcn_readfirstlane(uint32_t(rows) * row_bytes);
       from[3] = 0x00020000u;
-      offset = IMAJOR && column >= rows ? kOutside : row_of(tid) * row_bytes + column * 2;
-      step *= 2;
+      offset = IMAJOR && column >= rows ? kOutside : row_of(tid) * row_bytes + column * kElem;
+      step *= kElem;
     } else {
 #pragma unroll
       for (int j = 0; j < kEach; ++j) {
@@ -126,7 +143,7 @@ struct OperandTile {
       }
     }
   }
-  // Asks for the next step, of which k_left (at most 64) columns (k-major) or rows of memory (i-major) exist.
+  // Asks for the next step, of which k_left (at most KS) columns (k-major) or rows of memory (i-major) exist.
   __device__ __forceinline__ void issue(uint32_t lds, int k_left, int tid) {
     if constexpr (WHOLE16) {
       if constexpr (IMAJOR) from[2] = uint32_t(k_left) * row_bytes;
@@ -160,11 +177,14 @@ struct OperandTile {
       for (int j = 0; j < kEach; ++j) *reinterpret_cast<uint4 *>(lds + (j * THREADS + tid) * 16) = RowChunk::use(held[j], elements(j, tid), narrow);
     }
   }
-  // Fragment of 16 rows from `row` on (a multiple of 16), columns 32 half .. + 31 of the step: lane (i, g) = (lane % 16, lane / 16)
-  // gets row i, columns 8 g .. 8 g + 7.
+  // Fragment of 16 rows from `row` on (a multiple of 16), columns 32 half .. + 31 (float: 16 half .. + 15) of the step: lane (i, g) =
+  // (lane % 16, lane / 16) gets row i, columns 8 g .. 8 g + 7 (4 g .. 4 g + 3).
   static __device__ __forceinline__ s16x8_t fragment(const char *lds, int row, int half, int lane) {
     const int i = lane & 15, g = lane >> 4;
-    if constexpr (IMAJOR) {
+    if constexpr (IMAJOR && kElem == 4) {
+      const float *at = reinterpret_cast<const float *>(lds) + (half * 16 + 4 * g) * ROWS + ((row + i) ^ 16 * g);
+      return __builtin_bit_cast(s16x8_t, f32x4_t{at[0], at[ROWS], at[2 * ROWS], at[3 * ROWS]});
+    } else if constexpr (IMAJOR) {
       using P = __attribute__((address_space(3))) s16x4_t *;
       s16x4_t part[2];
 #pragma unroll
@@ -174,7 +194,7 @@ struct OperandTile {
       }
       return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      return *reinterpret_cast<const s16x8_t *>(lds + (row + i) * (KS * 2) + (KS == 64 ? ((half * 4 + g) ^ (i >> 1)) << 4 : (g ^ (i >> 2)) << 4));
+      return *reinterpret_cast<const s16x8_t *>(lds + (row + i) * (KS * kElem) + (KS * kElem == 128 ? ((half * 4 + g) ^ (i >> 1)) << 4 : (g ^ (i >> 2)) << 4));
     }
   }
 };
@@ -183,11 +203,12 @@ struct OperandTile {
 // wavefront's part.
 // STEPS: how many steps of KS columns are in LDS or on their way there.  8192 x 8192 x 2048, 256 x 256 tiles, k-major operands: two steps of 64
 // 250 us, four of 32 266; i-major ones 280 and 268.
-template <typename Type, int BM, int BN, int WM, int WN, bool A_IMAJOR, bool B_IMAJOR, bool WHOLE16, int STEPS = 2, int KS = 64>
+template <typename Type, int BM, int BN, int WM, int WN, bool A_IMAJOR, bool B_IMAJOR, bool WHOLE16, int STEPS = 2, int KS = Type::kStep>
 struct TileProduct {
   static constexpr int kThreads = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
-  using A = OperandTile<BM, A_IMAJOR, WHOLE16, kThreads, KS>;
-  using B = OperandTile<BN, B_IMAJOR, WHOLE16, kThreads, KS>;
+  using Elem = typename Type::Elem;
+  using A = OperandTile<Elem, BM, A_IMAJOR, WHOLE16, kThreads, KS>;
+  using B = OperandTile<Elem, BN, B_IMAJOR, WHOLE16, kThreads, KS>;
   static constexpr int kPart = A::kBytes + B::kBytes, kLds = STEPS * kPart;
   static_assert(STEPS >= 2 && (WHOLE16 || STEPS == 2), "");
   f32x4_t acc[FM][FN];
@@ -221,7 +242,7 @@ struct TileProduct {
     __builtin_amdgcn_sched_barrier(0);
   }
   // a, b: the tile's first elements; K columns; rows and columns of the tile that exist.  Every thread of the workgroup calls it.
-  __device__ __forceinline__ void run(char *lds, const uint16_t *a, int64_t lda, int a_rows, const uint16_t *b, int64_t ldb, int b_rows, int64_t K) {
+  __device__ __forceinline__ void run(char *lds, const Elem *a, int64_t lda, int a_rows, const Elem *b, int64_t ldb, int b_rows, int64_t K) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = wave / WN * (BM / WM), col = wave % WN * (BN / WN);
     const uint32_t base = lds_address(lds);
@@ -241,7 +262,7 @@ struct TileProduct {
       // Small tiles, whose runs would be too short to cover a read: all that the next step needs is read while a step is multiplied.  Steps
       // behind the last are asked for and read too, as zeros.
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) issue(i * kPart, K - i * kTileK);
+      for (int i = 0; i < STEPS; ++i) issue(i * kPart, K - i * KS);
       s16x8_t va[2][2][FM], vb[2][2][FN];
       const auto read = [&](s16x8_t (&x)[2][FM], s16x8_t (&y)[2][FN], int part) {
 #pragma unroll
@@ -256,14 +277,14 @@ struct TileProduct {
       __syncthreads();
       read(va[0], vb[0], 0);
       int now = 0;
-      for (int64_t k = K; k > 0; k -= 2 * kTileK) {
+      for (int64_t k = K; k > 0; k -= 2 * KS) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           lds_loads_done<(STEPS - 2) * (A::kEach + B::kEach)>();
           __syncthreads();                       // the next step is there, and this one has been read by all
           const int next = now + kPart == kLds ? 0 : now + kPart;
           read(va[i ^ 1], vb[i ^ 1], next);
-          issue(now, k - (STEPS + i) * kTileK);
+          issue(now, k - (STEPS + i) * KS);
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int kk = 0; kk < 2; ++kk)
@@ -276,7 +297,7 @@ struct TileProduct {
         }
       }
       lds_loads_done<0>();                       // nothing may arrive once the workgroup has given its LDS back
-    } else if constexpr (WHOLE16 && KS == 32) {
+    } else if constexpr (WHOLE16 && KS * sizeof(Elem) == 64) {
       // As below, with two runs a step.
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) issue(i * kPart, K - i * KS);
@@ -307,13 +328,13 @@ struct TileProduct {
       // been read, and its part of LDS gets the step that is STEPS further on.  Steps behind the last are asked for and read too, as zeros,
       // so that the loop has no branches.
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) issue(i * kPart, K - i * kTileK);
+      for (int i = 0; i < STEPS; ++i) issue(i * kPart, K - i * KS);
       lds_loads_done<(STEPS - 1) * (A::kEach + B::kEach)>();
       __syncthreads();
       read_b(b0, lds, 0, col, lane);
       read_a(a0, lds, 0, 0, row, lane);
       int now = 0;
-      for (int64_t k = K; k > 0; k -= kTileK) {
+      for (int64_t k = K; k > 0; k -= KS) {
         read_a(a1, lds + now, 0, 1, row, lane);
         multiply<0>(a0, b0);
         read_b(b1, lds + now, 1, col, lane);
@@ -327,18 +348,18 @@ struct TileProduct {
         read_b(b0, lds + next, 0, col, lane);
         read_a(a0, lds + next, 0, 0, row, lane);
         multiply<1>(a1, b1);
-        issue(now, k - STEPS * kTileK);
+        issue(now, k - STEPS * KS);
         now = next;
       }
       lds_loads_done<0>();                       // nothing may arrive once the workgroup has given its LDS back
     } else {
       issue(0, K);
       int now = 0;
-      for (int64_t k = K; k > 0; k -= kTileK, now ^= kPart) {
+      for (int64_t k = K; k > 0; k -= KS, now ^= kPart) {
         ta.land(lds + now, tid);
         tb.land(lds + now + A::kBytes, tid);
         __syncthreads();                         // one a step: what is written next is the half that was read before the last one
-        issue(now ^ kPart, k - kTileK);
+        issue(now ^ kPart, k - KS);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
           read_b(b0, lds + now, kk, col, lane);

@@ -163,19 +163,19 @@ __device__ __forceinline__ void grouped_tile(const GroupedArgs &a, const RowTile
 }
 
 // Tiles of 256 rows whose expert has no more than 128 left are half the work as one of 128.
-template <int BM, int BN, int WM, int WN, int STEPS, bool W_IMAJOR, bool WHOLE16>
+template <typename Type, int BM, int BN, int WM, int WN, int STEPS, bool W_IMAJOR, bool WHOLE16>
 __global__ __launch_bounds__(WM *WN * 64) void grouped_kernel(const GroupedArgs a) {
-  using P = TileProduct<Bf16, BM, BN, WM, WN, false, W_IMAJOR, WHOLE16, STEPS>;
+  using P = TileProduct<Type, BM, BN, WM, WN, false, W_IMAJOR, WHOLE16, STEPS>;
   __shared__ __attribute__((aligned(16))) char lds[P::kLds];
   const RowTile t = row_tile<BM>(a.ends, a.n_experts, a.rows, a.tiles_n);
   if (t.expert < 0) return;
   if constexpr (BM == 256) {
     if (t.rows <= BM / 2) {
-      grouped_tile<TileProduct<Bf16, BM / 2, BN, WM, WN, false, W_IMAJOR, WHOLE16>, BM / 2, BN, WM, WN, uint16_t>(a, t, lds, W_IMAJOR);
+      grouped_tile<TileProduct<Type, BM / 2, BN, WM, WN, false, W_IMAJOR, WHOLE16>, BM / 2, BN, WM, WN, typename Type::Elem>(a, t, lds, W_IMAJOR);
       return;
     }
   }
-  grouped_tile<P, BM, BN, WM, WN, uint16_t>(a, t, lds, W_IMAJOR);
+  grouped_tile<P, BM, BN, WM, WN, typename Type::Elem>(a, t, lds, W_IMAJOR);
 }
 
 // A few rows, as one decoded token's choices: sixteen weight rows a workgroup, whose four wavefronts take every fourth run of columns (32 of
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(WM *WN * 64) void grouped_f32_kernel(const GroupedA
 
 // The same for transposed float weights, whose rows lie along the result: a lane reads four columns of one of four rows of a step, a wavefront 64 columns of
 // the result, and each of four instructions takes one column of every lane.  Eight wavefronts take every eighth four rows, sixteen of them at
-// once.  One row each for 8 of 128 matrices 1536 x 2048: 19 us, with tiles 42; 32 rows 69 and 127.  (The same with bfloat16 widened
+// once.  One row each for 8 of 128 matrices 1536 x 2048: 19 us, with tiles 38; 32 rows 69 and 116.  (The same with bfloat16 widened
 // on the way was slower than its tiles: 23 and 14 for 8 of them.)
 constexpr int kFewTBlock = 512, kFewTWaves = kFewTBlock / 64, kFewTCols = 64;
 
@@ -315,6 +315,8 @@ struct WeightGradArgs {
   int past;                    // gradients that no cache would keep for who reads them go past the caches: 805 MB in 555 instead of 576 us
 };
 
+constexpr int kPartRows = 64;            // a part of an expert's rows is a multiple of these
+
 // Each die gets an eighth of every expert's tiles (another one for each expert, where eighths differ), since experts differ in their rows: where dies
 // had experts of their own, the last one to finish kept the others waiting (65536 rows over 128 experts: 634 -> 570 us).
 template <typename P, int BM, int BN, int WM, int WN, typename Elem>
@@ -328,8 +330,8 @@ __device__ __forceinline__ void weight_grad_tile(const WeightGradArgs &a, char *
   for (int e = lane; e < expert; e += 64) before = max(before, a.ends[e]);
   int begin = __builtin_amdgcn_readfirstlane(min(wave_max(before), a.rows));
   int end = __builtin_amdgcn_readfirstlane(min(max(a.ends[expert], begin), a.rows));
-  if (a.parts > 1) {                             // a part is a whole number of steps
-    const int64_t length = ((int64_t(end - begin) + kTileK - 1) / kTileK + a.parts - 1) / a.parts * kTileK;
+  if (a.parts > 1) {
+    const int64_t length = ((int64_t(end - begin) + kPartRows - 1) / kPartRows + a.parts - 1) / a.parts * kPartRows;
     const int64_t from = begin + part * length, to = from + length;
     begin = int(from < end ? from : end);
     end = int(to < end ? to : end);
@@ -369,11 +371,11 @@ __global__ __launch_bounds__(256) void weight_grad_join_kernel(const WeightGradA
   else store4(static_cast<float *>(a.dw) + to, sum, n);
 }
 
-template <int BM, int BN, int WM, int WN, int STEPS, bool WHOLE16, int KS = 64>
+template <typename Type, int BM, int BN, int WM, int WN, int STEPS, bool WHOLE16, int KS = Type::kStep>
 __global__ __launch_bounds__(WM *WN * 64) void weight_grad_kernel(const WeightGradArgs a) {
-  using P = TileProduct<Bf16, BM, BN, WM, WN, true, true, WHOLE16, STEPS, KS>;
+  using P = TileProduct<Type, BM, BN, WM, WN, true, true, WHOLE16, STEPS, KS>;
   __shared__ __attribute__((aligned(16))) char lds[P::kLds];
-  weight_grad_tile<P, BM, BN, WM, WN, uint16_t>(a, lds);
+  weight_grad_tile<P, BM, BN, WM, WN, typename Type::Elem>(a, lds);
 }
 
 template <int BM, int BN, int WM, int WN>
@@ -389,8 +391,9 @@ constexpr int64_t kCacheBytes = int64_t(256) << 20;     // memory-side
 constexpr int64_t kMostExpertStride = int64_t(1) << 40;
 inline int64_t tiles_of(int64_t n, int tile) { return (n + tile - 1) / tile; }
 // Whether rows of `width` values can travel straight to LDS.
-inline bool whole16(const void *p, int64_t stride, int width) {
-  return !misaligned(p, 16) && stride % 8 == 0 && width % 8 == 0 && stride >= width && stride <= kMostTileStride;
+inline bool whole16(const void *p, int64_t stride, int width, int elem) {
+  const int of = 16 / elem;
+  return !misaligned(p, 16) && stride % of == 0 && width % of == 0 && stride >= width && stride <= kMostTileStride;
 }
 
 // Workgroups of a launch of `threads` each, or 0 where a launch cannot have so many.
@@ -418,10 +421,16 @@ struct Choice {
   void (*kernel)(Args);
   int bm, bn, threads;
 };
-template <int BM, int BN, int WM, int WN, int STEPS, bool W_IMAJOR, bool WHOLE16>
-Choice<GroupedArgs> grouped_choice() { return {grouped_kernel<BM, BN, WM, WN, STEPS, W_IMAJOR, WHOLE16>, BM, BN, WM * WN * 64}; }
-template <int BM, int BN, int WM, int WN, bool W_IMAJOR>
-Choice<GroupedArgs> grouped_f32_choice() { return {grouped_f32_kernel<BM, BN, WM, WN, W_IMAJOR>, BM, BN, WM * WN * 64}; }
+template <typename Type, int BM, int BN, int WM, int WN, int STEPS, bool W_IMAJOR, bool WHOLE16>
+Choice<GroupedArgs> grouped_choice() { return {grouped_kernel<Type, BM, BN, WM, WN, STEPS, W_IMAJOR, WHOLE16>, BM, BN, WM * WN * 64}; }
+// Float: 64 x 64, since accumulators and LDS of four workgroups then fit a compute unit, and a product of 16 x 16 x 4 takes as long as the larger ones'
+// fewer reads would save (32768 rows, 8 of 2048 x 2048: 2170 us, 127 TFLOP/s; 128 x 128 2097; but 4096 rows, 8 of 1024 x 2048 168 and 249);
+// three steps under way leave room for three workgroups (2227).  Through registers 2500.
+template <bool W_IMAJOR>
+Choice<GroupedArgs> grouped_f32_choice(bool whole) {
+  if (whole) return grouped_choice<F32, 64, 64, 2, 4, 2, W_IMAJOR, true>();
+  return {grouped_f32_kernel<64, 64, 2, 4, W_IMAJOR>, 64, 64, 512};
+}
 
 // Large tiles need few reads for their products, small ones leave fewer places empty and are more.  By rows an expert has on average,
 // where there are as many tiles as compute units: 256 x 256 from 128 rows on (128 matrices of 1536 x 2048, 256 rows each: 305 us, 128 x 128 325),
@@ -433,23 +442,22 @@ Choice<GroupedArgs> choose_grouped(int64_t rows, int n_experts, int n) {
   const int64_t mean = rows / n_experts;
   const auto tiles = [&](int tile) { return n_experts * tiles_of(mean, tile) * tiles_of(n, tile); };
   if constexpr (WHOLE16) {
-    if (mean >= 128 && tiles(256) >= kComputeUnits) return grouped_choice<256, 256, 2, 4, 2, W_IMAJOR, WHOLE16>();
+    if (mean >= 128 && tiles(256) >= kComputeUnits) return grouped_choice<Bf16, 256, 256, 2, 4, 2, W_IMAJOR, WHOLE16>();
   }
-  if (mean >= 48 && tiles(128) >= kComputeUnits) return grouped_choice<128, 128, 2, 4, 2, W_IMAJOR, WHOLE16>();
-  return grouped_choice<64, 128, 2, 4, WHOLE16 ? 3 : 2, W_IMAJOR, WHOLE16>();
+  if (mean >= 48 && tiles(128) >= kComputeUnits) return grouped_choice<Bf16, 128, 128, 2, 4, 2, W_IMAJOR, WHOLE16>();
+  return grouped_choice<Bf16, 64, 128, 2, 4, WHOLE16 ? 3 : 2, W_IMAJOR, WHOLE16>();
 }
-// Whether a kernel for few rows takes a product: up to 16 rows an expert.
-//   bfloat16, not transposed: up to 48 Mi weights to read.  Beyond that (16 rows of 1536 x 2048: 20.3 us, with tiles 20.8; 4 of 5760 x 2880: 31.8
-//   and 28.3) its reads of 64 bytes a row are slower than those of the tiles.  Transposed: never.
-//   float, not transposed: the same, and up to 8 rows an expert of any size (32 rows over 128 of 1536 x 2048: 80 us, with tiles 127; 200 over 32 of
-//   2880 x 2880: 294 and 340; 400 over those of 2880 x 5760: 809 and 686).
-//   float, transposed: sums of at least 128 products (100 rows of 16 experts, 333 x 777: 9.4 us, with tiles 13.8; 128 rows over 128 of
-//   1536 x 2048: 166 and 299; but 20 rows of 16 experts, 64 x 64: 7.1 and 5.1).
+// Whether a kernel for few rows takes a product.
+//   bfloat16, not transposed: up to 16 rows an expert, and up to 48 Mi weights to read.  Beyond that (16 rows of 1536 x 2048: 20.3 us, with tiles
+//   20.8; 4 of 5760 x 2880: 31.8 and 28.3) its reads of 64 bytes a row are slower than those of the tiles.  Transposed: never.
+//   float, not transposed: the same, and up to 4 rows an expert of any size (32 rows over 128 of 1536 x 2048: 80 us, with tiles 109; 512 rows 349
+//   and 386; but 200 over 32 of 2880 x 2880 294 and 288).
+//   float, transposed: sums of at least 128 products, and up to 16 rows an expert with up to 48 Mi weights (100 rows of 16 experts, 333 x 777: 9.4 us, with
+//   tiles 13.9; but 20 rows of 16, 64 x 64: 7.1 and 4.6), or up to 8 (200 over 32 of 2880 x 2880: 221 and 288; but 400 over 32 of 2880 x 5760 609 and 562).
 bool few_rows(int dtype, bool transpose, int64_t rows, int n_experts, int n, int k) {
-  if (rows > 16 * int64_t(n_experts)) return false;
-  if (transpose) return dtype == MOE_SPEC_F32 && n >= 128;
-  if (dtype == MOE_SPEC_F32 && rows <= 8 * int64_t(n_experts)) return true;
-  return (rows < n_experts ? rows : n_experts) * int64_t(n) * k <= int64_t(48) << 20;
+  if (transpose && (dtype != MOE_SPEC_F32 || n < 128)) return false;
+  if (dtype == MOE_SPEC_F32 && rows <= (transpose ? 8 : 4) * int64_t(n_experts)) return true;
+  return rows <= 16 * int64_t(n_experts) && (rows < n_experts ? rows : n_experts) * int64_t(n) * k <= int64_t(48) << 20;
 }
 
 // How a weight gradient is split: tiles of the matrices, and parts of each expert's rows where those alone leave half of the compute units
@@ -462,15 +470,15 @@ WeightGradSplit split_weight_grad(int dtype, bool whole, int64_t rows, int n_exp
   if (!narrow && whole && tiles(256) >= kComputeUnits) return {256, 1};
   const int tile = narrow ? 64 : 128;
   int64_t parts = tiles(tile) > kComputeUnits / 2 ? 1 : 2 * kComputeUnits / tiles(tile);
-  const int64_t most = rows / n_experts / (3 * kTileK);
+  const int64_t most = rows / n_experts / (3 * kPartRows);
   if (parts > most) parts = most;
   return {tile, int(parts < 1 ? 1 : parts > 64 ? 64 : parts)};
 }
 
 // Through registers: 99 experts of 72 x 218 9.6 us with 64 x 128, 12.7 with 128 x 128; 8 of 1001 x 1501, 4000 rows, 42 and 39.
 Choice<WeightGradArgs> staged_weight_grad(int n_experts, int n, int k) {
-  if (n_experts * tiles_of(n, 128) * tiles_of(k, 128) >= kComputeUnits) return {weight_grad_kernel<128, 128, 2, 4, 2, false>, 128, 128, 512};
-  return {weight_grad_kernel<64, 128, 2, 4, 2, false>, 64, 128, 512};
+  if (n_experts * tiles_of(n, 128) * tiles_of(k, 128) >= kComputeUnits) return {weight_grad_kernel<Bf16, 128, 128, 2, 4, 2, false>, 128, 128, 512};
+  return {weight_grad_kernel<Bf16, 64, 128, 2, 4, 2, false>, 64, 128, 512};
 }
 
 }  // namespace
@@ -497,11 +505,11 @@ extern "C" int moe_spec_grouped_product(void *stream, int dtype, const void *x, 
   if (n == 1) w_stride = k;
   if (n_experts == 1) w_expert_stride = 0;
   GroupedArgs a{x, w, y, ends, x_stride, w_stride, w_expert_stride, y_stride, in, int(rows), n_experts, out, 0, out_dtype == MOE_SPEC_BF16};
-  const bool whole = whole16(x, x_stride, in) && whole16(w, w_stride, k) && w_expert_stride % 8 == 0;
+  const bool whole = whole16(x, x_stride, in, elem) && whole16(w, w_stride, k, elem) && w_expert_stride % (16 / elem) == 0;
   const bool few = few_rows(dtype, transpose, rows, n_experts, n, k), wide = dtype == MOE_SPEC_F32;
   const Choice<GroupedArgs> c = few && transpose ? Choice<GroupedArgs>{grouped_few_transposed_kernel, 16, kFewTCols, kFewTBlock}
                                 : few ? Choice<GroupedArgs>{wide ? grouped_few_kernel<float> : grouped_few_kernel<uint16_t>, 16, 16, kFewBlock}
-                                : wide ? (transpose ? grouped_f32_choice<64, 64, 2, 4, true>() : grouped_f32_choice<64, 64, 2, 4, false>())
+                                : wide ? (transpose ? grouped_f32_choice<true>(whole) : grouped_f32_choice<false>(whole))
                                 : transpose           ? (whole ? choose_grouped<true, true>(rows, n_experts, out) : choose_grouped<true, false>(rows, n_experts, out))
                                                       : (whole ? choose_grouped<false, true>(rows, n_experts, out) : choose_grouped<false, false>(rows, n_experts, out));
   a.tiles_n = int(tiles_of(out, c.bn));
@@ -536,7 +544,7 @@ extern "C" int moe_spec_grouped_weight_grad(void *stream, int dtype, const void 
   if (rows && (dw == dy || dw == x)) return train_fail(MOE_SPEC_EINVAL, "grouped_weight_grad: dw must not be dy or x");
   if (rows <= 1) dy_stride = n, x_stride = k;
   if (n_experts == 1) dw_expert_stride = 0;
-  const bool whole = whole16(dy, dy_stride, n) && whole16(x, x_stride, k);
+  const bool whole = whole16(dy, dy_stride, n, elem) && whole16(x, x_stride, k, elem);
   // the workspace is that of sixteen-byte rows, whatever these are, so that its size goes by sizes alone
   const WeightGradSplit split = split_weight_grad(dtype, true, rows, n_experts, n, k);
   const size_t need = moe_spec_grouped_weight_grad_workspace_bytes(dtype, rows, n_experts, n, k);
@@ -546,11 +554,11 @@ extern "C" int moe_spec_grouped_weight_grad(void *stream, int dtype, const void 
                    static_cast<float *>(workspace), int64_t(n_experts) * n * k * size_of(out_dtype) > kCacheBytes};
   // Large tiles take four steps of 32 rows: an expert's rows are few steps, and the first arrives sooner (512 rows an expert, 128 of
   // 1536 x 2048: 562 -> 521 us).
-  const Choice<WeightGradArgs> c = dtype == MOE_SPEC_F32 ? Choice<WeightGradArgs>{weight_grad_f32_kernel<64, 64, 2, 4>, 64, 64, 512}
+  const Choice<WeightGradArgs> c = dtype == MOE_SPEC_F32 ? Choice<WeightGradArgs>{whole ? weight_grad_kernel<F32, 64, 64, 2, 4, 2, true> : weight_grad_f32_kernel<64, 64, 2, 4>, 64, 64, 512}
                                    : !whole              ? staged_weight_grad(n_experts, n, k)
-                                   : split.tile == 256   ? Choice<WeightGradArgs>{weight_grad_kernel<256, 256, 2, 4, 4, true, 32>, 256, 256, 512}
-                                   : split.tile == 128   ? Choice<WeightGradArgs>{weight_grad_kernel<128, 128, 2, 4, 2, true>, 128, 128, 512}
-                                                         : Choice<WeightGradArgs>{weight_grad_kernel<64, 64, 2, 2, 4, true>, 64, 64, 256};
+                                   : split.tile == 256   ? Choice<WeightGradArgs>{weight_grad_kernel<Bf16, 256, 256, 2, 4, 4, true, 32>, 256, 256, 512}
+                                   : split.tile == 128   ? Choice<WeightGradArgs>{weight_grad_kernel<Bf16, 128, 128, 2, 4, 2, true>, 128, 128, 512}
+                                                         : Choice<WeightGradArgs>{weight_grad_kernel<Bf16, 64, 64, 2, 2, 4, true>, 64, 64, 256};
   a.tiles_n = int(tiles_of(n, c.bm));
   a.tiles_k = int(tiles_of(k, c.bn));
   const unsigned grid = grid_of(int64_t(n_experts) * a.parts * tiles_of(int64_t(a.tiles_n) * a.tiles_k, 8) * 8, c.threads);
