@@ -29,7 +29,7 @@ struct MuonStack {
   int rows, cols, m, n, ld_m, ld_n, slices, slice_rows;
 };
 // Settings of a call, and the stacks of a launch: up to N of them.  One stack by itself needs no search and has a dependent read of the
-// argument block fewer, up to four have a short one: up to 0.9 us a launch (18 launches; one matrix of 256 x 256: 96 -> 80 us, three: 169 -> 161).
+// argument block fewer, up to four have a short one: up to 0.9 us a launch (17 launches; one matrix of 256 x 256: 94 -> 78 us, three: 162 -> 154).
 struct MuonSettings {
   float mu, decay, rate, scale, ca, cb, cc;
   const float *scale_dev;
@@ -77,8 +77,8 @@ struct Chunk {
 };
 
 // A workgroup's part of a matrix that is gone through as it lies: whole rows, kAhead chunks a thread at a time.  Parts of 4096 values in two rounds of
-// loads at once stream at 4.4 (momentum), 4.8 (X_0) and 4.8 TB/s (result) over 75 M values and start small matrices on more compute units; parts of
-// 16384 at 4.0, 4.7 and 4.7, with one chunk at a time 4.7, 4.5 and 4.4.
+// loads at once stream at 4.4 (momentum) and 4.8 TB/s (X_0) over 75 M values and start small matrices on more compute units; parts of
+// 16384 at 4.0 and 4.7, with one chunk at a time 4.7 and 4.5.
 constexpr int kAhead = 2;
 struct Slice {
   int64_t matrix;
@@ -277,67 +277,16 @@ struct Result {
   }
 };
 
-template <int N>
-__global__ __launch_bounds__(kMuonBlock) void muon_finish_kernel(const MuonArgs<N> a) {
-  __shared__ __attribute__((aligned(16))) uint16_t tile[kTurn][kTurn + 8];
-  const int which = stack_of(a.first, blockIdx.x);
-  const MuonStack &t = a.t[which];
-  const uint32_t at = blockIdx.x - a.first[which];
-  if (t.rows <= t.cols) {
-    const Slice slice(t, at);
-    const uint16_t *x = t.x[a.which] + slice.matrix * t.m * t.ld_n;
-    for (int i = threadIdx.x; i < slice.chunks; i += kAhead * kMuonBlock) {
-      Result r[kAhead];
-#pragma unroll
-      for (int q = 0; q < kAhead; ++q) {
-        slice.place(r[q], i + q * kMuonBlock, t.cols);
-        r[q].load(t, slice.matrix);
-        if (r[q].n > 0) r[q].x = *reinterpret_cast<const uint4 *>(x + int64_t(r[q].row) * t.ld_n + r[q].col);
-      }
-#pragma unroll
-      for (int q = 0; q < kAhead; ++q) r[q].store(a, t, slice.matrix);
-    }
-    return;
-  }
-  const Turn turn(t, at);
-  const uint16_t *x = t.x[a.which] + turn.matrix * t.m * t.ld_n;
-  Result r[2];
-  uint4 v[2];
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int i = threadIdx.x + q * kMuonBlock, across = i / (kTurn / 8), down = i % (kTurn / 8) * 8;
-    v[q] = uint4{0, 0, 0, 0};
-    if (turn.col0 + across < t.cols && turn.row0 + down < t.ld_n) v[q] = *reinterpret_cast<const uint4 *>(x + int64_t(turn.col0 + across) * t.ld_n + turn.row0 + down);
-    r[q].row = turn.row0 + i / (kTurn / 8);
-    r[q].col = turn.col0 + i % (kTurn / 8) * 8;
-    r[q].n = r[q].row < t.rows ? t.cols - r[q].col : 0;
-    r[q].load(t, turn.matrix);
-  }
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int i = threadIdx.x + q * kMuonBlock, across = i / (kTurn / 8), down = i % (kTurn / 8) * 8;
-    uint16_t e[8];
-    __builtin_memcpy(e, &v[q], 16);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) tile[down + j][across] = e[j];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    r[q].x = *reinterpret_cast<const uint4 *>(&tile[r[q].row - turn.row0][r[q].col - turn.col0]);
-    r[q].store(a, t, turn.matrix);
-  }
-}
-
-// One product for every matrix.  SQUARE: A = X X^T; POLYNOMIAL: B = a I + b A + c A A; APPLY: X' = B X.  A and B are symmetric: of them
-// only tiles on and below the diagonal are worked out, and written to both places.
-enum MuonProduct { SQUARE, POLYNOMIAL, APPLY };
+// One product for every matrix.  SQUARE: A = X X^T; POLYNOMIAL: B = a I + b A + c A A; APPLY: X' = B X; RESULT: the last of those,
+// which goes to the parameters and copies instead.  A and B are symmetric: of them only tiles on and below the diagonal are worked out, and written
+// to both places.
+enum MuonProduct { SQUARE, POLYNOMIAL, APPLY, RESULT };
 
 template <int TILE, int WM, int WN, int STEPS, MuonProduct KIND, int N>
 __global__ __launch_bounds__(WM *WN * 64) void muon_product_kernel(const MuonArgs<N> a) {
 #pragma clang fp contract(off)                   // a matrix gets the same bits in every launch's company
-  constexpr bool SYMMETRIC = KIND != APPLY;
-  using P = TileProduct<F16, TILE, TILE, WM, WN, false, KIND == APPLY, true, STEPS>;
+  constexpr bool SYMMETRIC = KIND == SQUARE || KIND == POLYNOMIAL;
+  using P = TileProduct<F16, TILE, TILE, WM, WN, false, !SYMMETRIC, true, STEPS>;
   using R = ResultTile<TILE / WM, TILE / WN>;
   __shared__ __attribute__((aligned(16))) char lds[P::kLds];
   const uint32_t share = (a.total + 7) / 8, logical = blockIdx.x % 8 * share + blockIdx.x / 8;      // a die gets a run of tiles
@@ -362,9 +311,9 @@ __global__ __launch_bounds__(WM *WN * 64) void muon_product_kernel(const MuonArg
   const int rows = min(TILE, t.m - row0), some = min(TILE, cols - col0), K = KIND == SQUARE ? t.n : t.m;
   if constexpr (KIND == SQUARE) p.run(lds, x + int64_t(row0) * t.ld_n, t.ld_n, rows, x + int64_t(col0) * t.ld_n, t.ld_n, some, K);
   if constexpr (KIND == POLYNOMIAL) p.run(lds, ta + int64_t(row0) * t.ld_m, t.ld_m, rows, ta + int64_t(col0) * t.ld_m, t.ld_m, some, K);
-  if constexpr (KIND == APPLY) p.run(lds, tb + int64_t(row0) * t.ld_m, t.ld_m, rows, x + col0, t.ld_n, some, K);
+  if constexpr (!SYMMETRIC) p.run(lds, tb + int64_t(row0) * t.ld_m, t.ld_m, rows, x + col0, t.ld_n, some, K);
   const int ld = SYMMETRIC ? t.ld_m : t.ld_n;
-  uint16_t *out = KIND == APPLY ? t.x[a.which ^ 1] + matrix * t.m * t.ld_n : (KIND == SQUARE ? t.a : t.b) + matrix * t.m * t.ld_m;
+  uint16_t *out = !SYMMETRIC ? t.x[a.which ^ 1] + matrix * t.m * t.ld_n : (KIND == SQUARE ? t.a : t.b) + matrix * t.m * t.ld_m;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
   const int wave_row = row0 + wave / WN * (TILE / WM), wave_col = col0 + wave % WN * (TILE / WN);
   char *mine = lds + wave * R::kBytes;
@@ -390,6 +339,30 @@ __global__ __launch_bounds__(WM *WN * 64) void muon_product_kernel(const MuonArg
       __builtin_memcpy(&w, e, 8);
       R::put(mine, f, h, w, lane);
     }
+  }
+  if constexpr (KIND == RESULT) {
+    // as many chunks at once as a lane has registers for
+    constexpr int kGroup = R::kEach < 4 ? R::kEach : 4;
+    const bool upright = t.rows > t.cols;        // a column of X is a row of the matrix
+#pragma unroll
+    for (int from = 0; from < R::kEach; from += kGroup) {
+      Result result[kGroup];
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) {
+        const int q = from + j;
+        constexpr int kDown = TILE / WM / 32;    // runs of 32 rows of X
+        const int r = upright ? q % kDown * 32 + 8 * g : (q * 64 + lane) / R::kAcross;
+        const int c = upright ? q / kDown * 16 : (q * 64 + lane) % R::kAcross * 8;
+        result[j].row = upright ? wave_col + c + i : wave_row + r;
+        result[j].col = upright ? wave_row + r : wave_col + c;
+        result[j].n = result[j].row < t.rows ? t.cols - result[j].col : 0;
+        result[j].load(t, matrix);
+        result[j].x = upright ? R::column(mine, r, c, lane) : R::chunk(mine, r, c / 8);
+      }
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) result[j].store(a, t, matrix);
+    }
+    return;
   }
 #pragma unroll
   for (int q = 0; q < R::kEach; ++q) {
@@ -581,7 +554,7 @@ const char *iteration_fault(const double *c, int iterations) {
   return nullptr;
 }
 
-// All launches for up to kPerMuonLaunch stacks; a's scalars are set.  Stops at the first that fails.
+// Where each stack's workgroups begin in a launch, and how many there are.
 template <int N, typename Count>
 void firsts(MuonArgs<N> &a, int n, Count workgroups, unsigned &grid) {
   grid = 0;
@@ -593,7 +566,7 @@ void firsts(MuonArgs<N> &a, int n, Count workgroups, unsigned &grid) {
 
 inline int64_t tiles(int64_t n, int tile) { return (n + tile - 1) / tile; }
 inline int64_t begin_blocks(const MuonStack &t) { return t.count * t.slices; }
-// Of the launches that bring X and take the result.
+// Of the launch that brings X.
 inline int64_t turn_blocks(const MuonStack &t) {
   return t.rows <= t.cols ? begin_blocks(t) : t.count * tiles(t.rows, kTurn) * tiles(t.cols, kTurn);
 }
@@ -609,21 +582,24 @@ inline int64_t most_blocks(const MuonStack &t) {
 constexpr int64_t kMostMuonBlocks = (int64_t(1) << 32) / kMuonBlock - 1;
 
 // One product over n stacks.  A compute unit holds one workgroup of 256 x 256 tiles, two of 128 x 128 or four of 64 x 64, which take about
-// 1 : 0.62 : 0.6 of the time for a round of them (256 x 256 tiles reach 1050 TFLOP/s, 128 x 128 820, 64 x 64 420): the tile whose rounds are done first.
+// 1 : 0.62 : 0.6 of the time for a round of them (256 x 256 tiles reach 1050 TFLOP/s, 128 x 128 820, 64 x 64 420): the tile whose rounds are done first.  The last product,
+// whose workgroups then read and write parameters, has two of them a compute unit, so that one's products cover another's traffic: 48 matrices of
+// 768 x 2048 1791 us, with 256 x 256 tiles there 1810, with a launch for the parameters 1807 (one matrix of 256 x 256: 78 and 80).
 template <MuonProduct KIND, int N>
 hipError_t run_product(MuonArgs<N> &a, int n, hipStream_t s) {
-  int tile = 256, best = 256;
-  double least = 0.0;
-  const auto blocks = [&](const MuonStack &t) { return KIND == APPLY ? apply_blocks(t, tile) : square_blocks(t, tile); };
+  int tile = KIND == RESULT ? 128 : 256, best = tile;
+  double least = INFINITY;
+  const auto blocks = [&](const MuonStack &t) { return KIND == APPLY || KIND == RESULT ? apply_blocks(t, tile) : square_blocks(t, tile); };
   for (; tile >= 64; tile /= 2) {
     firsts(a, n, blocks, a.total);
     const double time = tile == 256 ? (a.total + 255) / 256 : tile == 128 ? 0.62 * ((a.total + 511) / 512) : 0.6 * ((a.total + 1023) / 1024);
-    if (tile == 256 || time < least) best = tile, least = time;
+    if (time < least) best = tile, least = time;
   }
   tile = best;
   firsts(a, n, blocks, a.total);
   const unsigned grid = (a.total + 7) / 8 * 8;
-  if (tile == 256) return launch(muon_product_kernel<256, 2, 4, 2, KIND, N>, grid, 512, s, a);
+  if constexpr (KIND != RESULT)
+    if (tile == 256) return launch(muon_product_kernel<256, 2, 4, 2, KIND, N>, grid, 512, s, a);
   if (tile == 128) return launch(muon_product_kernel<128, 2, 4, 2, KIND, N>, grid, 512, s, a);
   return launch(muon_product_kernel<64, 2, 2, 4, KIND, N>, grid, 256, s, a);
 }
@@ -639,6 +615,7 @@ const char *stack_fault(int64_t count, int64_t rows, int64_t cols) {
   return most_blocks(t) > kMostMuonBlocks ? "more matrices than one launch can take" : nullptr;
 }
 
+// All launches for up to N stacks; a's scalars are set.  Stops at the first that fails.
 template <int N>
 hipError_t run_launches(MuonArgs<N> &a, int n, int iterations, bool grad_bf16, hipStream_t s) {
   unsigned grid;
@@ -652,12 +629,9 @@ hipError_t run_launches(MuonArgs<N> &a, int n, int iterations, bool grad_bf16, h
     a.which = i & 1;
     e = run_product<SQUARE>(a, n, s);
     if (e == hipSuccess) e = run_product<POLYNOMIAL>(a, n, s);
-    if (e == hipSuccess) e = run_product<APPLY>(a, n, s);
+    if (e == hipSuccess) e = i + 1 < iterations ? run_product<APPLY>(a, n, s) : run_product<RESULT>(a, n, s);
   }
-  if (e != hipSuccess) return e;
-  a.which = iterations & 1;
-  firsts(a, n, turn_blocks, grid);
-  return launch(muon_finish_kernel<N>, grid, kMuonBlock, s, a);
+  return e;
 }
 
 template <int N>
