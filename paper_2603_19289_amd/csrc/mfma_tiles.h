@@ -146,17 +146,10 @@ struct OperandTile {
   // Asks for the next step, of which k_left (at most KS) columns (k-major) or rows of memory (i-major) exist.
   __device__ __forceinline__ void issue(uint32_t lds, int k_left, int tid) {
     if constexpr (WHOLE16) {
-      if constexpr (IMAJOR) from[2] = uint32_t(k_left) * row_bytes;
-      const uint32_t mine = !IMAJOR && column >= k_left ? kOutside : offset;
-      const uint32_t base = __builtin_amdgcn_readfirstlane(lds + (tid & ~63) * 16);
+      limit(k_left);
 #pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const uint32_t o = mine + j * kApart * row_bytes;
-        load_to_lds(from, j == 0 || mine != kOutside ? o : kOutside, base + j * THREADS * 16);
-      }
-      const uint64_t p = (uint64_t(from[1]) << 32 | from[0]) + uint64_t(step);
-      from[0] = uint32_t(p);
-      from[1] = uint32_t(p >> 32);
+      for (int j = 0; j < kEach; ++j) issue_chunk(lds, j, k_left, tid);
+      advance();
     } else {
       k_held = k_left;
 #pragma unroll
@@ -165,6 +158,19 @@ struct OperandTile {
         at[j] += step;
       }
     }
+  }
+  // The same in parts, straight to LDS: limit, each chunk, advance.
+  __device__ __forceinline__ void limit(int k_left) {
+    if constexpr (IMAJOR) from[2] = uint32_t(k_left) * row_bytes;
+  }
+  __device__ __forceinline__ void issue_chunk(uint32_t lds, int j, int k_left, int tid) {
+    const uint32_t mine = !IMAJOR && column >= k_left ? kOutside : offset, o = mine + j * kApart * row_bytes;
+    load_to_lds(from, j == 0 || mine != kOutside ? o : kOutside, __builtin_amdgcn_readfirstlane(lds + (tid & ~63) * 16) + j * THREADS * 16);
+  }
+  __device__ __forceinline__ void advance() {
+    const uint64_t p = (uint64_t(from[1]) << 32 | from[0]) + uint64_t(step);
+    from[0] = uint32_t(p);
+    from[1] = uint32_t(p >> 32);
   }
   // How many elements of a thread's chunk j exist.
   __device__ __forceinline__ int elements(int j, int tid) const {
@@ -240,6 +246,33 @@ struct TileProduct {
       for (int h = 0; h < FN; ++h) acc[UPPER * FH + f][h] = Type::mfma(b[h], a[f], acc[UPPER * FH + f][h]);
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
+  }
+  // The same for large tiles, where a wavefront's reads and loads, asked for at once, would hold up its products while the others' go first: a quarter
+  // of them, between(f), behind each row of products.  256 x 256, 16 x 2048 rows of 2048 to 4096 columns: 494 -> 474 us, 1160 TFLOP/s; 65536 rows of
+  // 128 experts, 1536 x 2048: 478 -> 450.  i-major operands are read ahead all the same (32768 rows, 32 of 5760 x 2880, transposed: 1095 us, between the
+  // products 1120), and shorter runs
+  // have no room for it (8 of 1024 x 4096 orthogonalised, mostly by 128 x 128: 795 us, with it 835).
+  static constexpr bool kLong = FH >= 4, kReadAhead = B_IMAJOR;
+  template <int UPPER, typename Between>
+  __device__ __forceinline__ void multiply(const s16x8_t (&a)[FH], const s16x8_t (&b)[FN], Between between) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int f = 0; f < FH; ++f) {
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int h = 0; h < FN; ++h) acc[UPPER * FH + f][h] = Type::mfma(b[h], a[f], acc[UPPER * FH + f][h]);
+      __builtin_amdgcn_s_setprio(0);
+      __builtin_amdgcn_sched_barrier(0);
+      between(f);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  static __device__ __forceinline__ void read_a(s16x8_t (&v)[FH], int f, const char *part, int kk, int upper, int row, int lane) {
+    v[f] = A::fragment(part, row + 16 * (upper * FH + f), kk, lane);
+  }
+  static __device__ __forceinline__ void read_b(s16x8_t (&v)[FN], int f, const char *part, int kk, int col, int lane) {
+#pragma unroll
+    for (int h = 0; h < FN; ++h) if (h * FH / FN == f) v[h] = B::fragment(part + A::kBytes, col + 16 * h, kk, lane);
   }
   // a, b: the tile's first elements; K columns; rows and columns of the tile that exist.  Every thread of the workgroup calls it.
   __device__ __forceinline__ void run(char *lds, const Elem *a, int64_t lda, int a_rows, const Elem *b, int64_t ldb, int b_rows, int64_t K) {
@@ -335,20 +368,53 @@ struct TileProduct {
       read_a(a0, lds, 0, 0, row, lane);
       int now = 0;
       for (int64_t k = K; k > 0; k -= KS) {
-        read_a(a1, lds + now, 0, 1, row, lane);
-        multiply<0>(a0, b0);
-        read_b(b1, lds + now, 1, col, lane);
-        read_a(a0, lds + now, 1, 0, row, lane);
-        multiply<1>(a1, b0);
-        read_a(a1, lds + now, 1, 1, row, lane);
-        multiply<0>(a0, b1);
-        lds_loads_done<(STEPS - 2) * (A::kEach + B::kEach)>();
-        __syncthreads();
         const int next = now + kPart == kLds ? 0 : now + kPart;
-        read_b(b0, lds + next, 0, col, lane);
-        read_a(a0, lds + next, 0, 0, row, lane);
-        multiply<1>(a1, b1);
-        issue(now, k - STEPS * KS);
+        const char *part = lds + now, *following = lds + next;
+        const auto there = [] {
+          lds_loads_done<(STEPS - 2) * (A::kEach + B::kEach)>();
+          __syncthreads();
+        };
+        if constexpr (kLong) {
+          multiply<0>(a0, b0, [&](int f) { read_a(a1, f, part, 0, 1, row, lane); });
+          if constexpr (kReadAhead) read_b(b1, part, 1, col, lane);
+          multiply<1>(a1, b0, [&](int f) {
+            if constexpr (!kReadAhead) read_b(b1, f, part, 1, col, lane);
+            read_a(a0, f, part, 1, 0, row, lane);
+          });
+          multiply<0>(a0, b1, [&](int f) { read_a(a1, f, part, 1, 1, row, lane); });
+          there();
+          if constexpr (kReadAhead) read_b(b0, following, 0, col, lane);
+          const int64_t ahead = k - STEPS * KS;
+          const int left = int(ahead < KS ? (ahead > 0 ? ahead : 0) : int64_t(KS));
+          ta.limit(left);
+          tb.limit(left);
+          multiply<1>(a1, b1, [&](int f) {
+            if constexpr (!kReadAhead) read_b(b0, f, following, 0, col, lane);
+            read_a(a0, f, following, 0, 0, row, lane);
+            constexpr int kAll = A::kEach + B::kEach;
+#pragma unroll
+            for (int j = 0; j < kAll; ++j) {
+              if (j * FH / kAll != f) continue;
+              if (j < A::kEach) ta.issue_chunk(base + now, j, left, tid);
+              else tb.issue_chunk(base + now + A::kBytes, j - A::kEach, left, tid);
+            }
+          });
+          ta.advance();
+          tb.advance();
+        } else {
+          read_a(a1, part, 0, 1, row, lane);
+          multiply<0>(a0, b0);
+          read_b(b1, part, 1, col, lane);
+          read_a(a0, part, 1, 0, row, lane);
+          multiply<1>(a1, b0);
+          read_a(a1, part, 1, 1, row, lane);
+          multiply<0>(a0, b1);
+          there();
+          read_b(b0, following, 0, col, lane);
+          read_a(a0, following, 0, 0, row, lane);
+          multiply<1>(a1, b1);
+          issue(now, k - STEPS * KS);
+        }
         now = next;
       }
       lds_loads_done<0>();                       // nothing may arrive once the workgroup has given its LDS back
