@@ -33,7 +33,7 @@ __device__ __forceinline__ TilePlace tile_place(int at, int rows, int cols, int 
 
 // Which tile of at most BM rows of one expert, and of which columns, this workgroup takes.  Consecutive workgroups go to the eight
 // dies in turn; each die gets a run of tiles: large ones in strips of 6 rows of the 32 that a die's compute units work on (32 experts of 5760 x 2880,
-// 1024 rows each, transposed: 1147 -> 1114 us), others columns first.
+// 1024 rows each, transposed: 1147 -> 1114 us then, 1078 now), others columns first.
 template <int BM>
 __device__ __forceinline__ RowTile row_tile(const int32_t *ends, int n_experts, int rows, int tiles_n) {
   const int lane = threadIdx.x & 63;
@@ -433,8 +433,8 @@ Choice<GroupedArgs> grouped_f32_choice(bool whole) {
 }
 
 // Large tiles need few reads for their products, small ones leave fewer places empty and are more.  By rows an expert has on average,
-// where there are as many tiles as compute units: 256 x 256 from 128 rows on (128 matrices of 1536 x 2048, 256 rows each: 305 us, 128 x 128 325),
-// 128 x 128 from 48 (32 of 5760 x 2880, 64 rows each: 230 us; 64 x 128 271), otherwise 64 x 128 with three steps under way (12 rows each: 149 and
+// where there are as many tiles as compute units: 256 x 256 from 128 rows on (128 matrices of 1536 x 2048, 256 rows each: 286 us, 128 x 128 333),
+// 128 x 128 from 48 (32 of 5760 x 2880, 64 rows each: 243 us; 64 x 128 284), otherwise 64 x 128 with three steps under way (12 rows each: 149 and
 // 186 us, 5.5 and 5.9 TB/s; 128 x 128 149 and 187; 8 matrices of 512 x 2048: 14 us, 128 x 128 24).
 // Through registers the same two smaller tiles (8 experts of 1001 x 1501, 500 rows each: 42 and 47 us; 16 of 333 x 777, 31 rows each: 18 and 15).
 template <bool W_IMAJOR, bool WHOLE16>
