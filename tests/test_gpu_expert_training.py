@@ -145,6 +145,20 @@ def test_weight_gradients_of_long_groups(sizes, n, k, dtype):
         assert torch.equal(out[:, :, :k], want.to(kind)) and torch.all(out[:, :, k:] == 2.0)
 
 
+@pytest.mark.parametrize("transpose", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes,n,k", [([2, 0, -1], 7000, 3701), ([7], 7104, 7104), ([1, 16, 0, 6], 4000, 3328)], ids=str)
+def test_few_rows_of_large_matrices(sizes, n, k, dtype, transpose):
+    from paper_2603_19289_amd import training as T
+    ends, rows, n, k = groups((sizes, n, k))
+    g = torch.Generator("cuda").manual_seed(rows + n)
+    x, w = (torch.randint(-3, 4, s, generator=g, device="cuda").to(TYPES[dtype]) for s in ((rows, n if transpose else k), (len(ends), n, k)))
+    got = T.grouped_product(x, w, i32(ends), transpose=transpose, dtype=torch.float32)
+    for i, (b, f) in enumerate(bounds(ends, rows)):
+        assert torch.equal(got[b:f], (x[b:f].double() @ (w[i].double() if transpose else w[i].double().t())).float()), i
+    assert not got[ends[-1]:].any()
+
+
 @pytest.mark.parametrize("dtype,rows,experts,n,k", [("f32", 333, 3, 130, 700), ("bf16", 333, 3, 136, 704), ("bf16", 50, 7, 96, 2048), ("bf16", 301, 2, 75, 333)])
 def test_products_of_any_values(dtype, rows, experts, n, k):
     """2 u for each term of a sum, and for float32 the products' own rounding; half a step of what goes out."""
@@ -516,6 +530,25 @@ def test_muon_copies_into_expert_blocks(rows, cols):
     assert torch.all(blocks == 6.0)
     with pytest.raises(ValueError):
         T.Muon([p], lr=0.1, copies=[torch.zeros(4, cols, rows, dtype=torch.bfloat16, device="cuda").transpose(1, 2)])
+
+
+@pytest.mark.parametrize("shape", [(300, 200), (20, 70, 130), (9, 130, 66), (5, 777, 1111), (5, 1111, 777), (3, 1500, 1030)], ids=str)
+def test_muon_of_larger_matrices(shape):
+    """Every size of tile, wide and upright: parameters go by what orthogonalise returns, which is off from the update by one rounding to bfloat16;
+    a matrix of a stack gets what it gets by itself; copies are the parameters rounded."""
+    from paper_2603_19289_amd import training as T
+    g = torch.randn(shape, generator=rng(1)).cuda()
+    p = torch.randn(shape, generator=rng(2)).cuda() * 0.1
+    before, copy = p.double(), torch.zeros(shape, device="cuda", dtype=torch.bfloat16)
+    lr, decay, rms = 0.1, 0.3, 0.2
+    T.Muon([p], lr=lr, momentum=0.0, nesterov=False, weight_decay=decay, update_rms=rms, copies=[copy]).step([g])
+    o = T.orthogonalise(g)
+    for i in range(shape[0] if len(shape) == 3 else 0):
+        assert torch.equal(T.orthogonalise(g[i]), o[i]), i
+    rate, o = lr * rms * math.sqrt(max(shape[-2:])), o.double()
+    bound = rate * o.abs() * half(torch.bfloat16) / (1 - half(torch.bfloat16)) + 4 * U * (before.abs() + rate * o.abs())
+    close(p, (before * (1 - lr * decay) - rate * o).cpu(), bound.cpu(), shape)
+    assert torch.equal(copy, p.to(torch.bfloat16))
 
 
 def test_muon_leaves_out_parameters_without_gradient():
