@@ -105,10 +105,13 @@ struct TileProductF32 {
           for (int h = 0; h < FN; ++h) acc[f][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(vb[h], va[f], acc[f][h], 0, 0, 0);
       }
     };
+    RunOfSums<FM, FN> sums;
     for (int64_t k = K; k > 0; k -= 2 * A::kStep) {
       step(k, ta[0], tb[0], lds);
       if (k > A::kStep) step(k - A::kStep, ta[1], tb[1], lds + kPart);
+      sums.behind(acc, 2 * A::kStep);
     }
+    sums.end(acc);
   }
 };
 

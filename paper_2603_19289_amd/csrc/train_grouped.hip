@@ -164,7 +164,7 @@ __device__ __forceinline__ void grouped_tile(const GroupedArgs &a, const RowTile
 
 // Tiles of 256 rows whose expert has no more than 128 left are half the work as one of 128.
 template <typename Type, int BM, int BN, int WM, int WN, int STEPS, bool W_IMAJOR, bool WHOLE16>
-__global__ __launch_bounds__(WM *WN * 64) void grouped_kernel(const GroupedArgs a) {
+__global__ __launch_bounds__(WM *WN * 64, Type::kWaves) void grouped_kernel(const GroupedArgs a) {
   using P = TileProduct<Type, BM, BN, WM, WN, false, W_IMAJOR, WHOLE16, STEPS>;
   __shared__ __attribute__((aligned(16))) char lds[P::kLds];
   const RowTile t = row_tile<BM>(a.ends, a.n_experts, a.rows, a.tiles_n);
@@ -372,7 +372,7 @@ __global__ __launch_bounds__(256) void weight_grad_join_kernel(const WeightGradA
 }
 
 template <typename Type, int BM, int BN, int WM, int WN, int STEPS, bool WHOLE16, int KS = Type::kStep>
-__global__ __launch_bounds__(WM *WN * 64) void weight_grad_kernel(const WeightGradArgs a) {
+__global__ __launch_bounds__(WM *WN * 64, Type::kWaves) void weight_grad_kernel(const WeightGradArgs a) {
   using P = TileProduct<Type, BM, BN, WM, WN, true, true, WHOLE16, STEPS, KS>;
   __shared__ __attribute__((aligned(16))) char lds[P::kLds];
   weight_grad_tile<P, BM, BN, WM, WN, typename Type::Elem>(a, lds);
@@ -423,9 +423,9 @@ struct Choice {
 };
 template <typename Type, int BM, int BN, int WM, int WN, int STEPS, bool W_IMAJOR, bool WHOLE16>
 Choice<GroupedArgs> grouped_choice() { return {grouped_kernel<Type, BM, BN, WM, WN, STEPS, W_IMAJOR, WHOLE16>, BM, BN, WM * WN * 64}; }
-// Float: 64 x 64, since accumulators and LDS of four workgroups then fit a compute unit, and a product of 16 x 16 x 4 takes as long as the larger ones'
-// fewer reads would save (32768 rows, 8 of 2048 x 2048: 2170 us, 127 TFLOP/s; 128 x 128 2097; but 4096 rows, 8 of 1024 x 2048 168 and 249);
-// three steps under way leave room for three workgroups (2227).  Through registers 2500.
+// Float: 64 x 64, of which three workgroups fit a compute unit; its instructions take eight times as long as those of 16 bits, so that fewer reads
+// gain little (32768 rows, 8 of 2048 x 2048: 2165 us, 127 TFLOP/s; 128 x 128 2097; but 4096 rows, 8 of 1024 x 2048 171 and 249).  Three steps under
+// way: 2227.  Through registers 2500.
 template <bool W_IMAJOR>
 Choice<GroupedArgs> grouped_f32_choice(bool whole) {
   if (whole) return grouped_choice<F32, 64, 64, 2, 4, 2, W_IMAJOR, true>();
