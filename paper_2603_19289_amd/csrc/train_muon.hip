@@ -598,8 +598,8 @@ inline int64_t most_blocks(const MuonStack &t) {
 }
 constexpr int64_t kMostMuonBlocks = (int64_t(1) << 32) / kMuonBlock - 1;
 
-// One product over n stacks.  A compute unit holds one workgroup of 256 x 256 tiles, two of 128 x 128 or four of 64 x 64, which take about
-// 1 : 0.62 : 0.6 of the time for a round of them (256 x 256 tiles reach 1050 TFLOP/s, 128 x 128 820, 64 x 64 420): the tile whose rounds are done first.  The last product,
+// One product over n stacks.  256 tiles of 256 x 256 are a round of what the compute units hold, and so are 512 of 128 x 128; they take about 1 : 0.62 of the
+// time, and two rounds of 64 x 64, 1024 tiles, 0.6 (256 x 256 tiles reach 1050 TFLOP/s, 128 x 128 820, 64 x 64 420): the tile that is done first.  The last product,
 // whose workgroups then read and write parameters, has two of them a compute unit, so that one's products cover another's traffic: 48 matrices of
 // 768 x 2048 1791 us, with 256 x 256 tiles there 1810, with a launch for the parameters 1807 (one matrix of 256 x 256: 78 and 80).
 template <MuonProduct KIND, int N>
