@@ -533,11 +533,11 @@ inline int round8(int n) { return (n + 7) / 8 * 8; }
 inline size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 // Whether a matrix is one workgroup's: it fits into LDS, and its products (16 rows squared times columns) are few enough for one compute unit.  In
-// microseconds, with one workgroup and with launches over many: 8 x 8 15 and 50, 305 x 11 23 and 65, 16 x 1500 55 and 83, 64 x 256 66 and 66,
-// 64 x 350 85 and 64.
+// microseconds, with one workgroup and with launches over many: 8 x 8 15 and 50, 16 x 1500 55 and 78, 32 x 700 55 and 66, 48 x 400 60 and 62,
+// 64 x 192 53 and 56, 64 x 256 65 and 56.
 inline bool is_small(const MuonStack &t) {
   const int high = (t.m + 15) / 16;
-  return t.m <= kSmallRows && high * 16 * small_ld(t.n) <= kSmallFloats && high * high * t.n <= 4096;
+  return t.m <= kSmallRows && high * 16 * small_ld(t.n) <= kSmallFloats && high * high * t.n <= 3600;
 }
 
 // Sizes of a stack and the workspace that it takes.
