@@ -52,11 +52,26 @@ __device__ __forceinline__ uint32_t lds_address(const void *p) { return uint32_t
 
 // 16 bytes a lane from memory to LDS at base + 16 lane (base is the wavefront's), through a buffer descriptor: what lies outside of its
 // bounds arrives as zeros.  Written as an instruction, since the compiler would wait for it before every later LDS read, whichever
-// half that reads; it has no output register.  lds_loads_done() and a barrier come before the first read.
+// half that reads; it has no output register.  lds_loads_done() and a barrier come before the first read.  Nor does the compiler keep a
+// vector instruction's write of the descriptor (readfirstlane, a spilled word's readlane) five wait states away, as the hardware wants: the
+// instructions in front of the load are as many, whatever is scheduled before them, and m0 wants one of its own.  A step's loads go two
+// at a time, so that the second needs no more than that (256 x 256 orthogonalised: 79 us, each by itself 82; Muon of an estimator 156 and 159); those
+// between a large tile's products by themselves (32768 rows, 32 of 5760 x 2880, transposed: 1088 us, two at a time 1110).
+// m0 is reserved, so that nothing lives there for long; that it is named keeps other writes of it and their readers together.
 typedef __attribute__((ext_vector_type(4))) uint32_t Buffer;
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(Buffer from, uint32_t offset, uint32_t base) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(from), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(from), "s"(base) : "memory", "m0");
 }
+// Two of them, the second APART bytes further on in LDS.
+template <int APART>
+__device__ __forceinline__ void load_two_to_lds(Buffer from, uint32_t first, uint32_t second, uint32_t base) {
+  asm volatile("s_mov_b32 m0, %3\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
+               "s_add_u32 m0, %3, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               ::"v"(first), "v"(second), "s"(from), "s"(base), "n"(APART) : "memory", "m0", "scc");
+}
+#pragma clang diagnostic pop
 // Until at most LEFT of this wavefront's loads are on their way.
 template <int LEFT>
 __device__ __forceinline__ void lds_loads_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
@@ -148,7 +163,7 @@ struct OperandTile {
     if constexpr (WHOLE16) {
       limit(k_left);
 #pragma unroll
-      for (int j = 0; j < kEach; ++j) issue_chunk(lds, j, k_left, tid);
+      for (int j = 0; j < kEach; j += kTogether) issue_chunks<kTogether>(lds, j, k_left, tid);
       advance();
     } else {
       k_held = k_left;
@@ -159,13 +174,17 @@ struct OperandTile {
       }
     }
   }
-  // The same in parts, straight to LDS: limit, each chunk, advance.
+  // The same in parts, straight to LDS: limit, one chunk or two after the other, advance.
+  static constexpr int kTogether = kEach % 2 == 0 ? 2 : 1;
   __device__ __forceinline__ void limit(int k_left) {
     if constexpr (IMAJOR) from[2] = uint32_t(k_left) * row_bytes;
   }
-  __device__ __forceinline__ void issue_chunk(uint32_t lds, int j, int k_left, int tid) {
-    const uint32_t mine = !IMAJOR && column >= k_left ? kOutside : offset, o = mine + j * kApart * row_bytes;
-    load_to_lds(from, j == 0 || mine != kOutside ? o : kOutside, __builtin_amdgcn_readfirstlane(lds + (tid & ~63) * 16) + j * THREADS * 16);
+  template <int N>
+  __device__ __forceinline__ void issue_chunks(uint32_t lds, int j, int k_left, int tid) {
+    const uint32_t mine = !IMAJOR && column >= k_left ? kOutside : offset, base = __builtin_amdgcn_readfirstlane(lds + (tid & ~63) * 16) + j * THREADS * 16;
+    const auto place = [&](int i) { return i == 0 || mine != kOutside ? mine + i * kApart * row_bytes : kOutside; };
+    if constexpr (N == 2) load_two_to_lds<THREADS * 16>(from, place(j), place(j + 1), base);
+    else load_to_lds(from, place(j), base);
   }
   __device__ __forceinline__ void advance() {
     const uint64_t p = (uint64_t(from[1]) << 32 | from[0]) + uint64_t(step);
@@ -430,8 +449,8 @@ struct TileProduct {
 #pragma unroll
             for (int j = 0; j < kAll; ++j) {
               if (j * FH / kAll != f) continue;
-              if (j < A::kEach) ta.issue_chunk(base + now, j, left, tid);
-              else tb.issue_chunk(base + now + A::kBytes, j - A::kEach, left, tid);
+              if (j < A::kEach) ta.template issue_chunks<1>(base + now, j, left, tid);
+              else tb.template issue_chunks<1>(base + now + A::kBytes, j - A::kEach, left, tid);
             }
           });
           ta.advance();
