@@ -81,3 +81,82 @@ def test_muon_by_large_tiles(shapes, tiles, held, grad):
             step_of = 2.0 ** -8 * o.abs() / (1 - 2.0 ** -8)               # the rounding to bfloat16
             bound = rate * step_of + 4 * U * (b[i].abs() + rate * o.abs())
             assert ((t[i].double() - (b[i] * (1 - lr * decay) - rate * o)).abs() <= bound).all(), (s, i)
+
+
+# 32 experts: empty ones, single rows, what fills half a tile or one more row than that, whole tiles, strips of more than six tiles
+ROWS = [0, 1, 100, 128, 129, 256, 257, 300, 400, 500, 384, 1700, 0, 0, 255, 2049] + [311] * 14 + [31, 640]
+
+
+def whole_numbers(g, *shape, dtype=torch.bfloat16, most=3):
+    return torch.randint(-most, most + 1, shape, generator=g, device="cuda").to(dtype)
+
+
+def ends_of(sizes):
+    return torch.tensor(sizes).cumsum(0).tolist()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("transpose", [False, True])
+@pytest.mark.parametrize("n,k", [(1032, 1096), (1280, 1024), (1096, 72)], ids=str)
+def test_products_by_large_tiles(n, k, transpose, dtype):
+    """Sums that end inside a step, inputs and results that are parts of wider rows, rows behind the last group."""
+    from paper_2603_19289_amd import training as T
+    if transpose:
+        n, k = k, n
+    ends, tail = ends_of(ROWS), 57
+    rows, width, out_width = ends[-1] + tail, n if transpose else k, k if transpose else n
+    g = torch.Generator("cuda").manual_seed(n + k)
+    x, w = whole_numbers(g, rows, width + 16)[:, 8:8 + width], whole_numbers(g, len(ROWS), n, k)
+    out = torch.full((rows, out_width + 5), 9.0, dtype=TYPES[dtype], device="cuda")
+    _, names = launched(lambda: T.grouped_product(x, w, i32(ends), transpose=transpose, dtype=TYPES[dtype], out=out[:, 2:2 + out_width]), "grouped_kernel")
+    assert any(re.search(rf"grouped_kernel<moe_spec::Bf16, 256, 256, .*{str(transpose).lower()}, true>", v) for v in names), sorted(set(names))
+    got = out[:, 2:2 + out_width]
+    for e, (b, f) in enumerate(bounds(ends, rows)):
+        want = x[b:f].double() @ (w[e].double() if transpose else w[e].double().t())
+        assert torch.equal(got[b:f], want.to(TYPES[dtype])), (e, b, f)
+    assert not got[ends[-1]:].any()
+    got.fill_(9.0)
+    assert torch.all(out == 9.0)                     # nothing beside it was written
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("dtype,experts,n,k,kernel", [("bf16", 11, 1032, 1096, "weight_grad_kernel<moe_spec::Bf16, 256, 256, 2, 4, 4, true, 32>"),
+                                                      ("bf16", 121, 1032, 1096, "weight_grad_kernel<moe_spec::Bf16, 256, 256, 2, 4, 4, true, 32>"),
+                                                      ("bf16", 121, 1031, 1097, "weight_grad_kernel<moe_spec::Bf16, 128, 128, 2, 4, 2, false, 64>"),
+                                                      ("bf16", 255, 20, 27001, "weight_grad_kernel<moe_spec::Bf16, 128, 128, 2, 4, 2, false, 64>"),
+                                                      ("f32", 121, 1032, 1096, "weight_grad_kernel<moe_spec::F32, 64, 64, 2, 4, 2, true, 32>"),
+                                                      ("f32", 121, 1031, 1097, "weight_grad_f32_kernel<64, 64, 2, 4>")])
+def test_weight_gradients_by_large_tiles_and_past_the_caches(dtype, experts, n, k, kernel, out):
+    """256 x 256 tiles, and results over 256 MiB, which are stored otherwise, of every kernel that can have one.  Groups of every number of rows about
+    the steps of 32 and 64; parts of larger blocks."""
+    from paper_2603_19289_amd import training as T
+    sizes = ([0, 1, 31, 32, 33, 63, 64, 65, 300, 127, 96] * experts)[:experts]
+    ends = ends_of(sizes)
+    rows = ends[-1] + 3
+    g = torch.Generator("cuda").manual_seed(n + experts)
+    dy, x = whole_numbers(g, rows, n, dtype=TYPES[dtype]), whole_numbers(g, rows, k, dtype=TYPES[dtype])
+    dy[ends[-1]:], x[ends[-1]:] = float("nan"), float("inf")           # belong to nobody
+    blocks = torch.full((experts, n * k + 40), 7.0, dtype=TYPES[out], device="cuda")
+    into = blocks[:, 16:16 + n * k].unflatten(1, (n, k))
+    assert (experts * n * k * into.element_size() > 1 << 28) == (experts > 11)
+    _, names = launched(lambda: T.grouped_weight_grad(dy, x, i32(ends), dtype=TYPES[out], out=into), kernel)
+    assert any(kernel in v for v in names), sorted(set(names))
+    for e, (b, f) in enumerate(bounds(ends, rows)):
+        assert torch.equal(into[e], (dy[b:f].double().t() @ x[b:f].double()).to(TYPES[out])), e
+    into.fill_(7.0)
+    assert torch.all(blocks == 7.0)
+
+
+@pytest.mark.parametrize("most", [0, 1, 64])
+def test_products_by_large_tiles_where_one_expert_has_all_rows(most):
+    """... or nearly: the others are empty, or have a row or a few."""
+    from paper_2603_19289_amd import training as T
+    sizes = [most, 9000, most, most] * 8
+    sizes[9:] = [most] * (len(sizes) - 9)
+    ends = ends_of(sizes)
+    g = torch.Generator("cuda").manual_seed(most)
+    x, w = whole_numbers(g, ends[-1], 136), whole_numbers(g, len(sizes), 1040, 136)
+    y, names = launched(lambda: T.grouped_product(x, w, i32(ends)), "grouped_kernel")
+    assert any("grouped_kernel<moe_spec::Bf16, 256, 256" in v for v in names)
+    for e, (b, f) in enumerate(bounds(ends, len(x))):
+        assert torch.equal(y[b:f], (x[b:f].double() @ w[e].double().t()).to(torch.bfloat16)), e
