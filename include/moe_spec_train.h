@@ -165,8 +165,14 @@ int moe_spec_swiglu_backward(void *stream, int dtype, const void *dh, int64_t dh
  * with (a, b, c) = coefficients, which pushes every singular value towards one; 3.4445, -4.7750, 2.0315 and five iterations bring
  * those above a hundredth of the norm to between 0.7 and 1.2.  g dev: count matrices [rows, cols] of type dtype, g_stride elements
  * between rows, g_matrix_stride between matrices; out dev, the same in bfloat16.  A matrix of zeros stays one; one that holds
- * what is not finite becomes NaN, and no other.  The iterates are float16: the result is off by 0.1 to 0.3 % of its norm where singular
- * values differ by less than a hundred, and a direction whose singular value is below some 2^-12 of the norm is mostly rounding. */
+ * what is not finite becomes NaN, and no other.  Coefficients lie between -16 and 16, iterations between 1 and 64.
+ * Matrices of a workgroup (up to 64 rows, or columns where those are fewer, s of them, and ceil(s / 16)^2 times the other side up to 3600) are
+ * float throughout.  The iterates X, A and a I + b A + c A A of others are float16: coefficients that take a value of them beyond 1000 in so many
+ * iterations, for any matrix and with a 64th each time for roundings, are refused (beyond 2^60 and with 2^-18 for the small ones).  What that leaves, of the result's norm and before its rounding to bfloat16, with
+ * the coefficients above: 0.1 to 0.2 % after five iterations where singular values lie within a factor of ten or are a random matrix's, 0.2 to 0.3 %
+ * where two are a hundred times the others, 2 to 3 % where two stand a hundred-fold out of noise or they fall like 1 / i^2 (a direction
+ * whose singular value is below some 2^-12 of the norm is mostly rounding); 0.3 to 0.4 % after twenty iterations of the first kind, and up to 5 %
+ * after 64. */
 size_t moe_spec_orthogonalise_workspace_bytes(int64_t count, int rows, int cols);
 int moe_spec_orthogonalise(void *stream, int dtype, const void *g, int64_t g_matrix_stride, int64_t g_stride, int64_t count, int rows,
                            int cols, const double *coefficients, int iterations, void *out, int64_t out_matrix_stride, int64_t out_stride,
@@ -188,7 +194,7 @@ typedef struct {
 
 typedef struct {
   double lr, momentum, weight_decay, update_rms, grad_scale;
-  double coefficients[3];
+  double coefficients[3];         /* and iterations: limits as above */
   const float *grad_scale_dev;    /* dev, or NULL: a second factor of the gradients */
   int32_t iterations, nesterov, grad_dtype;
 } moe_spec_muon_config;

@@ -1,9 +1,10 @@
 // Updates of matrices by the orthogonal factor of their momentum (Muon), many matrices in a few launches.
 //   X_0 = U / |U|_F (turned so that it has at most as many rows as columns), then as often as asked
 //   A = X X^T,  B = a I + b A + c A A,  X <- B X
-// The iteration runs on the matrix cores with X, A and B in float16 and sums in float: |X| stays below 1.3 and every value of A and B below 15,
-// so float16's range is enough, and its 11 bits are what a bfloat16 result can show (0.1 % of the result after five iterations; bfloat16
-// iterates are off by 1 %).  The three are held 64-fold, so that the smallest values that count stay above float16's denormal ones.
+// The iteration runs on the matrix cores with X, A and B in float16 and sums in float: with the usual coefficients |X| stays below 1.3 and every
+// value of A and B below 15, so float16's range is enough (others are looked at before a call begins, iterates_within()), and its 11 bits are what a
+// bfloat16 result can show (0.1 % of the result after five iterations; bfloat16 iterates are off by 1 %).  The three are held 64-fold, so that the
+// smallest values that count stay above float16's denormal ones.  Matrices that one workgroup takes have no float16 in them.
 // Three products an iteration, each one launch over all matrices of a call; a matrix that the framework holds upright is laid on its side
 // on the way in and stood up on the way out.
 #include <math.h>
@@ -571,6 +572,38 @@ const char *iteration_fault(const double *c, int iterations) {
   return nullptr;
 }
 
+// Whether X, A and B stay within `most` for every matrix.  An iteration takes each singular value s to s q(s^2), q(t) = a + b t + c t^2, of which it
+// makes A's eigenvalues s^2 and B's q(s^2), and no value of a matrix is larger than its largest singular value.  They begin in [0, 1] and after
+// an iteration fill [0, top] with top the largest |s q(s^2)| there: at the end or where the slope a + 3 b t + 5 c t^2 is zero; q has its own at an
+// end or at -b / 2c.  Roundings may take top further, by `slack` of it each time.
+bool iterates_within(double most, double slack, const double *coefficients, int iterations) {
+  const double a = coefficients[0], b = coefficients[1], c = coefficients[2];
+  const auto q = [=](double t) { return fabs(a + t * (b + t * c)); };
+  double flat[2] = {-1.0, -1.0};                         // t where the slope is zero, negative: none
+  if (const double d = 9.0 * b * b - 20.0 * a * c; d >= 0.0) {
+    const double r = -0.5 * (3.0 * b + copysign(sqrt(d), b));
+    if (c != 0.0) flat[0] = r / (5.0 * c);
+    if (r != 0.0) flat[1] = a / r;
+  }
+  double top = 1.0;
+  for (int i = 0; i < iterations; ++i) {
+    top *= 1.0 + slack;
+    const double end = top * top;
+    double largest = fmax(q(0.0), q(end)), next = top * q(end);
+    if (c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < end) largest = fmax(largest, q(-b / (2.0 * c)));
+    for (const double t : flat) if (t > 0.0 && t < end) next = fmax(next, sqrt(t) * q(t));
+    if (!(end <= most && largest <= most && next <= most)) return false;
+    top = next;
+  }
+  return true;
+}
+// 65504 is what float16 holds, and X, A and B are held 64-fold: 1023.  A 64th is 32 roundings of float16; those of a matrix, each
+// another way, come to about 2 in any one direction.  Of a matrix of one workgroup A A in float has to stay in range, with 64 of float's roundings.
+const char *range_fault(const MuonStack &t, const double *coefficients, int iterations) {
+  if (is_small(t)) return iterates_within(double(int64_t(1) << 60), 64.0 / (1 << 24), coefficients, iterations) ? nullptr : "coefficients that take iterates out of float's range";
+  return iterates_within(1000.0, 1.0 / 64, coefficients, iterations) ? nullptr : "coefficients that take iterates beyond 1000, which matrices of more than one workgroup cannot hold";
+}
+
 // Where each stack's workgroups begin in a launch, and how many there are.
 template <int N, typename Count>
 void firsts(MuonArgs<N> &a, int n, Count workgroups, unsigned &grid) {
@@ -715,11 +748,20 @@ extern "C" int moe_spec_muon_step(void *stream, const moe_spec_muon_tensor *tens
     if (m.copy_stride != 0 && (m.copy_stride < int64_t(m.rows) * m.cols || m.copy_stride > int64_t(1) << 40))
       return train_fail(MOE_SPEC_EINVAL, "muon_step: tensor %d has a copy_stride below a matrix or above 2^40", i);
   }
+  bool any = false, seen[2] = {false, false};
+  for (int i = 0; i < n_tensors; ++i) {
+    const moe_spec_muon_tensor &m = tensors[i];
+    if (m.count == 0 || m.rows == 0 || m.cols == 0) continue;
+    any = true;
+    MuonStack t;
+    shape(t, m.count, m.rows, m.cols);
+    if (seen[is_small(t)]) continue;                     // the same for all of a kind
+    seen[is_small(t)] = true;
+    if (const char *why = range_fault(t, cfg->coefficients, cfg->iterations)) return train_fail(MOE_SPEC_EINVAL, "muon_step: tensor %d: %s", i, why);
+  }
   const size_t need = moe_spec_muon_workspace_bytes(tensors, n_tensors);
   if (need && (!workspace || misaligned(workspace, 16) || workspace_bytes < need))
     return train_fail(MOE_SPEC_EINVAL, "muon_step: the workspace is null, not aligned to 16 bytes or smaller than %zu bytes", need);
-  bool any = false;
-  for (int i = 0; i < n_tensors; ++i) any = any || (tensors[i].count && tensors[i].rows && tensors[i].cols);
   if (!any) return MOE_SPEC_OK;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const OnDeviceOf on(s);
@@ -792,6 +834,7 @@ extern "C" int moe_spec_orthogonalise(void *stream, int dtype, const void *g, in
   MuonArgs<kPerMuonLaunch> a{};
   MuonStack &t = a.t[0];
   const size_t need = shape(t, count, rows, cols);
+  if (const char *why = range_fault(t, coefficients, iterations)) return train_fail(MOE_SPEC_EINVAL, "orthogonalise: %s", why);
   if (need && (!workspace || misaligned(workspace, 16) || workspace_bytes < need))
     return train_fail(MOE_SPEC_EINVAL, "orthogonalise: the workspace is null, not aligned to 16 bytes or smaller than %zu bytes", need);
   const hipStream_t s = static_cast<hipStream_t>(stream);

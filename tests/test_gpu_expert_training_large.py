@@ -160,3 +160,17 @@ def test_products_by_large_tiles_where_one_expert_has_all_rows(most):
     assert any("grouped_kernel<moe_spec::Bf16, 256, 256" in v for v in names)
     for e, (b, f) in enumerate(bounds(ends, len(x))):
         assert torch.equal(y[b:f], (x[b:f].double() @ w[e].double().t()).to(torch.bfloat16)), e
+
+
+@pytest.mark.parametrize("coefficients,iterations", [((1.5, -0.5, 0.0), 12), ((15 / 8, -10 / 8, 3 / 8), 8), ((3.0, -3.2, 1.2), 6), ((2.0, -1.5, 0.5), 10), ((4.0, 0.0, 0.0), 3),
+                                                     ((16.0, 0.0, 0.0), 2), ((0.0, 0.0, 8.0), 1), ((0.0, 15.0, 0.0), 1), ((-1.0, 0.0, 0.0), 7)], ids=str)
+@pytest.mark.parametrize("rows,cols", [(100, 130), (300, 270)])
+def test_orthogonalise_with_other_coefficients(rows, cols, coefficients, iterations):
+    """Matrices that are held in float16, and one strong direction, which has the norm almost to itself; iterates up to 256."""
+    from paper_2603_19289_amd import training as T
+    g = torch.Generator().manual_seed(rows)
+    strong = torch.randn(rows, 1, generator=g) @ torch.randn(1, cols, generator=g)
+    for v in (torch.randn(rows, cols, generator=g), strong, strong + 0.2 * torch.randn(rows, cols, generator=g)):
+        got = T.orthogonalise(v.to("cuda"), coefficients=coefficients, iterations=iterations).cpu().double()
+        want, err = orthogonal(v, iterations, coefficients)
+        assert (got - want).norm() <= err + 2.0 ** -8 * want.norm()
