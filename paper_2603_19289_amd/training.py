@@ -409,10 +409,17 @@ def swiglu_backward(dh: torch.Tensor, a: torch.Tensor, weight: Optional[torch.Te
 ORTHOGONALISE = (3.4445, -4.7750, 2.0315)          # coefficients of its iteration
 
 
+def _three(coefficients):
+    c = tuple(coefficients)
+    if len(c) != 3:
+        raise ValueError("the iteration has three coefficients")
+    return (C.c_double * 3)(*c)
+
+
 def orthogonalise(g: torch.Tensor, *, iterations: int = 5, coefficients=ORTHOGONALISE, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Matrices [rows, cols] or stacks of them [count, rows, cols], float32 or bfloat16, with their singular values pushed towards one
     -> bfloat16, of g's shape.  Formula and accuracy are in include/moe_spec_train.h."""
-    dtype = _TYPES.get(g.dtype)
+    dtype, c = _TYPES.get(g.dtype), _three(coefficients)
     if dtype is None or g.dim() not in (2, 3) or not g.is_cuda or (g.stride(-1) != 1 and g.shape[-1] > 1):
         raise ValueError("g must be a float32 or bfloat16 matrix on a GPU, or a stack of them, whose rows are contiguous")
     given = out is not None
@@ -422,7 +429,7 @@ def orthogonalise(g: torch.Tensor, *, iterations: int = 5, coefficients=ORTHOGON
     need = lib.moe_spec_orthogonalise_workspace_bytes(count, rows, cols)
     space = g.new_empty(need, dtype=torch.uint8) if need else None
     _queue(g.device, lib.moe_spec_orthogonalise, dtype, g.data_ptr(), g.stride(0) if g.dim() == 3 else 0, g.stride(-2), count, rows, cols,
-           (C.c_double * 3)(*coefficients), iterations, out.data_ptr(), out.stride(0) if g.dim() == 3 else 0, out.stride(-2),
+           c, iterations, out.data_ptr(), out.stride(0) if g.dim() == 3 else 0, out.stride(-2),
            space.data_ptr() if need else None, need)
     if given:
         increment_version(out)
@@ -445,6 +452,7 @@ class Muon:
             raise ValueError("no parameters")
         self.lr, self.momentum, self.nesterov, self.weight_decay = lr, momentum, nesterov, weight_decay
         self.update_rms, self.iterations, self.coefficients = update_rms, iterations, tuple(coefficients)
+        _three(self.coefficients)
         self.device = self.params[0].device
         self.copies = list(copies) if copies is not None else [None] * len(self.params)
         self._m = list(states["m"]) if states is not None else [torch.zeros_like(p, memory_format=torch.contiguous_format) for p in self.params]
@@ -503,7 +511,7 @@ class Muon:
                 self._tensor(g, "a gradient", dtype, shape)
                 d.grad, d.count = g.data_ptr(), shape[0] if len(shape) == 3 else 1
         c = M.MuonConfig(lr=self.lr, momentum=self.momentum, weight_decay=self.weight_decay, update_rms=self.update_rms, grad_scale=1.0,
-                         coefficients=self.coefficients, iterations=self.iterations, nesterov=bool(self.nesterov), grad_dtype=_TYPES[dtype])
+                         coefficients=_three(self.coefficients), iterations=self.iterations, nesterov=bool(self.nesterov), grad_dtype=_TYPES[dtype])
         if isinstance(grad_scale, torch.Tensor):
             if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.device != self.device:
                 raise ValueError("grad_scale must be a number or one float32 value on the parameters' GPU")

@@ -8,8 +8,9 @@ import pytest
 import torch
 
 from paper_2603_19289_amd import moe_spec as M
+from paper_2603_19289_amd import training as T
 
-from .test_expert_training_refusals import muon, orthogonalise, refused
+from .test_expert_training_refusals import muon, orthogonalise, recorded, refused  # noqa: F401
 
 LARGE, SMALL = dict(rows=80, cols=96), dict(rows=16, cols=24, g_matrix_stride=16 * 24, out_matrix_stride=16 * 24, out_stride=24, g_stride=24)
 
@@ -59,3 +60,19 @@ def test_what_is_refused_is_what_would_not_fit():
                 assert (got == M.EHIP) == (most <= limit), (c, n, most)
             assert got == M.EINVAL or largest(c, n) <= limit, (c, n)
     assert 200 < taken < 700                      # both answers are given
+
+
+@pytest.mark.parametrize("coefficients", [(), (1.5, -0.5), (3.4445, -4.775, 2.0315, 0.0)])
+def test_the_iteration_has_three_coefficients(recorded, coefficients):  # noqa: F811
+    """Two were taken as if the third were zero."""
+    p = torch.zeros(70, 90)
+    for call in (lambda: T.orthogonalise(p, coefficients=coefficients), lambda: T.Muon([p], lr=0.1, coefficients=coefficients)):
+        with pytest.raises(ValueError, match="three"):
+            call()
+    opt = T.Muon([p], lr=0.1)
+    opt.coefficients = coefficients                # settings may be changed between steps
+    with pytest.raises(ValueError, match="three"):
+        opt.step([p.clone()])
+    opt.coefficients = [1.5, -0.5, 0.0]
+    opt.step([p.clone()])
+    assert list(recorded[-1][2]._obj.coefficients) == [1.5, -0.5, 0.0]
