@@ -206,8 +206,9 @@ __global__ __launch_bounds__(kFewBlock) void grouped_few_kernel(const GroupedArg
     }
     return v;
   };
-  f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};        // of each round's, so that a long sum's roundings stay small, as the tiles' do
   for (int first = (wave * 4 + g) * V; first - g * V < K; first += kFewWaves * kFewDeep * 4 * V) {
+    f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
     uint4 vw[kFewDeep], vx[kFewDeep];
 #pragma unroll
     for (int d = 0; d < kFewDeep; ++d) {
@@ -225,17 +226,18 @@ __global__ __launch_bounds__(kFewBlock) void grouped_few_kernel(const GroupedArg
         for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[j], fx[j], acc, 0, 0, 0);
       }
     }
+    sum += acc;
   }
-  part[wave][lane] = acc;
+  part[wave][lane] = sum;
   __syncthreads();
   if (wave > 0) return;
 #pragma unroll
-  for (int v = 1; v < kFewWaves; ++v) acc += part[v][lane];
+  for (int v = 1; v < kFewWaves; ++v) sum += part[v][lane];
   if (i >= t.rows) return;
   const int64_t at = (t.row0 + int64_t(i)) * a.y_stride + col0 + 4 * g;
   const int n = a.n - col0 - 4 * g;
-  if (a.out_bf16) store8(static_cast<uint16_t *>(a.y) + at, uint4{pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), 0, 0}, n < 4 ? n : 4);
-  else store4(static_cast<float *>(a.y) + at, acc, n);
+  if (a.out_bf16) store8(static_cast<uint16_t *>(a.y) + at, uint4{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]), 0, 0}, n < 4 ? n : 4);
+  else store4(static_cast<float *>(a.y) + at, sum, n);
 }
 
 template <int BM, int BN, int WM, int WN, bool W_IMAJOR>
@@ -260,14 +262,17 @@ __global__ __launch_bounds__(kFewTBlock) void grouped_few_transposed_kernel(cons
   const int col0 = t.tile_n * kFewTCols, K = t.expert == a.n_experts ? 0 : int(a.k), mine = col0 + 4 * i, n = a.n - mine;
   const float *w = static_cast<const float *>(a.w) + (t.expert == a.n_experts ? 0 : t.expert * a.w_expert) + mine;
   const float *x = static_cast<const float *>(a.x) + (t.row0 + int64_t(min(i, t.rows - 1))) * a.x_stride;
-  f32x4_t acc[4];
+  f32x4_t sums[4];                               // of each round's, as above
 #pragma unroll
-  for (int j = 0; j < 4; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int j = 0; j < 4; ++j) sums[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   // rows of weights behind the last are the first one's, and count for nothing
   const auto walk = [&](auto whole) {
     for (int first = 4 * wave; first < K; first += kFewTWaves * kFewDeep * 4) {
+      f32x4_t acc[4];
       Run<float, 4> vw[kFewDeep];
       float vx[kFewDeep];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int d = 0; d < kFewDeep; ++d) {
         const int at = first + d * kFewTWaves * 4 + g, k = at < K ? at : 0;
@@ -283,12 +288,14 @@ __global__ __launch_bounds__(kFewTBlock) void grouped_few_transposed_kernel(cons
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? f[j] : 0.0f, v, acc[j], 0, 0, 0);
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sums[j] += acc[j];
     }
   };
   if (a.n - col0 >= kFewTCols) walk(std::true_type());
   else walk(std::false_type());
 #pragma unroll
-  for (int j = 0; j < 4; ++j) part[wave][j][lane] = acc[j];
+  for (int j = 0; j < 4; ++j) part[wave][j][lane] = sums[j];
   __syncthreads();
   // lane (token i, g), value q of column set j: column col0 + 4 (4 g + q) + j
   for (int q = threadIdx.x; q < t.rows * kFewTCols; q += kFewTBlock) {
