@@ -139,14 +139,14 @@ int moe_spec_adamw_read_moments(void *stream, const moe_spec_adamw_tensor *tenso
  *   y_r = W_e^T x_r    transpose = 1: x dev [rows, n] -> y dev [rows, k], the gradient with respect to the other form's x
  * w dev: n_experts matrices [n, k] (1 <= n_experts <= MOE_SPEC_MAX_EXPERTS), w_stride elements between their rows and
  * w_expert_stride between matrices (gate and up rows of expert blocks are one such matrix, as the pool has them); x and w of type dtype, y of
- * out_dtype.  ends dev [n_experts].  Rows of y behind the last group are set to zero.  Sums are float, in an order that sizes and
- * groups alone decide. */
+ * out_dtype.  ends dev [n_experts].  Rows of y behind the last group are set to zero.  Sums are float, in an order that sizes,
+ * groups, strides and alignment decide: equal calls have equal bits.  What is written overlaps nothing that is read. */
 int moe_spec_grouped_product(void *stream, int dtype, const void *x, int64_t x_stride, int64_t rows, const void *w, int64_t w_stride,
                              int64_t w_expert_stride, int n_experts, int n, int k, const int32_t *ends, int transpose, int out_dtype,
                              void *y, int64_t y_stride);
 
 /* Gradient of the matrices: dw dev, n_experts matrices [n, k] of out_dtype, dw_e = sum over the group's rows of dy_r x_r^T, written, not
- * added to; zeros for an expert without rows.  dy dev [rows, n], x dev [rows, k], groups as above. */
+ * added to; zeros for an expert without rows.  dy dev [rows, n], x dev [rows, k], groups and sums as above, of up to 64 parts of a group's rows. */
 size_t moe_spec_grouped_weight_grad_workspace_bytes(int dtype, int64_t rows, int n_experts, int n, int k);
 int moe_spec_grouped_weight_grad(void *stream, int dtype, const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int64_t rows,
                                  int n_experts, int n, int k, const int32_t *ends, int out_dtype, void *dw, int64_t dw_stride,
@@ -163,16 +163,16 @@ int moe_spec_swiglu_backward(void *stream, int dtype, const void *dh, int64_t dh
 /* Orthogonalised matrices.  X = g / |g|_F (Frobenius norm, in double), then `iterations` times
  *   X <- a X + (b A + c A A) X,  A = X X^T (or X^T X, where that is smaller)
  * with (a, b, c) = coefficients, which pushes every singular value towards one; 3.4445, -4.7750, 2.0315 and five iterations bring
- * those above a hundredth of the norm to between 0.7 and 1.2.  g dev: count matrices [rows, cols] of type dtype, g_stride elements
+ * those above a hundredth of the norm to between 0.68 and 1.14.  g dev: count matrices [rows, cols] of type dtype, g_stride elements
  * between rows, g_matrix_stride between matrices; out dev, the same in bfloat16.  A matrix of zeros stays one; one that holds
  * what is not finite becomes NaN, and no other.  Coefficients lie between -16 and 16, iterations between 1 and 64.
- * Matrices of a workgroup (up to 64 rows, or columns where those are fewer, s of them, and ceil(s / 16)^2 times the other side up to 3600) are
- * float throughout.  The iterates X, A and a I + b A + c A A of others are float16: coefficients that take a value of them beyond 1000 in so many
- * iterations, for any matrix and with a 64th each time for roundings, are refused (beyond 2^60 and with 2^-18 for the small ones).  What that leaves, of the result's norm and before its rounding to bfloat16, with
- * the coefficients above: 0.1 to 0.2 % after five iterations where singular values lie within a factor of ten or are a random matrix's, 0.2 to 0.3 %
- * where two are a hundred times the others, 2 to 3 % where two stand a hundred-fold out of noise or they fall like 1 / i^2 (a direction
- * whose singular value is below some 2^-12 of the norm is mostly rounding); 0.3 to 0.4 % after twenty iterations of the first kind, and up to 5 %
- * after 64. */
+ * Small matrices are float throughout: a side of up to 16 and one of up to 1532, 32 and 764, 48 and 400, or 64 and 225.  The iterates X, A and
+ * a I + b A + c A A of others are float16: coefficients that take a value of them beyond 1000 in so many iterations, for any matrix and with a
+ * 64th each time for roundings, are refused (beyond 2^60 and with 2^-18 for small matrices).  What float16 leaves, of the result's norm and
+ * before its rounding to bfloat16, with the coefficients above: 0.1 to 0.2 % after five iterations where singular values lie within a
+ * factor of ten or are a random matrix's, 0.2 to 0.3 % where two are a hundred times the others, 2 to 3 % where two stand a hundred-fold out of
+ * noise or they fall like 1 / i^2 (a direction whose singular value is below some 2^-12 of the norm is mostly rounding); 0.3 to 0.4 %
+ * after twenty iterations of the first kind, and up to 5 % after 64. */
 size_t moe_spec_orthogonalise_workspace_bytes(int64_t count, int rows, int cols);
 int moe_spec_orthogonalise(void *stream, int dtype, const void *g, int64_t g_matrix_stride, int64_t g_stride, int64_t count, int rows,
                            int cols, const double *coefficients, int iterations, void *out, int64_t out_matrix_stride, int64_t out_stride,

@@ -495,7 +495,8 @@ struct TileProduct {
 };
 
 // A wavefront's part of a 16-bit result in LDS, row by row, so that it leaves in rows of 16 bytes a lane instead of 8 bytes of 16 rows.
-// The 16-byte chunk c of row r lies at place c ^ (r / 2 % chunks).
+// The 16-byte chunk c of row r lies at place c ^ (r / 2 % chunks).  This way out has what bank conflicts there are: 1024 cycles a tile of 256 x 256,
+// 347 of 128 x 128, whatever its sums' length (1 % of LDS cycles at 5760 columns, 11 % at 512).
 template <int ROWS, int COLS>
 struct ResultTile {
   static constexpr int kAcross = COLS / 8, kBytes = ROWS * COLS * 2, kEach = ROWS * kAcross / 64;
