@@ -168,11 +168,11 @@ int moe_spec_swiglu_backward(void *stream, int dtype, const void *dh, int64_t dh
  * what is not finite becomes NaN, and no other.  Coefficients lie between -16 and 16, iterations between 1 and 64.
  * Small matrices are float throughout: a side of up to 16 and one of up to 1532, 32 and 764, 48 and 400, or 64 and 225.  The iterates X, A and
  * a I + b A + c A A of others are float16: coefficients that take a value of them beyond 1000 in so many iterations, for any matrix and with a
- * 64th each time for roundings, are refused (beyond 2^60 and with 2^-18 for small matrices).  What float16 leaves, of the result's norm and
- * before its rounding to bfloat16, with the coefficients above: 0.1 to 0.2 % after five iterations where singular values lie within a
- * factor of ten or are a random matrix's, 0.2 to 0.3 % where two are a hundred times the others, 2 to 3 % where two stand a hundred-fold out of
- * noise or they fall like 1 / i^2 (a direction whose singular value is below some 2^-12 of the norm is mostly rounding); 0.3 to 0.4 %
- * after twenty iterations of the first kind, and up to 5 % after 64. */
+ * 64th each time for roundings, are refused (beyond 2^60 and with 2^-18 for small matrices).  X is kept to 22 bits in the first of them, so
+ * that the result, before its rounding to bfloat16 and with the coefficients above, is off by 0.05 to 0.2 % of its norm after five iterations whatever
+ * the spectrum (0.35 % where all singular values are equal), by 0.1 to 0.7 % after ten (1 %).  These coefficients do not settle, and carry roundings
+ * on: 0.2 to 2 % after twenty, 0.2 to 3 % after 64 (4 and 10 %); singular values below some 2^-20 of the norm, which come up by
+ * then, are mostly rounding. */
 size_t moe_spec_orthogonalise_workspace_bytes(int64_t count, int rows, int cols);
 int moe_spec_orthogonalise(void *stream, int dtype, const void *g, int64_t g_matrix_stride, int64_t g_stride, int64_t count, int rows,
                            int cols, const double *coefficients, int iterations, void *out, int64_t out_matrix_stride, int64_t out_stride,

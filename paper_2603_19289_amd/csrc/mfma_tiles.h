@@ -506,6 +506,12 @@ struct ResultTile {
     const int row = 16 * f + (lane & 15), col = 16 * h + 4 * (lane >> 4);
     *reinterpret_cast<uint2 *>(lds + place(row, col >> 3) + (col & 4) * 2) = v;
   }
+  // What is put, or will be, at the same place.
+  static __device__ __forceinline__ uint2 get(const char *lds, int f, int h, int lane) {
+    const int row = 16 * f + (lane & 15), col = 16 * h + 4 * (lane >> 4);
+    return *reinterpret_cast<const uint2 *>(lds + place(row, col >> 3) + (col & 4) * 2);
+  }
+  static __device__ __forceinline__ void set(char *lds, int row, int c, uint4 v) { *reinterpret_cast<uint4 *>(lds + place(row, c)) = v; }
   static __device__ __forceinline__ uint4 chunk(const char *lds, int row, int c) { return *reinterpret_cast<const uint4 *>(lds + place(row, c)); }
   // Eight rows from `row` on (a multiple of 8) of column `col` + lane % 16 (col a multiple of 16; row the same for 16 lanes).
   static __device__ __forceinline__ uint4 column(const char *lds, int row, int col, int lane) {

@@ -29,7 +29,7 @@ def launched(call, *parts):
     return result, names
 
 
-KINDS = ["SQUARE", "POLYNOMIAL", "APPLY", "RESULT"]
+KINDS = ["SQUARE", "POLYNOMIAL", "APPLY", "RESULT", "APPLY_TAKE", "APPLY_PASS"]
 
 
 def muon_tiles(names):
@@ -43,7 +43,7 @@ def muon_tiles(names):
     return tiles, stacks
 
 
-# stacks of matrices; tiles of X X^T, of B, of B X, of the last product; how many stacks a launch's arguments hold
+# stacks of matrices; tiles of X X^T, of B, of B X in its three forms, of the last product; how many stacks a launch's arguments hold
 STACKS = [([(42, 521, 1003)], (256, 256, 256, 128), 1),
           ([(28, 520, 695)], (128, 128, 256, 128), 1),
           ([(20, 1003, 521), (11, 600, 1001), (11, 521, 1024)], (256, 256, 256, 128), 4),
@@ -67,8 +67,8 @@ def test_muon_by_large_tiles(shapes, tiles, held, grad):
             t.copy_(b)
         T.Muon(p, lr=lr, momentum=0.0, nesterov=False, weight_decay=decay, update_rms=rms, copies=copies).step(grads)
     copies = [torch.zeros(s, device="cuda", dtype=torch.bfloat16) for s in shapes]
-    _, names = launched(step, *(f"MuonProduct){i}," for i in range(4)))
-    assert muon_tiles(names) == ({k: {t} for k, t in zip(KINDS, tiles)}, {held}), sorted(set(names))
+    _, names = launched(step, *(f"MuonProduct){i}," for i in range(6)))
+    assert muon_tiles(names) == ({k: {t} for k, t in zip(KINDS, (*tiles, tiles[2], tiles[2]))}, {held}), sorted(set(names))
     for s, t, b, v, c in zip(shapes, p, before, grads, copies):
         rate = lr * rms * math.sqrt(max(s[1:]))
         assert torch.equal(c, t.to(torch.bfloat16))
