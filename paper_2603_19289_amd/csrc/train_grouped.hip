@@ -33,7 +33,7 @@ __device__ __forceinline__ TilePlace tile_place(int at, int rows, int cols, int 
 
 // Which tile of at most BM rows of one expert, and of which columns, this workgroup takes.  Consecutive workgroups go to the eight
 // dies in turn; each die gets a run of tiles: large ones in strips of 6 rows of the 32 that a die's compute units work on (32 experts of 5760 x 2880,
-// 1024 rows each, transposed: 1147 -> 1114 us then, 1078 now), others columns first.
+// 1024 rows each, transposed: 1147 -> 1114 us then, 1105 now), others columns first.
 template <int BM>
 __device__ __forceinline__ RowTile row_tile(const int32_t *ends, int n_experts, int rows, int tiles_n) {
   const int lane = threadIdx.x & 63;

@@ -183,7 +183,7 @@ __device__ __forceinline__ Normaliser normaliser(const MuonStack &t, int64_t mat
 }
 
 // X_0 as float16.  A matrix that is not upright as it lies; an upright one is laid on its side, tiles of 64 x 64 through LDS, whose columns are read
-// value by value: half of the LDS cycles are bank conflicts, behind a memory that is at 4.6 TB/s meanwhile.
+// value by value: two thirds of the LDS cycles are bank conflicts, behind a memory that is at 5.2 TB/s meanwhile.
 struct Turn {
   int64_t matrix;
   int row0, col0;
@@ -732,7 +732,7 @@ constexpr int64_t kMostMuonBlocks = (int64_t(1) << 32) / kMuonBlock - 1;
 // One product over n stacks.  256 tiles of 256 x 256 are a round of what the compute units hold, and so are 512 of 128 x 128; they take about 1 : 0.62 of the
 // time, and two rounds of 64 x 64, 1024 tiles, 0.6 (256 x 256 tiles reach 1050 TFLOP/s, 128 x 128 820, 64 x 64 420): the tile that is done first.  The last product,
 // whose workgroups then read and write parameters, has two of them a compute unit, so that one's products cover another's traffic: 48 matrices of
-// 768 x 2048 1791 us, with 256 x 256 tiles there 1810, with a launch for the parameters 1807 (one matrix of 256 x 256: 78 and 80).
+// 768 x 2048 1791 us (before rests), with 256 x 256 tiles there 1810, with a launch for the parameters 1807 (one matrix of 256 x 256: 78 and 80).
 template <MuonProduct KIND, int N>
 hipError_t run_product(MuonArgs<N> &a, int n, hipStream_t s) {
   int tile = KIND == RESULT ? 128 : 256, best = tile;
