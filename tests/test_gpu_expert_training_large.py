@@ -174,3 +174,45 @@ def test_orthogonalise_with_other_coefficients(rows, cols, coefficients, iterati
         got = T.orthogonalise(v.to("cuda"), coefficients=coefficients, iterations=iterations).cpu().double()
         want, err = orthogonal(v, iterations, coefficients)
         assert (got - want).norm() <= err + 2.0 ** -8 * want.norm()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n,k", [(5, 65536, 9), (300, 65536, 8), (300, 8, 65536), (3, 65535, 24), (70, 65536, 1)])
+def test_widest_matrices(rows, n, k, dtype):
+    """65536 rows or columns of a matrix, in all three directions."""
+    from paper_2603_19289_amd import training as T
+    g = torch.Generator("cuda").manual_seed(rows + n)
+    ends = [rows // 3, rows]
+    t = TYPES[dtype]
+    x, dy, w = (whole_numbers(g, *s, dtype=t, most=2) for s in ((rows, k), (rows, n), (2, n, k)))
+    y, dx, dw = (f(torch.float32) for f in (lambda d: T.grouped_product(x, w, i32(ends), dtype=d), lambda d: T.grouped_product(dy, w, i32(ends), transpose=True, dtype=d),
+                                            lambda d: T.grouped_weight_grad(dy, x, i32(ends), dtype=d)))
+    for e, (b, f) in enumerate(bounds(ends, rows)):
+        assert torch.equal(y[b:f], (x[b:f].double() @ w[e].double().t()).float())
+        assert torch.equal(dx[b:f], (dy[b:f].double() @ w[e].double()).float())
+        assert torch.equal(dw[e], (dy[b:f].double().t() @ x[b:f].double()).float())
+
+
+@pytest.mark.parametrize("rows,cols", [(2_100_003, 3), (270_001, 136), (66_001, 2056)])
+def test_swiglu_of_more_rows_than_a_launch_has_at_once(rows, cols):
+    """The same bits as the first and the last rows have by themselves."""
+    from paper_2603_19289_amd import training as T
+    g = torch.Generator("cuda").manual_seed(cols)
+    a = torch.randn(rows, 2 * cols, generator=g, device="cuda").bfloat16()
+    dh, weight = torch.randn(rows, cols, generator=g, device="cuda").bfloat16(), torch.rand(rows, generator=g, device="cuda")
+    h, (da, dw) = T.swiglu_forward(a, weight), T.swiglu_backward(dh, a, weight)
+    for some in (slice(0, 1000), slice(rows // 2, rows // 2 + 1000), slice(rows - 1000, rows)):
+        assert torch.equal(h[some], T.swiglu_forward(a[some], weight[some]))
+        for got, want in zip((da, dw), T.swiglu_backward(dh[some], a[some], weight[some])):
+            assert torch.equal(got[some], want)
+
+
+@pytest.mark.parametrize("shape", [(66, 65536), (65536, 66), (1, 65536), (3, 2, 65535)], ids=str)
+def test_orthogonalise_the_widest(shape):
+    from paper_2603_19289_amd import training as T
+    v = torch.randn(shape, generator=torch.Generator("cuda").manual_seed(len(shape)), device="cuda")
+    got = T.orthogonalise(v).double()
+    for m, o in zip(v.view(-1, *shape[-2:]), got.view(-1, *shape[-2:])):
+        want, err = orthogonal(m.cpu() if m.shape[0] <= m.shape[1] else m.t().cpu())
+        o = o.cpu() if m.shape[0] <= m.shape[1] else o.t().cpu()
+        assert (o - want).norm() <= err + 2.0 ** -8 * want.norm()
