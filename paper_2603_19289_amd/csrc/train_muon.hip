@@ -311,7 +311,8 @@ struct Result {
 };
 
 // One product for every matrix.  SQUARE: A = X X^T; POLYNOMIAL: B = a I + b A + c A A; APPLY: X' = B X; RESULT: the last of those,
-// which goes to the parameters and copies instead.  A and B are symmetric: of them only tiles on and below the diagonal are worked out, and written
+// which goes to the parameters and copies instead; APPLY_TAKE and APPLY_PASS: B X and a times the rests of X, the second with rests of its own, in the
+// place of those that it took up.  A and B are symmetric: of them only tiles on and below the diagonal are worked out, and written
 // to both places.
 enum MuonProduct { SQUARE, POLYNOMIAL, APPLY, RESULT, APPLY_TAKE, APPLY_PASS };
 
